@@ -246,8 +246,8 @@ def _run_own(s):
     if op == "prompt":
         E.ee_prompt_attn(s["q"], s["k"], s["v"], s["tok_off"], s["scale"], s["out"], s["ws"], lse=s["lse"])
     else:
-        E.ee_chunk_attn(s["q"], s["k_cache"], s["v_cache"], s["block_table"], s["ctx_len"], s["max_ctx"], s["tok_off"],
-                        s["t_max"], s["scale"], s["out"], s["ws"], lse=s["lse"])
+        E.ee_chunk_attn(s["q"], s["k_cache"], s["v_cache"], s["block_table"], s["ctx_len"], s["tok_off"], s["scale"],
+                        s["out"], s["ws"], lse=s["lse"])
     return {"out": s["out"], "lse": s["lse"]}
 
 
