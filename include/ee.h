@@ -25,6 +25,11 @@
  *   ee_lmhead_pack_weights / ee_lmhead_accept_packed
  *                        the LM-head weights rearranged once into the
  *                        kernel's tile order, and the LM head reading them
+ *   ee_prompt_slots / ee_rope_append / ee_prompt_attn / ee_chunk_attn
+ *                        prompt intake: cache pages and slots for new tokens,
+ *                        rotary positions and the K/V write into the slots,
+ *                        causal attention of whole prompts and of chunks of
+ *                        them over the cache the steps above read
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -72,6 +77,7 @@ extern "C" {
 #define EE_MAX_MATCHES 1024
 #define EE_MAX_LM_NODES 2048
 #define EE_MAX_CHAIN 2048   /* nodes of one linear draft (long reuse drafts) */
+#define EE_MAX_SEQS 4096    /* sequences of one ee_prompt_slots call */
 
 typedef uint16_t ee_bf16;                 /* raw bfloat16 bits */
 typedef struct CUstream_st* ee_stream_t;  /* same type as cudaStream_t */
@@ -87,9 +93,11 @@ typedef enum {
 
 /* Bits of the device error word. */
 #define EE_DEVERR_MATCH_ARGS   0x01  /* cursor < 0 or orig_off decreasing */
-#define EE_DEVERR_TREE         0x02  /* parent[] violates 0 <= parent[i] < i, or T outside 1..128 */
-#define EE_DEVERR_PAGE         0x04  /* block_table entry outside [0, num_pages) for a needed slot */
-#define EE_DEVERR_CTX          0x08  /* ctx_len < 0 or above the max_ctx passed by the host */
+#define EE_DEVERR_TREE         0x02  /* parent[] violates 0 <= parent[i] < i, or T outside 1..128; tok_off decreasing
+                                        or outside [0, total] */
+#define EE_DEVERR_PAGE         0x04  /* block_table entry outside [0, num_pages) for a needed slot; no free page left */
+#define EE_DEVERR_CTX          0x08  /* ctx_len < 0 or above the max_ctx passed by the host; a length or position out
+                                        of range */
 #define EE_DEVERR_FP16_RANGE   0x10  /* reserved (no current kernel sets it) */
 #define EE_DEVERR_TIMEOUT      0x20  /* a bounded device wait gave up: arrival counts may be left part-way, so the
                                         next call needs ee_workspace_init first */
@@ -537,6 +545,130 @@ ee_status ee_kv_compact_inplace(ee_bf16* k_cache, ee_bf16* v_cache, int64_t cach
                                 const int32_t* path, const int32_t* accept_len, int32_t B,
                                 int32_t total_nodes, int32_t max_T, int32_t n_kv, int32_t head_dim,
                                 int32_t* dst_slot, void* ws, size_t ws_bytes, ee_stream_t stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Prompt intake.  A session's prompt (the instruction and the original code,
+ * Sec. III-A) has to be in the paged cache before its first verification step;
+ * the paper leaves this to its serving framework.  New tokens of all sequences
+ * are PACKED: sequence s owns tokens tok_off[s] .. tok_off[s+1]-1 (T_s >= 0 of
+ * them), token i of it has position ctx_len[s] + i.  A pass is
+ *
+ *   ee_prompt_slots (once), then per layer  projection (the caller's)
+ *     -> ee_rope_append -> ee_prompt_attn or ee_chunk_attn
+ *
+ * and leaves the cache, block table and context lengths as the verification
+ * entry points take them.  Queries, keys and values are
+ * [tokens][heads][head_dim] with the heads of a token contiguous and
+ * `*_stride` elements from one token to the next (a multiple of 8, at least
+ * heads * head_dim): views of one fused projection's output need no copy.
+ *
+ * ee_prompt_workspace_size: workspace bytes of the four calls at any size
+ * (device error word and partial results of split attention work; 44.9 MB).
+ * A larger workspace, also one that the verification entry points use, does
+ * as well.
+ */
+size_t ee_prompt_workspace_size(void);
+
+/*
+ * ee_prompt_slots -- cache pages, positions and slots of new tokens, from
+ * lengths that live on the device.  Sequence s holds held[s] pages
+ * (block_table[s][0 .. held[s]) ) with ctx_len[s] tokens in them and receives
+ * new_len[s] >= 0 more.  It needs ceil((ctx + new + reserve) / EE_PAGE) pages
+ * (none when ctx + new == 0): `reserve` positions past the new tokens, e.g.
+ * for the draft trees of the steps that follow.  Pages it lacks come from the
+ * end of the free list: with n counting all pages given in this call, sequence
+ * by sequence and in position order, the n-th is free_pages[*free_cnt - 1 - n].
+ *   ctx_len, new_len, held int32 [B]; block_table int32 [B][max_pages] in/out:
+ *     only entries [held, held_out) are written
+ *   free_pages int32 [n_free], free_cnt int32 [1] (0 <= *free_cnt <= n_free)
+ *   total      tokens the caller packed: the sum of new_len
+ *   tok_off    int32 [B+1] out: exclusive sum of new_len
+ *   pos        int32 [total] out: position of each packed token
+ *   slot       int32 [total] out: page * EE_PAGE + position % EE_PAGE
+ *   ctx_out, held_out int32 [B], free_out int32 [1] out: the lengths, pages
+ *     held and free pages afterwards; they must not alias their inputs, which
+ *     stay as they are (a call may be repeated)
+ * Device errors: EE_DEVERR_CTX for a negative length or page count, a context
+ * that its pages do not hold or a sequence that max_pages do not hold (it gets
+ * no tokens and no pages), and for a sum of new_len other than `total` (tokens
+ * past `total` are dropped, surplus entries get pos and slot -1).
+ * EE_DEVERR_PAGE when the free list is too short: then no sequence gets pages,
+ * every slot is -1, and ctx_out, held_out and free_out repeat the inputs; and
+ * for a free page outside [0, num_pages), whose tokens get slot -1.
+ * 1 <= B <= EE_MAX_SEQS; num_pages and max_pages below 2^27, total and reserve
+ * at most 2^30.
+ */
+ee_status ee_prompt_slots(const int32_t* ctx_len, const int32_t* new_len, const int32_t* held, int32_t B,
+                          int32_t total, int32_t reserve, int32_t* block_table, int32_t max_pages,
+                          const int32_t* free_pages, int32_t n_free, const int32_t* free_cnt, int32_t num_pages,
+                          int32_t* tok_off, int32_t* pos, int32_t* slot, int32_t* ctx_out, int32_t* held_out,
+                          int32_t* free_out, void* ws, size_t ws_bytes, ee_stream_t stream);
+
+/*
+ * ee_rope_append -- rotary positions and the cache write, ONE layer: with (c, s)
+ * = the cosine and sine of token t's position for pair i < head_dim / 2,
+ *   (x[i], x[i + 64]) -> (x[i] c - x[i + 64] s, x[i + 64] c + x[i] s)
+ * for every head of q (to q_out) and k; rotated k and v as it is go to the
+ * cache at slot[t], rotated k also to k_out when it is not NULL.  fp32, rounded
+ * once to bf16.
+ *   rope  fp32 [n_pos][head_dim]: cosines of a position's 64 pairs, then sines
+ *   pos, slot int32 [total] (from ee_prompt_slots); slot -1: no cache write
+ *   q_out may be q, and k_out may be k, with the same stride (in place)
+ *   k_cache/v_cache bf16 [num_pages][n_kv][EE_PAGE][head_dim], this layer's
+ * Tokens of one call must have distinct slots.  head_dim must be 128; bf16
+ * arrays and rope 16-byte aligned.
+ * Device errors: EE_DEVERR_CTX (a position outside [0, n_pos): the token is
+ * skipped), EE_DEVERR_PAGE (a slot below -1 or past the cache: not written).
+ */
+ee_status ee_rope_append(const ee_bf16* q, int64_t q_stride, const ee_bf16* k, int64_t k_stride,
+                         const ee_bf16* v, int64_t v_stride, const float* rope, int32_t n_pos,
+                         const int32_t* pos, const int32_t* slot, int32_t total, int32_t n_q, int32_t n_kv,
+                         int32_t head_dim, ee_bf16* q_out, int64_t q_out_stride, ee_bf16* k_out_or_null,
+                         int64_t k_out_stride, ee_bf16* k_cache, ee_bf16* v_cache, int32_t num_pages,
+                         void* ws, size_t ws_bytes, ee_stream_t stream);
+
+/*
+ * ee_prompt_attn -- causal attention of whole prompts over their own packed
+ * K/V, ONE layer: token i of a sequence attends to its tokens 0 .. i,
+ *   out[i][h] = sum_j softmax_j(scale * q[i][h] . k_j) v_j,  KV head h / (n_q/n_kv),
+ *   lse[i][h] = ln sum_j exp(scale * q[i][h] . k_j)         (when not NULL).
+ *   q, k, v bf16, strided as above (k rotated: ee_rope_append's k_out)
+ *   tok_off int32 [B+1]; sequences of any length, none included
+ *   out     bf16 [total][n_q][head_dim], lse_or_null fp32 [total][n_q]
+ * Tokens outside every sequence are not written.  Values of tokens a query does
+ * not see never reach its output, whatever they hold.  Scores, softmax
+ * statistics and sums are fp32; probabilities are rounded to bf16 for the
+ * product with V (as their sum is not, the error of an output is about the
+ * output's own rounding).  head_dim must be 128, n_q a multiple of n_kv with at
+ * most 128 query heads per KV head; arrays 16-byte aligned.
+ * Device errors: EE_DEVERR_TREE (a bad tok_off: that sequence is skipped),
+ * EE_DEVERR_TIMEOUT (outputs undefined).
+ */
+ee_status ee_prompt_attn(const ee_bf16* q, int64_t q_stride, const ee_bf16* k, int64_t k_stride,
+                         const ee_bf16* v, int64_t v_stride, const int32_t* tok_off, int32_t B, int32_t total,
+                         int32_t n_q, int32_t n_kv, int32_t head_dim, float scale, ee_bf16* out,
+                         float* lse_or_null, void* ws, size_t ws_bytes, ee_stream_t stream);
+
+/*
+ * ee_chunk_attn -- the same attention of a chunk of new tokens over the paged
+ * cache, which holds the sequence's context and the chunk itself (written by
+ * ee_rope_append): token i of sequence s attends to positions 0 .. ctx_len[s] +
+ * i.  Chunks of any length, from the single tokens of plain decoding to a whole
+ * prompt (ctx_len 0), mixed in one call; unlike ee_chain_verify_attn there is no
+ * limit on the chunk and the output is bf16.
+ *   ctx_len int32 [B]: positions BEFORE the chunk; block_table int32
+ *   [B][max_pages] with a page for each of a sequence's ctx_len + T positions
+ * Other arguments, precision and errors as ee_prompt_attn.  A missing page sets
+ * EE_DEVERR_PAGE and its keys are skipped; a query whose every key is skipped
+ * gets out 0 and lse -inf.  EE_DEVERR_CTX: a negative ctx_len or more positions
+ * than max_pages hold (the sequence is skipped).
+ */
+ee_status ee_chunk_attn(const ee_bf16* q, int64_t q_stride, const ee_bf16* k_cache, const ee_bf16* v_cache,
+                        int32_t num_pages, const int32_t* block_table, int32_t max_pages,
+                        const int32_t* ctx_len, const int32_t* tok_off, int32_t B, int32_t total, int32_t n_q,
+                        int32_t n_kv, int32_t head_dim, float scale, ee_bf16* out, float* lse_or_null, void* ws,
+                        size_t ws_bytes, ee_stream_t stream);
 
 #ifdef __cplusplus
 }

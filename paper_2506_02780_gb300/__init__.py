@@ -22,6 +22,7 @@ EE_PAGE = 16
 EE_HEAD_DIM = 128
 EE_MAX_TREE = 128
 EE_MAX_LM_NODES = 2048
+EE_MAX_SEQS = 4096
 
 STATUS = {0: "ok", 1: "invalid argument", 2: "unsupported configuration", 3: "CUDA error",
           4: "device error word set", 5: "workspace too small"}
@@ -34,7 +35,8 @@ EXPORTS = ("ee_version", "ee_status_string", "ee_workspace_size", "ee_workspace_
            "ee_lmhead_accept", "ee_lmhead_verify", "ee_lmhead_accept_static", "ee_kv_compact",
            "ee_selftest_timeout", "ee_tree_verify_attn_inplace", "ee_kv_compact_inplace",
            "ee_chain_verify_attn", "ee_build_reuse_tree", "ee_advance", "ee_lmhead_packed_bytes",
-           "ee_lmhead_pack_weights", "ee_lmhead_accept_packed")
+           "ee_lmhead_pack_weights", "ee_lmhead_accept_packed", "ee_prompt_workspace_size", "ee_prompt_slots",
+           "ee_rope_append", "ee_prompt_attn", "ee_chunk_attn")
 
 VERIFY_MODES = {"greedy": 0, "direct": 1, "topk": 2, "entropy": 3}
 
@@ -90,6 +92,12 @@ _SIGS = {
     "ee_kv_compact": ([_P, _P, _I64, _P, _P, _I64, _I, _I, _P, _I, _P, _P, _P, _P, _P, _I, _I, _I, _I,
                        _P, _P, _SZ, _P], _I),
     "ee_selftest_timeout": ([_P, _SZ, _P, _P], _I),
+    "ee_prompt_workspace_size": ([], _SZ),
+    "ee_prompt_slots": ([_P, _P, _P, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P, _P, _P, _P, _P, _P, _P, _SZ, _P], _I),
+    "ee_rope_append": ([_P, _I64, _P, _I64, _P, _I64, _P, _I, _P, _P, _I, _I, _I, _I, _P, _I64, _P, _I64, _P, _P, _I,
+                        _P, _SZ, _P], _I),
+    "ee_prompt_attn": ([_P, _I64, _P, _I64, _P, _I64, _P, _I, _I, _I, _I, _I, _F, _P, _P, _P, _SZ, _P], _I),
+    "ee_chunk_attn": ([_P, _I64, _P, _P, _I, _P, _I, _P, _P, _I, _I, _I, _I, _I, _F, _P, _P, _P, _SZ, _P], _I),
 }
 
 
@@ -117,6 +125,20 @@ def _p(t):
     if not t.is_contiguous():
         raise ValueError("libee takes contiguous tensors only")
     return ctypes.c_void_p(t.data_ptr())
+
+
+def _rows(t, name):
+    """(pointer, token stride) of a [tokens, heads, head_dim] bf16 tensor whose heads
+    are contiguous within a token: a view of a fused projection's output will do."""
+    if t is None:
+        return None, 0
+    _check(t, torch.bfloat16, name)
+    if not t.is_cuda:
+        raise ValueError("libee takes CUDA tensors only")
+    n, h, d = t.shape
+    if (n and h > 1 and t.stride(1) != d) or (n and t.stride(2) != 1):
+        raise ValueError(f"the heads of {name} must be contiguous within a token")
+    return t.data_ptr(), (t.stride(0) if n > 1 else h * d)
 
 
 def _check(t, dtype, name):
@@ -379,3 +401,109 @@ def ee_advance(out_tok, out_len, draft_tok, cpos, node_off, path, accept_len, bo
         lib().ee_advance(_p(out_tok), _p(out_len), cap, _p(draft_tok), _p(cpos), _p(node_off), _p(path),
                          _p(accept_len), _p(bonus), B, draft_tok.numel(), path.shape[1], tail.shape[1], _p(tail),
                          _p(cursor), _p(last_tok), _p(ws), ws.numel(), _stream(stream)))
+
+
+def ee_prompt_workspace_size() -> int:
+    return int(lib().ee_prompt_workspace_size())
+
+
+def new_prompt_workspace(device="cuda", stream=None):
+    """Allocate (through torch) and zero a workspace for the prompt-intake calls."""
+    ws = torch.empty(ee_prompt_workspace_size(), dtype=torch.uint8, device=device)
+    ee_workspace_init(ws, stream)
+    return ws
+
+
+def _i32s(**tensors):
+    for name, t in tensors.items():
+        _check(t, torch.int32, name)
+
+
+def ee_prompt_slots(ctx_len, new_len, held, block_table, free_pages, free_cnt, num_pages, reserve, tok_off, pos, slot,
+                    ctx_out, held_out, free_out, ws, stream=None):
+    """Pages, positions and slots of new tokens from their lengths (all on the device);
+    `pos` and `slot` have one entry for each packed token."""
+    _i32s(ctx_len=ctx_len, new_len=new_len, held=held, block_table=block_table, free_pages=free_pages,
+          free_cnt=free_cnt, tok_off=tok_off, pos=pos, slot=slot, ctx_out=ctx_out, held_out=held_out, free_out=free_out)
+    B, max_pages = block_table.shape
+    total = pos.numel()
+    if not (ctx_len.numel() == new_len.numel() == held.numel() == ctx_out.numel() == held_out.numel() == B
+            and tok_off.numel() == B + 1 and slot.numel() == total and free_cnt.numel() == free_out.numel() == 1):
+        raise ValueError("ee_prompt_slots: lengths need B entries, tok_off B + 1, slot as many as pos, the counts one")
+    st = lib().ee_prompt_slots(_p(ctx_len), _p(new_len), _p(held), B, total, int(reserve), _p(block_table), max_pages,
+                               _p(free_pages), free_pages.numel(), _p(free_cnt), int(num_pages), _p(tok_off), _p(pos),
+                               _p(slot), _p(ctx_out), _p(held_out), _p(free_out), _p(ws), ws.numel(), _stream(stream))
+    _ok("ee_prompt_slots", st)
+
+
+def ee_rope_append(q, k, v, rope, pos, slot, q_out, k_cache, v_cache, ws, k_out=None, stream=None):
+    """Rotary positions of q (to q_out) and k, and the write of k and v into the cache
+    at `slot` (one layer); q, k, v, q_out and k_out [tokens, heads, 128] may be views of
+    wider rows, q_out may be q and k_out may be k."""
+    _i32s(pos=pos, slot=slot)
+    _check(rope, torch.float32, "rope")
+    _check(k_cache, torch.bfloat16, "k_cache")
+    _check(v_cache, torch.bfloat16, "v_cache")
+    total, n_q, d = q.shape
+    n_kv = k.shape[1]
+    num_pages = k_cache.shape[0]
+    if (k.shape != (total, n_kv, d) or v.shape != k.shape or q_out.shape != q.shape or pos.numel() != total
+            or slot.numel() != total or rope.dim() != 2 or rope.shape[1] != d
+            or k_cache.shape != (num_pages, n_kv, EE_PAGE, d) or v_cache.shape != k_cache.shape
+            or (k_out is not None and k_out.shape != k.shape)):
+        raise ValueError("ee_rope_append: shapes do not fit together")
+    qp, qs = _rows(q, "q")
+    kp, ks = _rows(k, "k")
+    vp, vs = _rows(v, "v")
+    op, os_ = _rows(q_out, "q_out")
+    rp, rs = _rows(k_out, "k_out")
+    st = lib().ee_rope_append(qp, qs, kp, ks, vp, vs, _p(rope), rope.shape[0], _p(pos), _p(slot), total, n_q, n_kv, d,
+                              op, os_, rp, rs, _p(k_cache), _p(v_cache), num_pages, _p(ws), ws.numel(),
+                              _stream(stream))
+    _ok("ee_rope_append", st)
+
+
+def _attn_outputs(out, lse, total, n_q, d):
+    _check(out, torch.bfloat16, "out")
+    if out.shape != (total, n_q, d):
+        raise ValueError("out must have the shape of q")
+    if lse is not None:
+        _check(lse, torch.float32, "lse")
+        if lse.shape != (total, n_q):
+            raise ValueError("lse must be [tokens, query heads]")
+
+
+def ee_prompt_attn(q, k, v, tok_off, scale, out, ws, lse=None, stream=None):
+    """Causal attention of packed whole prompts over their own K/V (one layer)."""
+    _i32s(tok_off=tok_off)
+    total, n_q, d = q.shape
+    n_kv = k.shape[1]
+    if k.shape != (total, n_kv, d) or v.shape != k.shape:
+        raise ValueError("k and v must be [tokens, KV heads, head_dim] for q's tokens")
+    _attn_outputs(out, lse, total, n_q, d)
+    qp, qs = _rows(q, "q")
+    kp, ks = _rows(k, "k")
+    vp, vs = _rows(v, "v")
+    st = lib().ee_prompt_attn(qp, qs, kp, ks, vp, vs, _p(tok_off), tok_off.numel() - 1, total, n_q, n_kv, d,
+                              float(scale), _p(out), _p(lse), _p(ws), ws.numel(), _stream(stream))
+    _ok("ee_prompt_attn", st)
+
+
+def ee_chunk_attn(q, k_cache, v_cache, block_table, ctx_len, tok_off, scale, out, ws, lse=None, stream=None):
+    """Causal attention of chunks of new tokens whose K/V sit at cache positions
+    ctx + i, after ctx cached ones (one layer)."""
+    _i32s(block_table=block_table, ctx_len=ctx_len, tok_off=tok_off)
+    _check(k_cache, torch.bfloat16, "k_cache")
+    _check(v_cache, torch.bfloat16, "v_cache")
+    total, n_q, d = q.shape
+    num_pages, n_kv = k_cache.shape[0], k_cache.shape[1]
+    B, max_pages = block_table.shape
+    if (k_cache.shape != (num_pages, n_kv, EE_PAGE, d) or v_cache.shape != k_cache.shape or ctx_len.numel() != B
+            or tok_off.numel() != B + 1):
+        raise ValueError("ee_chunk_attn: shapes do not fit together")
+    _attn_outputs(out, lse, total, n_q, d)
+    qp, qs = _rows(q, "q")
+    st = lib().ee_chunk_attn(qp, qs, _p(k_cache), _p(v_cache), num_pages, _p(block_table), max_pages, _p(ctx_len),
+                             _p(tok_off), B, total, n_q, n_kv, d, float(scale), _p(out), _p(lse), _p(ws), ws.numel(),
+                             _stream(stream))
+    _ok("ee_chunk_attn", st)

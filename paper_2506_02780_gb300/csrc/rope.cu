@@ -1,0 +1,172 @@
+// ee_rope_append: rotary positions of a layer's packed q and k, and the write of
+// rotated k and of v into the paged cache.
+//
+// The pair (x[i], x[i + 64]) of every head is turned by its position's angle; the
+// table holds 64 cosines and 64 sines of each position in fp32.  Bound by HBM: a
+// token's (n_q + 2 n_kv) heads of 256 bytes are read and written once, its 512 table
+// bytes once.  Eight lanes hold a head: lane j its elements 8 j .. 8 j + 7 and 64 + 8 j
+// .. 64 + 8 j + 7 (two 16-byte accesses, both halves of each of its pairs), so a
+// warp turns four heads at a time, and the sixteen cosines and sines of a lane stay
+// in its registers while the warp walks the token's heads.
+#include "ee_common.cuh"
+
+namespace {
+
+constexpr int kD = EE_HEAD_DIM;
+constexpr int kThreads = 128;
+constexpr int kWarps = kThreads / 32;
+constexpr int kPer = 4;      // heads a warp turns at once
+constexpr int kUnroll = 3;   // rounds of loads in flight
+
+struct RopeParams {
+  const __nv_bfloat16 *q, *k, *v;
+  __nv_bfloat16 *q_out, *k_out, *k_cache, *v_cache;
+  int64_t q_stride, k_stride, v_stride, qo_stride, ko_stride;
+  const float* rope;
+  const int32_t *pos, *slot;
+  int32_t* err;
+  int total, n_q, n_kv, n_pos, num_pages;
+  int wpt;                   // warps that share a token's heads
+};
+
+// (a, b) -> (a c - b s, b c + a s) on eight pairs of bf16
+__device__ __forceinline__ void turn8(uint4& a, uint4& b, const float (&c)[8], const float (&s)[8]) {
+  uint32_t* pa = reinterpret_cast<uint32_t*>(&a);
+  uint32_t* pb = reinterpret_cast<uint32_t*>(&b);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(pa + i));
+    const float2 y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(pb + i));
+    const __nv_bfloat162 u = __floats2bfloat162_rn(fmaf(x.x, c[2 * i], -(y.x * s[2 * i])),
+                                                   fmaf(x.y, c[2 * i + 1], -(y.y * s[2 * i + 1])));
+    const __nv_bfloat162 w = __floats2bfloat162_rn(fmaf(y.x, c[2 * i], x.x * s[2 * i]),
+                                                   fmaf(y.y, c[2 * i + 1], x.y * s[2 * i + 1]));
+    pa[i] = *reinterpret_cast<const uint32_t*>(&u);
+    pb[i] = *reinterpret_cast<const uint32_t*>(&w);
+  }
+}
+
+__global__ void __launch_bounds__(kThreads) rope_append_kernel(const RopeParams p) {
+  ee::pdl_allow_next();
+  ee::pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const int64_t w = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  const int t = (int)(w / p.wpt), part = (int)(w - (int64_t)t * p.wpt);
+  if (t >= p.total) return;
+  const int pos = p.pos[t];
+  int slot = p.slot[t];
+  if (pos < 0 || pos >= p.n_pos) {
+    if (lane == 0 && part == 0) ee::flag_error(p.err, EE_DEVERR_CTX);
+    return;
+  }
+  if (slot < 0 || slot >= p.num_pages * EE_PAGE) {
+    if (slot != -1 && lane == 0 && part == 0) ee::flag_error(p.err, EE_DEVERR_PAGE);
+    slot = -1;
+  }
+  const int sub = lane >> 3, j = 8 * (lane & 7);
+  float c[8], s[8];
+  {
+    const float4* cs = reinterpret_cast<const float4*>(p.rope + (size_t)pos * kD + j);
+    *reinterpret_cast<float4*>(&c[0]) = cs[0];
+    *reinterpret_cast<float4*>(&c[4]) = cs[1];
+    *reinterpret_cast<float4*>(&s[0]) = cs[16];
+    *reinterpret_cast<float4*>(&s[4]) = cs[17];
+  }
+  // heads: q, then k, then v; cache row of KV head h: base + h * EE_PAGE rows
+  const int nh = p.n_q + 2 * p.n_kv;
+  const size_t crow = slot < 0 ? 0 : ((size_t)(slot / EE_PAGE) * p.n_kv * EE_PAGE + slot % EE_PAGE) * kD;
+  const int step = kPer * p.wpt;
+  for (int h0 = kPer * part + sub; h0 < nh; h0 += kUnroll * step) {
+    uint4 a[kUnroll], b[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int h = h0 + u * step;
+      if (h < nh) {
+        const __nv_bfloat16* src = h < p.n_q ? p.q + (size_t)t * p.q_stride + (size_t)h * kD
+                                   : h < p.n_q + p.n_kv
+                                       ? p.k + (size_t)t * p.k_stride + (size_t)(h - p.n_q) * kD
+                                       : p.v + (size_t)t * p.v_stride + (size_t)(h - p.n_q - p.n_kv) * kD;
+        a[u] = *reinterpret_cast<const uint4*>(src + j);
+        b[u] = *reinterpret_cast<const uint4*>(src + kD / 2 + j);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int h = h0 + u * step;
+      if (h >= nh) break;
+      if (h < p.n_q + p.n_kv) turn8(a[u], b[u], c, s);
+      if (h < p.n_q) {
+        __nv_bfloat16* dst = p.q_out + (size_t)t * p.qo_stride + (size_t)h * kD;
+        *reinterpret_cast<uint4*>(dst + j) = a[u];
+        *reinterpret_cast<uint4*>(dst + kD / 2 + j) = b[u];
+      } else {
+        const bool is_k = h < p.n_q + p.n_kv;
+        const int hk = h - p.n_q - (is_k ? 0 : p.n_kv);
+        if (is_k && p.k_out) {
+          __nv_bfloat16* dst = p.k_out + (size_t)t * p.ko_stride + (size_t)hk * kD;
+          *reinterpret_cast<uint4*>(dst + j) = a[u];
+          *reinterpret_cast<uint4*>(dst + kD / 2 + j) = b[u];
+        }
+        if (slot >= 0) {
+          __nv_bfloat16* dst = (is_k ? p.k_cache : p.v_cache) + crow + (size_t)hk * (EE_PAGE * kD);
+          *reinterpret_cast<uint4*>(dst + j) = a[u];
+          *reinterpret_cast<uint4*>(dst + kD / 2 + j) = b[u];
+        }
+      }
+    }
+  }
+}
+
+bool good_stride(int64_t stride, int heads) { return stride % 8 == 0 && stride >= (int64_t)heads * kD; }
+
+}  // namespace
+
+extern "C" ee_status ee_rope_append(const ee_bf16* q, int64_t q_stride, const ee_bf16* k, int64_t k_stride,
+                                    const ee_bf16* v, int64_t v_stride, const float* rope, int32_t n_pos,
+                                    const int32_t* pos, const int32_t* slot, int32_t total, int32_t n_q, int32_t n_kv,
+                                    int32_t head_dim, ee_bf16* q_out, int64_t q_out_stride, ee_bf16* k_out_or_null,
+                                    int64_t k_out_stride, ee_bf16* k_cache, ee_bf16* v_cache, int32_t num_pages,
+                                    void* ws, size_t ws_bytes, ee_stream_t stream) {
+  if (total < 0 || n_q < 1 || n_kv < 1 || n_pos < 1 || num_pages < 1) return EE_ERR_INVALID_ARG;
+  if (head_dim != EE_HEAD_DIM || num_pages >= (1 << 27) || n_q > (1 << 20) || n_kv > (1 << 20))
+    return EE_ERR_UNSUPPORTED;
+  if (total == 0) return EE_OK;
+  if (!q || !k || !v || !rope || !pos || !slot || !q_out || !k_cache || !v_cache || !ws || !ee::aligned(ws, 256))
+    return EE_ERR_INVALID_ARG;
+  if (!good_stride(q_stride, n_q) || !good_stride(k_stride, n_kv) || !good_stride(v_stride, n_kv) ||
+      !good_stride(q_out_stride, n_q) || (k_out_or_null && !good_stride(k_out_stride, n_kv)))
+    return EE_ERR_INVALID_ARG;
+  for (const void* a : {(const void*)q, (const void*)k, (const void*)v, (const void*)rope, (const void*)q_out,
+                        (const void*)k_out_or_null, (const void*)k_cache, (const void*)v_cache})
+    if (!ee::aligned(a, 16)) return EE_ERR_INVALID_ARG;
+  if (ws_bytes < ee::kWorkspaceBytes) return EE_ERR_WORKSPACE;
+  RopeParams p;
+  p.q = reinterpret_cast<const __nv_bfloat16*>(q);
+  p.k = reinterpret_cast<const __nv_bfloat16*>(k);
+  p.v = reinterpret_cast<const __nv_bfloat16*>(v);
+  p.q_out = reinterpret_cast<__nv_bfloat16*>(q_out);
+  p.k_out = reinterpret_cast<__nv_bfloat16*>(k_out_or_null);
+  p.k_cache = reinterpret_cast<__nv_bfloat16*>(k_cache);
+  p.v_cache = reinterpret_cast<__nv_bfloat16*>(v_cache);
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.qo_stride = q_out_stride;
+  p.ko_stride = k_out_stride;
+  p.rope = rope;
+  p.pos = pos;
+  p.slot = slot;
+  p.err = ee::err_word(ws);
+  p.total = total;
+  p.n_q = n_q;
+  p.n_kv = n_kv;
+  p.n_pos = n_pos;
+  p.num_pages = num_pages;
+  // one warp walks a token's heads, several where the tokens alone leave SMs idle
+  const int rounds = (n_q + 2 * n_kv + kPer - 1) / kPer;
+  const int64_t warps = (int64_t)ee::kNumSMs * 32;
+  p.wpt = (int)std::min<int64_t>(rounds, std::max<int64_t>(1, warps / total));
+  const int64_t grid = ((int64_t)total * p.wpt + kWarps - 1) / kWarps;
+  EE_CUDA_OK(ee::launch_pdl(rope_append_kernel, dim3((unsigned)grid), dim3(kThreads), 0, (cudaStream_t)stream, 1, p));
+  return EE_OK;
+}
