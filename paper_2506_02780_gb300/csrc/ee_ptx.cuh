@@ -220,6 +220,17 @@ __device__ __forceinline__ bool wait_count_geq(const uint32_t* cnt, uint32_t tar
     if (cycles() - t0 > kWaitLimitCycles) return false;
   return true;
 }
+// gpu-scope release increment that wraps from `last` to zero, and the bounded wait of
+// an arriver for the wrap
+__device__ __forceinline__ void red_inc_release(uint32_t* a, uint32_t last) {
+  asm volatile("red.release.gpu.global.inc.u32 [%0], %1;" ::"l"(a), "r"(last) : "memory");
+}
+__device__ __forceinline__ bool wait_count_zero(const uint32_t* cnt) {
+  const long long t0 = cycles();
+  while (ld_acquire(cnt) != 0)
+    if (cycles() - t0 > kWaitLimitCycles) return false;
+  return true;
+}
 // gpu-scope release add / acquire load on a 64-bit count, and a bounded wait for
 // it to reach `target` (false when the time limit passed first)
 __device__ __forceinline__ void red_add_release64(unsigned long long* a, unsigned long long v) {

@@ -16,10 +16,10 @@
 // Work.  The keys of all units (plus a constant for each: a unit's start and end) are
 // laid on one line, cut into equal shares, one for each CTA; one CTA runs on each SM.
 // A share may begin and end inside a unit.  Such a unit's pieces leave (m, l) and the
-// unnormalised O in the workspace, count their tiles done and, once all are, each
-// merge a part of the rows and columns with weights 2^(m - max).  Every length follows
-// from the device's offsets: long prompts, ragged batches and single tokens over long
-// contexts are one case.  The launch is cooperative, so a wait for another CTA ends.
+// unnormalised O in the workspace, meet at a count and each merge a part of the rows
+// and columns with weights 2^(m - max).  Every length follows from the device's
+// offsets: long prompts, ragged batches and single tokens over long contexts are one
+// case.  The launch is cooperative, so a wait for another CTA ends.
 //
 // Roles of a CTA's twelve warps; all walk the share's segments (tile ranges of units)
 // by themselves, from a ring the scheduler fills:
@@ -28,9 +28,9 @@
 //          next (whose S takes the place of P: MMAs of one thread run in order);
 //   2      finds the segments, streams Q;
 //   3      cleans V where the causal edge or the sequence's end lies in a tile: the
-//          MMA multiplies masked rows by P = 0, and 0 times a NaN is a NaN.  Rows past
-//          the unit are zeroed, non-finite values of rows that some query must not see
-//          are zeroed and added at the end for the queries that do;
+//          MMA multiplies masked rows by P = 0, and 0 times a NaN is a NaN.  Non-finite
+//          values of rows that some query must not see are zeroed, and added at the end
+//          for the queries that do;
 //   4-7    softmax of row tile A, one row per thread; 8-11 of row tile B.
 // TMEM: S/P of A and B, O of A and B, 128 columns each.
 #include "ee_common.cuh"
@@ -50,20 +50,24 @@ constexpr int kZones = 4;                     // cleaned V tiles in flight (at m
 constexpr int kMasks = 8;                     // page masks in flight (K runs at most 4 tiles ahead of the softmax)
 constexpr uint32_t kHalf = kKT * 128;         // 64 of a tile's 128 columns
 constexpr uint32_t kTile = 2 * kHalf;         // 32 KB
-constexpr uint32_t kOffKV = 0, kOffQ = kRing * kTile, kOffBar = kOffQ + 2 * kTile;
-constexpr uint32_t kNumBars = 2 * kRing + 4 + 8 + 2 * kSegs + kZones + 1;
+constexpr uint32_t kOffKV = 0, kOffQ = kRing * kTile, kOffOut = kOffQ + 2 * kTile;
+constexpr uint32_t kOutBytes = 32 * 64;       // a softmax warp's rows x 32 columns of bf16, on their way out
+constexpr uint32_t kOffBar = kOffOut + 8 * kOutBytes;
+constexpr uint32_t kNumBars = 2 * kRing + 4 + 10 + 2 * kSegs + kZones + 1;
 constexpr uint32_t kSmemBytes = 1024 + kOffBar + 8 * kNumBars;
 constexpr uint32_t kTmemCols = 512, kColO = 256;
 constexpr float kRescaleLog2 = 8.0f;          // O is rescaled when a maximum grows by 2^8
 // work in keys: a unit's own constant, and the smallest share of a CTA
 constexpr int kUnitKeys = 3 * kKT, kMinShare = 5 * kKT;
+static_assert(kMinShare >= kKT, "every CTA between a unit's first and last piece holds one");
 constexpr int kWarpKV = 0, kWarpMma = 1, kWarpQ = 2, kWarpClean = 3, kWarpSoft = 4;
 constexpr int kSegReaders = 3 + 8;            // warps 0, 1, 3 and the softmax warps
 constexpr int kRegsLaunch = 168, kRegsSoft = 208, kRegsOther = 88;
+static_assert(kRing == 4, "two slots each for K and V tiles");
 static_assert(256 * kRegsSoft + 128 * kRegsOther <= kThreads * kRegsLaunch, "register split");
-static_assert(kSmemBytes <= 227 * 1024 - 4096, "shared memory budget");
-// counters of a split unit in the trailer of its first piece's slot, past the word
-// that the verification attention keeps there
+static_assert(kSmemBytes <= 227 * 1024 - 1024, "shared memory budget");
+// count of a split unit's finished pieces, in the trailer of its first piece's slot
+// past the word that the verification attention keeps there
 constexpr size_t kCntOff = kAttnCntOff + 64;
 
 struct PromptParams {
@@ -78,6 +82,15 @@ struct PromptParams {
   float scale, scale_log2;
 };
 
+// The code that a CTA runs over and over is kept small (loops over the two row tiles
+// and over column blocks stay rolled, rare paths are calls): warps of six kinds
+// share one instruction cache, and a segment's start and end run all of it.
+__device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return mbar_wait(bar, parity, abort_flag);
+}
+__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return mbar_try(bar, parity) || wait_slow(bar, parity, abort_flag);
+}
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -92,6 +105,43 @@ __device__ __forceinline__ float fmax3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
+}
+
+// the largest of a row's 128 scores (a NaN is passed over)
+__device__ __forceinline__ float row_max(const uint32_t (&sr)[128]) {
+  float mx[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) mx[k] = fmaxf(__uint_as_float(sr[k]), __uint_as_float(sr[8 + k]));
+#pragma unroll
+  for (int c = 16; c < 128; c += 16)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) mx[k] = fmax3(mx[k], __uint_as_float(sr[c + k]), __uint_as_float(sr[c + 8 + k]));
+  return fmax3(fmax3(mx[0], mx[1], mx[2]), fmax3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7]));
+}
+
+// P = 2^(S sl2 + nms) of half a row, rounded to bf16 over S in tensor memory; the fp32
+// values' sums in ls (set by half 0, added to by half 1).  Scale and shift and the sums
+// take one packed instruction a pair of columns.
+template <int kHalfRow>
+__device__ __forceinline__ void exp_half(const uint32_t (&sr)[128], uint32_t tS, float sl2, float nms,
+                                         uint64_t (&ls)[4]) {
+  const uint64_t sl2x2 = f2_pack(__float_as_uint(sl2), __float_as_uint(sl2));
+  const uint64_t nmsx2 = f2_pack(__float_as_uint(nms), __float_as_uint(nms));
+#pragma unroll
+  for (int c = 2 * kHalfRow; c < 2 * kHalfRow + 2; ++c) {
+    uint32_t pw[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int x = 32 * c + 2 * e;
+      uint32_t y0, y1;
+      f2_unpack(f2_fma(f2_pack(sr[x], sr[x + 1]), sl2x2, nmsx2), y0, y1);
+      const float p0 = ex2(__uint_as_float(y0)), p1 = ex2(__uint_as_float(y1));
+      const uint64_t pp = f2_pack(__float_as_uint(p0), __float_as_uint(p1));
+      ls[e & 3] = c == 0 && e < 4 ? pp : f2_add(ls[e & 3], pp);
+      pw[e] = bf16x2_rn(p1, p0);
+    }
+    tc_st16_nowait(tS + 16 * c, pw);
+  }
 }
 
 // One sequence: first token, tokens, cached positions (T = 0: nothing to do).
@@ -135,8 +185,13 @@ __device__ __forceinline__ int tiles_before(int64_t y, int n) {
   const int64_t j = (y - kUnitKeys + kKT / 2) >> 7;
   return (int)min(max(j, (int64_t)0), (int64_t)n);
 }
-// start of CTA c's share of W places cut for N
-__device__ __forceinline__ int64_t share_start(int64_t W, int N, int c) { return W * c / N; }
+// W places cut for N CTAs: CTA c's share starts at floor(c W / N)
+struct Shares {
+  int64_t W, q;
+  int N, r;
+  __device__ __forceinline__ Shares(int64_t w, int n) : W(w), q(w / n), N(n), r((int)(w - w / n * n)) {}
+  __device__ __forceinline__ int64_t start(int c) const { return q * c + (r * c) / N; }
+};
 
 // A segment: tiles [j0, j1) of a unit.
 struct Seg {
@@ -144,7 +199,7 @@ struct Seg {
   int hk, tok0;            // KV head, the unit's first token
   int j0, j1, n_tiles;     // n_tiles: of the whole unit; j1 = 0: no more segments
   int nA, nB;              // tiles each row tile needs (B: 0 without tokens)
-  int c0, c1;              // first and last CTA that may hold a piece
+  int c0, c1;              // first and last CTA that hold a piece
   int64_t X;               // the unit's first place
 };
 
@@ -163,66 +218,127 @@ __device__ __forceinline__ const __nv_bfloat16* v_row(const PromptParams& p, con
   }
 }
 
+// Adds the non-finite values of keys [key0, key1] to one row that sees them: to its
+// output `out`, or (out NULL) to its unnormalised O in the partial slot `part` (column
+// chunks of four, kRows apart).
+template <bool kPaged>
+__device__ __forceinline__ void add_nonfinite(const PromptParams& p, Seg s, int key0, int key1,
+                                           __nv_bfloat16* out, float* part) {
+#pragma unroll 1
+  for (int key = key0; key <= key1; ++key) {
+    const __nv_bfloat16* v = v_row<kPaged>(p, s, key);
+    if (!v) continue;
+#pragma unroll 1
+    for (int e = 0; e < kD; ++e) {
+      const float x = __bfloat162float(v[e]);
+      if (isfinite(x)) continue;
+      if (out) {
+        volatile uint16_t* o = reinterpret_cast<volatile uint16_t*>(out) + e;
+        *o = __bfloat16_as_ushort(__float2bfloat16_rn(__bfloat162float(__ushort_as_bfloat16(*o)) + x));
+      } else {
+        volatile float* o = part + (size_t)(e >> 2) * (4 * kRows) + (e & 3);
+        *o = *o + x;
+      }
+    }
+  }
+}
+
 __device__ __forceinline__ uint32_t nonfinite2(uint32_t x) {   // 0xffff in each half that is
   const uint32_t lo = (x & 0x7f80u) == 0x7f80u ? 0xffffu : 0u;
   const uint32_t hi = (x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
   return lo | hi;
 }
 
-// Rows and columns of a split unit merged by one of its pieces: thread t of nthr.
-// Items are (8-column group, row), the rows fastest, so that a warp's loads of a
-// piece's slot (column-chunk major) are contiguous.
-__device__ __forceinline__ void merge_piece(const PromptParams& p, const Seg& s, const int16_t* list, int K, int64_t lo,
-                                            int64_t hi, int t, int nthr) {
-  const int w = 2 * p.tpt;
-  const int nt = min(w, s.T - s.tok0);                       // tokens of the unit
+// (m, l, o) of one piece or lane joined to a running one
+struct Joined {
+  float M = -INFINITY, L = 0.f, a[8] = {};
+  __device__ __forceinline__ void add(float m, float l, const float (&o)[8]) {
+    const float m_new = fmaxf(M, m);
+    const float fa = M == m_new ? 1.f : ex2(M - m_new), fb = m == m_new ? 1.f : ex2(m - m_new);
+    M = m_new;
+    L = fmaf(L, fa, l * fb);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a[e] = fmaf(a[e], fa, o[e] * fb);
+  }
+};
+
+// Items [lo, hi) of a split unit merged by one of its pieces: thread t of nthr.  An
+// item is eight columns of a row, numbered rows fastest, so that a warp's loads of a
+// slot (column-chunk major) are contiguous.  A thread loads four items of a piece at a
+// time (a round trip to L2 costs about 1,000 cycles).  With few items and many pieces
+// `sub` lanes share an item, each over every sub-th piece.
+__device__ __forceinline__ void merge_items(const PromptParams& p, const Seg& s, int lo, int hi, int t, int nthr) {
+  constexpr int kItems = 4;
+  const int K = s.c1 - s.c0 + 1;
+  int sub = 1;
+  while (sub < 32 && sub < K && (hi - lo) * 2 * sub <= nthr) sub *= 2;
+  const int nt = min(2 * p.tpt, s.T - s.tok0);               // tokens of the unit
   const int rows_a = min(nt, p.tpt) * p.g, rows = nt * p.g;  // rows of A, of both
-  for (int64_t i = lo + t; i < hi; i += nthr) {
-    const int cg = (int)(i / rows), r = (int)(i - (int64_t)cg * rows);
-    const int st = r >= rows_a, rr = st ? r - rows_a : r;
-    float M = -INFINITY;
-    for (int k = 0; k < K; ++k)
-      if (list[k] >= 0)
-        M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(
-                                p.part + (size_t)(2 * list[k] + st) * kAttnPartBytes + kAttnMlOff) + rr).x);
-    float a[8] = {}, L = 0.f;
-#pragma unroll 4
-    for (int k = 0; k < K; ++k) {
-      if (list[k] < 0) continue;
-      const uint8_t* slot = p.part + (size_t)(2 * list[k] + st) * kAttnPartBytes;
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot + kAttnMlOff) + rr);
-      const float4* O = reinterpret_cast<const float4*>(slot) + (size_t)(2 * cg) * kRows + rr;
-      // a row without keys in the piece has l = 0 and no O (a sum that is NaN has one)
-      if (ml.y == 0.f) continue;
-      const float4 u = __ldcg(O), v = __ldcg(O + kRows);
-      const float f = ml.x == -INFINITY ? 1.f : ex2(ml.x - M);
-      L = fmaf(f, ml.y, L);
-      a[0] = fmaf(f, u.x, a[0]);
-      a[1] = fmaf(f, u.y, a[1]);
-      a[2] = fmaf(f, u.z, a[2]);
-      a[3] = fmaf(f, u.w, a[3]);
-      a[4] = fmaf(f, v.x, a[4]);
-      a[5] = fmaf(f, v.y, a[5]);
-      a[6] = fmaf(f, v.z, a[6]);
-      a[7] = fmaf(f, v.w, a[7]);
+  const int k0 = t & (sub - 1);
+  const int step = nthr / sub;
+  // whole warps walk together: the lanes of an item meet in shuffles
+#pragma unroll 1
+  for (int i0 = lo + t / sub; i0 - (t & 31) / sub < hi; i0 += kItems * step) {
+    Joined x[kItems];
+    int st[kItems], rr[kItems], cg[kItems];
+#pragma unroll
+    for (int n = 0; n < kItems; ++n) {
+      const int i = min(i0 + n * step, hi - 1);
+      cg[n] = i / rows;
+      const int r = i - cg[n] * rows;
+      st[n] = r >= rows_a;
+      rr[n] = st[n] ? r - rows_a : r;
     }
-    const float il = L == 0.f ? 0.f : 1.f / L;
-    const int tok = s.tok0 + (st ? p.tpt : 0) + rr / p.g, h = s.hk * p.g + rr % p.g;
-    const size_t row = (size_t)(s.o + tok) * p.n_q + h;
-    uint4 o;
-    o.x = bf16x2_rn(a[1] * il, a[0] * il);
-    o.y = bf16x2_rn(a[3] * il, a[2] * il);
-    o.z = bf16x2_rn(a[5] * il, a[4] * il);
-    o.w = bf16x2_rn(a[7] * il, a[6] * il);
-    *reinterpret_cast<uint4*>(p.out + row * kD + 8 * cg) = o;
-    if (cg == 0 && p.lse) p.lse[row] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+#pragma unroll 1
+    for (int k = k0; k < K; k += sub) {
+      float2 ml[kItems];
+      float4 u[kItems], v[kItems];
+      const int c = s.c0 + k;                                // CTA c's last segment, or its first
+#pragma unroll
+      for (int n = 0; n < kItems; ++n) {
+        const uint8_t* slot = p.part + (size_t)(2 * (2 * c + (k == 0)) + st[n]) * kAttnPartBytes;
+        const float4* O = reinterpret_cast<const float4*>(slot) + (size_t)(2 * cg[n]) * kRows + rr[n];
+        ml[n] = __ldcg(reinterpret_cast<const float2*>(slot + kAttnMlOff) + rr[n]);
+        u[n] = __ldcg(O);
+        v[n] = __ldcg(O + kRows);
+      }
+#pragma unroll
+      for (int n = 0; n < kItems; ++n) {
+        // a row without keys in the piece has l = 0 and no O (a sum that is NaN has one)
+        if (ml[n].y == 0.f) continue;
+        const float o[8] = {u[n].x, u[n].y, u[n].z, u[n].w, v[n].x, v[n].y, v[n].z, v[n].w};
+        x[n].add(ml[n].x, ml[n].y, o);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < kItems; ++n) {
+      for (int d = 1; d < sub; d *= 2) {
+        float o[8];
+        const float Mo = __shfl_xor_sync(0xffffffffu, x[n].M, d), Lo = __shfl_xor_sync(0xffffffffu, x[n].L, d);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = __shfl_xor_sync(0xffffffffu, x[n].a[e], d);
+        x[n].add(Mo, Lo, o);
+      }
+      if (k0 != 0 || i0 + n * step >= hi) continue;
+      const float il = x[n].L == 0.f ? 0.f : 1.f / x[n].L;
+      const int tok = rr[n] / p.g, h = rr[n] - tok * p.g;
+      const size_t row = (size_t)(s.o + s.tok0 + (st[n] ? p.tpt : 0) + tok) * p.n_q + s.hk * p.g + h;
+      uint4 o;
+      o.x = bf16x2_rn(x[n].a[1] * il, x[n].a[0] * il);
+      o.y = bf16x2_rn(x[n].a[3] * il, x[n].a[2] * il);
+      o.z = bf16x2_rn(x[n].a[5] * il, x[n].a[4] * il);
+      o.w = bf16x2_rn(x[n].a[7] * il, x[n].a[6] * il);
+      *reinterpret_cast<uint4*>(p.out + row * kD + 8 * cg[n]) = o;
+      if (cg[n] == 0 && p.lse)
+        p.lse[row] = x[n].L == 0.f ? -INFINITY : (x[n].M + log2f(x[n].L)) * 0.6931471805599453f;
+    }
   }
 }
 
 template <bool kPaged>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                   const __grid_constant__ CUtensorMap tmV, const PromptParams p) {
+                   const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PromptParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem =
       reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -232,12 +348,12 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   __shared__ int s_bad[kSegs];                   // V values taken out of the segment's tiles
   __shared__ uint32_t s_mask[kMasks];            // per tile: 16-key blocks in a valid page
   __shared__ int64_t s_scan[kThreads / 32];
-  __shared__ int s_first;                        // the share's first sequence, and
-  __shared__ int64_t s_firstX;                   // its first place
+  __shared__ int s_first;                        // the share's first sequence,
+  __shared__ Seq s_firstseq;
+  __shared__ int64_t s_firstX;                   // and its first place
   __shared__ int s_kvissued[kRing], s_zissued[kZones], s_qissued[2];   // phases of copies started (-1: none)
   __shared__ Seg s_pc[2];                        // pieces of split units
   __shared__ int s_npc;
-  __shared__ int16_t s_list[2][kNumSMsMax];      // their pieces' slot pairs (-1: empty)
   __shared__ int s_ready[2];
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -245,7 +361,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   const uint32_t sKV = sbase + kOffKV, sQ = sbase + kOffQ, bar0 = sbase + kOffBar;
   const uint32_t kv_full = bar0, kv_empty = kv_full + 8 * kRing;
   const uint32_t q_full = kv_empty + 8 * kRing, q_empty = q_full + 16;
-  const uint32_t s_full = q_empty + 16, p_full = s_full + 16, pv_done = p_full + 16, o_free = pv_done + 16;
+  const uint32_t s_full = q_empty + 16, p_half = s_full + 16, p_full = p_half + 16;
+  const uint32_t pv_done = p_full + 16, o_free = pv_done + 16;
   const uint32_t seg_full = o_free + 16, seg_empty = seg_full + 8 * kSegs, z_full = seg_empty + 8 * kSegs;
   const uint32_t drain = z_full + 8 * kZones;
 
@@ -255,31 +372,21 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmV)) : "memory");
     s_abort = 0;
     s_npc = 0;
-    s_first = p.B;
-    s_firstX = 0;
-    for (int i = 0; i < kRing; ++i) {
-      mbar_init(kv_full + 8 * i, 1);
-      mbar_init(kv_empty + 8 * i, 1);
-      s_kvissued[i] = -1;
+    for (int i = 0; i < kRing; ++i) s_kvissued[i] = -1;
+    for (int i = 0; i < kZones; ++i) s_zissued[i] = -1;
+    for (int i = 0; i < 2; ++i) s_qissued[i] = -1;
+  }
+  if (warp == kWarpKV) {   // one barrier a lane
+    for (int i = lane; i < (int)kNumBars; i += 32) {
+      const uint32_t bar = bar0 + 8 * i;
+      const uint32_t count = bar >= s_full && bar < p_half     ? kPaged + 1   // the commit (paged: and a release of the page mask)
+                             : bar >= p_half && bar < pv_done    ? 4    // warps
+                             : bar >= pv_done && bar < o_free    ? 2    // the commit, and a release of s_bad
+                             : bar >= o_free && bar < seg_full   ? 4
+                             : bar >= seg_empty && bar < z_full ? kSegReaders
+                                                                 : 1;
+      mbar_init(bar, count);
     }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(q_full + 8 * i, 1);
-      mbar_init(q_empty + 8 * i, 1);
-      mbar_init(s_full + 8 * i, 2);
-      mbar_init(p_full + 8 * i, 4);
-      mbar_init(pv_done + 8 * i, 2);
-      mbar_init(o_free + 8 * i, 4);
-      s_qissued[i] = -1;
-    }
-    for (int i = 0; i < kSegs; ++i) {
-      mbar_init(seg_full + 8 * i, 1);
-      mbar_init(seg_empty + 8 * i, kSegReaders);
-    }
-    for (int i = 0; i < kZones; ++i) {
-      mbar_init(z_full + 8 * i, 1);
-      s_zissued[i] = -1;
-    }
-    mbar_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kWarpMma) {
@@ -299,16 +406,16 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 
   // ---- the line of work: its length, this CTA's share and where that begins ----
   const int w = 2 * p.tpt;
-  int64_t W, x0, x1;
-  int N;
+  int64_t W = 0;
+  int64_t base = 0, sum = 0;
+  const int per = (p.B + kThreads - 1) / kThreads;   // sequences of a thread
+  const int b0 = min(tid * per, p.B), b1 = min(b0 + per, p.B);
+  Seq sq{0, 0, 0};
   {
-    const int per = (p.B + kThreads - 1) / kThreads;
-    const int b0 = min(tid * per, p.B), b1 = min(b0 + per, p.B);
-    int64_t sum = 0;
     int err = 0;
     for (int s = b0; s < b1; ++s) {
-      const Seq q = load_seq<kPaged>(p, s, err);
-      sum += head_places(q.ctx, q.T, w) * p.n_kv;
+      sq = load_seq<kPaged>(p, s, err);
+      sum += head_places(sq.ctx, sq.T, w) * p.n_kv;
     }
     if (err && blockIdx.x == 0) flag_error(p.err, err);
     int64_t incl = sum;
@@ -319,30 +426,30 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     }
     if (lane == 31) s_scan[warp] = incl;
     __syncthreads();
-    int64_t base = 0;
-    W = 0;
 #pragma unroll
     for (int i = 0; i < kThreads / 32; ++i) {
       if (i < warp) base += s_scan[i];
       W += s_scan[i];
     }
-    N = (int)min((int64_t)gridDim.x, max(W / kMinShare, (int64_t)1));
-    const int c = blockIdx.x;
-    x0 = c < N ? share_start(W, N, c) : W;
-    x1 = c < N ? share_start(W, N, c + 1) : W;
-    int64_t at = base + incl - sum;
-    if (x0 < x1 && x0 >= at && x0 < at + sum) {
-      for (int s = b0; s < b1; ++s) {
-        const Seq q = load_seq<kPaged>(p, s, err);
-        const int64_t n = head_places(q.ctx, q.T, w) * p.n_kv;
-        if (x0 < at + n) {
-          s_first = s;
-          s_firstX = at;
-          break;
-        }
-        at += n;
+    base += incl - sum;
+  }
+  const Shares sh(W, (int)min((int64_t)gridDim.x, max(W / kMinShare, (int64_t)1)));
+  const bool works = (int)blockIdx.x < sh.N && W > 0;
+  const int64_t x0 = works ? sh.start(blockIdx.x) : W, x1 = works ? sh.start(blockIdx.x + 1) : W;
+  if (works && x0 >= base && x0 < base + sum) {
+    int s = b0;
+    if (per > 1) {
+      int err = 0;
+      for (;; ++s) {
+        sq = load_seq<kPaged>(p, s, err);
+        const int64_t n = head_places(sq.ctx, sq.T, w) * p.n_kv;
+        if (x0 < base + n) break;
+        base += n;
       }
     }
+    s_first = s;
+    s_firstseq = sq;
+    s_firstX = base;
   }
   tc_fence_before();
   __syncthreads();
@@ -350,7 +457,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
 
   auto wait = [&](uint32_t bar, int use) -> bool {
-    return __all_sync(0xffffffffu, mbar_wait(bar, (uint32_t)(use & 1), &s_abort));
+    return __all_sync(0xffffffffu, wait_bar(bar, (uint32_t)(use & 1), &s_abort));
   };
   // segment i of the share (false: there is none, or a wait gave up)
   auto receive = [&](int i, Seg& s) -> bool {
@@ -435,15 +542,14 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       // ---------------- segments and Q ----------------
       // lane l holds sequence base + l, so that many short sequences cost one
       // round trip for 32 of them
-      int base = s_first, err = 0;
+      int s = works ? s_first : p.B, base = s + 1, err = 0;   // (a CTA without a share: none is set)
       Seq mine{0, 0, 0};
       auto load32 = [&]() {
         mine = Seq{0, 0, 0};
         if (base + lane < p.B) mine = load_seq<kPaged>(p, base + lane, err);
       };
       load32();
-      int s = base;
-      int64_t X = x0 < x1 ? s_firstX : x1;   // the next unit's first place
+      int64_t X = works ? s_firstX : x1;                      // the next unit's first place
       int o = 0, T = 0, ctx = 0, hk = 0, n = 0;
       auto take = [&]() {        // sequence s from its lane
         if (s - base >= 32) {
@@ -454,8 +560,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         T = __shfl_sync(0xffffffffu, mine.T, s - base);
         ctx = __shfl_sync(0xffffffffu, mine.ctx, s - base);
       };
-      if (x0 < x1) {
-        take();
+      if (works) {
+        o = s_firstseq.o;
+        T = s_firstseq.T;
+        ctx = s_firstseq.ctx;
         const int64_t per_head = head_places(ctx, T, w);
         int64_t rem = x0 - X;
         hk = (int)(rem / per_head);
@@ -504,11 +612,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           g.nB = T > tok0 + p.tpt ? tiles : 0;
           g.c0 = g.c1 = 0;
           if (j1 - j0 < tiles) {
-            // CTA c holds a first piece when its share starts before the second tile's
-            // places do, and any piece when it starts before the last one's
+            // the first piece is the last CTA's whose share starts before the second
+            // tile's places do, the last piece that of the last CTA whose share starts
+            // before the last tile's; shares are no shorter than a tile, so every CTA
+            // between them holds one
             const int64_t y = g.X + kUnitKeys + kKT / 2;
-            g.c0 = (int)((y * N + W - 1) / W) - 1;
-            g.c1 = min((int)(((y + (int64_t)kKT * (tiles - 1)) * N + W - 1) / W) - 1, N - 1);
+            g.c0 = (int)((y * sh.N + W - 1) / W) - 1;
+            g.c1 = min((int)(((y + (int64_t)kKT * (tiles - 1)) * sh.N + W - 1) / W) - 1, sh.N - 1);
           }
           return true;
         }
@@ -529,27 +639,28 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         __syncwarp();
         return true;
       };
+      // segment i is published before Q of segment i - 1 is waited for
       Seg cur, nxt;
-      bool more = find(cur);
-      bool go = publish(0, cur);
-      int uses[2] = {0, 0};
+      uint32_t q_phase = 3;      // bit st: parity that the row tile's Q buffer is free at
+      bool more = true, go = true;
+#pragma unroll 1
       for (int i = 0; more && go; ++i) {
         more = find(nxt);
-        go = publish(i + 1, nxt);
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          if (!go || !active(cur, st, cur.j0)) continue;
-          go = wait(q_empty + 8 * st, uses[st] + 1);
+        go = publish(i, nxt);
+#pragma unroll 1
+        for (int st = 0; st < 2 && i > 0 && go; ++st) {
+          if (!active(cur, st, cur.j0)) continue;
+          go = wait(q_empty + 8 * st, q_phase >> st);
           if (go && elect_one()) {
             const uint32_t full = q_full + 8 * st, dst = sQ + st * kTile;
             const int tok = cur.o + cur.tok0 + st * p.tpt;
             mbar_expect_tx(full, 2u * 128u * p.g * p.tpt);
             tma_load_3d(dst, &tmQ, full, 0, cur.hk * p.g, tok);
             tma_load_3d(dst + kHalf, &tmQ, full, 64, cur.hk * p.g, tok);
-            s_qissued[st] = uses[st];
+            s_qissued[st] = (int)(~q_phase >> st & 1);
           }
           __syncwarp();
-          ++uses[st];
+          q_phase ^= 1u << st;
         }
         cur = nxt;
       }
@@ -566,30 +677,31 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           go = wait(z_full + 8 * (zone % kZones), zone / kZones);
           if (!go) break;
           uint8_t* v = smem + kOffKV + slot * kTile;
-          const int r0 = max(first + 1 - j * kKT, 0), r1 = min(last + 1 - j * kKT, kKT);
-          uint32_t seen = 0;
-          // a row's 128 bytes in each half are a permutation of its 16-byte chunks
-          for (int c = r0 * 8 + lane; c < kKT * 8; c += 32) {
+          const int r0 = max(first + 1 - j * kKT, 0), r1 = last + 1 - j * kKT;   // rows some, no query sees
+          // a row's 128 bytes in each half are a permutation of its 16-byte chunks;
+          // four loads in flight, and nothing to write as a rule
+          bool seen = false, wrote = false;
+          for (int c0 = r0 * 8 + lane; c0 < kKT * 8; c0 += 2 * 32) {
+            uint4 x[4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              uint4* a = reinterpret_cast<uint4*>(v + h * kHalf + 16 * c);
-              if ((c >> 3) >= r1) {
-                *a = make_uint4(0, 0, 0, 0);
-              } else {
-                uint4 x = *a;
-                const uint32_t m0 = nonfinite2(x.x), m1 = nonfinite2(x.y), m2 = nonfinite2(x.z), m3 = nonfinite2(x.w);
-                if (m0 | m1 | m2 | m3) {
-                  seen = 1;
-                  x.x &= ~m0;
-                  x.y &= ~m1;
-                  x.z &= ~m2;
-                  x.w &= ~m3;
-                  *a = x;
-                }
+            for (int u = 0; u < 4; ++u) {
+              const int c = min(c0 + 32 * (u >> 1), kKT * 8 - 1);
+              x[u] = *reinterpret_cast<const uint4*>(v + (u & 1) * kHalf + 16 * c);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const int c = min(c0 + 32 * (u >> 1), kKT * 8 - 1);
+              const uint32_t m0 = nonfinite2(x[u].x), m1 = nonfinite2(x[u].y), m2 = nonfinite2(x[u].z),
+                             m3 = nonfinite2(x[u].w);
+              if (m0 | m1 | m2 | m3) {
+                wrote = true;
+                seen |= (c >> 3) < r1;
+                *reinterpret_cast<uint4*>(v + (u & 1) * kHalf + 16 * c) =
+                    make_uint4(x[u].x & ~m0, x[u].y & ~m1, x[u].z & ~m2, x[u].w & ~m3);
               }
             }
           }
-          fence_async_smem();   // generic-proxy writes, read by the tensor core
+          if (wrote) fence_async_smem();   // generic-proxy writes, read by the tensor core
           if (__any_sync(0xffffffffu, seen) && lane == 0) s_bad[i % kSegs] = 1;
           __syncwarp();
           if (lane == 0) mbar_arrive(kv_full + 8 * slot);
@@ -602,94 +714,131 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       const uint32_t id_qk = idesc_f16(kRows, kKT, 1, 1, 0), id_pv = idesc_f16(kRows, kD, 1, 1, 1);
       const uint64_t dq0 = smem_desc_sw128(__shfl_sync(0xffffffffu, sQ, 0));
       const uint64_t dk0 = smem_desc_sw128(__shfl_sync(0xffffffffu, sKV, 0));
-      const uint64_t dv0 = smem_desc_sw128_mn(__shfl_sync(0xffffffffu, sKV, 0), kHalf, 1024);
-      int q_uses[2] = {0, 0}, o_uses[2] = {0, 0}, p_uses[2] = {0, 0};
-      // S = Q K^T of row tile st and tile j (the CTA's tile-th)
-      auto qk = [&](const Seg& s, int st, int j, int tile) {
-        if (elect_one()) {
-          const uint64_t dk = dk0 + (uint64_t)(((2 * tile) % kRing) * (kTile >> 4));
-          const uint64_t dq = dq0 + (uint64_t)(st * (kTile >> 4));
+      const uint64_t dv0 = smem_desc_sw128_mn(__shfl_sync(0xffffffffu, sKV + kTile, 0), kHalf, 1024);
+      // (within elect_one) S = Q K^T of row tile st, K in its slot `odd`
+      auto qk = [&](int st, uint32_t odd) {
+        const uint64_t dk = dk0 + (uint64_t)(odd * (2 * kTile >> 4));
+        const uint64_t dq = dq0 + (uint64_t)(st * (kTile >> 4));
 #pragma unroll
-          for (int kk = 0; kk < kD / 16; ++kk) {
-            const uint64_t off = ((kk >> 2) * kHalf + (kk & 3) * 32) >> 4;
-            tc_mma(tmem + st * kKT, dq + off, dk + off, id_qk, kk > 0 ? 1u : 0u);
-          }
-          tc_commit(s_full + 8 * st);
-          mbar_arrive(s_full + 8 * st);   // releases the tile's page mask (acquired with kv_full)
-          if (j + 1 == s.j1 || !active(s, st, j + 1)) tc_commit(q_empty + 8 * st);
+        for (int kk = 0; kk < kD / 16; ++kk) {
+          const uint64_t off = ((kk >> 2) * kHalf + (kk & 3) * 32) >> 4;
+          tc_mma(tmem + st * kKT, dq + off, dk + off, id_qk, kk > 0 ? 1u : 0u);
         }
-        __syncwarp();
+        tc_commit(s_full + 8 * st);
+        if constexpr (kPaged) mbar_arrive(s_full + 8 * st);   // releases the page mask (acquired with kv_full)
       };
-      auto pv = [&](const Seg& s, int st, int j, int tile) {
-        if (elect_one()) {
-          const uint64_t dv = dv0 + (uint64_t)(((2 * tile + 1) % kRing) * (kTile >> 4));
+      // (within elect_one) O += P V for half of the keys, V in its slot `odd`
+      auto pv = [&](int st, uint32_t odd, int half, bool acc) {
+        const uint64_t dv = dv0 + (uint64_t)(odd * (2 * kTile >> 4));
 #pragma unroll
-          for (int kk = 0; kk < kKT / 16; ++kk)
-            tc_mma_ts(tmem + kColO + st * kD, tmem + st * kKT + 8 * kk, dv + (uint64_t)(kk * (2048 >> 4)), id_pv,
-                      (j > s.j0 || kk > 0) ? 1u : 0u);
-          if (j + 1 == s.j1 || !active(s, st, j + 1)) {
-            tc_commit(pv_done + 8 * st);
-            mbar_arrive(pv_done + 8 * st);   // releases s_bad (acquired with kv_full)
-          }
+        for (int k = 0; k < kKT / 32; ++k) {
+          const int kk = half * (kKT / 32) + k;
+          tc_mma_ts(tmem + kColO + st * kD, tmem + st * kKT + 8 * kk, dv + (uint64_t)(kk * (2048 >> 4)), id_pv,
+                    (acc || kk > 0) ? 1u : 0u);
         }
-        __syncwarp();
       };
-      Seg s, nx;
-      int i = 0, tile = 0;
-      bool go = receive(0, s);
-      int j = s.j0;
-      if (go) {
-        go = wait(kv_full, 0);
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          if (!go || !active(s, st, j)) continue;
-          go = wait(q_full + 8 * st, q_uses[st]++);
-          tc_fence_after();
-          if (go) qk(s, st, j, 0);
-        }
-        if (go && elect_one()) tc_commit(kv_empty);
-        __syncwarp();
-      }
+      // A wait without a vote: `go` is this lane's, voted on once a step.  (An MMA issued
+      // after a wait gave up reads stale operands; the outputs are then undefined anyway.)
+      bool go = true;
+      auto meet = [&](uint32_t bar, uint32_t parity) { go = wait_bar(bar, parity & 1, &s_abort) && go; };
+      // K and V of tile t: slots 2 (t & 1) and 2 (t & 1) + 1, both in their (t >> 1)-th use
+      auto k_bar = [&](int t) { return kv_full + 16 * (t & 1); };
+      auto v_bar = [&](int t) { return kv_full + 16 * (t & 1) + 8; };
+      Seg s;
+      s.j0 = s.j1 = s.nA = s.nB = 0;
+      int i = -1, j = -1, tile = -1;   // before the first tile: a step without P V
+      uint32_t p_phase = 0, q_phase = 0, o_phase = 3;
       while (go) {
-        nx = s;
+        // ---- tiles that both row tiles need, up to the last but one, past a segment's
+        // first: waits between two products cost the tensor core what they take (its
+        // queue holds a few MMAs), so there is one before each half of P V and none
+        // before Q K^T
+        const int both = j > s.j0 ? min(s.j1, min(s.nA, s.nB)) - 1 : j;
+#pragma unroll 1
+        for (; j < both && go; ++j, ++tile) {
+          const uint32_t odd = tile & 1;
+          meet(v_bar(tile), tile >> 1);
+          meet(k_bar(tile + 1), (tile + 1) >> 1);
+#pragma unroll 1
+          for (int st = 0; st < 2; ++st) {
+            meet(p_half + 8 * st, p_phase);
+            tc_fence_after();
+            if (elect_one()) pv(st, odd, 0, true);
+            __syncwarp();
+            meet(p_full + 8 * st, p_phase);
+            tc_fence_after();
+            if (elect_one()) {
+              pv(st, odd, 1, true);
+              qk(st, odd ^ 1);
+              if (j + 2 == s.j1 || !active(s, st, j + 2)) tc_commit(q_empty + 8 * st);
+            }
+            __syncwarp();
+            p_phase = (p_phase >> 1) | ((~p_phase & 1) << 1);   // the bits take turns, each inverted
+          }
+          if (elect_one()) {
+            tc_commit(kv_empty + 16 * odd + 8);
+            tc_commit(kv_empty + 16 * (odd ^ 1));
+          }
+          go = __all_sync(0xffffffffu, go);
+        }
+        if (!go) break;
+        // ---- any other tile: a segment's first or last, or one that one row tile needs ----
+        Seg nx = s;
         int jn = j + 1;
+        const bool cur = i >= 0, fresh = jn >= s.j1;
         bool has = true;
-        const bool fresh = jn == s.j1;
         if (fresh) {
           has = receive(i + 1, nx);
           jn = nx.j0;
-          if (s_abort) break;
+          if (s_abort || !(cur || has)) break;
         }
-        const int vi = 2 * tile + 1, ki = 2 * tile + 2;
-        go = wait(kv_full + 8 * (vi % kRing), vi / kRing);
-        bool k_in = false;
-#pragma unroll
+        const uint32_t odd = tile & 1;
+        if (cur) meet(v_bar(tile), tile >> 1);
+        if (has) meet(k_bar(tile + 1), (tile + 1) >> 1);
+#pragma unroll 1
         for (int st = 0; st < 2; ++st) {
-          if (go && active(s, st, j)) {
-            go = wait(p_full + 8 * st, p_uses[st]++);
-            if (go && j == s.j0) {
-              if (o_uses[st] > 0) go = wait(o_free + 8 * st, o_uses[st] - 1);   // the last segment's O is read
-              ++o_uses[st];
+          if (cur && active(s, st, j)) {
+            if (j == s.j0) {   // the last segment's O is read
+              meet(o_free + 8 * st, o_phase >> st);
+              o_phase ^= 1u << st;
+            }
+            meet(p_half + 8 * st, p_phase >> st);
+            tc_fence_after();
+            if (elect_one()) pv(st, odd, 0, j > s.j0);
+            __syncwarp();
+            meet(p_full + 8 * st, p_phase >> st);
+            p_phase ^= 1u << st;
+            tc_fence_after();
+            if (elect_one()) {
+              pv(st, odd, 1, true);
+              if (fresh || !active(s, st, jn)) {
+                tc_commit(pv_done + 8 * st);
+                mbar_arrive(pv_done + 8 * st);   // releases s_bad (acquired with kv_full)
+              }
+            }
+            __syncwarp();
+          }
+          if (has && active(nx, st, jn)) {
+            if (fresh) {
+              meet(q_full + 8 * st, q_phase >> st);
+              q_phase ^= 1u << st;
             }
             tc_fence_after();
-            if (go) pv(s, st, j, tile);
-          }
-          if (go && has && active(nx, st, jn)) {
-            if (!k_in) go = wait(kv_full + 8 * (ki % kRing), ki / kRing);
-            k_in = true;
-            if (go && fresh) go = wait(q_full + 8 * st, q_uses[st]++);
-            tc_fence_after();
-            if (go) qk(nx, st, jn, tile + 1);
+            if (elect_one()) {
+              qk(st, odd ^ 1);
+              if (jn + 1 == nx.j1 || !active(nx, st, jn + 1)) tc_commit(q_empty + 8 * st);
+            }
+            __syncwarp();
           }
         }
-        if (go && elect_one()) {
-          tc_commit(kv_empty + 8 * (vi % kRing));
-          if (has) tc_commit(kv_empty + 8 * (ki % kRing));
+        if (elect_one()) {
+          if (cur) tc_commit(kv_empty + 16 * odd + 8);
+          if (has) tc_commit(kv_empty + 16 * (odd ^ 1));
         }
         __syncwarp();
-        if (!has) break;
+        go = __all_sync(0xffffffffu, go) && has;
         if (fresh) {
-          release(i);
+          if (cur) release(i);
           ++i;
           s = nx;
         }
@@ -735,6 +884,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     const uint32_t lane_base = (uint32_t)(qd * 32) << 16;
     const uint32_t tS = tmem + lane_base + st * kKT, tO = tmem + lane_base + kColO + st * kD;
     const float sl2 = p.scale_log2;
+    uint8_t* s_out = smem + kOffOut + (warp - kWarpSoft) * kOutBytes;
     Seg s;
     int tile = 0, uses = 0, o_uses = 0;
     bool go = true;
@@ -752,76 +902,74 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         ++uses;
         if (warp_rows) {
           tc_fence_after();
+          const uint32_t pm = kPaged ? s_mask[(tile + j - s.j0) % kMasks] : 0xFFu;
+          const int base = j * kKT;
+          if (base + kKT - 1 > tile_first || pm != 0xFFu) {
+            // scores that a row must not see become -inf in tensor memory, from the first
+            // 16-key block with one on
+            const int nvis = pos + 1 - base;
+#pragma unroll 1
+            for (int c = pm != 0xFFu ? 0 : max(tile_first + 1 - base, 0) >> 4; c < kKT / 16; ++c) {
+              const int nv = (pm >> c) & 1u ? nvis - 16 * c : 0;
+              uint32_t sv[16];
+              tc_ld16(tS + 16 * c, sv);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) sv[e] = e < nv ? sv[e] : __float_as_uint(-INFINITY);
+              tc_st16_nowait(tS + 16 * c, sv);
+            }
+            tc_wait_st();
+          }
           uint32_t sr[128];
 #pragma unroll
           for (int c = 0; c < 4; ++c) tc_ld32_nowait(tS + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(&sr[32 * c]));
-          const uint32_t pm = kPaged ? s_mask[(tile + j - s.j0) % kMasks] : 0xFFu;
-          const int base = j * kKT;
           tc_wait_ld32(*reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
 #pragma unroll
           for (int c = 1; c < 4; ++c) tc_pin32(*reinterpret_cast<uint32_t(*)[32]>(&sr[32 * c]));
-          if (base + kKT - 1 > tile_first || pm != 0xFFu) {
-            const int nvis = pos + 1 - base;
-#pragma unroll
-            for (int c = 0; c < 128; ++c)
-              if (c >= nvis || !((pm >> (c >> 4)) & 1u)) sr[c] = __float_as_uint(-INFINITY);
-          }
-          float mx[8];
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            mx[k] = fmaxf(__uint_as_float(sr[k]), __uint_as_float(sr[8 + k]));
-#pragma unroll
-          for (int c = 16; c < 128; c += 16)
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-              mx[k] = fmax3(mx[k], __uint_as_float(sr[c + k]), __uint_as_float(sr[c + 8 + k]));
-          const float tmax = fmax3(fmax3(mx[0], mx[1], mx[2]), fmax3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7]));
-          const float m_new = fmaxf(m, tmax);
-          const bool need = (m_new - m) * sl2 > kRescaleLog2;   // true when m = -inf < m_new
-          if (j > s.j0 && __any_sync(0xffffffffu, need)) {
-            // S of this tile was issued after P V of the one before: O holds it
-            const float f = need ? ex2((m - m_new) * sl2) : 1.f;
-#pragma unroll 1
-            for (int c = 0; c < 8; ++c) {
-              uint32_t ov[16];
-              tc_ld16(tO + 16 * c, ov);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * f);
-              tc_st16_nowait(tO + 16 * c, ov);
-            }
-          }
-          if (need) {
-            l *= ex2((m - m_new) * sl2);
-            m = m_new;
-          }
-          const float nms = m == -INFINITY ? 0.f : -m * sl2;
-          const uint64_t sl2x2 = f2_pack(__float_as_uint(sl2), __float_as_uint(sl2));
-          const uint64_t nmsx2 = f2_pack(__float_as_uint(nms), __float_as_uint(nms));
+          if (j == s.j0) m = row_max(sr);
+          // The first half of P is formed with the running maximum as it was, while the
+          // tile's own is found beside it (exponentials keep the other pipes free); only
+          // where it has grown by more than 2^8 is O rescaled and the half formed again.
           uint64_t ls[4];
+          float nms;
+#pragma unroll 1
+          for (;;) {
+            nms = m == -INFINITY ? 0.f : -m * sl2;
+            exp_half<0>(sr, tS, sl2, nms, ls);
+            const float tmax = row_max(sr);
+            const bool need = (tmax - m) * sl2 > kRescaleLog2;   // true when m = -inf < tmax
+            if (!__any_sync(0xffffffffu, need)) break;
+            // S of this tile was issued after P V of the one before: O holds it
+            const float f = need ? ex2((m - tmax) * sl2) : 1.f;
+            if (j > s.j0) {
+#pragma unroll 1
+              for (int c = 0; c < 8; ++c) {
+                uint32_t ov[16];
+                tc_ld16(tO + 16 * c, ov);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t pw[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int x = 32 * c + 2 * e;
-              uint32_t y0, y1;
-              f2_unpack(f2_fma(f2_pack(sr[x], sr[x + 1]), sl2x2, nmsx2), y0, y1);
-              const float p0 = ex2(__uint_as_float(y0)), p1 = ex2(__uint_as_float(y1));
-              const uint64_t pp = f2_pack(__float_as_uint(p0), __float_as_uint(p1));
-              ls[e & 3] = c == 0 && e < 4 ? pp : f2_add(ls[e & 3], pp);
-              pw[e] = bf16x2_rn(p1, p0);
+                for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * f);
+                tc_st16_nowait(tO + 16 * c, ov);
+              }
             }
-            tc_st16_nowait(tS + 16 * c, pw);
+            l *= f;
+            m = need ? tmax : m;
           }
           tc_wait_st();
           tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_half + 8 * st);
+          exp_half<1>(sr, tS, sl2, nms, ls);
+          tc_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_full + 8 * st);
           ls[0] = f2_add(f2_add(ls[0], ls[1]), f2_add(ls[2], ls[3]));
           uint32_t a0, a1;
           f2_unpack(ls[0], a0, a1);
           l += __uint_as_float(a0) + __uint_as_float(a1);
+        } else if (lane == 0) {
+          mbar_arrive(p_half + 8 * st);
+          mbar_arrive(p_full + 8 * st);
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_full + 8 * st);
       }
       tile += s.j1 - s.j0;
       if (!go) break;
@@ -835,31 +983,26 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         ++o_uses;
         tc_fence_after();
       }
-      const bool bad = any && s_bad[i % kSegs] != 0;
       const float il = l == 0.f ? 0.f : 1.f / l;
-      const size_t row = (size_t)(s.o + tok) * p.n_q + s.hk * p.g + head;
+      // output rows: from the row tile's first, by token and head
+      const size_t row0 = (size_t)(s.o + s.tok0 + st * p.tpt) * p.n_q + s.hk * p.g;
+      const uint32_t orow = vrow ? (uint32_t)tok_r * p.n_q + head : UINT32_MAX;
       const int slot = whole ? 0 : 2 * (2 * (int)blockIdx.x + (s.j0 == 0 ? 1 : 0)) + st;
       uint8_t* part = p.part + (size_t)slot * kAttnPartBytes;
       if (any && warp_rows) {
+        uint32_t dst[4];       // the output rows whose pieces this lane carries out
+        if (whole) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dst[e] = __shfl_sync(0xffffffffu, orow, 8 * e + (lane >> 2));
+        }
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           uint32_t ov[32];
           tc_ld32_nowait(tO + 32 * c, ov);
           tc_wait_ld32(ov);
-          if (bad && vrow) {
-            const int k1 = min(pos, s.j1 * kKT - 1);
-            for (int key = max(s.ctx + s.tok0 + 1, s.j0 * kKT); key <= k1; ++key) {
-              const __nv_bfloat16* v = v_row<kPaged>(p, s, key);
-              if (!v) continue;
-#pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                const float x = __bfloat162float(v[32 * c + e]);
-                if (!isfinite(x)) ov[e] = __float_as_uint(__uint_as_float(ov[e]) + x);
-              }
-            }
-          }
-          if (vrow && whole) {
-            uint4* dst = reinterpret_cast<uint4*>(p.out + row * kD + 32 * c);
+          if (whole) {
+            // through shared memory: a row's 64 bytes leave from four neighbouring lanes
+            // (one lane a row touches 32 lines with each store: 3,500 cycles a row tile)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               uint4 x;
@@ -867,20 +1010,38 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
               x.y = bf16x2_rn(__uint_as_float(ov[8 * e + 3]) * il, __uint_as_float(ov[8 * e + 2]) * il);
               x.z = bf16x2_rn(__uint_as_float(ov[8 * e + 5]) * il, __uint_as_float(ov[8 * e + 4]) * il);
               x.w = bf16x2_rn(__uint_as_float(ov[8 * e + 7]) * il, __uint_as_float(ov[8 * e + 6]) * il);
-              dst[e] = x;
+              *reinterpret_cast<uint4*>(s_out + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) = x;
             }
+            __syncwarp();
+            uint4 x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int rr = 8 * e + (lane >> 2);
+              x[e] = *reinterpret_cast<const uint4*>(s_out + rr * 64 + (((lane ^ (rr >> 1)) & 3) << 4));
+            }
+            __nv_bfloat16* o = p.out + row0 * kD + 32 * c + 8 * (lane & 3);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (dst[e] != UINT32_MAX) *reinterpret_cast<uint4*>(o + (size_t)dst[e] * kD) = x[e];
+            __syncwarp();
           } else if (vrow) {
-            float4* dst = reinterpret_cast<float4*>(part) + (size_t)(8 * c) * kRows + r;
+            float4* o = reinterpret_cast<float4*>(part) + (size_t)(8 * c) * kRows + r;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              __stcg(dst + (size_t)e * kRows,
+              __stcg(o + (size_t)e * kRows,
                      make_float4(__uint_as_float(ov[4 * e]), __uint_as_float(ov[4 * e + 1]),
                                  __uint_as_float(ov[4 * e + 2]), __uint_as_float(ov[4 * e + 3])));
           }
         }
+        if (s_bad[i % kSegs]) {   // values taken out of V: for the rows that see them
+          __syncwarp();
+          if (vrow)
+            add_nonfinite<kPaged>(p, s, max(s.ctx + s.tok0 + 1, s.j0 * kKT), min(pos, s.j1 * kKT - 1),
+                                  whole ? p.out + (row0 + orow) * kD : nullptr, reinterpret_cast<float*>(part) + 4 * r);
+        }
         tc_fence_before();
       }
-      if (vrow && whole && p.lse) p.lse[row] = l == 0.f ? -INFINITY : fmaf(m, p.scale, logf(l));
+      if (vrow && whole && p.lse) p.lse[row0 + orow] = l == 0.f ? -INFINITY : fmaf(m, p.scale, logf(l));
       if (vrow && !whole)
         __stcg(reinterpret_cast<float2*>(part + kAttnMlOff) + r, make_float2(m == -INFINITY ? m : m * sl2, l));
       __syncwarp();
@@ -900,35 +1061,18 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   const int pi = (tid - 32 * kWarpSoft) / nthr, t = (tid - 32 * kWarpSoft) - pi * nthr;
   const Seg s = s_pc[pi];
   const int K = s.c1 - s.c0 + 1, mine = (int)blockIdx.x - s.c0;
-  unsigned int* cnt =
-      reinterpret_cast<unsigned int*>(p.part + (size_t)(2 * (2 * s.c0 + 1)) * kAttnPartBytes + kCntOff);
   if (t == 0) {
-    atom_add_acq_rel(cnt, (unsigned)(s.j1 - s.j0));
-    const bool ok = wait_count_geq(cnt, (unsigned)s.n_tiles);
+    // the count wraps to zero with the last arrival: nothing resets it
+    uint32_t* cnt = reinterpret_cast<uint32_t*>(p.part + (size_t)(2 * (2 * s.c0 + 1)) * kAttnPartBytes + kCntOff);
+    red_inc_release(cnt, (uint32_t)(K - 1));
+    const bool ok = wait_count_zero(cnt);
     if (!ok) flag_error(p.err, EE_DEVERR_TIMEOUT);
     s_ready[pi] = ok;
   }
-  for (int k = t; k < K; k += nthr) {
-    const int c = s.c0 + k;
-    const int j0 = k == 0 ? 0 : tiles_before(share_start(W, N, c) - s.X, s.n_tiles);
-    const int j1 = tiles_before(share_start(W, N, c + 1) - s.X, s.n_tiles);
-    s_list[pi][k] = j0 < j1 ? (int16_t)(2 * c + (k == 0 ? 1 : 0)) : (int16_t)-1;
-  }
   asm volatile("bar.sync %0, %1;" ::"r"(2 + pi), "r"(nthr) : "memory");
   if (!s_ready[pi]) return;
-  {
-    const int64_t items = (int64_t)min(w, s.T - s.tok0) * p.g * (kD / 8);
-    merge_piece(p, s, s_list[pi], K, items * mine / K, items * (mine + 1) / K, t, nthr);
-  }
-  // the last piece to have read the partials clears the counts for the next launch
-  asm volatile("bar.sync %0, %1;" ::"r"(2 + pi), "r"(nthr) : "memory");
-  if (t == 0) {
-    const unsigned left = atom_add_acq_rel(cnt + 1, (unsigned)(s.j1 - s.j0)) + (unsigned)(s.j1 - s.j0);
-    if (left == (unsigned)s.n_tiles) {
-      cnt[0] = 0;
-      cnt[1] = 0;
-    }
-  }
+  const int items = min(w, s.T - s.tok0) * p.g * (kD / 8);
+  merge_items(p, s, items * mine / K, items * (mine + 1) / K, t, nthr);
 }
 
 bool good_stride(int64_t stride, int heads) { return stride % 8 == 0 && stride >= (int64_t)heads * kD; }
