@@ -61,6 +61,7 @@ constexpr float kRescaleLog2 = 8.0f;          // O is rescaled when a maximum gr
 constexpr int kUnitKeys = 3 * kKT, kMinShare = 5 * kKT;
 static_assert(kMinShare >= kKT, "every CTA between a unit's first and last piece holds one");
 constexpr int kWarpKV = 0, kWarpMma = 1, kWarpQ = 2, kWarpClean = 3, kWarpSoft = 4;
+constexpr int kVBox = 32;                     // packed V: rows of a box
 constexpr int kSegReaders = 3 + 8;            // warps 0, 1, 3 and the softmax warps
 constexpr int kRegsLaunch = 168, kRegsSoft = 208, kRegsOther = 88;
 static_assert(kRing == 4, "two slots each for K and V tiles");
@@ -185,12 +186,24 @@ __device__ __forceinline__ int tiles_before(int64_t y, int n) {
   const int64_t j = (y - kUnitKeys + kKT / 2) >> 7;
   return (int)min(max(j, (int64_t)0), (int64_t)n);
 }
-// W places cut for N CTAs: CTA c's share starts at floor(c W / N)
+// W places (below 2^56) cut for N CTAs: CTA c's share starts at floor(c W / N)
 struct Shares {
-  int64_t W, q;
+  int64_t W, q;      // q = W / N, r = W mod N, by two 32-bit divisions
   int N, r;
-  __device__ __forceinline__ Shares(int64_t w, int n) : W(w), q(w / n), N(n), r((int)(w - w / n * n)) {}
+  __device__ __forceinline__ Shares(int64_t w, int n) : W(w), N(n) {
+    const uint32_t a = (uint32_t)(w >> 24), b = (uint32_t)w & 0xFFFFFFu;
+    const uint32_t q1 = a / (uint32_t)n, lo = ((a - q1 * (uint32_t)n) << 24) + b, q0 = lo / (uint32_t)n;
+    q = ((int64_t)q1 << 24) + q0;
+    r = (int)(lo - q0 * (uint32_t)n);
+  }
   __device__ __forceinline__ int64_t start(int c) const { return q * c + (r * c) / N; }
+  // the last CTA whose share starts before place y (y > 0)
+  __device__ __forceinline__ int before(int64_t y) const {
+    int c = min(max((int)((float)y / (float)W * N), 0), N - 1);
+    while (start(c) >= y) --c;
+    while (c + 1 < N && start(c + 1) < y) ++c;
+    return c;
+  }
 };
 
 // A segment: tiles [j0, j1) of a unit.
@@ -264,8 +277,8 @@ struct Joined {
 
 // Items [lo, hi) of a split unit merged by one of its pieces: thread t of nthr.  An
 // item is eight columns of a row, numbered rows fastest, so that a warp's loads of a
-// slot (column-chunk major) are contiguous.  A thread loads four items of a piece at a
-// time (a round trip to L2 costs about 1,000 cycles).  With few items and many pieces
+// slot (column-chunk major) are contiguous.  A thread loads four items of two pieces at
+// a time (a round trip to L2 costs about 1,000 cycles).  With few items and many pieces
 // `sub` lanes share an item, each over every sub-th piece.
 __device__ __forceinline__ void merge_items(const PromptParams& p, const Seg& s, int lo, int hi, int t, int nthr) {
   constexpr int kItems = 4;
@@ -290,25 +303,29 @@ __device__ __forceinline__ void merge_items(const PromptParams& p, const Seg& s,
       rr[n] = st[n] ? r - rows_a : r;
     }
 #pragma unroll 1
-    for (int k = k0; k < K; k += sub) {
-      float2 ml[kItems];
-      float4 u[kItems], v[kItems];
-      const int c = s.c0 + k;                                // CTA c's last segment, or its first
+    for (int k = k0; k < K; k += 2 * sub) {
+      float2 ml[2][kItems];
+      float4 u[2][kItems], v[2][kItems];
 #pragma unroll
-      for (int n = 0; n < kItems; ++n) {
-        const uint8_t* slot = p.part + (size_t)(2 * (2 * c + (k == 0)) + st[n]) * kAttnPartBytes;
-        const float4* O = reinterpret_cast<const float4*>(slot) + (size_t)(2 * cg[n]) * kRows + rr[n];
-        ml[n] = __ldcg(reinterpret_cast<const float2*>(slot + kAttnMlOff) + rr[n]);
-        u[n] = __ldcg(O);
-        v[n] = __ldcg(O + kRows);
-      }
+      for (int q = 0; q < 2; ++q)
 #pragma unroll
-      for (int n = 0; n < kItems; ++n) {
-        // a row without keys in the piece has l = 0 and no O (a sum that is NaN has one)
-        if (ml[n].y == 0.f) continue;
-        const float o[8] = {u[n].x, u[n].y, u[n].z, u[n].w, v[n].x, v[n].y, v[n].z, v[n].w};
-        x[n].add(ml[n].x, ml[n].y, o);
-      }
+        for (int n = 0; n < kItems; ++n) {
+          const int kk = min(k + q * sub, K - 1), c = s.c0 + kk;   // CTA c's last segment, or its first
+          const uint8_t* slot = p.part + (size_t)(2 * (2 * c + (kk == 0)) + st[n]) * kAttnPartBytes;
+          const float4* O = reinterpret_cast<const float4*>(slot) + (size_t)(2 * cg[n]) * kRows + rr[n];
+          ml[q][n] = __ldcg(reinterpret_cast<const float2*>(slot + kAttnMlOff) + rr[n]);
+          u[q][n] = __ldcg(O);
+          v[q][n] = __ldcg(O + kRows);
+        }
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int n = 0; n < kItems; ++n) {
+          // a row without keys in the piece has l = 0 and no O (a sum that is NaN has one)
+          if (k + q * sub >= K || ml[q][n].y == 0.f) continue;
+          const float o[8] = {u[q][n].x, u[q][n].y, u[q][n].z, u[q][n].w, v[q][n].x, v[q][n].y, v[q][n].z, v[q][n].w};
+          x[n].add(ml[q][n].x, ml[q][n].y, o);
+        }
     }
 #pragma unroll
     for (int n = 0; n < kItems; ++n) {
@@ -480,9 +497,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       bool go = true;
       for (int i = 0; go && receive(i, s); ++i) {
         // paged: lane l holds the page of 16-key block l % 8 of the (l / 8)-th of four tiles
+        const int last = s.ctx + min(s.T, s.tok0 + w) - 1;
         auto fetch = [&](int j) -> int32_t {
           const int key = (j + (lane >> 3)) * kKT + 16 * (lane & 7);
-          const bool need = (j + (lane >> 3)) < s.j1 && key < s.ctx + s.T;
+          const bool need = (j + (lane >> 3)) < s.j1 && key <= last;
           return need ? max(ld_nc_pinned(p.block_table + (size_t)s.s * p.max_pages + key / EE_PAGE), -1) : INT32_MIN;
         };
         int32_t ids = INT32_MIN, ids_next = INT32_MIN;
@@ -501,9 +519,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             for (int b = 0; b < 8; ++b) {
               const int32_t id = __shfl_sync(0xffffffffu, ids, 8 * q + b);
               const bool ok = id >= 0 && id < p.num_pages;
-              // rows wholly out of range are filled with zeros
+              // (rows wholly out of range are filled with zeros)
               row[b] = ok ? (id * p.n_kv + s.hk) * EE_PAGE : -EE_PAGE;
-              okm |= ok ? 1u << b : 0u;
+              okm |= ok || id == INT32_MIN ? 1u << b : 0u;   // past the unit: masked as such
               bad |= !ok && id != INT32_MIN;
             }
             if (bad && lane == 0) flag_error(p.err, EE_DEVERR_PAGE);
@@ -525,9 +543,17 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                   tma_load_2d(dst + b * 2048, tm, full, 0, row[b]);
                   tma_load_2d(dst + kHalf + b * 2048, tm, full, 64, row[b]);
                 }
-              } else {
+              } else if (kv == 0) {
                 tma_load_3d(dst, tm, full, 0, s.hk, s.o + j * kKT);
                 tma_load_3d(dst + kHalf, tm, full, 64, s.hk, s.o + j * kKT);
+              } else {
+#pragma unroll
+                for (int b = 0; b < kKT / kVBox; ++b) {
+                  // boxes past the unit are filled with zeros
+                  const int at = j * kKT + kVBox * b <= last ? s.o + j * kKT + kVBox * b : p.total;
+                  tma_load_3d(dst + b * kVBox * 128, tm, full, 0, s.hk, at);
+                  tma_load_3d(dst + kHalf + b * kVBox * 128, tm, full, 64, s.hk, at);
+                }
               }
               if (z) s_zissued[zone % kZones] = zone / kZones;
               else s_kvissued[slot] = use;
@@ -566,8 +592,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         ctx = s_firstseq.ctx;
         const int64_t per_head = head_places(ctx, T, w);
         int64_t rem = x0 - X;
-        hk = (int)(rem / per_head);
+        hk = min((int)((float)rem / (float)per_head), p.n_kv - 1);
         rem -= hk * per_head;
+        for (; rem < 0; rem += per_head) --hk;
+        for (; rem >= per_head; rem -= per_head) ++hk;
         X += hk * per_head;
         int lo = 0, hi = num_units(T, w);
         while (hi - lo > 1) {
@@ -617,8 +645,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             // before the last tile's; shares are no shorter than a tile, so every CTA
             // between them holds one
             const int64_t y = g.X + kUnitKeys + kKT / 2;
-            g.c0 = (int)((y * sh.N + W - 1) / W) - 1;
-            g.c1 = min((int)(((y + (int64_t)kKT * (tiles - 1)) * sh.N + W - 1) / W) - 1, sh.N - 1);
+            g.c0 = sh.before(y);
+            g.c1 = sh.before(y + (int64_t)kKT * (tiles - 1));
           }
           return true;
         }
@@ -677,28 +705,36 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           go = wait(z_full + 8 * (zone % kZones), zone / kZones);
           if (!go) break;
           uint8_t* v = smem + kOffKV + slot * kTile;
-          const int r0 = max(first + 1 - j * kKT, 0), r1 = last + 1 - j * kKT;   // rows some, no query sees
+          // rows that some query must not see, and where those end that one does; past the
+          // box that holds the last of them the tile is zero
+          const int r0 = max(first + 1 - j * kKT, 0), r1 = min(last + 1 - j * kKT, kKT);
+          const int r2 = kPaged ? (r1 + EE_PAGE - 1) / EE_PAGE * EE_PAGE : (r1 + kVBox - 1) / kVBox * kVBox;
           // a row's 128 bytes in each half are a permutation of its 16-byte chunks;
           // four loads in flight, and nothing to write as a rule
           bool seen = false, wrote = false;
-          for (int c0 = r0 * 8 + lane; c0 < kKT * 8; c0 += 2 * 32) {
+#pragma unroll 1
+          for (int c0 = r0 * 8 + lane; c0 < r2 * 8; c0 += 2 * 32) {
             uint4 x[4];
+            uint32_t any = 0;      // (e + 1) << 7 reaches bit 15 where the exponent is all ones
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-              const int c = min(c0 + 32 * (u >> 1), kKT * 8 - 1);
+              const int c = min(c0 + 32 * (u >> 1), r2 * 8 - 1);
               x[u] = *reinterpret_cast<const uint4*>(v + (u & 1) * kHalf + 16 * c);
             }
 #pragma unroll
+            for (int u = 0; u < 4; ++u)
+              any |= ((x[u].x & 0x7f807f80u) + 0x00800080u) | ((x[u].y & 0x7f807f80u) + 0x00800080u) |
+                     ((x[u].z & 0x7f807f80u) + 0x00800080u) | ((x[u].w & 0x7f807f80u) + 0x00800080u);
+            if (!(any & 0x80008000u)) continue;
+            wrote = true;
+#pragma unroll 1
             for (int u = 0; u < 4; ++u) {
-              const int c = min(c0 + 32 * (u >> 1), kKT * 8 - 1);
-              const uint32_t m0 = nonfinite2(x[u].x), m1 = nonfinite2(x[u].y), m2 = nonfinite2(x[u].z),
-                             m3 = nonfinite2(x[u].w);
-              if (m0 | m1 | m2 | m3) {
-                wrote = true;
-                seen |= (c >> 3) < r1;
-                *reinterpret_cast<uint4*>(v + (u & 1) * kHalf + 16 * c) =
-                    make_uint4(x[u].x & ~m0, x[u].y & ~m1, x[u].z & ~m2, x[u].w & ~m3);
-              }
+              const int c = min(c0 + 32 * (u >> 1), r2 * 8 - 1);
+              uint4* a = reinterpret_cast<uint4*>(v + (u & 1) * kHalf + 16 * c);
+              const uint4 y = *a;
+              const uint32_t m0 = nonfinite2(y.x), m1 = nonfinite2(y.y), m2 = nonfinite2(y.z), m3 = nonfinite2(y.w);
+              seen |= (m0 | m1 | m2 | m3) != 0 && (c >> 3) < r1;
+              *a = make_uint4(y.x & ~m0, y.y & ~m1, y.z & ~m2, y.w & ~m3);
             }
           }
           if (wrote) fence_async_smem();   // generic-proxy writes, read by the tensor core
@@ -750,18 +786,19 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       uint32_t p_phase = 0, q_phase = 0, o_phase = 3;
       while (go) {
         // ---- tiles that both row tiles need, up to the last but one, past a segment's
-        // first: waits between two products cost the tensor core what they take (its
-        // queue holds a few MMAs), so there is one before each half of P V and none
-        // before Q K^T
+        // first: a wait between two products costs the tensor core what it takes (about
+        // 100 cycles; the queue holds a few MMAs), so there is one before each half of P V
+        // and none before Q K^T, and K and V are looked at beside the first
         const int both = j > s.j0 ? min(s.j1, min(s.nA, s.nB)) - 1 : j;
 #pragma unroll 1
         for (; j < both && go; ++j, ++tile) {
           const uint32_t odd = tile & 1;
-          meet(v_bar(tile), tile >> 1);
-          meet(k_bar(tile + 1), (tile + 1) >> 1);
 #pragma unroll 1
           for (int st = 0; st < 2; ++st) {
+            const bool v_in = mbar_try(v_bar(tile), (tile >> 1) & 1), k_in = mbar_try(k_bar(tile + 1), ((tile + 1) >> 1) & 1);
             meet(p_half + 8 * st, p_phase);
+            if (!v_in) meet(v_bar(tile), tile >> 1);
+            if (!k_in) meet(k_bar(tile + 1), (tile + 1) >> 1);
             tc_fence_after();
             if (elect_one()) pv(st, odd, 0, true);
             __syncwarp();
@@ -1182,7 +1219,7 @@ extern "C" ee_status ee_prompt_attn(const ee_bf16* q, int64_t q_stride, const ee
   p.v_stride = v_stride;
   CUtensorMap tmQ, tmK, tmV;
   if (!token_map(&tmQ, q, n_q, total, q_stride, p.g, p.tpt) || !token_map(&tmK, k, n_kv, total, k_stride, 1, kKT) ||
-      !token_map(&tmV, v, n_kv, total, v_stride, 1, kKT))
+      !token_map(&tmV, v, n_kv, total, v_stride, 1, kVBox))
     return EE_ERR_CUDA;
   return launch<false>(tmQ, tmK, tmV, p, ctas, stream);
 }
