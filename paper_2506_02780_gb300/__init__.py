@@ -127,18 +127,28 @@ def _p(t):
     return ctypes.c_void_p(t.data_ptr())
 
 
+def _tp(t, dtype, name):
+    """Pointer of a contiguous CUDA tensor of this type (the prompt-intake calls: some take
+    a dozen tensors and run for a few microseconds, so each is looked at once)."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"libee takes {'contiguous' if t.is_cuda else 'CUDA'} tensors only ({name})")
+
+
 def _rows(t, name):
     """(pointer, token stride) of a [tokens, heads, head_dim] bf16 tensor whose heads
     are contiguous within a token: a view of a fused projection's output will do."""
-    if t is None:
-        return None, 0
-    _check(t, torch.bfloat16, name)
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
     if not t.is_cuda:
-        raise ValueError("libee takes CUDA tensors only")
+        raise ValueError(f"libee takes CUDA tensors only ({name})")
     n, h, d = t.shape
-    if (n and h > 1 and t.stride(1) != d) or (n and t.stride(2) != 1):
+    s0, s1, s2 = t.stride()
+    if n and ((h > 1 and s1 != d) or s2 != 1):
         raise ValueError(f"the heads of {name} must be contiguous within a token")
-    return t.data_ptr(), (t.stride(0) if n > 1 else h * d)
+    return t.data_ptr(), (s0 if n > 1 else h * d)
 
 
 def _check(t, dtype, name):
@@ -146,7 +156,15 @@ def _check(t, dtype, name):
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
 
 
+# The current stream's handle without building a torch.cuda.Stream around it (3 us
+# a call on the GB300's host), where this torch has the accessors.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream):
+    if stream is None and _raw_stream is not None and _raw_device is not None:
+        return _raw_stream(_raw_device())
     s = torch.cuda.current_stream() if stream is None else stream
     return ctypes.c_void_p(s.cuda_stream)
 
@@ -414,96 +432,99 @@ def new_prompt_workspace(device="cuda", stream=None):
     return ws
 
 
-def _i32s(**tensors):
-    for name, t in tensors.items():
-        _check(t, torch.int32, name)
-
-
 def ee_prompt_slots(ctx_len, new_len, held, block_table, free_pages, free_cnt, num_pages, reserve, tok_off, pos, slot,
                     ctx_out, held_out, free_out, ws, stream=None):
     """Pages, positions and slots of new tokens from their lengths (all on the device);
     `pos` and `slot` have one entry for each packed token."""
-    _i32s(ctx_len=ctx_len, new_len=new_len, held=held, block_table=block_table, free_pages=free_pages,
-          free_cnt=free_cnt, tok_off=tok_off, pos=pos, slot=slot, ctx_out=ctx_out, held_out=held_out, free_out=free_out)
+    i32 = torch.int32
     B, max_pages = block_table.shape
     total = pos.numel()
     if not (ctx_len.numel() == new_len.numel() == held.numel() == ctx_out.numel() == held_out.numel() == B
             and tok_off.numel() == B + 1 and slot.numel() == total and free_cnt.numel() == free_out.numel() == 1):
         raise ValueError("ee_prompt_slots: lengths need B entries, tok_off B + 1, slot as many as pos, the counts one")
-    st = lib().ee_prompt_slots(_p(ctx_len), _p(new_len), _p(held), B, total, int(reserve), _p(block_table), max_pages,
-                               _p(free_pages), free_pages.numel(), _p(free_cnt), int(num_pages), _p(tok_off), _p(pos),
-                               _p(slot), _p(ctx_out), _p(held_out), _p(free_out), _p(ws), ws.numel(), _stream(stream))
-    _ok("ee_prompt_slots", st)
+    st = lib().ee_prompt_slots(_tp(ctx_len, i32, "ctx_len"), _tp(new_len, i32, "new_len"), _tp(held, i32, "held"), B,
+                               total, reserve, _tp(block_table, i32, "block_table"), max_pages,
+                               _tp(free_pages, i32, "free_pages"), free_pages.numel(), _tp(free_cnt, i32, "free_cnt"),
+                               num_pages, _tp(tok_off, i32, "tok_off"), _tp(pos, i32, "pos"), _tp(slot, i32, "slot"),
+                               _tp(ctx_out, i32, "ctx_out"), _tp(held_out, i32, "held_out"),
+                               _tp(free_out, i32, "free_out"), ws.data_ptr(), ws.numel(), _stream(stream))
+    if st:
+        raise EEError("ee_prompt_slots", st)
 
 
 def ee_rope_append(q, k, v, rope, pos, slot, q_out, k_cache, v_cache, ws, k_out=None, stream=None):
     """Rotary positions of q (to q_out) and k, and the write of k and v into the cache
     at `slot` (one layer); q, k, v, q_out and k_out [tokens, heads, 128] may be views of
     wider rows, q_out may be q and k_out may be k."""
-    _i32s(pos=pos, slot=slot)
-    _check(rope, torch.float32, "rope")
-    _check(k_cache, torch.bfloat16, "k_cache")
-    _check(v_cache, torch.bfloat16, "v_cache")
-    total, n_q, d = q.shape
-    n_kv = k.shape[1]
-    num_pages = k_cache.shape[0]
-    if (k.shape != (total, n_kv, d) or v.shape != k.shape or q_out.shape != q.shape or pos.numel() != total
+    bf16 = torch.bfloat16
+    total, n_q, d = shape = q.shape
+    kv = k.shape
+    n_kv = kv[1]
+    cache = k_cache.shape
+    if (kv != (total, n_kv, d) or v.shape != kv or q_out.shape != shape or pos.numel() != total
             or slot.numel() != total or rope.dim() != 2 or rope.shape[1] != d
-            or k_cache.shape != (num_pages, n_kv, EE_PAGE, d) or v_cache.shape != k_cache.shape
-            or (k_out is not None and k_out.shape != k.shape)):
+            or cache != (cache[0], n_kv, EE_PAGE, d) or v_cache.shape != cache
+            or (k_out is not None and k_out.shape != kv)):
         raise ValueError("ee_rope_append: shapes do not fit together")
     qp, qs = _rows(q, "q")
     kp, ks = _rows(k, "k")
     vp, vs = _rows(v, "v")
     op, os_ = _rows(q_out, "q_out")
-    rp, rs = _rows(k_out, "k_out")
-    st = lib().ee_rope_append(qp, qs, kp, ks, vp, vs, _p(rope), rope.shape[0], _p(pos), _p(slot), total, n_q, n_kv, d,
-                              op, os_, rp, rs, _p(k_cache), _p(v_cache), num_pages, _p(ws), ws.numel(),
-                              _stream(stream))
-    _ok("ee_rope_append", st)
+    rp, rs = (None, 0) if k_out is None else _rows(k_out, "k_out")
+    st = lib().ee_rope_append(qp, qs, kp, ks, vp, vs, _tp(rope, torch.float32, "rope"), rope.shape[0],
+                              _tp(pos, torch.int32, "pos"), _tp(slot, torch.int32, "slot"), total, n_q, n_kv, d, op,
+                              os_, rp, rs, _tp(k_cache, bf16, "k_cache"), _tp(v_cache, bf16, "v_cache"), cache[0],
+                              ws.data_ptr(), ws.numel(), _stream(stream))
+    if st:
+        raise EEError("ee_rope_append", st)
 
 
-def _attn_outputs(out, lse, total, n_q, d):
-    _check(out, torch.bfloat16, "out")
-    if out.shape != (total, n_q, d):
+def _attn_outputs(out, lse, shape):
+    """An attention's outputs fit queries of this shape."""
+    if out.dtype is not torch.bfloat16:
+        raise TypeError(f"out must be {torch.bfloat16}, got {out.dtype}")
+    if out.shape != shape:
         raise ValueError("out must have the shape of q")
-    if lse is not None:
-        _check(lse, torch.float32, "lse")
-        if lse.shape != (total, n_q):
-            raise ValueError("lse must be [tokens, query heads]")
+    if lse is not None and lse.shape != shape[:2]:
+        raise ValueError("lse must be [tokens, query heads]")
 
 
 def ee_prompt_attn(q, k, v, tok_off, scale, out, ws, lse=None, stream=None):
     """Causal attention of packed whole prompts over their own K/V (one layer)."""
-    _i32s(tok_off=tok_off)
-    total, n_q, d = q.shape
-    n_kv = k.shape[1]
-    if k.shape != (total, n_kv, d) or v.shape != k.shape:
+    total, n_q, d = shape = q.shape
+    kv = k.shape
+    if kv != (total, kv[1], d) or v.shape != kv:
         raise ValueError("k and v must be [tokens, KV heads, head_dim] for q's tokens")
-    _attn_outputs(out, lse, total, n_q, d)
+    _attn_outputs(out, lse, shape)
+    off = _tp(tok_off, torch.int32, "tok_off")
+    op = _tp(out, torch.bfloat16, "out")
+    lp = None if lse is None else _tp(lse, torch.float32, "lse")
     qp, qs = _rows(q, "q")
     kp, ks = _rows(k, "k")
     vp, vs = _rows(v, "v")
-    st = lib().ee_prompt_attn(qp, qs, kp, ks, vp, vs, _p(tok_off), tok_off.numel() - 1, total, n_q, n_kv, d,
-                              float(scale), _p(out), _p(lse), _p(ws), ws.numel(), _stream(stream))
-    _ok("ee_prompt_attn", st)
+    st = lib().ee_prompt_attn(qp, qs, kp, ks, vp, vs, off, tok_off.numel() - 1, total, n_q, kv[1], d, scale, op, lp,
+                              ws.data_ptr(), ws.numel(), _stream(stream))
+    if st:
+        raise EEError("ee_prompt_attn", st)
 
 
 def ee_chunk_attn(q, k_cache, v_cache, block_table, ctx_len, tok_off, scale, out, ws, lse=None, stream=None):
     """Causal attention of chunks of new tokens whose K/V sit at cache positions
     ctx + i, after ctx cached ones (one layer)."""
-    _i32s(block_table=block_table, ctx_len=ctx_len, tok_off=tok_off)
-    _check(k_cache, torch.bfloat16, "k_cache")
-    _check(v_cache, torch.bfloat16, "v_cache")
-    total, n_q, d = q.shape
-    num_pages, n_kv = k_cache.shape[0], k_cache.shape[1]
+    i32, bf16 = torch.int32, torch.bfloat16
+    total, n_q, d = shape = q.shape
+    cache = k_cache.shape
     B, max_pages = block_table.shape
-    if (k_cache.shape != (num_pages, n_kv, EE_PAGE, d) or v_cache.shape != k_cache.shape or ctx_len.numel() != B
+    if (len(cache) != 4 or cache[2] != EE_PAGE or cache[3] != d or v_cache.shape != cache or ctx_len.numel() != B
             or tok_off.numel() != B + 1):
         raise ValueError("ee_chunk_attn: shapes do not fit together")
-    _attn_outputs(out, lse, total, n_q, d)
+    _attn_outputs(out, lse, shape)
+    table, ctx, off = _tp(block_table, i32, "block_table"), _tp(ctx_len, i32, "ctx_len"), _tp(tok_off, i32, "tok_off")
+    op = _tp(out, bf16, "out")
+    lp = None if lse is None else _tp(lse, torch.float32, "lse")
     qp, qs = _rows(q, "q")
-    st = lib().ee_chunk_attn(qp, qs, _p(k_cache), _p(v_cache), num_pages, _p(block_table), max_pages, _p(ctx_len),
-                             _p(tok_off), B, total, n_q, n_kv, d, float(scale), _p(out), _p(lse), _p(ws), ws.numel(),
-                             _stream(stream))
-    _ok("ee_chunk_attn", st)
+    st = lib().ee_chunk_attn(qp, qs, _tp(k_cache, bf16, "k_cache"), _tp(v_cache, bf16, "v_cache"), cache[0],
+                             table, max_pages, ctx, off, B, total, n_q, cache[1], d, scale, op, lp, ws.data_ptr(),
+                             ws.numel(), _stream(stream))
+    if st:
+        raise EEError("ee_chunk_attn", st)

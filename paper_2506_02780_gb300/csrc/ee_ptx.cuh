@@ -220,6 +220,10 @@ __device__ __forceinline__ bool wait_count_geq(const uint32_t* cnt, uint32_t tar
     if (cycles() - t0 > kWaitLimitCycles) return false;
   return true;
 }
+// gpu-scope release add on a 32-bit count
+__device__ __forceinline__ void red_add_release(uint32_t* a, uint32_t v) {
+  asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(a), "r"(v) : "memory");
+}
 // gpu-scope release increment that wraps from `last` to zero, and the bounded wait of
 // an arriver for the wrap
 __device__ __forceinline__ void red_inc_release(uint32_t* a, uint32_t last) {

@@ -15,11 +15,13 @@
 //
 // Work.  The keys of all units (plus a constant for each: a unit's start and end) are
 // laid on one line, cut into equal shares, one for each CTA; one CTA runs on each SM.
-// A share may begin and end inside a unit.  Such a unit's pieces leave (m, l) and the
-// unnormalised O in the workspace, meet at a count and each merge a part of the rows
-// and columns with weights 2^(m - max).  Every length follows from the device's
-// offsets: long prompts, ragged batches and single tokens over long contexts are one
-// case.  The launch is cooperative, so a wait for another CTA ends.
+// A share may begin and end inside a unit.  Such a unit's pieces are joined with weights
+// 2^(m - max): of up to kDirect pieces all but the first leave (m, l) and the
+// unnormalised O in the workspace and the first piece's CTA joins them to its own on
+// the way out; of more (few units, long contexts) all do, meet at a count and each join
+// a part of the rows and columns.  Every length follows from the device's offsets: long
+// prompts, ragged batches and single tokens over long contexts are one case.  The
+// launch is cooperative, so a wait for another CTA ends.
 //
 // Roles of a CTA's twelve warps; all walk the share's segments (tile ranges of units)
 // by themselves, from a ring the scheduler fills:
@@ -51,14 +53,14 @@ constexpr int kMasks = 8;                     // page masks in flight (K runs at
 constexpr uint32_t kHalf = kKT * 128;         // 64 of a tile's 128 columns
 constexpr uint32_t kTile = 2 * kHalf;         // 32 KB
 constexpr uint32_t kOffKV = 0, kOffQ = kRing * kTile, kOffOut = kOffQ + 2 * kTile;
-constexpr uint32_t kOutBytes = 32 * 64;       // a softmax warp's rows x 32 columns of bf16, on their way out
+constexpr uint32_t kOutBytes = 32 * 128;      // a softmax warp's rows x 64 columns of bf16, on their way out
 constexpr uint32_t kOffBar = kOffOut + 8 * kOutBytes;
 constexpr uint32_t kNumBars = 2 * kRing + 4 + 10 + 2 * kSegs + kZones + 1;
 constexpr uint32_t kSmemBytes = 1024 + kOffBar + 8 * kNumBars;
 constexpr uint32_t kTmemCols = 512, kColO = 256;
 constexpr float kRescaleLog2 = 8.0f;          // O is rescaled when a maximum grows by 2^8
 // work in keys: a unit's own constant, and the smallest share of a CTA
-constexpr int kUnitKeys = 3 * kKT, kMinShare = 5 * kKT;
+constexpr int kUnitKeys = 256, kMinShare = 5 * kKT;
 static_assert(kMinShare >= kKT, "every CTA between a unit's first and last piece holds one");
 constexpr int kWarpKV = 0, kWarpMma = 1, kWarpQ = 2, kWarpClean = 3, kWarpSoft = 4;
 constexpr int kVBox = 32;                     // packed V: rows of a box
@@ -67,9 +69,11 @@ constexpr int kRegsLaunch = 168, kRegsSoft = 208, kRegsOther = 88;
 static_assert(kRing == 4, "two slots each for K and V tiles");
 static_assert(256 * kRegsSoft + 128 * kRegsOther <= kThreads * kRegsLaunch, "register split");
 static_assert(kSmemBytes <= 227 * 1024 - 1024, "shared memory budget");
-// count of a split unit's finished pieces, in the trailer of its first piece's slot
-// past the word that the verification attention keeps there
-constexpr size_t kCntOff = kAttnCntOff + 64;
+// counts of a split unit's finished pieces, in the trailer of its first piece's slots
+// past the word that the verification attention keeps there: one for each softmax
+// warp (units of at most kDirect pieces), one for all (of more)
+constexpr size_t kCntOff = kAttnCntOff + 64, kCntAllOff = kAttnCntOff + 128;
+constexpr int kDirect = 3;
 
 struct PromptParams {
   const __nv_bfloat16* v;       // V once more, for values the MMA must not see
@@ -200,7 +204,9 @@ struct Shares {
   // the last CTA whose share starts before place y (y > 0)
   __device__ __forceinline__ int before(int64_t y) const {
     int c = min(max((int)((float)y / (float)W * N), 0), N - 1);
+#pragma unroll 1
     while (start(c) >= y) --c;
+#pragma unroll 1
     while (c + 1 < N && start(c + 1) < y) ++c;
     return c;
   }
@@ -277,13 +283,14 @@ struct Joined {
 
 // Items [lo, hi) of a split unit merged by one of its pieces: thread t of nthr.  An
 // item is eight columns of a row, numbered rows fastest, so that a warp's loads of a
-// slot (column-chunk major) are contiguous.  A thread loads four items of two pieces at
+// slot (column-chunk major) are contiguous.  A thread loads two items of two pieces at
 // a time (a round trip to L2 costs about 1,000 cycles).  With few items and many pieces
 // `sub` lanes share an item, each over every sub-th piece.
 __device__ __forceinline__ void merge_items(const PromptParams& p, const Seg& s, int lo, int hi, int t, int nthr) {
-  constexpr int kItems = 4;
+  constexpr int kItems = 2;
   const int K = s.c1 - s.c0 + 1;
   int sub = 1;
+#pragma unroll 1
   while (sub < 32 && sub < K && (hi - lo) * 2 * sub <= nthr) sub *= 2;
   const int nt = min(2 * p.tpt, s.T - s.tok0);               // tokens of the unit
   const int rows_a = min(nt, p.tpt) * p.g, rows = nt * p.g;  // rows of A, of both
@@ -329,6 +336,7 @@ __device__ __forceinline__ void merge_items(const PromptParams& p, const Seg& s,
     }
 #pragma unroll
     for (int n = 0; n < kItems; ++n) {
+#pragma unroll 1
       for (int d = 1; d < sub; d *= 2) {
         float o[8];
         const float Mo = __shfl_xor_sync(0xffffffffu, x[n].M, d), Lo = __shfl_xor_sync(0xffffffffu, x[n].L, d);
@@ -389,11 +397,15 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmV)) : "memory");
     s_abort = 0;
     s_npc = 0;
+#pragma unroll 1
     for (int i = 0; i < kRing; ++i) s_kvissued[i] = -1;
+#pragma unroll 1
     for (int i = 0; i < kZones; ++i) s_zissued[i] = -1;
+#pragma unroll 1
     for (int i = 0; i < 2; ++i) s_qissued[i] = -1;
   }
   if (warp == kWarpKV) {   // one barrier a lane
+#pragma unroll 1
     for (int i = lane; i < (int)kNumBars; i += 32) {
       const uint32_t bar = bar0 + 8 * i;
       const uint32_t count = bar >= s_full && bar < p_half     ? kPaged + 1   // the commit (paged: and a release of the page mask)
@@ -413,6 +425,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   // rows of the Q tiles past g * tpt are never loaded
+#pragma unroll 1
   for (int i = tid; i < 2 * 2 * (kRows - p.g * p.tpt) * 8; i += kThreads) {
     const int c = i & 7, r = i >> 3, per = kRows - p.g * p.tpt;
     *reinterpret_cast<uint4*>(smem + kOffQ + (r / per) * kHalf + (p.g * p.tpt + r % per) * 128 + 16 * c) =
@@ -430,6 +443,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   Seq sq{0, 0, 0};
   {
     int err = 0;
+#pragma unroll 1
     for (int s = b0; s < b1; ++s) {
       sq = load_seq<kPaged>(p, s, err);
       sum += head_places(sq.ctx, sq.T, w) * p.n_kv;
@@ -457,6 +471,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     int s = b0;
     if (per > 1) {
       int err = 0;
+#pragma unroll 1
       for (;; ++s) {
         sq = load_seq<kPaged>(p, s, err);
         const int64_t n = head_places(sq.ctx, sq.T, w) * p.n_kv;
@@ -495,6 +510,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       Seg s;
       int tile = 0, zone = 0;
       bool go = true;
+#pragma unroll 1
       for (int i = 0; go && receive(i, s); ++i) {
         // paged: lane l holds the page of 16-key block l % 8 of the (l / 8)-th of four tiles
         const int last = s.ctx + min(s.T, s.tok0 + w) - 1;
@@ -505,6 +521,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         };
         int32_t ids = INT32_MIN, ids_next = INT32_MIN;
         if constexpr (kPaged) ids_next = fetch(s.j0);
+#pragma unroll 1
         for (int j = s.j0; j < s.j1 && go; ++j, ++tile) {
           int row[8];
           uint32_t okm = 0;
@@ -526,7 +543,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             }
             if (bad && lane == 0) flag_error(p.err, EE_DEVERR_PAGE);
           }
-#pragma unroll
+#pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {
             const int idx = 2 * tile + kv, slot = idx % kRing, use = idx / kRing;
             go = go && wait(kv_empty + 8 * slot, use + 1);
@@ -594,10 +611,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         int64_t rem = x0 - X;
         hk = min((int)((float)rem / (float)per_head), p.n_kv - 1);
         rem -= hk * per_head;
+#pragma unroll 1
         for (; rem < 0; rem += per_head) --hk;
+#pragma unroll 1
         for (; rem >= per_head; rem -= per_head) ++hk;
         X += hk * per_head;
         int lo = 0, hi = num_units(T, w);
+#pragma unroll 1
         while (hi - lo > 1) {
           const int mid = (lo + hi) >> 1;
           if (places_before(ctx, w, mid) <= rem) lo = mid; else hi = mid;
@@ -607,6 +627,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       }
       // the next non-empty segment of the share
       auto find = [&](Seg& g) -> bool {
+#pragma unroll 1
         while (X < x1) {
           if (n >= num_units(T, w)) {          // next head, or next sequence with tokens
             n = 0;
@@ -658,7 +679,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (lane == 0) {
           s_seg[i % kSegs] = g;
           s_bad[i % kSegs] = 0;
-          if (g.j1 - g.j0 < g.n_tiles && g.j1 > 0) {
+          if (g.j1 > 0 && g.j1 - g.j0 < g.n_tiles && g.c1 - g.c0 >= kDirect) {
             s_pc[s_npc & 1] = g;
             s_npc = s_npc + 1;
           }
@@ -697,8 +718,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       Seg s;
       int tile = 0, zone = 0;
       bool go = true;
+#pragma unroll 1
       for (int i = 0; go && receive(i, s); ++i) {
         const int first = s.ctx + s.tok0, last = s.ctx + min(s.T, s.tok0 + w) - 1;
+#pragma unroll 1
         for (int j = s.j0; j < s.j1 && go; ++j, ++tile) {
           if (!in_zone(s, j)) continue;
           const int slot = (2 * tile + 1) % kRing;
@@ -891,10 +914,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     if (s_abort) {
       if (tid == 0) {
         flag_error(p.err, EE_DEVERR_TIMEOUT);
+#pragma unroll 1
         for (int i = 0; i < kRing; ++i)
           if (s_kvissued[i] >= 0) mbar_wait_plain(kv_full + 8 * i, (uint32_t)(s_kvissued[i] & 1));
+#pragma unroll 1
         for (int i = 0; i < kZones; ++i)
           if (s_zissued[i] >= 0) mbar_wait_plain(z_full + 8 * i, (uint32_t)(s_zissued[i] & 1));
+#pragma unroll 1
         for (int i = 0; i < 2; ++i)
           if (s_qissued[i] >= 0) mbar_wait_plain(q_full + 8 * i, (uint32_t)(s_qissued[i] & 1));
       }
@@ -925,6 +951,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     Seg s;
     int tile = 0, uses = 0, o_uses = 0;
     bool go = true;
+#pragma unroll 1
     for (int i = 0; go && receive(i, s); ++i) {
       const int tok = s.tok0 + st * p.tpt + tok_r;
       const bool vrow = tok_r < p.tpt && tok < s.T;
@@ -933,6 +960,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       const int tile_first = s.ctx + s.tok0 + st * p.tpt;      // the row tile's first row's
       const int j_end = min(s.j1, st ? s.nB : s.nA);
       float m = -INFINITY, l = 0.f;                            // m in raw score units (scale > 0)
+#pragma unroll 1
       for (int j = s.j0; j < j_end; ++j) {
         go = wait(s_full + 8 * st, uses);
         if (!go) break;
@@ -1020,47 +1048,104 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         ++o_uses;
         tc_fence_after();
       }
-      const float il = l == 0.f ? 0.f : 1.f / l;
+      // Few pieces: the first piece's CTA, which comes to it last of all its segments, joins
+      // the others' partials, which their CTAs left long before (as their first segment),
+      // to its own O on the way out.  Many: each piece leaves a partial (below).
+      const bool direct = !whole && s.c1 - s.c0 < kDirect, first = direct && s.j0 == 0;
+      const bool fin = whole || first;
+      const int others = first ? s.c1 - s.c0 : 0;
+      uint32_t* cnt = reinterpret_cast<uint32_t*>(p.part + (size_t)(2 * (2 * s.c0 + 1) + st) * kAttnPartBytes + kCntOff) + qd;
+      if (first) {
+        bool done = true;
+        if (lane == 0) {
+          done = wait_count_geq(cnt, (uint32_t)others);
+          *cnt = 0;              // for the next launch
+          if (!done) s_abort = 1;
+        }
+        go = __all_sync(0xffffffffu, done);
+        if (!go) break;
+      }
+      float M = m == -INFINITY ? m : m * sl2, fx[kDirect - 1] = {}, f0 = 1.f;   // M: of base-2 exponents
+      const float m2 = M;
+      {
+        float2 ml[kDirect - 1];
+#pragma unroll
+        for (int k = 0; k < kDirect - 1; ++k)
+          ml[k] = k < others && vrow
+                      ? __ldcg(reinterpret_cast<const float2*>(p.part + (size_t)(4 * (s.c0 + 1 + k) + st) * kAttnPartBytes + kAttnMlOff) + r)
+                      : make_float2(-INFINITY, 0.f);
+        if (first) {
+#pragma unroll
+          for (int k = 0; k < kDirect - 1; ++k) M = fmaxf(M, ml[k].x);
+          f0 = m2 == M ? 1.f : ex2(m2 - M);
+          l *= f0;
+#pragma unroll
+          for (int k = 0; k < kDirect - 1; ++k) {
+            // (a row without keys in the piece has l = 0 and no O)
+            fx[k] = ml[k].y == 0.f ? 0.f : ml[k].x == M ? 1.f : ex2(ml[k].x - M);
+            l = fmaf(ml[k].y, fx[k], l);
+          }
+        }
+      }
+      const float il = l == 0.f ? 0.f : 1.f / l, s0 = f0 * il;
       // output rows: from the row tile's first, by token and head
       const size_t row0 = (size_t)(s.o + s.tok0 + st * p.tpt) * p.n_q + s.hk * p.g;
       const uint32_t orow = vrow ? (uint32_t)tok_r * p.n_q + head : UINT32_MAX;
-      const int slot = whole ? 0 : 2 * (2 * (int)blockIdx.x + (s.j0 == 0 ? 1 : 0)) + st;
+      const int slot = fin ? 0 : 2 * (2 * (int)blockIdx.x + (s.j0 == 0 ? 1 : 0)) + st;
       uint8_t* part = p.part + (size_t)slot * kAttnPartBytes;
       if (any && warp_rows) {
-        uint32_t dst[4];       // the output rows whose pieces this lane carries out
-        if (whole) {
+        uint32_t dst[8];       // the output rows whose pieces this lane carries out
 #pragma unroll
-          for (int e = 0; e < 4; ++e) dst[e] = __shfl_sync(0xffffffffu, orow, 8 * e + (lane >> 2));
-        }
+        for (int e = 0; e < 8; ++e) dst[e] = __shfl_sync(0xffffffffu, orow, 4 * e + (lane >> 3));
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           uint32_t ov[32];
           tc_ld32_nowait(tO + 32 * c, ov);
           tc_wait_ld32(ov);
-          if (whole) {
-            // through shared memory: a row's 64 bytes leave from four neighbouring lanes
+          if (fin) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * s0);
+#pragma unroll 1
+            for (int k = 0; k < others; ++k) {
+              const float f = (k == 0 ? fx[0] : fx[1]) * il;
+              const float4* o = reinterpret_cast<const float4*>(p.part + (size_t)(4 * (s.c0 + 1 + k) + st) * kAttnPartBytes) +
+                                (size_t)(8 * c) * kRows + r;
+              float4 x[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] = f != 0.f && vrow ? __ldcg(o + e * kRows) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                ov[4 * e] = __float_as_uint(fmaf(x[e].x, f, __uint_as_float(ov[4 * e])));
+                ov[4 * e + 1] = __float_as_uint(fmaf(x[e].y, f, __uint_as_float(ov[4 * e + 1])));
+                ov[4 * e + 2] = __float_as_uint(fmaf(x[e].z, f, __uint_as_float(ov[4 * e + 2])));
+                ov[4 * e + 3] = __float_as_uint(fmaf(x[e].w, f, __uint_as_float(ov[4 * e + 3])));
+              }
+            }
+            // through shared memory: a row's 128 bytes leave from eight neighbouring lanes
             // (one lane a row touches 32 lines with each store: 3,500 cycles a row tile)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               uint4 x;
-              x.x = bf16x2_rn(__uint_as_float(ov[8 * e + 1]) * il, __uint_as_float(ov[8 * e]) * il);
-              x.y = bf16x2_rn(__uint_as_float(ov[8 * e + 3]) * il, __uint_as_float(ov[8 * e + 2]) * il);
-              x.z = bf16x2_rn(__uint_as_float(ov[8 * e + 5]) * il, __uint_as_float(ov[8 * e + 4]) * il);
-              x.w = bf16x2_rn(__uint_as_float(ov[8 * e + 7]) * il, __uint_as_float(ov[8 * e + 6]) * il);
-              *reinterpret_cast<uint4*>(s_out + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) = x;
+              x.x = bf16x2_rn(__uint_as_float(ov[8 * e + 1]), __uint_as_float(ov[8 * e]));
+              x.y = bf16x2_rn(__uint_as_float(ov[8 * e + 3]), __uint_as_float(ov[8 * e + 2]));
+              x.z = bf16x2_rn(__uint_as_float(ov[8 * e + 5]), __uint_as_float(ov[8 * e + 4]));
+              x.w = bf16x2_rn(__uint_as_float(ov[8 * e + 7]), __uint_as_float(ov[8 * e + 6]));
+              *reinterpret_cast<uint4*>(s_out + lane * 128 + (((4 * (c & 1) + e) ^ (lane & 7)) << 4)) = x;
             }
-            __syncwarp();
-            uint4 x[4];
+            if (c & 1) {
+              __syncwarp();
+              uint4 x[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int rr = 8 * e + (lane >> 2);
-              x[e] = *reinterpret_cast<const uint4*>(s_out + rr * 64 + (((lane ^ (rr >> 1)) & 3) << 4));
+              for (int e = 0; e < 8; ++e) {
+                const int rr = 4 * e + (lane >> 3);
+                x[e] = *reinterpret_cast<const uint4*>(s_out + rr * 128 + (((lane ^ rr) & 7) << 4));
+              }
+              __nv_bfloat16* o = p.out + row0 * kD + 32 * (c - 1) + 8 * (lane & 7);
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (dst[e] != UINT32_MAX) *reinterpret_cast<uint4*>(o + (size_t)dst[e] * kD) = x[e];
+              __syncwarp();
             }
-            __nv_bfloat16* o = p.out + row0 * kD + 32 * c + 8 * (lane & 3);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (dst[e] != UINT32_MAX) *reinterpret_cast<uint4*>(o + (size_t)dst[e] * kD) = x[e];
-            __syncwarp();
           } else if (vrow) {
             float4* o = reinterpret_cast<float4*>(part) + (size_t)(8 * c) * kRows + r;
 #pragma unroll
@@ -1070,19 +1155,20 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                                  __uint_as_float(ov[4 * e + 2]), __uint_as_float(ov[4 * e + 3])));
           }
         }
-        if (s_bad[i % kSegs]) {   // values taken out of V: for the rows that see them
-          __syncwarp();
-          if (vrow)
-            add_nonfinite<kPaged>(p, s, max(s.ctx + s.tok0 + 1, s.j0 * kKT), min(pos, s.j1 * kKT - 1),
-                                  whole ? p.out + (row0 + orow) * kD : nullptr, reinterpret_cast<float*>(part) + 4 * r);
-        }
         tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(o_free + 8 * st);
+        if (s_bad[i % kSegs] && vrow)   // values taken out of V: for the rows that see them
+          add_nonfinite<kPaged>(p, s, max(s.ctx + s.tok0 + 1, s.j0 * kKT), min(pos, s.j1 * kKT - 1),
+                                fin ? p.out + (row0 + orow) * kD : nullptr, reinterpret_cast<float*>(part) + 4 * r);
+      } else if (any) {
+        tc_fence_before();
+        if (lane == 0) mbar_arrive(o_free + 8 * st);
       }
-      if (vrow && whole && p.lse) p.lse[row0 + orow] = l == 0.f ? -INFINITY : fmaf(m, p.scale, logf(l));
-      if (vrow && !whole)
-        __stcg(reinterpret_cast<float2*>(part + kAttnMlOff) + r, make_float2(m == -INFINITY ? m : m * sl2, l));
+      if (vrow && fin && p.lse) p.lse[row0 + orow] = l == 0.f ? -INFINITY : (M + log2f(l)) * 0.6931471805599453f;
+      if (vrow && !fin) __stcg(reinterpret_cast<float2*>(part + kAttnMlOff) + r, make_float2(m2, l));
       __syncwarp();
-      if (any && lane == 0) mbar_arrive(o_free + 8 * st);
+      if (direct && !first && lane == 0) red_add_release(cnt, 1);
       release(i);
     }
   }
@@ -1091,7 +1177,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   pdl_allow_next();
   if (s_abort) return;
 
-  // ---- pieces of split units: counted, waited for and merged ----
+  // ---- pieces of units split among many: counted, waited for and merged ----
   const int npc = s_npc;
   if (npc == 0) return;
   const int nthr = npc == 2 ? 128 : 256;
@@ -1100,7 +1186,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   const int K = s.c1 - s.c0 + 1, mine = (int)blockIdx.x - s.c0;
   if (t == 0) {
     // the count wraps to zero with the last arrival: nothing resets it
-    uint32_t* cnt = reinterpret_cast<uint32_t*>(p.part + (size_t)(2 * (2 * s.c0 + 1)) * kAttnPartBytes + kCntOff);
+    uint32_t* cnt = reinterpret_cast<uint32_t*>(p.part + (size_t)(2 * (2 * s.c0 + 1)) * kAttnPartBytes + kCntAllOff);
     red_inc_release(cnt, (uint32_t)(K - 1));
     const bool ok = wait_count_zero(cnt);
     if (!ok) flag_error(p.err, EE_DEVERR_TIMEOUT);
