@@ -220,15 +220,17 @@ __device__ __forceinline__ bool wait_count_geq(const uint32_t* cnt, uint32_t tar
     if (cycles() - t0 > kWaitLimitCycles) return false;
   return true;
 }
-// gpu-scope release add on a 32-bit count
-__device__ __forceinline__ void red_add_release(uint32_t* a, uint32_t v) {
-  asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(a), "r"(v) : "memory");
-}
-// gpu-scope release increment that wraps from `last` to zero, and the bounded wait of
-// an arriver for the wrap
+// gpu-scope release increment that wraps from `last` to zero
 __device__ __forceinline__ void red_inc_release(uint32_t* a, uint32_t last) {
   asm volatile("red.release.gpu.global.inc.u32 [%0], %1;" ::"l"(a), "r"(last) : "memory");
 }
+// the same with the count before it, and acquiring
+__device__ __forceinline__ uint32_t atom_inc_acq_rel(uint32_t* a, uint32_t last) {
+  uint32_t old;
+  asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(old) : "l"(a), "r"(last) : "memory");
+  return old;
+}
+// (the wait of an arriver of red_inc_release for the wrap)
 __device__ __forceinline__ bool wait_count_zero(const uint32_t* cnt) {
   const long long t0 = cycles();
   while (ld_acquire(cnt) != 0)

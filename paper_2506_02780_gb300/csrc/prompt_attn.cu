@@ -16,12 +16,12 @@
 // Work.  The keys of all units (plus a constant for each: a unit's start and end) are
 // laid on one line, cut into equal shares, one for each CTA; one CTA runs on each SM.
 // A share may begin and end inside a unit.  Such a unit's pieces are joined with weights
-// 2^(m - max): of up to kDirect pieces all but the first leave (m, l) and the
-// unnormalised O in the workspace and the first piece's CTA joins them to its own on
-// the way out; of more (few units, long contexts) all do, meet at a count and each join
-// a part of the rows and columns.  Every length follows from the device's offsets: long
-// prompts, ragged batches and single tokens over long contexts are one case.  The
-// launch is cooperative, so a wait for another CTA ends.
+// 2^(m - max): of up to kDirect pieces the last to finish joins the partials (m, l,
+// unnormalised O) that the others left in the workspace to its own O on the way out; of
+// more, all leave theirs, and the last to finish joins them or, in a call of few units,
+// all meet at a count and each join a part (such a call is launched cooperatively, so
+// that the wait ends).  Every length follows from the device's offsets: long prompts,
+// ragged batches and single tokens over long contexts are one case.
 //
 // Roles of a CTA's twelve warps; all walk the share's segments (tile ranges of units)
 // by themselves, from a ring the scheduler fills:
@@ -60,8 +60,9 @@ constexpr uint32_t kSmemBytes = 1024 + kOffBar + 8 * kNumBars;
 constexpr uint32_t kTmemCols = 512, kColO = 256;
 constexpr float kRescaleLog2 = 8.0f;          // O is rescaled when a maximum grows by 2^8
 // work in keys: a unit's own constant, and the smallest share of a CTA
-constexpr int kUnitKeys = 256, kMinShare = 5 * kKT;
-static_assert(kMinShare >= kKT, "every CTA between a unit's first and last piece holds one");
+constexpr int kUnitKeys = 320;
+constexpr int kShareMany = 5 * kKT, kShareFew = 5 * kKT / 4;
+static_assert(kShareFew >= kKT, "every CTA between a unit's first and last piece holds one");
 constexpr int kWarpKV = 0, kWarpMma = 1, kWarpQ = 2, kWarpClean = 3, kWarpSoft = 4;
 constexpr int kVBox = 32;                     // packed V: rows of a box
 constexpr int kSegReaders = 3 + 8;            // warps 0, 1, 3 and the softmax warps
@@ -84,6 +85,8 @@ struct PromptParams {
   uint8_t* part;
   int32_t* err;
   int B, total, num_pages, max_pages, n_q, n_kv, g, tpt;
+  int units;                    // of the call, at most
+  int min_share, coop;
   float scale, scale_log2;
 };
 
@@ -112,44 +115,31 @@ __device__ __forceinline__ float fmax3(float a, float b, float c) {
   return r;
 }
 
-// the largest of a row's 128 scores (a NaN is passed over)
-__device__ __forceinline__ float row_max(const uint32_t (&sr)[128]) {
-  float mx[8];
+// The larger of m and 32 scores (a NaN is passed over).
+__device__ __forceinline__ float max32(const uint32_t (&x)[32], float m) {
+  float a = m, b = __uint_as_float(x[0]);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) mx[k] = fmaxf(__uint_as_float(sr[k]), __uint_as_float(sr[8 + k]));
-#pragma unroll
-  for (int c = 16; c < 128; c += 16)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) mx[k] = fmax3(mx[k], __uint_as_float(sr[c + k]), __uint_as_float(sr[c + 8 + k]));
-  return fmax3(fmax3(mx[0], mx[1], mx[2]), fmax3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7]));
+  for (int k = 1; k < 31; k += 4) {
+    a = fmax3(a, __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+    if (k + 3 < 32) b = fmax3(b, __uint_as_float(x[k + 2]), __uint_as_float(x[k + 3]));
+  }
+  return fmax3(a, b, __uint_as_float(x[31]));
 }
-
-// P = 2^(S sl2 + nms) of half a row, rounded to bf16 over S in tensor memory; the fp32
-// values' sums in ls (set by half 0, added to by half 1).  Scale and shift and the sums
-// take one packed instruction a pair of columns.
-template <int kHalfRow>
-__device__ __forceinline__ void exp_half(const uint32_t (&sr)[128], uint32_t tS, float sl2, float nms,
-                                         uint64_t (&ls)[4]) {
-  const uint64_t sl2x2 = f2_pack(__float_as_uint(sl2), __float_as_uint(sl2));
-  const uint64_t nmsx2 = f2_pack(__float_as_uint(nms), __float_as_uint(nms));
+// P = 2^(S sl2 + nms) of 32 scores, rounded to bf16 and packed; the fp32 values are added
+// to ls.  Scale and shift and the sums take one packed instruction a pair.
+__device__ __forceinline__ void exp32(const uint32_t (&x)[32], uint64_t sl2x2, uint64_t nmsx2, uint64_t (&ls)[2],
+                                      uint32_t (&pw)[16]) {
 #pragma unroll
-  for (int c = 2 * kHalfRow; c < 2 * kHalfRow + 2; ++c) {
-    uint32_t pw[16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int x = 32 * c + 2 * e;
-      uint32_t y0, y1;
-      f2_unpack(f2_fma(f2_pack(sr[x], sr[x + 1]), sl2x2, nmsx2), y0, y1);
-      const float p0 = ex2(__uint_as_float(y0)), p1 = ex2(__uint_as_float(y1));
-      const uint64_t pp = f2_pack(__float_as_uint(p0), __float_as_uint(p1));
-      ls[e & 3] = c == 0 && e < 4 ? pp : f2_add(ls[e & 3], pp);
-      pw[e] = bf16x2_rn(p1, p0);
-    }
-    tc_st16_nowait(tS + 16 * c, pw);
+  for (int e = 0; e < 16; ++e) {
+    uint32_t y0, y1;
+    f2_unpack(f2_fma(f2_pack(x[2 * e], x[2 * e + 1]), sl2x2, nmsx2), y0, y1);
+    const float p0 = ex2(__uint_as_float(y0)), p1 = ex2(__uint_as_float(y1));
+    ls[e & 1] = f2_add(ls[e & 1], f2_pack(__float_as_uint(p0), __float_as_uint(p1)));
+    pw[e] = bf16x2_rn(p1, p0);
   }
 }
 
-// One sequence: first token, tokens, cached positions (T = 0: nothing to do).
+// One sequence: first token// One sequence: first token, tokens, cached positions (T = 0: nothing to do).
 struct Seq {
   int o, T, ctx;
 };
@@ -185,11 +175,16 @@ __device__ __forceinline__ int64_t head_places(int ctx, int T, int w) {
   const int64_t P = num_units(T, w);
   return places_before(ctx, w, P - 1) + ctx + T + kUnitConst;
 }
-// tiles of a unit of n that lie before place y of it
+// tiles of a unit of n that lie before place y of it; a cut within kSnap tiles of the
+// unit's start or end moves there
+constexpr int kSnap = 2;
 __device__ __forceinline__ int tiles_before(int64_t y, int n) {
   const int64_t j = (y - kUnitKeys + kKT / 2) >> 7;
-  return (int)min(max(j, (int64_t)0), (int64_t)n);
+  return j < kSnap ? 0 : j > n - kSnap ? n : (int)j;
 }
+// the first places that tiles_before puts past the unit's start, and at its end
+constexpr int kPastStart = kUnitKeys - kKT / 2 + kSnap * kKT;
+__device__ __forceinline__ int at_end(int n) { return kUnitKeys - kKT / 2 + (n - kSnap + 1) * kKT; }
 // W places (below 2^56) cut for N CTAs: CTA c's share starts at floor(c W / N)
 struct Shares {
   int64_t W, q;      // q = W / N, r = W mod N, by two 32-bit divisions
@@ -464,7 +459,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     }
     base += incl - sum;
   }
-  const Shares sh(W, (int)min((int64_t)gridDim.x, max(W / kMinShare, (int64_t)1)));
+  // as many CTAs as the units or the shortest share allow
+  const Shares sh(
+      W, (int)min((int64_t)gridDim.x, max(max(W / p.min_share, min(W / kShareFew, (int64_t)p.units)), (int64_t)1)));
   const bool works = (int)blockIdx.x < sh.N && W > 0;
   const int64_t x0 = works ? sh.start(blockIdx.x) : W, x1 = works ? sh.start(blockIdx.x + 1) : W;
   if (works && x0 >= base && x0 < base + sum) {
@@ -585,20 +582,19 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       // ---------------- segments and Q ----------------
       // lane l holds sequence base + l, so that many short sequences cost one
       // round trip for 32 of them
-      int s = works ? s_first : p.B, base = s + 1, err = 0;   // (a CTA without a share: none is set)
+      int s = works ? s_first : p.B, base = 0, err = 0;   // (a CTA without a share: none is set)
+      bool loaded = false;
       Seq mine{0, 0, 0};
-      auto load32 = [&]() {
+      auto load32 = [&](int from) {
+        base = from;
+        loaded = true;
         mine = Seq{0, 0, 0};
         if (base + lane < p.B) mine = load_seq<kPaged>(p, base + lane, err);
       };
-      load32();
       int64_t X = works ? s_firstX : x1;                      // the next unit's first place
       int o = 0, T = 0, ctx = 0, hk = 0, n = 0;
       auto take = [&]() {        // sequence s from its lane
-        if (s - base >= 32) {
-          base = s;
-          load32();
-        }
+        if (!loaded || s - base >= 32) load32(s);
         o = __shfl_sync(0xffffffffu, mine.o, s - base);
         T = __shfl_sync(0xffffffffu, mine.T, s - base);
         ctx = __shfl_sync(0xffffffffu, mine.ctx, s - base);
@@ -616,13 +612,15 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 #pragma unroll 1
         for (; rem >= per_head; rem -= per_head) ++hk;
         X += hk * per_head;
-        int lo = 0, hi = num_units(T, w);
+        // the last unit that starts at or before rem: places_before(n) <= rem solved for n,
+        // then put right (the root is off by a few units at most)
+        const int units = num_units(T, w);
+        const float b = (float)(ctx + kUnitConst) + 0.5f * w;
+        n = min(max((int)((sqrtf(b * b + 2.f * w * (float)rem) - b) / w), 0), units - 1);
 #pragma unroll 1
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (places_before(ctx, w, mid) <= rem) lo = mid; else hi = mid;
-        }
-        n = lo;
+        while (places_before(ctx, w, n) > rem) --n;
+#pragma unroll 1
+        while (n + 1 < units && places_before(ctx, w, n + 1) <= rem) ++n;
         X += places_before(ctx, w, n);
       }
       // the next non-empty segment of the share
@@ -661,13 +659,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           g.nB = T > tok0 + p.tpt ? tiles : 0;
           g.c0 = g.c1 = 0;
           if (j1 - j0 < tiles) {
-            // the first piece is the last CTA's whose share starts before the second
-            // tile's places do, the last piece that of the last CTA whose share starts
-            // before the last tile's; shares are no shorter than a tile, so every CTA
-            // between them holds one
-            const int64_t y = g.X + kUnitKeys + kKT / 2;
-            g.c0 = sh.before(y);
-            g.c1 = sh.before(y + (int64_t)kKT * (tiles - 1));
+            // the first piece is that of the last CTA whose share starts before kPastStart,
+            // the last piece that of the last whose share starts before at_end; shares are
+            // no shorter than a tile, so every CTA between them holds one
+            g.c0 = sh.before(g.X + kPastStart);
+            g.c1 = sh.before(g.X + at_end(tiles));
           }
           return true;
         }
@@ -688,16 +684,18 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         __syncwarp();
         return true;
       };
-      // segment i is published before Q of segment i - 1 is waited for
+      // The first segment's Q is loaded at once; from then on segment i is published
+      // before Q of segment i - 1, whose buffer may still be in use, is waited for.
       Seg cur, nxt;
       uint32_t q_phase = 3;      // bit st: parity that the row tile's Q buffer is free at
-      bool more = true, go = true;
+      bool go = true, more = true, pending = false;
 #pragma unroll 1
-      for (int i = 0; more && go; ++i) {
+      for (int i = 0; go && more; ++i) {
         more = find(nxt);
         go = publish(i, nxt);
+        if (i == 0) cur = nxt;
 #pragma unroll 1
-        for (int st = 0; st < 2 && i > 0 && go; ++st) {
+        for (int st = 0; st < 2 && go && (pending || (i == 0 && more)); ++st) {
           if (!active(cur, st, cur.j0)) continue;
           go = wait(q_empty + 8 * st, q_phase >> st);
           if (go && elect_one()) {
@@ -712,6 +710,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           q_phase ^= 1u << st;
         }
         cur = nxt;
+        pending = i > 0;
+        if (!loaded && more) load32(s + 1);   // the sequences to come, beside the first segment's work
       }
     } else if (warp == kWarpClean) {
       // ---------------- V where a query's last key or the unit's last lies inside a tile ----
@@ -984,28 +984,26 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             }
             tc_wait_st();
           }
-          uint32_t sr[128];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tc_ld32_nowait(tS + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(&sr[32 * c]));
-          tc_wait_ld32(*reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
-#pragma unroll
-          for (int c = 1; c < 4; ++c) tc_pin32(*reinterpret_cast<uint32_t(*)[32]>(&sr[32 * c]));
-          if (j == s.j0) m = row_max(sr);
-          // The first half of P is formed with the running maximum as it was, while the
-          // tile's own is found beside it (exponentials keep the other pipes free); only
-          // where it has grown by more than 2^8 is O rescaled and the half formed again.
-          uint64_t ls[4];
-          float nms;
+          // Two rolled passes over the tile's scores, 32 at a time with the next 32 on their
+          // way: the tile's maximum, then the exponentials.  (All 128 in registers and the
+          // passes unrolled is 7 KB of code, more than a scheduler's instruction cache keeps
+          // beside its other warps' code: 3 cycles an instruction instead of 1.5.)
+          uint32_t xa[32], xb[32];
+          float tmax = -INFINITY;
+          tc_ld32_nowait(tS, xa);
 #pragma unroll 1
-          for (;;) {
-            nms = m == -INFINITY ? 0.f : -m * sl2;
-            exp_half<0>(sr, tS, sl2, nms, ls);
-            const float tmax = row_max(sr);
-            const bool need = (tmax - m) * sl2 > kRescaleLog2;   // true when m = -inf < tmax
-            if (!__any_sync(0xffffffffu, need)) break;
-            // S of this tile was issued after P V of the one before: O holds it
+          for (int c = 0; c < 2; ++c) {
+            tc_wait_ld32(xa);
+            tc_ld32_nowait(tS + 64 * c + 32, xb);
+            tmax = max32(xa, tmax);
+            tc_wait_ld32(xb);
+            tc_ld32_nowait(tS + 64 * (c ^ 1), xa);   // (the second pass's first at last)
+            tmax = max32(xb, tmax);
+          }
+          const bool need = (tmax - m) * sl2 > kRescaleLog2;   // true when m = -inf < tmax
+          if (__any_sync(0xffffffffu, need)) {
             const float f = need ? ex2((m - tmax) * sl2) : 1.f;
-            if (j > s.j0) {
+            if (j > s.j0) {   // S of this tile was issued after P V of the one before: O holds it
 #pragma unroll 1
               for (int c = 0; c < 8; ++c) {
                 uint32_t ov[16];
@@ -1018,16 +1016,28 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             l *= f;
             m = need ? tmax : m;
           }
-          tc_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(p_half + 8 * st);
-          exp_half<1>(sr, tS, sl2, nms, ls);
-          tc_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(p_full + 8 * st);
-          ls[0] = f2_add(f2_add(ls[0], ls[1]), f2_add(ls[2], ls[3]));
+          const float nms = m == -INFINITY ? 0.f : -m * sl2;
+          const uint64_t sl2x2 = f2_pack(__float_as_uint(sl2), __float_as_uint(sl2));
+          const uint64_t nmsx2 = f2_pack(__float_as_uint(nms), __float_as_uint(nms));
+          uint64_t ls[2] = {0ull, 0ull};
+#pragma unroll 1
+          for (int c = 0; c < 2; ++c) {
+            // P of 64 keys goes to columns 32 c .. 32 c + 31, whose scores are in registers
+            uint32_t pw[16];
+            tc_wait_ld32(xa);
+            tc_ld32_nowait(tS + 64 * c + 32, xb);
+            exp32(xa, sl2x2, nmsx2, ls, pw);
+            tc_st16_nowait(tS + 32 * c, pw);
+            tc_wait_ld32(xb);
+            if (c == 0) tc_ld32_nowait(tS + 64, xa);
+            exp32(xb, sl2x2, nmsx2, ls, pw);
+            tc_st16_nowait(tS + 32 * c + 16, pw);
+            tc_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_half + 16 * c + 8 * st);   // (p_full follows p_half)
+          }
+          ls[0] = f2_add(ls[0], ls[1]);
           uint32_t a0, a1;
           f2_unpack(ls[0], a0, a1);
           l += __uint_as_float(a0) + __uint_as_float(a1);
@@ -1048,127 +1058,141 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         ++o_uses;
         tc_fence_after();
       }
-      // Few pieces: the first piece's CTA, which comes to it last of all its segments, joins
-      // the others' partials, which their CTAs left long before (as their first segment),
-      // to its own O on the way out.  Many: each piece leaves a partial (below).
-      const bool direct = !whole && s.c1 - s.c0 < kDirect, first = direct && s.j0 == 0;
-      const bool fin = whole || first;
-      const int others = first ? s.c1 - s.c0 : 0;
+      // Few pieces: each warp that finds its rows' other partials in place joins them to its
+      // own O on the way out, the others leave theirs (the first piece is its CTA's last
+      // segment and the others' first, so that it is mostly the one that joins).  The
+      // pieces are added in their order, whichever warp adds them.  Many: see below.
+      const int K = whole ? 1 : s.c1 - s.c0 + 1, own = whole ? 0 : (int)blockIdx.x - s.c0;
+      const bool direct = !whole && K <= kDirect;
       uint32_t* cnt = reinterpret_cast<uint32_t*>(p.part + (size_t)(2 * (2 * s.c0 + 1) + st) * kAttnPartBytes + kCntOff) + qd;
-      if (first) {
-        bool done = true;
-        if (lane == 0) {
-          done = wait_count_geq(cnt, (uint32_t)others);
-          *cnt = 0;              // for the next launch
-          if (!done) s_abort = 1;
-        }
-        go = __all_sync(0xffffffffu, done);
-        if (!go) break;
-      }
-      float M = m == -INFINITY ? m : m * sl2, fx[kDirect - 1] = {}, f0 = 1.f;   // M: of base-2 exponents
-      const float m2 = M;
-      {
-        float2 ml[kDirect - 1];
-#pragma unroll
-        for (int k = 0; k < kDirect - 1; ++k)
-          ml[k] = k < others && vrow
-                      ? __ldcg(reinterpret_cast<const float2*>(p.part + (size_t)(4 * (s.c0 + 1 + k) + st) * kAttnPartBytes + kAttnMlOff) + r)
-                      : make_float2(-INFINITY, 0.f);
-        if (first) {
-#pragma unroll
-          for (int k = 0; k < kDirect - 1; ++k) M = fmaxf(M, ml[k].x);
-          f0 = m2 == M ? 1.f : ex2(m2 - M);
-          l *= f0;
-#pragma unroll
-          for (int k = 0; k < kDirect - 1; ++k) {
-            // (a row without keys in the piece has l = 0 and no O)
-            fx[k] = ml[k].y == 0.f ? 0.f : ml[k].x == M ? 1.f : ex2(ml[k].x - M);
-            l = fmaf(ml[k].y, fx[k], l);
-          }
-        }
-      }
-      const float il = l == 0.f ? 0.f : 1.f / l, s0 = f0 * il;
+      bool fin = whole;
+      if (direct) fin = __shfl_sync(0xffffffffu, lane == 0 && ld_acquire(cnt) == (uint32_t)(K - 1), 0);
       // output rows: from the row tile's first, by token and head
       const size_t row0 = (size_t)(s.o + s.tok0 + st * p.tpt) * p.n_q + s.hk * p.g;
       const uint32_t orow = vrow ? (uint32_t)tok_r * p.n_q + head : UINT32_MAX;
-      const int slot = fin ? 0 : 2 * (2 * (int)blockIdx.x + (s.j0 == 0 ? 1 : 0)) + st;
-      uint8_t* part = p.part + (size_t)slot * kAttnPartBytes;
-      if (any && warp_rows) {
-        uint32_t dst[8];       // the output rows whose pieces this lane carries out
+      // partial slot of piece k: the first is its CTA's second
+      auto slot = [&](int k) { return p.part + (size_t)(2 * (2 * (s.c0 + k) + (k == 0)) + st) * kAttnPartBytes; };
+      const float m2 = m == -INFINITY ? m : m * sl2;      // of base-2 exponents
+      const bool bad = any && s_bad[i % kSegs];           // values taken out of V: for the rows that see them
+      const int key0 = max(s.ctx + s.tok0 + 1, s.j0 * kKT), key1 = min(pos, s.j1 * kKT - 1);
+      if (!fin) {
+        uint8_t* part = slot(own);
+        if (any && warp_rows) {
+          float4* o = reinterpret_cast<float4*>(part) + r;
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            uint32_t ov[32];
+            tc_ld32_nowait(tO + 32 * c, ov);
+            tc_wait_ld32(ov);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (vrow)
+                __stcg(o + (size_t)(8 * c + e) * kRows,
+                       make_float4(__uint_as_float(ov[4 * e]), __uint_as_float(ov[4 * e + 1]),
+                                   __uint_as_float(ov[4 * e + 2]), __uint_as_float(ov[4 * e + 3])));
+          }
+          if (bad && vrow) add_nonfinite<kPaged>(p, s, key0, key1, nullptr, reinterpret_cast<float*>(part) + 4 * r);
+        }
+        if (vrow) __stcg(reinterpret_cast<float2*>(part + kAttnMlOff) + r, make_float2(m2, l));
+        __syncwarp();
+        if (direct) {
+          const uint32_t before = lane == 0 ? atom_inc_acq_rel(cnt, (uint32_t)(K - 1)) : 0u;
+          fin = __shfl_sync(0xffffffffu, before, 0) == (uint32_t)(K - 1);
+        }
+      } else if (direct && lane == 0) {
+        *cnt = 0;                // for the next launch
+      }
+      if (fin && warp_rows) {
+        float M = m2, f[kDirect] = {1.f, 0.f, 0.f};
+        if (direct) {
+          float2 ml[kDirect];
+#pragma unroll
+          for (int k = 0; k < kDirect; ++k) {
+            ml[k] = k == own ? make_float2(m2, l) : make_float2(-INFINITY, 0.f);
+            if (k < K && k != own && vrow) ml[k] = __ldcg(reinterpret_cast<const float2*>(slot(k) + kAttnMlOff) + r);
+            M = fmaxf(M, ml[k].x);
+          }
+          l = 0.f;
+#pragma unroll
+          for (int k = 0; k < kDirect; ++k) {   // (a row without keys in the piece has l = 0 and no O)
+            f[k] = ml[k].y == 0.f ? 0.f : ml[k].x == M ? 1.f : ex2(ml[k].x - M);
+            l = fmaf(ml[k].y, f[k], l);
+          }
+        }
+        const float il = l == 0.f ? 0.f : 1.f / l;
+        uint32_t dst[8];         // the output rows whose pieces this lane carries out
 #pragma unroll
         for (int e = 0; e < 8; ++e) dst[e] = __shfl_sync(0xffffffffu, orow, 4 * e + (lane >> 3));
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           uint32_t ov[32];
-          tc_ld32_nowait(tO + 32 * c, ov);
-          tc_wait_ld32(ov);
-          if (fin) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * s0);
+          for (int e = 0; e < 32; ++e) ov[e] = 0u;
+          if (any) {
+            tc_ld32_nowait(tO + 32 * c, ov);
+            tc_wait_ld32(ov);
+          }
+          if (direct) {
+            float acc[32] = {};
 #pragma unroll 1
-            for (int k = 0; k < others; ++k) {
-              const float f = (k == 0 ? fx[0] : fx[1]) * il;
-              const float4* o = reinterpret_cast<const float4*>(p.part + (size_t)(4 * (s.c0 + 1 + k) + st) * kAttnPartBytes) +
-                                (size_t)(8 * c) * kRows + r;
+            for (int k = 0; k < K; ++k) {
+              const float fk = k == 0 ? f[0] : k == 1 ? f[1] : f[2];
               float4 x[8];
+              if (k == own) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] = f != 0.f && vrow ? __ldcg(o + e * kRows) : make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int e = 0; e < 8; ++e)
+                  x[e] = make_float4(__uint_as_float(ov[4 * e]), __uint_as_float(ov[4 * e + 1]),
+                                     __uint_as_float(ov[4 * e + 2]), __uint_as_float(ov[4 * e + 3]));
+              } else {
+                const float4* o = reinterpret_cast<const float4*>(slot(k)) + (size_t)(8 * c) * kRows + r;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                  x[e] = fk != 0.f && vrow ? __ldcg(o + e * kRows) : make_float4(0.f, 0.f, 0.f, 0.f);
+              }
+              if (fk == 0.f) continue;
 #pragma unroll
               for (int e = 0; e < 8; ++e) {
-                ov[4 * e] = __float_as_uint(fmaf(x[e].x, f, __uint_as_float(ov[4 * e])));
-                ov[4 * e + 1] = __float_as_uint(fmaf(x[e].y, f, __uint_as_float(ov[4 * e + 1])));
-                ov[4 * e + 2] = __float_as_uint(fmaf(x[e].z, f, __uint_as_float(ov[4 * e + 2])));
-                ov[4 * e + 3] = __float_as_uint(fmaf(x[e].w, f, __uint_as_float(ov[4 * e + 3])));
+                acc[4 * e] = fmaf(x[e].x, fk, acc[4 * e]);
+                acc[4 * e + 1] = fmaf(x[e].y, fk, acc[4 * e + 1]);
+                acc[4 * e + 2] = fmaf(x[e].z, fk, acc[4 * e + 2]);
+                acc[4 * e + 3] = fmaf(x[e].w, fk, acc[4 * e + 3]);
               }
             }
-            // through shared memory: a row's 128 bytes leave from eight neighbouring lanes
-            // (one lane a row touches 32 lines with each store: 3,500 cycles a row tile)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              uint4 x;
-              x.x = bf16x2_rn(__uint_as_float(ov[8 * e + 1]), __uint_as_float(ov[8 * e]));
-              x.y = bf16x2_rn(__uint_as_float(ov[8 * e + 3]), __uint_as_float(ov[8 * e + 2]));
-              x.z = bf16x2_rn(__uint_as_float(ov[8 * e + 5]), __uint_as_float(ov[8 * e + 4]));
-              x.w = bf16x2_rn(__uint_as_float(ov[8 * e + 7]), __uint_as_float(ov[8 * e + 6]));
-              *reinterpret_cast<uint4*>(s_out + lane * 128 + (((4 * (c & 1) + e) ^ (lane & 7)) << 4)) = x;
+            for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(acc[e]);
+          }
+          // through shared memory: a row's 128 bytes leave from eight neighbouring lanes
+          // (one lane a row touches 32 lines with each store: 3,500 cycles a row tile)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint4 x;
+            x.x = bf16x2_rn(__uint_as_float(ov[8 * e + 1]) * il, __uint_as_float(ov[8 * e]) * il);
+            x.y = bf16x2_rn(__uint_as_float(ov[8 * e + 3]) * il, __uint_as_float(ov[8 * e + 2]) * il);
+            x.z = bf16x2_rn(__uint_as_float(ov[8 * e + 5]) * il, __uint_as_float(ov[8 * e + 4]) * il);
+            x.w = bf16x2_rn(__uint_as_float(ov[8 * e + 7]) * il, __uint_as_float(ov[8 * e + 6]) * il);
+            *reinterpret_cast<uint4*>(s_out + lane * 128 + (((4 * (c & 1) + e) ^ (lane & 7)) << 4)) = x;
+          }
+          if (c & 1) {
+            __syncwarp();
+            uint4 x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int rr = 4 * e + (lane >> 3);
+              x[e] = *reinterpret_cast<const uint4*>(s_out + rr * 128 + (((lane ^ rr) & 7) << 4));
             }
-            if (c & 1) {
-              __syncwarp();
-              uint4 x[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const int rr = 4 * e + (lane >> 3);
-                x[e] = *reinterpret_cast<const uint4*>(s_out + rr * 128 + (((lane ^ rr) & 7) << 4));
-              }
-              __nv_bfloat16* o = p.out + row0 * kD + 32 * (c - 1) + 8 * (lane & 7);
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (dst[e] != UINT32_MAX) *reinterpret_cast<uint4*>(o + (size_t)dst[e] * kD) = x[e];
-              __syncwarp();
-            }
-          } else if (vrow) {
-            float4* o = reinterpret_cast<float4*>(part) + (size_t)(8 * c) * kRows + r;
+            __nv_bfloat16* o = p.out + row0 * kD + 32 * (c - 1) + 8 * (lane & 7);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              __stcg(o + (size_t)e * kRows,
-                     make_float4(__uint_as_float(ov[4 * e]), __uint_as_float(ov[4 * e + 1]),
-                                 __uint_as_float(ov[4 * e + 2]), __uint_as_float(ov[4 * e + 3])));
+              if (dst[e] != UINT32_MAX) *reinterpret_cast<uint4*>(o + (size_t)dst[e] * kD) = x[e];
+            __syncwarp();
           }
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(o_free + 8 * st);
-        if (s_bad[i % kSegs] && vrow)   // values taken out of V: for the rows that see them
-          add_nonfinite<kPaged>(p, s, max(s.ctx + s.tok0 + 1, s.j0 * kKT), min(pos, s.j1 * kKT - 1),
-                                fin ? p.out + (row0 + orow) * kD : nullptr, reinterpret_cast<float*>(part) + 4 * r);
-      } else if (any) {
-        tc_fence_before();
-        if (lane == 0) mbar_arrive(o_free + 8 * st);
+        if (vrow && p.lse) p.lse[row0 + orow] = l == 0.f ? -INFINITY : (M + log2f(l)) * 0.6931471805599453f;
+        if (bad && vrow) add_nonfinite<kPaged>(p, s, key0, key1, p.out + (row0 + orow) * kD, nullptr);
       }
-      if (vrow && fin && p.lse) p.lse[row0 + orow] = l == 0.f ? -INFINITY : (M + log2f(l)) * 0.6931471805599453f;
-      if (vrow && !fin) __stcg(reinterpret_cast<float2*>(part + kAttnMlOff) + r, make_float2(m2, l));
+      tc_fence_before();
       __syncwarp();
-      if (direct && !first && lane == 0) red_add_release(cnt, 1);
+      if (any && lane == 0) mbar_arrive(o_free + 8 * st);
       release(i);
     }
   }
@@ -1184,18 +1208,27 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   const int pi = (tid - 32 * kWarpSoft) / nthr, t = (tid - 32 * kWarpSoft) - pi * nthr;
   const Seg s = s_pc[pi];
   const int K = s.c1 - s.c0 + 1, mine = (int)blockIdx.x - s.c0;
+  const int items = min(w, s.T - s.tok0) * p.g * (kD / 8);
+  int lo = items * mine / K, hi = items * (mine + 1) / K;
   if (t == 0) {
     // the count wraps to zero with the last arrival: nothing resets it
     uint32_t* cnt = reinterpret_cast<uint32_t*>(p.part + (size_t)(2 * (2 * s.c0 + 1)) * kAttnPartBytes + kCntAllOff);
-    red_inc_release(cnt, (uint32_t)(K - 1));
-    const bool ok = wait_count_zero(cnt);
-    if (!ok) flag_error(p.err, EE_DEVERR_TIMEOUT);
-    s_ready[pi] = ok;
+    bool ready;
+    if (p.coop) {                // every CTA is resident: wait, and join a share
+      red_inc_release(cnt, (uint32_t)(K - 1));
+      ready = wait_count_zero(cnt);
+      if (!ready) flag_error(p.err, EE_DEVERR_TIMEOUT);
+    } else {                     // the last to arrive joins everything
+      ready = atom_inc_acq_rel(cnt, (uint32_t)(K - 1)) == (uint32_t)(K - 1);
+    }
+    s_ready[pi] = ready;
+  }
+  if (!p.coop) {
+    lo = 0;
+    hi = items;
   }
   asm volatile("bar.sync %0, %1;" ::"r"(2 + pi), "r"(nthr) : "memory");
-  if (!s_ready[pi]) return;
-  const int items = min(w, s.T - s.tok0) * p.g * (kD / 8);
-  merge_items(p, s, items * mine / K, items * (mine + 1) / K, t, nthr);
+  if (s_ready[pi]) merge_items(p, s, lo, hi, t, nthr);
 }
 
 bool good_stride(int64_t stride, int heads) { return stride % 8 == 0 && stride >= (int64_t)heads * kD; }
@@ -1257,7 +1290,7 @@ ee_status launch(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorM
   attr[1].id = cudaLaunchAttributeCooperative;
   attr[1].val.cooperative = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
+  cfg.numAttrs = p.coop ? 2 : 1;
   EE_CUDA_OK(cudaLaunchKernelEx(&cfg, prompt_attn_kernel<kPaged>, tmQ, tmK, tmV, p));
   return EE_OK;
 }
@@ -1278,6 +1311,14 @@ PromptParams params(const int32_t* tok_off, int B, int total, int n_q, int n_kv,
   p.tpt = kRows / p.g;
   p.scale = scale;
   p.scale_log2 = scale * 1.4426950408889634f;
+  // Units of the call: a sequence's last one may be partial.  Fewer than a third of the
+  // SMs: units are split among many CTAs, whose partials all of them join, which needs a
+  // cooperative launch (2 us more where a stream launches the calls one by one).
+  const int w = 2 * p.tpt;
+  p.units = (int)std::min<int64_t>((int64_t)n_kv * std::min<int64_t>((int64_t)total / w + B, total), INT32_MAX);
+  p.coop = p.units < kNumSMs / kDirect ? 1 : 0;
+  // Shortest share: with few rows a partial costs little to join.
+  p.min_share = (int64_t)total * p.g <= 32 * (int64_t)B ? kShareFew : kShareMany;
   return p;
 }
 
