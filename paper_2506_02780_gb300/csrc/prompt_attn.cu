@@ -60,15 +60,13 @@ constexpr uint32_t kSmemBytes = 1024 + kOffBar + 8 * kNumBars;
 constexpr uint32_t kTmemCols = 512, kColO = 256;
 constexpr float kRescaleLog2 = 8.0f;          // O is rescaled when a maximum grows by 2^8
 // work in keys: a unit's own constant, and the smallest share of a CTA
-constexpr int kUnitKeys = 320;
+constexpr int kUnitKeys = 256;
 constexpr int kShareMany = 5 * kKT, kShareFew = 5 * kKT / 4;
 static_assert(kShareFew >= kKT, "every CTA between a unit's first and last piece holds one");
 constexpr int kWarpKV = 0, kWarpMma = 1, kWarpQ = 2, kWarpClean = 3, kWarpSoft = 4;
 constexpr int kVBox = 32;                     // packed V: rows of a box
 constexpr int kSegReaders = 3 + 8;            // warps 0, 1, 3 and the softmax warps
-constexpr int kRegsLaunch = 168, kRegsSoft = 208, kRegsOther = 88;
 static_assert(kRing == 4, "two slots each for K and V tiles");
-static_assert(256 * kRegsSoft + 128 * kRegsOther <= kThreads * kRegsLaunch, "register split");
 static_assert(kSmemBytes <= 227 * 1024 - 1024, "shared memory budget");
 // counts of a split unit's finished pieces, in the trailer of its first piece's slots
 // past the word that the verification attention keeps there: one for each softmax
@@ -500,7 +498,6 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   };
 
   if (warp < kWarpSoft) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
     if (warp == kWarpKV) {
       // ---------------- K and V tiles ----------------
       // The V tiles that warp 3 cleans signal it, and it signals the MMA warp.
@@ -937,7 +934,6 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     }
     return;
   }
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
 
   // ---------------- softmax: one row per thread ----------------
   {
@@ -1080,14 +1076,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (any && warp_rows) {
           float4* o = reinterpret_cast<float4*>(part) + r;
 #pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
-            uint32_t ov[32];
-            tc_ld32_nowait(tO + 32 * c, ov);
-            tc_wait_ld32(ov);
+          for (int c = 0; c < 8; ++c) {
+            uint32_t ov[16];
+            tc_ld16(tO + 16 * c, ov);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
+            for (int e = 0; e < 4; ++e)
               if (vrow)
-                __stcg(o + (size_t)(8 * c + e) * kRows,
+                __stcg(o + (size_t)(4 * c + e) * kRows,
                        make_float4(__uint_as_float(ov[4 * e]), __uint_as_float(ov[4 * e + 1]),
                                    __uint_as_float(ov[4 * e + 2]), __uint_as_float(ov[4 * e + 3])));
           }
@@ -1124,34 +1119,31 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 #pragma unroll
         for (int e = 0; e < 8; ++e) dst[e] = __shfl_sync(0xffffffffu, orow, 4 * e + (lane >> 3));
 #pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
-          uint32_t ov[32];
+        for (int c = 0; c < 8; ++c) {
+          uint32_t ov[16];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) ov[e] = 0u;
-          if (any) {
-            tc_ld32_nowait(tO + 32 * c, ov);
-            tc_wait_ld32(ov);
-          }
+          for (int e = 0; e < 16; ++e) ov[e] = 0u;
+          if (any) tc_ld16(tO + 16 * c, ov);
           if (direct) {
-            float acc[32] = {};
+            float acc[16] = {};
 #pragma unroll 1
             for (int k = 0; k < K; ++k) {
               const float fk = k == 0 ? f[0] : k == 1 ? f[1] : f[2];
-              float4 x[8];
+              float4 x[4];
               if (k == own) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
+                for (int e = 0; e < 4; ++e)
                   x[e] = make_float4(__uint_as_float(ov[4 * e]), __uint_as_float(ov[4 * e + 1]),
                                      __uint_as_float(ov[4 * e + 2]), __uint_as_float(ov[4 * e + 3]));
               } else {
-                const float4* o = reinterpret_cast<const float4*>(slot(k)) + (size_t)(8 * c) * kRows + r;
+                const float4* o = reinterpret_cast<const float4*>(slot(k)) + (size_t)(4 * c) * kRows + r;
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
+                for (int e = 0; e < 4; ++e)
                   x[e] = fk != 0.f && vrow ? __ldcg(o + e * kRows) : make_float4(0.f, 0.f, 0.f, 0.f);
               }
               if (fk == 0.f) continue;
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
+              for (int e = 0; e < 4; ++e) {
                 acc[4 * e] = fmaf(x[e].x, fk, acc[4 * e]);
                 acc[4 * e + 1] = fmaf(x[e].y, fk, acc[4 * e + 1]);
                 acc[4 * e + 2] = fmaf(x[e].z, fk, acc[4 * e + 2]);
@@ -1159,20 +1151,20 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
               }
             }
 #pragma unroll
-            for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(acc[e]);
+            for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(acc[e]);
           }
           // through shared memory: a row's 128 bytes leave from eight neighbouring lanes
           // (one lane a row touches 32 lines with each store: 3,500 cycles a row tile)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+          for (int e = 0; e < 2; ++e) {
             uint4 x;
             x.x = bf16x2_rn(__uint_as_float(ov[8 * e + 1]) * il, __uint_as_float(ov[8 * e]) * il);
             x.y = bf16x2_rn(__uint_as_float(ov[8 * e + 3]) * il, __uint_as_float(ov[8 * e + 2]) * il);
             x.z = bf16x2_rn(__uint_as_float(ov[8 * e + 5]) * il, __uint_as_float(ov[8 * e + 4]) * il);
             x.w = bf16x2_rn(__uint_as_float(ov[8 * e + 7]) * il, __uint_as_float(ov[8 * e + 6]) * il);
-            *reinterpret_cast<uint4*>(s_out + lane * 128 + (((4 * (c & 1) + e) ^ (lane & 7)) << 4)) = x;
+            *reinterpret_cast<uint4*>(s_out + lane * 128 + (((2 * (c & 3) + e) ^ (lane & 7)) << 4)) = x;
           }
-          if (c & 1) {
+          if ((c & 3) == 3) {
             __syncwarp();
             uint4 x[8];
 #pragma unroll
@@ -1180,7 +1172,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
               const int rr = 4 * e + (lane >> 3);
               x[e] = *reinterpret_cast<const uint4*>(s_out + rr * 128 + (((lane ^ rr) & 7) << 4));
             }
-            __nv_bfloat16* o = p.out + row0 * kD + 32 * (c - 1) + 8 * (lane & 7);
+            __nv_bfloat16* o = p.out + row0 * kD + 16 * (c - 3) + 8 * (lane & 7);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
               if (dst[e] != UINT32_MAX) *reinterpret_cast<uint4*>(o + (size_t)dst[e] * kD) = x[e];
