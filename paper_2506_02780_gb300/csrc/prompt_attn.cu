@@ -137,7 +137,7 @@ __device__ __forceinline__ void exp32(const uint32_t (&x)[32], uint64_t sl2x2, u
   }
 }
 
-// One sequence: first token// One sequence: first token, tokens, cached positions (T = 0: nothing to do).
+// One sequence: first token, tokens, cached positions (T = 0: nothing to do).
 struct Seq {
   int o, T, ctx;
 };

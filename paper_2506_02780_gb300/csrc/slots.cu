@@ -10,13 +10,20 @@
 // repeated reads, which come from L2.  Then the CTAs share the tokens and the new
 // table entries; a token on a page given in this call takes it from the free list
 // directly, so no CTA reads what another writes.
+//
+// Bound by latency: the reads of the lengths, the scan, the bisections in shared memory
+// and the reads of the pages follow one another.  A thread takes four neighbouring tokens,
+// mostly of one sequence and page, and all its reads precede its writes (four tokens a
+// grid apart, each written before the next is read: 9.7 us for 1024 sequences).  Measured:
+// 8 sequences with a token each 3.7 us; 1024 sequences of up to 2048 new tokens, 2.6 MB in
+// all, 7.2 us.  512 threads: with 256 the latter takes 8.9 us, with 1024 the former 5.6 us.
 #include "ee_common.cuh"
 
 namespace {
 
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
-constexpr int kTokens = 4;   // tokens of a thread and round: that many bisections in flight
+constexpr int kTokens = 4;   // neighbouring tokens of a thread: mostly one bisection, one page, one store
 
 struct SlotParams {
   const int32_t *ctx_len, *new_len, *held;
@@ -24,14 +31,15 @@ struct SlotParams {
   const int32_t *free_pages, *free_cnt;
   int32_t *tok_off, *pos, *slot, *ctx_out, *held_out, *free_out, *err;
   int B, total, reserve, max_pages, n_free, num_pages;
+  bool vec;                    // pos and slot take 16-byte stores
 };
 
 // One sequence's share: tokens it gets and pages it is given (0 and 0 when its
 // lengths are out of range).
 __device__ __forceinline__ bool seq_share(const SlotParams& p, int s, int& ctx, int& held, int& t, int& give) {
-  ctx = p.ctx_len[s];
-  held = p.held[s];
-  t = p.new_len[s];
+  ctx = __ldg(p.ctx_len + s);   // (read-only: the loads of neighbouring sequences overlap)
+  held = __ldg(p.held + s);
+  t = __ldg(p.new_len + s);
   give = 0;
   const int64_t cap = (int64_t)p.max_pages * EE_PAGE;
   const int64_t end = (int64_t)ctx + t, want = end + p.reserve;
@@ -43,9 +51,9 @@ __device__ __forceinline__ bool seq_share(const SlotParams& p, int s, int& ctx, 
   return true;
 }
 
-// the last s with off[s] <= i
-__device__ __forceinline__ int seq_of(const int* off, int B, int i) {
-  int lo = 0, hi = B;
+// the last s in [lo, B) with off[s] <= i
+__device__ __forceinline__ int seq_of(const int* off, int lo, int B, int i) {
+  int hi = B;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (off[mid] <= i) lo = mid; else hi = mid;
@@ -70,6 +78,7 @@ __global__ void __launch_bounds__(kThreads) prompt_slots_kernel(const SlotParams
   const int s0 = min(tid * per, p.B), s1 = min(s0 + per, p.B);
   int64_t ts = 0, gs = 0;
   bool good = true;
+#pragma unroll 4
   for (int s = s0; s < s1; ++s) {
     int ctx, held, t, give;
     good &= seq_share(p, s, ctx, held, t, give);
@@ -141,47 +150,50 @@ __global__ void __launch_bounds__(kThreads) prompt_slots_kernel(const SlotParams
   };
   bool bad_page = false;
   const int step = gridDim.x * kThreads;
-  // the new entries of the table
-  for (int n = blockIdx.x * kThreads + tid; n < n_give; n += step) {
-    const int s = seq_of(s_give, p.B, n);
+  // the new entries of the table, 32 of a warp, dealt to all CTAs' first warps, second warps, ...
+  for (int n = (warp * gridDim.x + blockIdx.x) * 32 + lane; n < n_give; n += step) {
+    const int s = seq_of(s_give, 0, p.B, n);
     const int pg = fresh(n);
     bad_page |= pg < 0;
     p.block_table[(size_t)s * p.max_pages + s_held[s] + (n - s_give[s])] = pg;
   }
-  // the tokens: kTokens bisections side by side
-  for (int base = blockIdx.x * kThreads + tid; base < p.total; base += kTokens * step) {
-    int lo[kTokens], hi[kTokens];
+  // the tokens: all reads before the writes, so that they are in flight together
+  for (int64_t base = (int64_t)kTokens * (blockIdx.x * kThreads + tid); base < p.total; base += (int64_t)kTokens * step) {
+    const int i0 = (int)base;
+    int pos[kTokens], slot[kTokens], pg[kTokens];
+    int s = i0 < n_tok ? seq_of(s_tok, 0, p.B, i0) : 0;
 #pragma unroll
     for (int k = 0; k < kTokens; ++k) {
-      lo[k] = 0;
-      hi[k] = p.B;
+      const int i = i0 + k;
+      pos[k] = -1;
+      pg[k] = -1;
+      if (i >= n_tok) continue;
+      if (i >= s_tok[s + 1]) s = seq_of(s_tok, s + 1, p.B, i);
+      pos[k] = s_ctx[s] + (i - s_tok[s]);
+      const int j = pos[k] / EE_PAGE, h = s_held[s];
+      if (enough) {
+        const int32_t* at = j < h ? p.block_table + (size_t)s * p.max_pages + j
+                                  : p.free_pages + (cnt - 1 - (s_give[s] + j - h));
+        pg[k] = *at;
+      }
     }
-    for (int span = p.B; span > 1; span = (span + 1) >> 1)
-#pragma unroll
-      for (int k = 0; k < kTokens; ++k) {
-        const int mid = (lo[k] + hi[k]) >> 1;
-        if (hi[k] - lo[k] > 1) {
-          if (s_tok[mid] <= base + k * step) lo[k] = mid; else hi[k] = mid;
-        }
-      }
 #pragma unroll
     for (int k = 0; k < kTokens; ++k) {
-      const int i = base + k * step;
-      if (i >= p.total) break;
-      int pos = -1, slot = -1;
-      if (i < n_tok) {
-        const int s = lo[k];
-        pos = s_ctx[s] + (i - s_tok[s]);
-        const int j = pos / EE_PAGE, h = s_held[s];
-        if (enough) {
-          const int pg = j < h ? p.block_table[(size_t)s * p.max_pages + j] : fresh(s_give[s] + j - h);
-          const bool ok = pg >= 0 && pg < p.num_pages;
-          bad_page |= !ok;
-          slot = ok ? pg * EE_PAGE + pos % EE_PAGE : -1;
+      const bool ok = pg[k] >= 0 && pg[k] < p.num_pages;
+      bad_page |= enough && pos[k] >= 0 && !ok;
+      slot[k] = ok ? pg[k] * EE_PAGE + pos[k] % EE_PAGE : -1;
+    }
+    static_assert(kTokens == 4, "one 16-byte store");
+    if (p.vec && i0 + kTokens <= p.total) {
+      *reinterpret_cast<int4*>(p.pos + i0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+      *reinterpret_cast<int4*>(p.slot + i0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kTokens; ++k)
+        if (i0 + k < p.total) {
+          p.pos[i0 + k] = pos[k];
+          p.slot[i0 + k] = slot[k];
         }
-      }
-      p.pos[i] = pos;
-      p.slot[i] = slot;
     }
   }
   if (bad_page) ee::flag_error(p.err, EE_DEVERR_PAGE);
@@ -223,7 +235,8 @@ extern "C" ee_status ee_prompt_slots(const int32_t* ctx_len, const int32_t* new_
   if (ds != EE_OK) return ds;
   EE_CUDA_OK(set_attrs(dev));
   SlotParams p{ctx_len, new_len, held,     block_table, free_pages, free_cnt,        tok_off, pos,    slot,
-               ctx_out, held_out, free_out, ee::err_word(ws), B,    total, reserve, max_pages, n_free, num_pages};
+               ctx_out, held_out, free_out, ee::err_word(ws), B,    total, reserve, max_pages, n_free, num_pages,
+               ee::aligned(pos, 16) && ee::aligned(slot, 16)};
   // a CTA per round of its threads, two per SM at most: beyond that the scans repeat
   const int64_t want = ((int64_t)total + kThreads * kTokens - 1) / (kThreads * kTokens);
   const int grid = (int)std::min<int64_t>(std::max<int64_t>(want, 1), 2 * ee::kNumSMs);
