@@ -1054,77 +1054,70 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         ++o_uses;
         tc_fence_after();
       }
-      // Few pieces: each warp that finds its rows' other partials in place joins them to its
-      // own O on the way out, the others leave theirs (the first piece is its CTA's last
-      // segment and the others' first, so that it is mostly the one that joins).  The
-      // pieces are added in their order, whichever warp adds them.  Many: see below.
-      const int K = whole ? 1 : s.c1 - s.c0 + 1, own = whole ? 0 : (int)blockIdx.x - s.c0;
-      const bool direct = !whole && K <= kDirect;
-      uint32_t* cnt = reinterpret_cast<uint32_t*>(p.part + (size_t)(2 * (2 * s.c0 + 1) + st) * kAttnPartBytes + kCntOff) + qd;
-      bool fin = whole;
-      if (direct) fin = __shfl_sync(0xffffffffu, lane == 0 && ld_acquire(cnt) == (uint32_t)(K - 1), 0);
       // output rows: from the row tile's first, by token and head
       const size_t row0 = (size_t)(s.o + s.tok0 + st * p.tpt) * p.n_q + s.hk * p.g;
       const uint32_t orow = vrow ? (uint32_t)tok_r * p.n_q + head : UINT32_MAX;
-      // partial slot of piece k: the first is its CTA's second
-      auto slot = [&](int k) { return p.part + (size_t)(2 * (2 * (s.c0 + k) + (k == 0)) + st) * kAttnPartBytes; };
-      const float m2 = m == -INFINITY ? m : m * sl2;      // of base-2 exponents
+      float M = m == -INFINITY ? m : m * sl2;             // of base-2 exponents
       const bool bad = any && s_bad[i % kSegs];           // values taken out of V: for the rows that see them
       const int key0 = max(s.ctx + s.tok0 + 1, s.j0 * kKT), key1 = min(pos, s.j1 * kKT - 1);
-      if (!fin) {
-        uint8_t* part = slot(own);
-        if (any && warp_rows) {
-          float4* o = reinterpret_cast<float4*>(part) + r;
+      bool fin = whole;
+      if (!whole) {
+        // Few pieces: each warp that finds its rows' other partials in place joins them to
+        // its own O, in tensor memory, the others leave theirs (the first piece is its CTA's
+        // last segment and the others' first, so that it is mostly the one that joins).  The
+        // pieces are added in their order, whichever warp adds them.  Many: see below.
+        const int K = s.c1 - s.c0 + 1, own = (int)blockIdx.x - s.c0;
+        const bool direct = K <= kDirect;
+        uint32_t* cnt = reinterpret_cast<uint32_t*>(p.part + (size_t)(2 * (2 * s.c0 + 1) + st) * kAttnPartBytes + kCntOff) + qd;
+        if (direct) fin = __shfl_sync(0xffffffffu, lane == 0 && ld_acquire(cnt) == (uint32_t)(K - 1), 0);
+        // partial slot of piece k: the first is its CTA's second
+        auto slot = [&](int k) { return p.part + (size_t)(2 * (2 * (s.c0 + k) + (k == 0)) + st) * kAttnPartBytes; };
+        if (!fin) {
+          uint8_t* part = slot(own);
+          if (any && warp_rows) {
+            float4* o = reinterpret_cast<float4*>(part) + r;
 #pragma unroll 1
-          for (int c = 0; c < 8; ++c) {
-            uint32_t ov[16];
-            tc_ld16(tO + 16 * c, ov);
+            for (int c = 0; c < 8; ++c) {
+              uint32_t ov[16];
+              tc_ld16(tO + 16 * c, ov);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (vrow)
-                __stcg(o + (size_t)(4 * c + e) * kRows,
-                       make_float4(__uint_as_float(ov[4 * e]), __uint_as_float(ov[4 * e + 1]),
-                                   __uint_as_float(ov[4 * e + 2]), __uint_as_float(ov[4 * e + 3])));
+              for (int e = 0; e < 4; ++e)
+                if (vrow)
+                  __stcg(o + (size_t)(4 * c + e) * kRows,
+                         make_float4(__uint_as_float(ov[4 * e]), __uint_as_float(ov[4 * e + 1]),
+                                     __uint_as_float(ov[4 * e + 2]), __uint_as_float(ov[4 * e + 3])));
+            }
+            if (bad && vrow) add_nonfinite<kPaged>(p, s, key0, key1, nullptr, reinterpret_cast<float*>(part) + 4 * r);
           }
-          if (bad && vrow) add_nonfinite<kPaged>(p, s, key0, key1, nullptr, reinterpret_cast<float*>(part) + 4 * r);
+          if (vrow) __stcg(reinterpret_cast<float2*>(part + kAttnMlOff) + r, make_float2(M, l));
+          __syncwarp();
+          if (direct) {
+            const uint32_t before = lane == 0 ? atom_inc_acq_rel(cnt, (uint32_t)(K - 1)) : 0u;
+            fin = __shfl_sync(0xffffffffu, before, 0) == (uint32_t)(K - 1);
+          }
+        } else if (lane == 0) {
+          *cnt = 0;              // for the next launch
         }
-        if (vrow) __stcg(reinterpret_cast<float2*>(part + kAttnMlOff) + r, make_float2(m2, l));
-        __syncwarp();
-        if (direct) {
-          const uint32_t before = lane == 0 ? atom_inc_acq_rel(cnt, (uint32_t)(K - 1)) : 0u;
-          fin = __shfl_sync(0xffffffffu, before, 0) == (uint32_t)(K - 1);
-        }
-      } else if (direct && lane == 0) {
-        *cnt = 0;                // for the next launch
-      }
-      if (fin && warp_rows) {
-        float M = m2, f[kDirect] = {1.f, 0.f, 0.f};
-        if (direct) {
+        if (fin && warp_rows) {
           float2 ml[kDirect];
+          const float m_own = M;
 #pragma unroll
           for (int k = 0; k < kDirect; ++k) {
-            ml[k] = k == own ? make_float2(m2, l) : make_float2(-INFINITY, 0.f);
+            ml[k] = k == own ? make_float2(m_own, l) : make_float2(-INFINITY, 0.f);
             if (k < K && k != own && vrow) ml[k] = __ldcg(reinterpret_cast<const float2*>(slot(k) + kAttnMlOff) + r);
             M = fmaxf(M, ml[k].x);
           }
+          float f[kDirect];
           l = 0.f;
 #pragma unroll
           for (int k = 0; k < kDirect; ++k) {   // (a row without keys in the piece has l = 0 and no O)
             f[k] = ml[k].y == 0.f ? 0.f : ml[k].x == M ? 1.f : ex2(ml[k].x - M);
             l = fmaf(ml[k].y, f[k], l);
           }
-        }
-        const float il = l == 0.f ? 0.f : 1.f / l;
-        uint32_t dst[8];         // the output rows whose pieces this lane carries out
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dst[e] = __shfl_sync(0xffffffffu, orow, 4 * e + (lane >> 3));
 #pragma unroll 1
-        for (int c = 0; c < 8; ++c) {
-          uint32_t ov[16];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) ov[e] = 0u;
-          if (any) tc_ld16(tO + 16 * c, ov);
-          if (direct) {
+          for (int c = 0; c < 8; ++c) {
+            uint32_t ov[16];
+            tc_ld16(tO + 16 * c, ov);
             float acc[16] = {};
 #pragma unroll 1
             for (int k = 0; k < K; ++k) {
@@ -1152,32 +1145,49 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(acc[e]);
+            tc_st16_nowait(tO + 16 * c, ov);
           }
-          // through shared memory: a row's 128 bytes leave from eight neighbouring lanes
-          // (one lane a row touches 32 lines with each store: 3,500 cycles a row tile)
+          tc_wait_st();
+        }
+      }
+      if (fin && warp_rows) {
+        // Two rolled steps of 64 columns, 32 on their way while 32 are rounded (a wait for
+        // each load costs 400 cycles).  Through shared memory: a row's 128 bytes leave from
+        // eight neighbouring lanes (one lane a row touches 32 lines with each store).
+        const float il = l == 0.f ? 0.f : 1.f / l;
+        uint32_t xa[32], xb[32];
+        tc_ld32_nowait(tO, xa);
+        auto put = [&](const uint32_t (&x)[32], int at) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            uint4 x;
-            x.x = bf16x2_rn(__uint_as_float(ov[8 * e + 1]) * il, __uint_as_float(ov[8 * e]) * il);
-            x.y = bf16x2_rn(__uint_as_float(ov[8 * e + 3]) * il, __uint_as_float(ov[8 * e + 2]) * il);
-            x.z = bf16x2_rn(__uint_as_float(ov[8 * e + 5]) * il, __uint_as_float(ov[8 * e + 4]) * il);
-            x.w = bf16x2_rn(__uint_as_float(ov[8 * e + 7]) * il, __uint_as_float(ov[8 * e + 6]) * il);
-            *reinterpret_cast<uint4*>(s_out + lane * 128 + (((2 * (c & 3) + e) ^ (lane & 7)) << 4)) = x;
+          for (int e = 0; e < 4; ++e) {
+            uint4 y;
+            y.x = bf16x2_rn(__uint_as_float(x[8 * e + 1]) * il, __uint_as_float(x[8 * e]) * il);
+            y.y = bf16x2_rn(__uint_as_float(x[8 * e + 3]) * il, __uint_as_float(x[8 * e + 2]) * il);
+            y.z = bf16x2_rn(__uint_as_float(x[8 * e + 5]) * il, __uint_as_float(x[8 * e + 4]) * il);
+            y.w = bf16x2_rn(__uint_as_float(x[8 * e + 7]) * il, __uint_as_float(x[8 * e + 6]) * il);
+            *reinterpret_cast<uint4*>(s_out + lane * 128 + (((at + e) ^ (lane & 7)) << 4)) = y;
           }
-          if ((c & 3) == 3) {
-            __syncwarp();
-            uint4 x[8];
+        };
+        uint32_t dst[8];         // the output rows whose pieces this lane carries out
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int rr = 4 * e + (lane >> 3);
-              x[e] = *reinterpret_cast<const uint4*>(s_out + rr * 128 + (((lane ^ rr) & 7) << 4));
-            }
-            __nv_bfloat16* o = p.out + row0 * kD + 16 * (c - 3) + 8 * (lane & 7);
+        for (int e = 0; e < 8; ++e) dst[e] = __shfl_sync(0xffffffffu, orow, 4 * e + (lane >> 3));
+        __nv_bfloat16* out = p.out + row0 * kD + 8 * (lane & 7);
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+          tc_wait_ld32(xa);
+          tc_ld32_nowait(tO + 64 * c + 32, xb);
+          put(xa, 0);
+          tc_wait_ld32(xb);
+          if (c == 0) tc_ld32_nowait(tO + 64, xa);
+          put(xb, 4);
+          __syncwarp();
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (dst[e] != UINT32_MAX) *reinterpret_cast<uint4*>(o + (size_t)dst[e] * kD) = x[e];
-            __syncwarp();
+          for (int e = 0; e < 8; ++e) {
+            const int rr = 4 * e + (lane >> 3);
+            const uint4 x = *reinterpret_cast<const uint4*>(s_out + rr * 128 + (((lane ^ rr) & 7) << 4));
+            if (dst[e] != UINT32_MAX) *reinterpret_cast<uint4*>(out + (size_t)dst[e] * kD + 64 * c) = x;
           }
+          __syncwarp();
         }
         if (vrow && p.lse) p.lse[row0 + orow] = l == 0.f ? -INFINITY : (M + log2f(l)) * 0.6931471805599453f;
         if (bad && vrow) add_nonfinite<kPaged>(p, s, key0, key1, p.out + (row0 + orow) * kD, nullptr);
