@@ -59,9 +59,11 @@ constexpr uint32_t kNumBars = 2 * kRing + 4 + 10 + 2 * kSegs + kZones + 1;
 constexpr uint32_t kSmemBytes = 1024 + kOffBar + 8 * kNumBars;
 constexpr uint32_t kTmemCols = 512, kColO = 256;
 constexpr float kRescaleLog2 = 8.0f;          // O is rescaled when a maximum grows by 2^8
-// work in keys: a unit's own constant, and the smallest share of a CTA
-constexpr int kUnitKeys = 256;
-constexpr int kShareMany = 5 * kKT, kShareFew = 5 * kKT / 4;
+// Work in keys: the smallest share of a CTA, a unit's own constant, and how near (in tiles)
+// a cut comes to a unit's start or end before it moves there.  Calls of many rows and of few:
+// few rows' partials cost little to leave and to join.
+constexpr int kShareMany = 5 * kKT, kUnitMany = 256, kSnapMany = 2;
+constexpr int kShareFew = kKT, kUnitFew = 128, kSnapFew = 1;
 static_assert(kShareFew >= kKT, "every CTA between a unit's first and last piece holds one");
 constexpr int kWarpKV = 0, kWarpMma = 1, kWarpQ = 2, kWarpClean = 3, kWarpSoft = 4;
 constexpr int kVBox = 32;                     // packed V: rows of a box
@@ -85,6 +87,7 @@ struct PromptParams {
   int B, total, num_pages, max_pages, n_q, n_kv, g, tpt;
   int units;                    // of the call, at most
   int min_share, coop;
+  int unit_keys, snap;
   float scale, scale_log2;
 };
 
@@ -160,43 +163,44 @@ __device__ __forceinline__ Seq load_seq(const PromptParams& p, int s, int& err) 
 }
 
 // The line of work.  Unit n of a sequence and KV head: tokens [n w, (n + 1) w), w = 2
-// tpt, keys ctx + min(T, (n + 1) w); it takes that many places plus kUnitKeys + 64 (half
-// a tile: the last one is rarely full).
-constexpr int kUnitConst = kUnitKeys + kKT / 2;
+// tpt, keys ctx + min(T, (n + 1) w); it takes that many places plus `u`: unit_keys + 64
+// (half a tile: the last one is rarely full).
 __device__ __forceinline__ int num_units(int T, int w) { return (T + w - 1) / w; }
 // places of a sequence and head before unit n (n below the number of units)
-__device__ __forceinline__ int64_t places_before(int ctx, int w, int64_t n) {
-  return n * ((int64_t)ctx + kUnitConst) + n * (n + 1) / 2 * w;
+__device__ __forceinline__ int64_t places_before(int ctx, int w, int u, int64_t n) {
+  return n * ((int64_t)ctx + u) + n * (n + 1) / 2 * w;
 }
-__device__ __forceinline__ int64_t head_places(int ctx, int T, int w) {
+__device__ __forceinline__ int64_t head_places(int ctx, int T, int w, int u) {
   if (T == 0) return 0;
   const int64_t P = num_units(T, w);
-  return places_before(ctx, w, P - 1) + ctx + T + kUnitConst;
+  return places_before(ctx, w, u, P - 1) + ctx + T + u;
 }
-// tiles of a unit of n that lie before place y of it; a cut within kSnap tiles of the
+// tiles of a unit of n that lie before place y of it; a cut within `snap` tiles of the
 // unit's start or end moves there
-constexpr int kSnap = 2;
-__device__ __forceinline__ int tiles_before(int64_t y, int n) {
-  const int64_t j = (y - kUnitKeys + kKT / 2) >> 7;
-  return j < kSnap ? 0 : j > n - kSnap ? n : (int)j;
+__device__ __forceinline__ int tiles_before(const PromptParams& p, int64_t y, int n) {
+  const int64_t j = (y - p.unit_keys + kKT / 2) >> 7;
+  return j < p.snap ? 0 : j > n - p.snap ? n : (int)j;
 }
 // the first places that tiles_before puts past the unit's start, and at its end
-constexpr int kPastStart = kUnitKeys - kKT / 2 + kSnap * kKT;
-__device__ __forceinline__ int at_end(int n) { return kUnitKeys - kKT / 2 + (n - kSnap + 1) * kKT; }
+__device__ __forceinline__ int past_start(const PromptParams& p) { return p.unit_keys - kKT / 2 + p.snap * kKT; }
+__device__ __forceinline__ int at_end(const PromptParams& p, int n) {
+  return p.unit_keys - kKT / 2 + (n - p.snap + 1) * kKT;
+}
 // W places (below 2^56) cut for N CTAs: CTA c's share starts at floor(c W / N)
 struct Shares {
   int64_t W, q;      // q = W / N, r = W mod N, by two 32-bit divisions
   int N, r;
-  __device__ __forceinline__ Shares(int64_t w, int n) : W(w), N(n) {
+  uint32_t inv;      // 2^32 / N rounded up: (x inv) >> 32 = x / N for x below 2^17
+  __device__ __forceinline__ Shares(int64_t w, int n) : W(w), N(n), inv(0xFFFFFFFFu / (uint32_t)n + 1) {
     const uint32_t a = (uint32_t)(w >> 24), b = (uint32_t)w & 0xFFFFFFu;
     const uint32_t q1 = a / (uint32_t)n, lo = ((a - q1 * (uint32_t)n) << 24) + b, q0 = lo / (uint32_t)n;
     q = ((int64_t)q1 << 24) + q0;
     r = (int)(lo - q0 * (uint32_t)n);
   }
-  __device__ __forceinline__ int64_t start(int c) const { return q * c + (r * c) / N; }
+  __device__ __forceinline__ int64_t start(int c) const { return q * c + (N == 1 ? 0 : (int)__umulhi((uint32_t)(r * c), inv)); }
   // the last CTA whose share starts before place y (y > 0)
   __device__ __forceinline__ int before(int64_t y) const {
-    int c = min(max((int)((float)y / (float)W * N), 0), N - 1);
+    int c = min(max((int)(__fdividef((float)y, (float)W) * N), 0), N - 1);   // put right below
 #pragma unroll 1
     while (start(c) >= y) --c;
 #pragma unroll 1
@@ -276,80 +280,63 @@ struct Joined {
 
 // Items [lo, hi) of a split unit merged by one of its pieces: thread t of nthr.  An
 // item is eight columns of a row, numbered rows fastest, so that a warp's loads of a
-// slot (column-chunk major) are contiguous.  A thread loads two items of two pieces at
-// a time (a round trip to L2 costs about 1,000 cycles).  With few items and many pieces
-// `sub` lanes share an item, each over every sub-th piece.
+// slot (column-chunk major) are contiguous.  A thread loads from two pieces at a time (a
+// round trip to L2 costs about 1,000 cycles).  With few items and many pieces 2^sub lanes
+// share an item, each over every 2^sub-th piece.
 __device__ __forceinline__ void merge_items(const PromptParams& p, const Seg& s, int lo, int hi, int t, int nthr) {
-  constexpr int kItems = 2;
   const int K = s.c1 - s.c0 + 1;
-  int sub = 1;
+  int sub = 0;
 #pragma unroll 1
-  while (sub < 32 && sub < K && (hi - lo) * 2 * sub <= nthr) sub *= 2;
+  while (sub < 5 && 1 << sub < K && (hi - lo) << (sub + 1) <= nthr) ++sub;
   const int nt = min(2 * p.tpt, s.T - s.tok0);               // tokens of the unit
   const int rows_a = min(nt, p.tpt) * p.g, rows = nt * p.g;  // rows of A, of both
-  const int k0 = t & (sub - 1);
-  const int step = nthr / sub;
+  const int k0 = t & ((1 << sub) - 1);
   // whole warps walk together: the lanes of an item meet in shuffles
 #pragma unroll 1
-  for (int i0 = lo + t / sub; i0 - (t & 31) / sub < hi; i0 += kItems * step) {
-    Joined x[kItems];
-    int st[kItems], rr[kItems], cg[kItems];
-#pragma unroll
-    for (int n = 0; n < kItems; ++n) {
-      const int i = min(i0 + n * step, hi - 1);
-      cg[n] = i / rows;
-      const int r = i - cg[n] * rows;
-      st[n] = r >= rows_a;
-      rr[n] = st[n] ? r - rows_a : r;
-    }
+  for (int i0 = lo + (t >> sub); i0 - ((t & 31) >> sub) < hi; i0 += nthr >> sub) {
+    const int i = min(i0, hi - 1), cg = i / rows, r = i - cg * rows;
+    const int st = r >= rows_a, rr = st ? r - rows_a : r;
+    Joined x;
 #pragma unroll 1
-    for (int k = k0; k < K; k += 2 * sub) {
-      float2 ml[2][kItems];
-      float4 u[2][kItems], v[2][kItems];
+    for (int k = k0; k < K; k += 2 << sub) {
+      float2 ml[2];
+      float4 u[2], v[2];
 #pragma unroll
-      for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int n = 0; n < kItems; ++n) {
-          const int kk = min(k + q * sub, K - 1), c = s.c0 + kk;   // CTA c's last segment, or its first
-          const uint8_t* slot = p.part + (size_t)(2 * (2 * c + (kk == 0)) + st[n]) * kAttnPartBytes;
-          const float4* O = reinterpret_cast<const float4*>(slot) + (size_t)(2 * cg[n]) * kRows + rr[n];
-          ml[q][n] = __ldcg(reinterpret_cast<const float2*>(slot + kAttnMlOff) + rr[n]);
-          u[q][n] = __ldcg(O);
-          v[q][n] = __ldcg(O + kRows);
-        }
-#pragma unroll
-      for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int n = 0; n < kItems; ++n) {
-          // a row without keys in the piece has l = 0 and no O (a sum that is NaN has one)
-          if (k + q * sub >= K || ml[q][n].y == 0.f) continue;
-          const float o[8] = {u[q][n].x, u[q][n].y, u[q][n].z, u[q][n].w, v[q][n].x, v[q][n].y, v[q][n].z, v[q][n].w};
-          x[n].add(ml[q][n].x, ml[q][n].y, o);
-        }
-    }
-#pragma unroll
-    for (int n = 0; n < kItems; ++n) {
-#pragma unroll 1
-      for (int d = 1; d < sub; d *= 2) {
-        float o[8];
-        const float Mo = __shfl_xor_sync(0xffffffffu, x[n].M, d), Lo = __shfl_xor_sync(0xffffffffu, x[n].L, d);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = __shfl_xor_sync(0xffffffffu, x[n].a[e], d);
-        x[n].add(Mo, Lo, o);
+      for (int q = 0; q < 2; ++q) {
+        const int kk = min(k + (q << sub), K - 1), c = s.c0 + kk;   // CTA c's last segment, or its first
+        const uint8_t* slot = p.part + (size_t)(2 * (2 * c + (kk == 0)) + st) * kAttnPartBytes;
+        const float4* O = reinterpret_cast<const float4*>(slot) + (size_t)(2 * cg) * kRows + rr;
+        ml[q] = __ldcg(reinterpret_cast<const float2*>(slot + kAttnMlOff) + rr);
+        u[q] = __ldcg(O);
+        v[q] = __ldcg(O + kRows);
       }
-      if (k0 != 0 || i0 + n * step >= hi) continue;
-      const float il = x[n].L == 0.f ? 0.f : 1.f / x[n].L;
-      const int tok = rr[n] / p.g, h = rr[n] - tok * p.g;
-      const size_t row = (size_t)(s.o + s.tok0 + (st[n] ? p.tpt : 0) + tok) * p.n_q + s.hk * p.g + h;
-      uint4 o;
-      o.x = bf16x2_rn(x[n].a[1] * il, x[n].a[0] * il);
-      o.y = bf16x2_rn(x[n].a[3] * il, x[n].a[2] * il);
-      o.z = bf16x2_rn(x[n].a[5] * il, x[n].a[4] * il);
-      o.w = bf16x2_rn(x[n].a[7] * il, x[n].a[6] * il);
-      *reinterpret_cast<uint4*>(p.out + row * kD + 8 * cg[n]) = o;
-      if (cg[n] == 0 && p.lse)
-        p.lse[row] = x[n].L == 0.f ? -INFINITY : (x[n].M + log2f(x[n].L)) * 0.6931471805599453f;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        // a row without keys in the piece has l = 0 and no O (a sum that is NaN has one)
+        if (k + (q << sub) >= K || ml[q].y == 0.f) continue;
+        const float o[8] = {u[q].x, u[q].y, u[q].z, u[q].w, v[q].x, v[q].y, v[q].z, v[q].w};
+        x.add(ml[q].x, ml[q].y, o);
+      }
     }
+#pragma unroll 1
+    for (int d = 1; d < 1 << sub; d *= 2) {
+      float o[8];
+      const float Mo = __shfl_xor_sync(0xffffffffu, x.M, d), Lo = __shfl_xor_sync(0xffffffffu, x.L, d);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = __shfl_xor_sync(0xffffffffu, x.a[e], d);
+      x.add(Mo, Lo, o);
+    }
+    if (k0 != 0 || i0 >= hi) continue;
+    const float il = x.L == 0.f ? 0.f : 1.f / x.L;
+    const int tok = rr / p.g, h = rr - tok * p.g;
+    const size_t row = (size_t)(s.o + s.tok0 + (st ? p.tpt : 0) + tok) * p.n_q + s.hk * p.g + h;
+    uint4 o;
+    o.x = bf16x2_rn(x.a[1] * il, x.a[0] * il);
+    o.y = bf16x2_rn(x.a[3] * il, x.a[2] * il);
+    o.z = bf16x2_rn(x.a[5] * il, x.a[4] * il);
+    o.w = bf16x2_rn(x.a[7] * il, x.a[6] * il);
+    *reinterpret_cast<uint4*>(p.out + row * kD + 8 * cg) = o;
+    if (cg == 0 && p.lse) p.lse[row] = x.L == 0.f ? -INFINITY : (x.M + log2f(x.L)) * 0.6931471805599453f;
   }
 }
 
@@ -428,7 +415,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   pdl_wait();   // no global access before the previous kernel's writes are visible
 
   // ---- the line of work: its length, this CTA's share and where that begins ----
-  const int w = 2 * p.tpt;
+  const int w = 2 * p.tpt, u = p.unit_keys + kKT / 2;
   int64_t W = 0;
   int64_t base = 0, sum = 0;
   const int per = (p.B + kThreads - 1) / kThreads;   // sequences of a thread
@@ -439,7 +426,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 #pragma unroll 1
     for (int s = b0; s < b1; ++s) {
       sq = load_seq<kPaged>(p, s, err);
-      sum += head_places(sq.ctx, sq.T, w) * p.n_kv;
+      sum += head_places(sq.ctx, sq.T, w, u) * p.n_kv;
     }
     if (err && blockIdx.x == 0) flag_error(p.err, err);
     int64_t incl = sum;
@@ -450,16 +437,18 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     }
     if (lane == 31) s_scan[warp] = incl;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kThreads / 32; ++i) {
+    // (the first warps hold all sequences)
+#pragma unroll 1
+    for (int i = 0; i < min((p.B + 31) / 32, kThreads / 32); ++i) {
       if (i < warp) base += s_scan[i];
       W += s_scan[i];
     }
     base += incl - sum;
   }
   // as many CTAs as the units or the shortest share allow
-  const Shares sh(
-      W, (int)min((int64_t)gridDim.x, max(max(W / p.min_share, min(W / kShareFew, (int64_t)p.units)), (int64_t)1)));
+  // (W past the grid's worth of the larger share changes nothing: 32-bit divisions)
+  const uint32_t Wc = (uint32_t)min(W, (int64_t)gridDim.x * kShareMany);
+  const Shares sh(W, min((int)gridDim.x, max(max((int)(Wc / (uint32_t)p.min_share), min((int)(Wc / kShareFew), p.units)), 1)));
   const bool works = (int)blockIdx.x < sh.N && W > 0;
   const int64_t x0 = works ? sh.start(blockIdx.x) : W, x1 = works ? sh.start(blockIdx.x + 1) : W;
   if (works && x0 >= base && x0 < base + sum) {
@@ -469,7 +458,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 #pragma unroll 1
       for (;; ++s) {
         sq = load_seq<kPaged>(p, s, err);
-        const int64_t n = head_places(sq.ctx, sq.T, w) * p.n_kv;
+        const int64_t n = head_places(sq.ctx, sq.T, w, u) * p.n_kv;
         if (x0 < base + n) break;
         base += n;
       }
@@ -600,9 +589,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         o = s_firstseq.o;
         T = s_firstseq.T;
         ctx = s_firstseq.ctx;
-        const int64_t per_head = head_places(ctx, T, w);
+        const int64_t per_head = head_places(ctx, T, w, u);
         int64_t rem = x0 - X;
-        hk = min((int)((float)rem / (float)per_head), p.n_kv - 1);
+        hk = min((int)__fdividef((float)rem, (float)per_head), p.n_kv - 1);
         rem -= hk * per_head;
 #pragma unroll 1
         for (; rem < 0; rem += per_head) --hk;
@@ -612,13 +601,15 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         // the last unit that starts at or before rem: places_before(n) <= rem solved for n,
         // then put right (the root is off by a few units at most)
         const int units = num_units(T, w);
-        const float b = (float)(ctx + kUnitConst) + 0.5f * w;
-        n = min(max((int)((sqrtf(b * b + 2.f * w * (float)rem) - b) / w), 0), units - 1);
+        if (units > 1) {
+          const float b = (float)(ctx + u) + 0.5f * w;
+          n = min(max((int)((sqrtf(b * b + 2.f * w * (float)rem) - b) / w), 0), units - 1);
 #pragma unroll 1
-        while (places_before(ctx, w, n) > rem) --n;
+          while (places_before(ctx, w, u, n) > rem) --n;
 #pragma unroll 1
-        while (n + 1 < units && places_before(ctx, w, n + 1) <= rem) ++n;
-        X += places_before(ctx, w, n);
+          while (n + 1 < units && places_before(ctx, w, u, n + 1) <= rem) ++n;
+        }
+        X += places_before(ctx, w, u, n);
       }
       // the next non-empty segment of the share
       auto find = [&](Seg& g) -> bool {
@@ -636,9 +627,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           const int tok0 = n * w;
           const int keys = ctx + min(T, tok0 + w);
           const int tiles = (keys + kKT - 1) / kKT;
-          const int64_t len = keys + kUnitConst;
-          const int j0 = X < x0 ? tiles_before(x0 - X, tiles) : 0;
-          const int j1 = x1 >= X + len ? tiles : tiles_before(x1 - X, tiles);
+          const int64_t len = keys + u;
+          const int j0 = X < x0 ? tiles_before(p, x0 - X, tiles) : 0;
+          const int j1 = x1 >= X + len ? tiles : tiles_before(p, x1 - X, tiles);
           g.X = X;
           X += len;
           ++n;
@@ -656,11 +647,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           g.nB = T > tok0 + p.tpt ? tiles : 0;
           g.c0 = g.c1 = 0;
           if (j1 - j0 < tiles) {
-            // the first piece is that of the last CTA whose share starts before kPastStart,
+            // the first piece is that of the last CTA whose share starts before past_start,
             // the last piece that of the last whose share starts before at_end; shares are
             // no shorter than a tile, so every CTA between them holds one
-            g.c0 = sh.before(g.X + kPastStart);
-            g.c1 = sh.before(g.X + at_end(tiles));
+            g.c0 = sh.before(g.X + past_start(p));
+            g.c1 = sh.before(g.X + at_end(p, tiles));
           }
           return true;
         }
@@ -1107,45 +1098,43 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             if (k < K && k != own && vrow) ml[k] = __ldcg(reinterpret_cast<const float2*>(slot(k) + kAttnMlOff) + r);
             M = fmaxf(M, ml[k].x);
           }
+          static_assert(kDirect == 3, "own and two others");
           float f[kDirect];
           l = 0.f;
+          auto f_of = [&](int k) { return k == 0 ? f[0] : k == 1 ? f[1] : f[2]; };
+          auto at = [](const float4& x, int e) { return e == 0 ? x.x : e == 1 ? x.y : e == 2 ? x.z : x.w; };
 #pragma unroll
           for (int k = 0; k < kDirect; ++k) {   // (a row without keys in the piece has l = 0 and no O)
             f[k] = ml[k].y == 0.f ? 0.f : ml[k].x == M ? 1.f : ex2(ml[k].x - M);
             l = fmaf(ml[k].y, f[k], l);
           }
+          // 32 columns at a time, all pieces' in flight together
 #pragma unroll 1
-          for (int c = 0; c < 8; ++c) {
-            uint32_t ov[16];
-            tc_ld16(tO + 16 * c, ov);
-            float acc[16] = {};
-#pragma unroll 1
-            for (int k = 0; k < K; ++k) {
-              const float fk = k == 0 ? f[0] : k == 1 ? f[1] : f[2];
-              float4 x[4];
-              if (k == own) {
+          for (int c = 0; c < 4; ++c) {
+            uint32_t ov[32];
+            tc_ld32_nowait(tO + 32 * c, ov);
+            float4 x[kDirect - 1][8];            // the others', in order
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  x[e] = make_float4(__uint_as_float(ov[4 * e]), __uint_as_float(ov[4 * e + 1]),
-                                     __uint_as_float(ov[4 * e + 2]), __uint_as_float(ov[4 * e + 3]));
-              } else {
-                const float4* o = reinterpret_cast<const float4*>(slot(k)) + (size_t)(4 * c) * kRows + r;
+            for (int n = 0; n < kDirect - 1; ++n) {
+              const int k = n + (n >= own);
+              const float4* o = reinterpret_cast<const float4*>(slot(min(k, K - 1))) + (size_t)(8 * c) * kRows + r;
+              const bool read = k < K && vrow && f_of(k) != 0.f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  x[e] = fk != 0.f && vrow ? __ldcg(o + e * kRows) : make_float4(0.f, 0.f, 0.f, 0.f);
-              }
-              if (fk == 0.f) continue;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                acc[4 * e] = fmaf(x[e].x, fk, acc[4 * e]);
-                acc[4 * e + 1] = fmaf(x[e].y, fk, acc[4 * e + 1]);
-                acc[4 * e + 2] = fmaf(x[e].z, fk, acc[4 * e + 2]);
-                acc[4 * e + 3] = fmaf(x[e].w, fk, acc[4 * e + 3]);
-              }
+              for (int e = 0; e < 8; ++e) x[n][e] = read ? __ldcg(o + e * kRows) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
+            tc_wait_ld32(ov);
+            // (own's O is undefined where it has no keys)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(acc[e]);
-            tc_st16_nowait(tO + 16 * c, ov);
+            for (int e = 0; e < 32; ++e) ov[e] = f_of(own) == 0.f ? 0u : ov[e];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const float a = __uint_as_float(ov[e]), b = at(x[0][e >> 2], e & 3), d = at(x[1][e >> 2], e & 3);
+              float y = (own == 0 ? a : b) * f[0];
+              y = fmaf(own == 1 ? a : own == 0 ? b : d, f[1], y);
+              y = fmaf(own == 2 ? a : d, f[2], y);
+              ov[e] = __float_as_uint(y);
+            }
+            tc_st32_nowait(tO + 32 * c, ov);
           }
           tc_wait_st();
         }
@@ -1319,8 +1308,10 @@ PromptParams params(const int32_t* tok_off, int B, int total, int n_q, int n_kv,
   const int w = 2 * p.tpt;
   p.units = (int)std::min<int64_t>((int64_t)n_kv * std::min<int64_t>((int64_t)total / w + B, total), INT32_MAX);
   p.coop = p.units < kNumSMs / kDirect ? 1 : 0;
-  // Shortest share: with few rows a partial costs little to join.
-  p.min_share = (int64_t)total * p.g <= 32 * (int64_t)B ? kShareFew : kShareMany;
+  const bool few = (int64_t)total * p.g <= 32 * (int64_t)B;
+  p.min_share = few ? kShareFew : kShareMany;
+  p.unit_keys = few ? kUnitFew : kUnitMany;
+  p.snap = few ? kSnapFew : kSnapMany;
   return p;
 }
 
