@@ -1098,43 +1098,52 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             if (k < K && k != own && vrow) ml[k] = __ldcg(reinterpret_cast<const float2*>(slot(k) + kAttnMlOff) + r);
             M = fmaxf(M, ml[k].x);
           }
-          static_assert(kDirect == 3, "own and two others");
           float f[kDirect];
           l = 0.f;
-          auto f_of = [&](int k) { return k == 0 ? f[0] : k == 1 ? f[1] : f[2]; };
-          auto at = [](const float4& x, int e) { return e == 0 ? x.x : e == 1 ? x.y : e == 2 ? x.z : x.w; };
+          static_assert(kDirect == 3, "f by number");
 #pragma unroll
           for (int k = 0; k < kDirect; ++k) {   // (a row without keys in the piece has l = 0 and no O)
             f[k] = ml[k].y == 0.f ? 0.f : ml[k].x == M ? 1.f : ex2(ml[k].x - M);
             l = fmaf(ml[k].y, f[k], l);
           }
-          // 32 columns at a time, all pieces' in flight together
+          // 64 columns of a piece in flight at a time (a round trip to L2 costs about 1,000 cycles)
 #pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
-            uint32_t ov[32];
-            tc_ld32_nowait(tO + 32 * c, ov);
-            float4 x[kDirect - 1][8];            // the others', in order
+          for (int c = 0; c < 2; ++c) {
+            float acc[64] = {};
+#pragma unroll 1
+            for (int k = 0; k < K; ++k) {
+              const float fk = k == 0 ? f[0] : k == 1 ? f[1] : f[2];
+              uint32_t xa[32], xb[32];
+              if (k == own) {
+                tc_ld32_nowait(tO + 64 * c, xa);
+                tc_ld32_nowait(tO + 64 * c + 32, xb);
+                tc_wait_ld32(xa);
+                tc_wait_ld32(xb);
+              } else {
+                const uint4* o = reinterpret_cast<const uint4*>(slot(k)) + (size_t)(16 * c) * kRows + r;
 #pragma unroll
-            for (int n = 0; n < kDirect - 1; ++n) {
-              const int k = n + (n >= own);
-              const float4* o = reinterpret_cast<const float4*>(slot(min(k, K - 1))) + (size_t)(8 * c) * kRows + r;
-              const bool read = k < K && vrow && f_of(k) != 0.f;
+                for (int e = 0; e < 16; ++e) {
+                  const uint4 y = __ldcg(o + e * kRows);
+                  uint32_t* x = e < 8 ? xa + 4 * e : xb + 4 * (e - 8);
+                  x[0] = y.x;
+                  x[1] = y.y;
+                  x[2] = y.z;
+                  x[3] = y.w;
+                }
+              }
+              if (fk != 0.f) {     // (without keys there is no O)
 #pragma unroll
-              for (int e = 0; e < 8; ++e) x[n][e] = read ? __ldcg(o + e * kRows) : make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int e = 0; e < 64; ++e)
+                  acc[e] = fmaf(__uint_as_float(e < 32 ? xa[e] : xb[e - 32]), fk, acc[e]);
+              }
             }
-            tc_wait_ld32(ov);
-            // (own's O is undefined where it has no keys)
 #pragma unroll
-            for (int e = 0; e < 32; ++e) ov[e] = f_of(own) == 0.f ? 0u : ov[e];
+            for (int q = 0; q < 4; ++q) {
+              uint32_t y[16];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float a = __uint_as_float(ov[e]), b = at(x[0][e >> 2], e & 3), d = at(x[1][e >> 2], e & 3);
-              float y = (own == 0 ? a : b) * f[0];
-              y = fmaf(own == 1 ? a : own == 0 ? b : d, f[1], y);
-              y = fmaf(own == 2 ? a : d, f[2], y);
-              ov[e] = __float_as_uint(y);
+              for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(acc[16 * q + e]);
+              tc_st16_nowait(tO + 64 * c + 16 * q, y);
             }
-            tc_st32_nowait(tO + 32 * c, ov);
           }
           tc_wait_st();
         }
