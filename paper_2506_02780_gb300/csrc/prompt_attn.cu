@@ -62,7 +62,7 @@ constexpr float kRescaleLog2 = 8.0f;          // O is rescaled when a maximum gr
 // Work in keys: the smallest share of a CTA, a unit's own constant, and how near (in tiles)
 // a cut comes to a unit's start or end before it moves there.  Calls of many rows and of few:
 // few rows' partials cost little to leave and to join.
-constexpr int kShareMany = 5 * kKT, kUnitMany = 256, kSnapMany = 2;
+constexpr int kShareMany = 5 * kKT, kUnitMany = 192, kSnapMany = 2;
 constexpr int kShareFew = kKT, kUnitFew = 128, kSnapFew = 1;
 static_assert(kShareFew >= kKT, "every CTA between a unit's first and last piece holds one");
 constexpr int kWarpKV = 0, kWarpMma = 1, kWarpQ = 2, kWarpClean = 3, kWarpSoft = 4;
@@ -1060,7 +1060,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         const int K = s.c1 - s.c0 + 1, own = (int)blockIdx.x - s.c0;
         const bool direct = K <= kDirect;
         uint32_t* cnt = reinterpret_cast<uint32_t*>(p.part + (size_t)(2 * (2 * s.c0 + 1) + st) * kAttnPartBytes + kCntOff) + qd;
-        if (direct) fin = __shfl_sync(0xffffffffu, lane == 0 && ld_acquire(cnt) == (uint32_t)(K - 1), 0);
+        if (direct && own == 0) fin = __shfl_sync(0xffffffffu, lane == 0 && ld_acquire(cnt) == (uint32_t)(K - 1), 0);
         // partial slot of piece k: the first is its CTA's second
         auto slot = [&](int k) { return p.part + (size_t)(2 * (2 * (s.c0 + k) + (k == 0)) + st) * kAttnPartBytes; };
         if (!fin) {
