@@ -11,17 +11,32 @@
 // heads of tpt = 128 / g consecutive tokens (row = token * g + head: one TMA box of Q,
 // at most g - 1 rows empty, and a causal edge of tpt keys instead of 128).  A unit is
 // two row tiles, A and B, of one sequence and KV head: they share every K/V tile, and
-// while one's scores are in the softmax the tensor core works for the other.
+// while one's scores are in the softmax the tensor core works for the other.  (B sharing
+// A's rows where a unit has one row tile only, each on every other key tile, gained nothing:
+// such calls are bound by the cache.)
 //
 // Work.  The keys of all units (plus a constant for each: a unit's start and end) are
 // laid on one line, cut into equal shares, one for each CTA; one CTA runs on each SM.
 // A share may begin and end inside a unit.  Such a unit's pieces are joined with weights
 // 2^(m - max): of up to kDirect pieces the last to finish joins the partials (m, l,
-// unnormalised O) that the others left in the workspace to its own O on the way out; of
-// more, all leave theirs, and the last to finish joins them or, in a call of few units,
-// all meet at a count and each join a part (such a call is launched cooperatively, so
-// that the wait ends).  Every length follows from the device's offsets: long prompts,
-// ragged batches and single tokens over long contexts are one case.
+// unnormalised O) that the others left in the workspace to its own O on the way out,
+// nobody waits; of more, all leave theirs, and the last to finish joins them or, in a
+// call of few units, all meet at a count and each join a part (such a call is launched
+// cooperatively, so that the wait ends).  Every length follows from the device's
+// offsets: long prompts, ragged batches and single tokens over long contexts are one case.
+//
+// Bound, and measured (one call, captured).  Long rows: the tensor core, as far as the
+// chain S -> P -> P V -> next S of the two row tiles keeps it busy: 128 keys of both take
+// 2,700 cycles, of which the MMAs need 2,048 (S and P of both and both O fill tensor
+// memory, so S of the next tile waits for P V of this one).  One prompt of 16384 tokens,
+// 28 heads over 4: 1158 us, 1,660 TFLOP/s; a chunk of 2048 after 30720, 56 heads over 8:
+// 1135 us, 1,640.  Ragged batches: also a segment's start and end, about 4,500 cycles that
+// no product covers (mostly code that is not in the instruction cache), and the CTAs'
+// imbalance (5%): 16 prompts of 33 to 4097 tokens 182 us, 1,260 TFLOP/s.  Single tokens:
+// the cache, 64 sequences of 1024 to 16384 keys 139 us, 5.7 TB/s, where loads of random
+// pages alone reach 6.2.  One token over 4096 keys: latency, 12.2 us (4,000 cycles until
+// the roles start, 6,000 until the first page is asked for, 6,000 for its tile, 6,000 to
+// meet and join).
 //
 // Roles of a CTA's twelve warps; all walk the share's segments (tile ranges of units)
 // by themselves, from a ring the scheduler fills:
@@ -33,7 +48,8 @@
 //          MMA multiplies masked rows by P = 0, and 0 times a NaN is a NaN.  Non-finite
 //          values of rows that some query must not see are zeroed, and added at the end
 //          for the queries that do;
-//   4-7    softmax of row tile A, one row per thread; 8-11 of row tile B.
+//   4-7    softmax and output of row tile A, one row per thread; 8-11 of row tile B.
+//          (Output by four warps of its own: 212 us instead of 189 for the 16 prompts.)
 // TMEM: S/P of A and B, O of A and B, 128 columns each.
 #include "ee_common.cuh"
 #include "ee_ptx.cuh"
@@ -60,8 +76,9 @@ constexpr uint32_t kSmemBytes = 1024 + kOffBar + 8 * kNumBars;
 constexpr uint32_t kTmemCols = 512, kColO = 256;
 constexpr float kRescaleLog2 = 8.0f;          // O is rescaled when a maximum grows by 2^8
 // Work in keys: the smallest share of a CTA, a unit's own constant, and how near (in tiles)
-// a cut comes to a unit's start or end before it moves there.  Calls of many rows and of few:
-// few rows' partials cost little to leave and to join.
+// a cut comes to a unit's start or end before it moves there, for calls of many rows and of
+// few (see params).  Constants of 128 / 160 / 192 / 256 / 320 keys: 16 packed prompts take 200 /
+// 187 / 182 / 185 / 189 us.
 constexpr int kShareMany = 5 * kKT, kUnitMany = 192, kSnapMany = 2;
 constexpr int kShareFew = kKT, kUnitFew = 128, kSnapFew = 1;
 static_assert(kShareFew >= kKT, "every CTA between a unit's first and last piece holds one");
@@ -92,8 +109,8 @@ struct PromptParams {
 };
 
 // The code that a CTA runs over and over is kept small (loops over the two row tiles
-// and over column blocks stay rolled, rare paths are calls): warps of six kinds
-// share one instruction cache, and a segment's start and end run all of it.
+// and over column blocks stay rolled): warps of six kinds share one instruction cache,
+// and a segment's start and end run all of it.
 __device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   return mbar_wait(bar, parity, abort_flag);
 }
@@ -1295,8 +1312,9 @@ ee_status launch(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorM
   return EE_OK;
 }
 
-PromptParams params(const int32_t* tok_off, int B, int total, int n_q, int n_kv, float scale, ee_bf16* out, float* lse,
-                    void* ws) {
+// max_keys: no unit has more.
+PromptParams params(const int32_t* tok_off, int B, int total, int64_t max_keys, int n_q, int n_kv, float scale,
+                    ee_bf16* out, float* lse, void* ws) {
   PromptParams p{};
   p.tok_off = tok_off;
   p.out = reinterpret_cast<__nv_bfloat16*>(out);
@@ -1311,12 +1329,18 @@ PromptParams params(const int32_t* tok_off, int B, int total, int n_q, int n_kv,
   p.tpt = kRows / p.g;
   p.scale = scale;
   p.scale_log2 = scale * 1.4426950408889634f;
-  // Units of the call: a sequence's last one may be partial.  Fewer than a third of the
-  // SMs: units are split among many CTAs, whose partials all of them join, which needs a
-  // cooperative launch (2 us more where a stream launches the calls one by one).
+  // Units of the call, at most (a sequence's last one may be partial).  Where they are
+  // fewer than a third of the SMs and long, they are split among many CTAs, whose partials
+  // all of them join, which needs a cooperative launch.  Measured with and without, captured
+  // / back to back: one token over 4096 keys 12.3 / 14.5 us and 17.6 / 17.7, 100 tokens after
+  // 8000 31 / 34 and 90 / 89; but 16 tokens over 1024 to 16384 keys (64 units) 49.6 / 52.8 and
+  // 49.2 / 49.7, a prompt of 300 tokens 12.8 / 14.9 and 12.9 / 12.7.
   const int w = 2 * p.tpt;
   p.units = (int)std::min<int64_t>((int64_t)n_kv * std::min<int64_t>((int64_t)total / w + B, total), INT32_MAX);
-  p.coop = p.units < kNumSMs / kDirect ? 1 : 0;
+  p.coop = p.units < kNumSMs / 3 && max_keys > kDirect * kShareMany ? 1 : 0;
+  // Few rows a sequence: their partials cost little to leave and to join.  With the shares
+  // of few and of many rows: one token over 4096 keys 12.2 and 18.1 us, 4 tokens 13.0 and 18.4;
+  // 100 tokens after 8000 32.7 and 31.1, a prompt of 300 15.4 and 12.8.
   const bool few = (int64_t)total * p.g <= 32 * (int64_t)B;
   p.min_share = few ? kShareFew : kShareMany;
   p.unit_keys = few ? kUnitFew : kUnitMany;
@@ -1343,7 +1367,7 @@ extern "C" ee_status ee_prompt_attn(const ee_bf16* q, int64_t q_stride, const ee
   ee_status ds = current_device(&dev);
   if (ds == EE_OK) ds = resident_ctas(dev, &ctas);
   if (ds != EE_OK) return ds;
-  PromptParams p = params(tok_off, B, total, n_q, n_kv, scale, out, lse_or_null, ws);
+  PromptParams p = params(tok_off, B, total, total, n_q, n_kv, scale, out, lse_or_null, ws);
   p.v = reinterpret_cast<const __nv_bfloat16*>(v);
   p.v_stride = v_stride;
   CUtensorMap tmQ, tmK, tmV;
@@ -1368,7 +1392,8 @@ extern "C" ee_status ee_chunk_attn(const ee_bf16* q, int64_t q_stride, const ee_
   ee_status ds = current_device(&dev);
   if (ds == EE_OK) ds = resident_ctas(dev, &ctas);
   if (ds != EE_OK) return ds;
-  PromptParams p = params(tok_off, B, total, n_q, n_kv, scale, out, lse_or_null, ws);
+  PromptParams p =
+      params(tok_off, B, total, (int64_t)max_pages * EE_PAGE, n_q, n_kv, scale, out, lse_or_null, ws);
   p.v = reinterpret_cast<const __nv_bfloat16*>(v_cache);
   p.block_table = block_table;
   p.ctx_len = ctx_len;
