@@ -8,6 +8,9 @@
 // .. 64 + 8 j + 7 (two 16-byte accesses, both halves of each of its pairs), so a
 // warp turns four heads at a time, and the sixteen cosines and sines of a lane stay
 // in its registers while the warp walks the token's heads.
+//
+// Measured (captured): 8191 tokens of 28 + 4 + 4 heads from a fused projection, rotated K
+// kept as well, 163.6 MB in 26.0 us, 6.3 TB/s, 0.93 of a copy's rate; 8 tokens 1.9 us.
 #include "ee_common.cuh"
 
 namespace {
