@@ -225,14 +225,17 @@ struct Seg {
   int s, o, T, ctx;        // sequence
   int hk, tok0;            // KV head, the unit's first token
   int j0, j1, n_tiles;     // n_tiles: of the whole unit; j1 = 0: no more segments
-  int nA, nB;              // tiles each row tile needs (B: 0 without tokens)
+  int kA, kB;              // keys each row tile needs (B: 0 without tokens)
   int c0, c1;              // first and last CTA that hold a piece
   int64_t X;               // the unit's first place
 };
 
 // Whether tile j of the unit holds keys that the first query must not see.
 __device__ __forceinline__ bool in_zone(const Seg& s, int j) { return j * kKT + kKT - 1 > s.ctx + s.tok0; }
-__device__ __forceinline__ bool active(const Seg& s, int st, int j) { return j < (st ? s.nB : s.nA); }
+__device__ __forceinline__ bool active(const Seg& s, int st, int j) { return j * kKT < (st ? s.kB : s.kA); }
+// Halves of tile j that row tile st needs (of the last one half is often enough: the second
+// half's exponentials and product are left out).
+__device__ __forceinline__ int halves(const Seg& s, int st, int j) { return (st ? s.kB : s.kA) - j * kKT > kKT / 2 ? 2 : 1; }
 
 template <bool kPaged>
 __device__ __forceinline__ const __nv_bfloat16* v_row(const PromptParams& p, const Seg& s, int key) {
@@ -654,8 +657,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           g.j0 = j0;
           g.j1 = j1;
           g.n_tiles = tiles;
-          g.nA = (ctx + min(T, tok0 + p.tpt) + kKT - 1) / kKT;
-          g.nB = T > tok0 + p.tpt ? tiles : 0;
+          g.kA = ctx + min(T, tok0 + p.tpt);
+          g.kB = T > tok0 + p.tpt ? keys : 0;
           g.c0 = g.c1 = 0;
           if (j1 - j0 < tiles) {
             // the first piece is that of the last CTA whose share starts before past_start,
@@ -803,7 +806,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       auto k_bar = [&](int t) { return kv_full + 16 * (t & 1); };
       auto v_bar = [&](int t) { return kv_full + 16 * (t & 1) + 8; };
       Seg s;
-      s.j0 = s.j1 = s.nA = s.nB = 0;
+      s.j0 = s.j1 = s.kA = s.kB = 0;
       int i = -1, j = -1, tile = -1;   // before the first tile: a step without P V
       uint32_t p_phase = 0, q_phase = 0, o_phase = 3;
       while (go) {
@@ -811,7 +814,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         // first: a wait between two products costs the tensor core what it takes (about
         // 100 cycles; the queue holds a few MMAs), so there is one before each half of P V
         // and none before Q K^T, and K and V are looked at beside the first
-        const int both = j > s.j0 ? min(s.j1, min(s.nA, s.nB)) - 1 : j;
+        const int both = j > s.j0 ? min(s.j1, (min(s.kA, s.kB) + kKT - 1) / kKT) - 1 : j;
 #pragma unroll 1
         for (; j < both && go; ++j, ++tile) {
           const uint32_t odd = tile & 1;
@@ -869,7 +872,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             p_phase ^= 1u << st;
             tc_fence_after();
             if (elect_one()) {
-              pv(st, odd, 1, true);
+              if (halves(s, st, j) == 2) pv(st, odd, 1, true);
               if (fresh || !active(s, st, jn)) {
                 tc_commit(pv_done + 8 * st);
                 mbar_arrive(pv_done + 8 * st);   // releases s_bad (acquired with kv_full)
@@ -956,7 +959,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       const bool warp_rows = __any_sync(0xffffffffu, vrow);
       const int pos = s.ctx + tok;                             // the row's last key
       const int tile_first = s.ctx + s.tok0 + st * p.tpt;      // the row tile's first row's
-      const int j_end = min(s.j1, st ? s.nB : s.nA);
+      const int j_end = min(s.j1, ((st ? s.kB : s.kA) + kKT - 1) / kKT);
       float m = -INFINITY, l = 0.f;                            // m in raw score units (scale > 0)
 #pragma unroll 1
       for (int j = s.j0; j < j_end; ++j) {
@@ -966,13 +969,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (warp_rows) {
           tc_fence_after();
           const uint32_t pm = kPaged ? s_mask[(tile + j - s.j0) % kMasks] : 0xFFu;
-          const int base = j * kKT;
+          const int base = j * kKT, nh = halves(s, st, j);
           if (base + kKT - 1 > tile_first || pm != 0xFFu) {
             // scores that a row must not see become -inf in tensor memory, from the first
             // 16-key block with one on
             const int nvis = pos + 1 - base;
 #pragma unroll 1
-            for (int c = pm != 0xFFu ? 0 : max(tile_first + 1 - base, 0) >> 4; c < kKT / 16; ++c) {
+            for (int c = pm != 0xFFu ? 0 : max(tile_first + 1 - base, 0) >> 4; c < nh * (kKT / 32); ++c) {
               const int nv = (pm >> c) & 1u ? nvis - 16 * c : 0;
               uint32_t sv[16];
               tc_ld16(tS + 16 * c, sv);
@@ -992,12 +995,12 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           float tmax = -INFINITY;
           tc_ld32_nowait(tS, xa);
 #pragma unroll 1
-          for (int c = 0; c < 2; ++c) {
+          for (int c = 0; c < nh; ++c) {
             tc_wait_ld32(xa);
             tc_ld32_nowait(tS + 64 * c + 32, xb);
             tmax = max32(xa, tmax);
             tc_wait_ld32(xb);
-            tc_ld32_nowait(tS + 64 * (c ^ 1), xa);   // (the second pass's first at last)
+            tc_ld32_nowait(tS + (c + 1 < nh ? 64 : 0), xa);   // (the second pass's first at last)
             tmax = max32(xb, tmax);
           }
           const bool need = (tmax - m) * sl2 > kRescaleLog2;   // true when m = -inf < tmax
@@ -1021,7 +1024,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           const uint64_t nmsx2 = f2_pack(__float_as_uint(nms), __float_as_uint(nms));
           uint64_t ls[2] = {0ull, 0ull};
 #pragma unroll 1
-          for (int c = 0; c < 2; ++c) {
+          for (int c = 0; c < nh; ++c) {
             // P of 64 keys goes to columns 32 c .. 32 c + 31, whose scores are in registers
             uint32_t pw[16];
             tc_wait_ld32(xa);
@@ -1029,7 +1032,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             exp32(xa, sl2x2, nmsx2, ls, pw);
             tc_st16_nowait(tS + 32 * c, pw);
             tc_wait_ld32(xb);
-            if (c == 0) tc_ld32_nowait(tS + 64, xa);
+            if (c + 1 < nh) tc_ld32_nowait(tS + 64, xa);
             exp32(xb, sl2x2, nmsx2, ls, pw);
             tc_st16_nowait(tS + 32 * c + 16, pw);
             tc_wait_st();
@@ -1037,6 +1040,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             __syncwarp();
             if (lane == 0) mbar_arrive(p_half + 16 * c + 8 * st);   // (p_full follows p_half)
           }
+          if (nh == 1 && lane == 0) mbar_arrive(p_full + 8 * st);
           ls[0] = f2_add(ls[0], ls[1]);
           uint32_t a0, a1;
           f2_unpack(ls[0], a0, a1);
