@@ -34,9 +34,9 @@
 // no product covers (mostly code that is not in the instruction cache), and the CTAs'
 // imbalance (5%): 16 prompts of 33 to 4097 tokens 182 us, 1,260 TFLOP/s.  Single tokens:
 // the cache, 64 sequences of 1024 to 16384 keys 139 us, 5.7 TB/s, where loads of random
-// pages alone reach 6.2.  One token over 4096 keys: latency, 12.2 us (4,000 cycles until
-// the roles start, 6,000 until the first page is asked for, 6,000 for its tile, 6,000 to
-// meet and join).
+// pages alone reach 6.2.  One token over 4096 keys: latency, 12.1 us (4,000 cycles until
+// the roles start, 5,000 until the first page is asked for, 7,000 for its tile, 6,000 to
+// meet and join); a prompt of 37 tokens, 8 heads over 2: 7.6 us.
 //
 // Roles of a CTA's twelve warps; all walk the share's segments (tile ranges of units)
 // by themselves, from a ring the scheduler fills:
@@ -71,7 +71,7 @@ constexpr uint32_t kTile = 2 * kHalf;         // 32 KB
 constexpr uint32_t kOffKV = 0, kOffQ = kRing * kTile, kOffOut = kOffQ + 2 * kTile;
 constexpr uint32_t kOutBytes = 32 * 128;      // a softmax warp's rows x 64 columns of bf16, on their way out
 constexpr uint32_t kOffBar = kOffOut + 8 * kOutBytes;
-constexpr uint32_t kNumBars = 2 * kRing + 4 + 10 + 2 * kSegs + kZones + 1;
+constexpr uint32_t kNumBars = 2 * kRing + 4 + 10 + 3 * kSegs + kZones + 1;
 constexpr uint32_t kSmemBytes = 1024 + kOffBar + 8 * kNumBars;
 constexpr uint32_t kTmemCols = 512, kColO = 256;
 constexpr float kRescaleLog2 = 8.0f;          // O is rescaled when a maximum grows by 2^8
@@ -226,7 +226,7 @@ struct Seg {
   int hk, tok0;            // KV head, the unit's first token
   int j0, j1, n_tiles;     // n_tiles: of the whole unit; j1 = 0: no more segments
   int kA, kB;              // keys each row tile needs (B: 0 without tokens)
-  int c0, c1;              // first and last CTA that hold a piece
+  int c0, c1;              // first and last CTA that hold a piece (a split unit: set after the rest)
   int64_t X;               // the unit's first place
 };
 
@@ -383,7 +383,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   const uint32_t s_full = q_empty + 16, p_half = s_full + 16, p_full = p_half + 16;
   const uint32_t pv_done = p_full + 16, o_free = pv_done + 16;
   const uint32_t seg_full = o_free + 16, seg_empty = seg_full + 8 * kSegs, z_full = seg_empty + 8 * kSegs;
-  const uint32_t drain = z_full + 8 * kZones;
+  const uint32_t drain = z_full + 8 * kZones, cut_full = drain + 8;
 
   if (tid == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmQ)) : "memory");
@@ -660,13 +660,6 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           g.kA = ctx + min(T, tok0 + p.tpt);
           g.kB = T > tok0 + p.tpt ? keys : 0;
           g.c0 = g.c1 = 0;
-          if (j1 - j0 < tiles) {
-            // the first piece is that of the last CTA whose share starts before past_start,
-            // the last piece that of the last whose share starts before at_end; shares are
-            // no shorter than a tile, so every CTA between them holds one
-            g.c0 = sh.before(g.X + past_start(p));
-            g.c1 = sh.before(g.X + at_end(p, tiles));
-          }
           return true;
         }
         g.j1 = 0;
@@ -677,14 +670,31 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (lane == 0) {
           s_seg[i % kSegs] = g;
           s_bad[i % kSegs] = 0;
-          if (g.j1 > 0 && g.j1 - g.j0 < g.n_tiles && g.c1 - g.c0 >= kDirect) {
-            s_pc[s_npc & 1] = g;
-            s_npc = s_npc + 1;
-          }
           mbar_arrive(seg_full + 8 * (i % kSegs));
         }
         __syncwarp();
         return true;
+      };
+      // Which CTAs hold the unit's pieces, needed at the segment's end: after the segment and
+      // its Q are on their way (it takes about 800 cycles)
+      auto cut = [&](int i, Seg& g) {
+        if (g.j1 - g.j0 < g.n_tiles) {
+          // the first piece is that of the last CTA whose share starts before past_start,
+          // the last piece that of the last whose share starts before at_end; shares are
+          // no shorter than a tile, so every CTA between them holds one
+          g.c0 = sh.before(g.X + past_start(p));
+          g.c1 = sh.before(g.X + at_end(p, g.n_tiles));
+        }
+        if (lane == 0) {
+          s_seg[i % kSegs].c0 = g.c0;
+          s_seg[i % kSegs].c1 = g.c1;
+          if (g.c1 - g.c0 >= kDirect) {
+            s_pc[s_npc & 1] = g;
+            s_npc = s_npc + 1;
+          }
+          mbar_arrive(cut_full + 8 * (i % kSegs));
+        }
+        __syncwarp();
       };
       // The first segment's Q is loaded at once; from then on segment i is published
       // before Q of segment i - 1, whose buffer may still be in use, is waited for.
@@ -711,6 +721,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           __syncwarp();
           q_phase ^= 1u << st;
         }
+        if (go && more) cut(i, nxt);
         cur = nxt;
         pending = i > 0;
         if (!loaded && more) load32(s + 1);   // the sequences to come, beside the first segment's work
@@ -1075,12 +1086,14 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         // segment and the others' first, so that it is mostly the one that joins, and only it
         // looks before it leaves a partial).  The pieces are added in their order, whichever
         // warp adds them.  Many: see below.
-        const int K = s.c1 - s.c0 + 1, own = (int)blockIdx.x - s.c0;
+        go = wait(cut_full + 8 * (i % kSegs), i / kSegs);
+        if (!go) break;
+        const int c0 = s_seg[i % kSegs].c0, K = s_seg[i % kSegs].c1 - c0 + 1, own = (int)blockIdx.x - c0;
         const bool direct = K <= kDirect;
-        uint32_t* cnt = reinterpret_cast<uint32_t*>(p.part + (size_t)(2 * (2 * s.c0 + 1) + st) * kAttnPartBytes + kCntOff) + qd;
+        uint32_t* cnt = reinterpret_cast<uint32_t*>(p.part + (size_t)(2 * (2 * c0 + 1) + st) * kAttnPartBytes + kCntOff) + qd;
         if (direct && own == 0) fin = __shfl_sync(0xffffffffu, lane == 0 && ld_acquire(cnt) == (uint32_t)(K - 1), 0);
         // partial slot of piece k: the first is its CTA's second
-        auto slot = [&](int k) { return p.part + (size_t)(2 * (2 * (s.c0 + k) + (k == 0)) + st) * kAttnPartBytes; };
+        auto slot = [&](int k) { return p.part + (size_t)(2 * (2 * (c0 + k) + (k == 0)) + st) * kAttnPartBytes; };
         if (!fin) {
           uint8_t* part = slot(own);
           if (any && warp_rows) {
