@@ -21,8 +21,8 @@
 // 2^(m - max): of up to kDirect pieces the last to finish joins the partials (m, l,
 // unnormalised O) that the others left in the workspace to its own O on the way out,
 // nobody waits; of more, all leave theirs, and the last to finish joins them or, in a
-// call of few units, all meet at a count and each join a part (such a call is launched
-// cooperatively, so that the wait ends).  Every length follows from the device's
+// call of few long units, all meet at a count and each join a part (such a call is
+// launched cooperatively, so that the wait ends).  Every length follows from the device's
 // offsets: long prompts, ragged batches and single tokens over long contexts are one case.
 //
 // Bound, and measured (one call, captured).  Long rows: the tensor core, as far as the
@@ -34,9 +34,9 @@
 // no product covers (mostly code that is not in the instruction cache), and the CTAs'
 // imbalance (5%): 16 prompts of 33 to 4097 tokens 182 us, 1,260 TFLOP/s.  Single tokens:
 // the cache, 64 sequences of 1024 to 16384 keys 139 us, 5.7 TB/s, where loads of random
-// pages alone reach 6.2.  One token over 4096 keys: latency, 12.1 us (4,000 cycles until
-// the roles start, 5,000 until the first page is asked for, 7,000 for its tile, 6,000 to
-// meet and join); a prompt of 37 tokens, 8 heads over 2: 7.6 us.
+// pages alone reach 6.2.  One token over 4096 keys: latency, 12.2 us (4,000 cycles until
+// the roles start, 6,000 until the first page is asked for, 6,000 for its tile, 6,000 to
+// meet and join).
 //
 // Roles of a CTA's twelve warps; all walk the share's segments (tile ranges of units)
 // by themselves, from a ring the scheduler fills:
@@ -208,7 +208,9 @@ struct Shares {
     q = ((int64_t)q1 << 24) + q0;
     r = (int)(lo - q0 * (uint32_t)n);
   }
-  __device__ __forceinline__ int64_t start(int c) const { return q * c + (N == 1 ? 0 : (int)__umulhi((uint32_t)(r * c), inv)); }
+  __device__ __forceinline__ int64_t start(int c) const {
+    return q * c + (N == 1 ? 0 : (int)__umulhi((uint32_t)(r * c), inv));
+  }
   // the last CTA whose share starts before place y (y > 0)
   __device__ __forceinline__ int before(int64_t y) const {
     int c = min(max((int)(__fdividef((float)y, (float)W) * N), 0), N - 1);   // put right below
@@ -402,12 +404,12 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 #pragma unroll 1
     for (int i = lane; i < (int)kNumBars; i += 32) {
       const uint32_t bar = bar0 + 8 * i;
-      const uint32_t count = bar >= s_full && bar < p_half     ? kPaged + 1   // the commit (paged: and a release of the page mask)
-                             : bar >= p_half && bar < pv_done    ? 4    // warps
-                             : bar >= pv_done && bar < o_free    ? 2    // the commit, and a release of s_bad
-                             : bar >= o_free && bar < seg_full   ? 4
+      const uint32_t count = bar >= s_full && bar < p_half      ? kPaged + 1   // the commit (paged: and the page mask's release)
+                             : bar >= p_half && bar < pv_done   ? 4            // warps
+                             : bar >= pv_done && bar < o_free   ? 2            // the commit, and a release of s_bad
+                             : bar >= o_free && bar < seg_full  ? 4
                              : bar >= seg_empty && bar < z_full ? kSegReaders
-                                                                 : 1;
+                                                                : 1;
       mbar_init(bar, count);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -462,7 +464,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   // as many CTAs as the units or the shortest share allow
   // (W past the grid's worth of the larger share changes nothing: 32-bit divisions)
   const uint32_t Wc = (uint32_t)min(W, (int64_t)gridDim.x * kShareMany);
-  const Shares sh(W, min((int)gridDim.x, max(max((int)(Wc / (uint32_t)p.min_share), min((int)(Wc / kShareFew), p.units)), 1)));
+  const int want = max((int)(Wc / (uint32_t)p.min_share), min((int)(Wc / kShareFew), p.units));
+  const Shares sh(W, min((int)gridDim.x, max(want, 1)));
   const bool works = (int)blockIdx.x < sh.N && W > 0;
   const int64_t x0 = works ? sh.start(blockIdx.x) : W, x1 = works ? sh.start(blockIdx.x + 1) : W;
   if (works && x0 >= base && x0 < base + sum) {
@@ -831,7 +834,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           const uint32_t odd = tile & 1;
 #pragma unroll 1
           for (int st = 0; st < 2; ++st) {
-            const bool v_in = mbar_try(v_bar(tile), (tile >> 1) & 1), k_in = mbar_try(k_bar(tile + 1), ((tile + 1) >> 1) & 1);
+            const bool v_in = mbar_try(v_bar(tile), (tile >> 1) & 1);
+            const bool k_in = mbar_try(k_bar(tile + 1), ((tile + 1) >> 1) & 1);
             meet(p_half + 8 * st, p_phase);
             if (!v_in) meet(v_bar(tile), tile >> 1);
             if (!k_in) meet(k_bar(tile + 1), (tile + 1) >> 1);
@@ -1090,7 +1094,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         if (!go) break;
         const int c0 = s_seg[i % kSegs].c0, K = s_seg[i % kSegs].c1 - c0 + 1, own = (int)blockIdx.x - c0;
         const bool direct = K <= kDirect;
-        uint32_t* cnt = reinterpret_cast<uint32_t*>(p.part + (size_t)(2 * (2 * c0 + 1) + st) * kAttnPartBytes + kCntOff) + qd;
+        uint32_t* cnt =
+            reinterpret_cast<uint32_t*>(p.part + (size_t)(2 * (2 * c0 + 1) + st) * kAttnPartBytes + kCntOff) + qd;
         if (direct && own == 0) fin = __shfl_sync(0xffffffffu, lane == 0 && ld_acquire(cnt) == (uint32_t)(K - 1), 0);
         // partial slot of piece k: the first is its CTA's second
         auto slot = [&](int k) { return p.part + (size_t)(2 * (2 * (c0 + k) + (k == 0)) + st) * kAttnPartBytes; };

@@ -159,6 +159,21 @@ def test_captured_decode(E):
         P.assert_attn(out[s:s + 1], None, P.ref_rows(pi.q_rot[s:s + 1], K, V, n - 1, SCALE), f"sequence {s}")
 
 
+def test_nothing_new(E):
+    """A pass without tokens between two with: lengths and cache stay, the output is empty."""
+    pi = make(2, 8, 2, L=1)
+    kept = [[], []]
+    gen = torch.Generator("cuda").manual_seed(2)
+    take(pi, gen, [5, 40], True, kept)
+    table, cache = pi.block_table.clone(), pi.k_cache.clone()
+    q, k, v = P.packed_qkv(gen, 0, 8, 2, fused=True)
+    pi.admit(P.i32([0, 0]), 0)
+    assert pi.attend(0, q, k, v).shape == (0, 8, D)
+    assert pi.ctx_len.tolist() == [5, 40] == pi.ctx_before.tolist() and torch.equal(pi.block_table, table)
+    assert torch.equal(pi.k_cache.view(torch.int16), cache.view(torch.int16)) and pi.errors() == 0
+    take(pi, gen, [1, 2], False, kept)
+
+
 def test_no_room(E):
     """More pages than are free: the error word says so, nothing is written, lengths stay."""
     pi = make(2, 8, 2, L=1, num_pages=4)
