@@ -952,11 +952,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       tc_fence_after();
       asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(s_tmem), "r"(kTmemCols) : "memory");
     }
-    return;
-  }
-
-  // ---------------- softmax: one row per thread ----------------
-  {
+  } else {
+    // ---------------- softmax: one row per thread ----------------
     const int st = (warp - kWarpSoft) >> 2, qd = warp & 3;
     const int r = qd * 32 + lane;
     const int tok_r = r / p.g, head = r - tok_r * p.g;
@@ -1231,17 +1228,17 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       if (any && lane == 0) mbar_arrive(o_free + 8 * st);
       release(i);
     }
+    tc_fence_before();
+    __syncthreads();
+    pdl_allow_next();
   }
-  tc_fence_before();
-  __syncthreads();
-  pdl_allow_next();
   if (s_abort) return;
 
   // ---- pieces of units split among many: counted, waited for and merged ----
   const int npc = s_npc;
   if (npc == 0) return;
-  const int nthr = npc == 2 ? 128 : 256;
-  const int pi = (tid - 32 * kWarpSoft) / nthr, t = (tid - 32 * kWarpSoft) - pi * nthr;
+  const int nthr = npc == 2 ? kThreads / 2 : kThreads;
+  const int pi = tid >= nthr, t = tid - pi * nthr;
   const Seg s = s_pc[pi];
   const int K = s.c1 - s.c0 + 1, mine = (int)blockIdx.x - s.c0;
   const int items = min(w, s.T - s.tok0) * p.g * (kD / 8);
