@@ -34,9 +34,9 @@
 // no product covers (mostly code that is not in the instruction cache), and the CTAs'
 // imbalance (5%): 16 prompts of 33 to 4097 tokens 182 us, 1,260 TFLOP/s.  Single tokens:
 // the cache, 64 sequences of 1024 to 16384 keys 139 us, 5.7 TB/s, where loads of random
-// pages alone reach 6.2.  One token over 4096 keys: latency, 12.2 us (4,000 cycles until
-// the roles start, 6,000 until the first page is asked for, 6,000 for its tile, 6,000 to
-// meet and join).
+// pages alone reach 6.2.  One token over 4096 keys: latency, 12.0 us (4,000 cycles until
+// the roles start, 5,000 until the first page is asked for, 7,000 for its tile, 6,000 to
+// meet and join); a prompt of 37 tokens, 8 heads over 2: 7.6 us.
 //
 // Roles of a CTA's twelve warps; all walk the share's segments (tile ranges of units)
 // by themselves, from a ring the scheduler fills:
@@ -49,7 +49,7 @@
 //          values of rows that some query must not see are zeroed, and added at the end
 //          for the queries that do;
 //   4-7    softmax and output of row tile A, one row per thread; 8-11 of row tile B.
-//          (Output by four warps of its own: 212 us instead of 189 for the 16 prompts.)
+//          (Output by four warps of its own: 214 us instead of 190 for the 16 prompts.)
 // TMEM: S/P of A and B, O of A and B, 128 columns each.
 #include "ee_common.cuh"
 #include "ee_ptx.cuh"
@@ -1348,15 +1348,15 @@ PromptParams params(const int32_t* tok_off, int B, int total, int64_t max_keys, 
   // Units of the call, at most (a sequence's last one may be partial).  Where they are
   // fewer than a third of the SMs and long, they are split among many CTAs, whose partials
   // all of them join, which needs a cooperative launch.  Measured with and without, captured
-  // / back to back: one token over 4096 keys 12.3 / 14.5 us and 17.6 / 17.7, 100 tokens after
-  // 8000 31 / 34 and 90 / 89; but 16 tokens over 1024 to 16384 keys (64 units) 49.6 / 52.8 and
-  // 49.2 / 49.7, a prompt of 300 tokens 12.8 / 14.9 and 12.9 / 12.7.
+  // / back to back: one token over 4096 keys 12.0 / 14.4 us and 17.3 / 17.4, 100 tokens after
+  // 8000 27 / 30 and 66 / 66; but 16 tokens over 1024 to 16384 keys (64 units) 49.9 / 52.8 and
+  // 49.1 / 49.7, a prompt of 300 tokens 12.2 / 14.5 and 12.2 / 12.1.
   const int w = 2 * p.tpt;
   p.units = (int)std::min<int64_t>((int64_t)n_kv * std::min<int64_t>((int64_t)total / w + B, total), INT32_MAX);
   p.coop = p.units < kNumSMs / 3 && max_keys > kDirect * kShareMany ? 1 : 0;
   // Few rows a sequence: their partials cost little to leave and to join.  With the shares
-  // of few and of many rows: one token over 4096 keys 12.2 and 18.1 us, 4 tokens 13.0 and 18.4;
-  // 100 tokens after 8000 32.7 and 31.1, a prompt of 300 15.4 and 12.8.
+  // of few and of many rows: one token over 4096 keys 12.0 and 17.7 us, 4 tokens 12.7 and 17.8;
+  // 100 tokens after 8000 28.4 and 27.0, a prompt of 300 15.2 and 12.2.
   const bool few = (int64_t)total * p.g <= 32 * (int64_t)B;
   p.min_share = few ? kShareFew : kShareMany;
   p.unit_keys = few ? kUnitFew : kUnitMany;
