@@ -301,9 +301,12 @@ struct Joined {
 // share an item, each over every 2^sub-th piece.
 __device__ __forceinline__ void merge_items(const PromptParams& p, const Seg& s, int lo, int hi, int t, int nthr) {
   const int K = s.c1 - s.c0 + 1;
+  // (the sum's order depends on it: where any piece's CTA may be the one that joins, it must
+  // not follow from how many units that one has)
+  const int lanes = p.coop ? nthr : kThreads / 2;
   int sub = 0;
 #pragma unroll 1
-  while (sub < 5 && 1 << sub < K && (hi - lo) << (sub + 1) <= nthr) ++sub;
+  while (sub < 5 && 1 << sub < K && (hi - lo) << (sub + 1) <= lanes) ++sub;
   const int nt = min(2 * p.tpt, s.T - s.tok0);               // tokens of the unit
   const int rows_a = min(nt, p.tpt) * p.g, rows = nt * p.g;  // rows of A, of both
   const int k0 = t & ((1 << sub) - 1);

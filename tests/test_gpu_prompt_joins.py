@@ -85,6 +85,18 @@ def test_joined_pieces(E, ws, heads, lens, ctxs, climb):
     assert E.ee_read_errors(ws) == 0
 
 
+def test_the_same_bits_whoever_joins(E, ws):
+    """Units in many pieces that the last CTA to arrive joins: which one that is, and whether
+    it has a second unit to join, differs from run to run; the sum's order must not."""
+    heads, lens, ctxs = (56, 8), [1, 1, 0, 3, 1, 1, 1], [2442, 3623, 6356, 0, 0, 2641, 0]
+    q, kc, vc, table = inputs(heads, lens, ctxs, 0)
+    out, z = run(E, ws, q, kc, vc, table, lens, ctxs)
+    check(out, z, q, kc, vc, table, lens, ctxs)
+    for _ in range(100):
+        again, za = run(E, ws, q, kc, vc, table, lens, ctxs)
+        assert torch.equal(out, again) and torch.equal(z, za)
+
+
 @pytest.mark.parametrize("heads,lens,ctxs", [CASES[0], CASES[1], CASES[3], CASES[6], CASES[8]])
 @pytest.mark.parametrize("part", ["first half", "second half", "all"])
 def test_pieces_without_a_key(E, ws, heads, lens, ctxs, part):
