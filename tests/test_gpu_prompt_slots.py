@@ -255,3 +255,23 @@ def test_rope_cache_past_four_gib(E, ws):
     near(kc[-1, :, -9:].transpose(0, 1), rotated(k, rope, pos))
     assert torch.equal(vc[-1, :, -9:].transpose(0, 1), v)
     assert E.ee_read_errors(ws) == 0
+
+
+@pytest.mark.parametrize("shift", [1, 2, 3])
+@pytest.mark.parametrize("B,new_hi,ctx_hi", [(1, 9, 40), (70, 1, 100), (300, 37, 90)])
+def test_slots_at_any_alignment(E, ws, shift, B, new_hi, ctx_hi):
+    """pos and slot need four-byte alignment only; what lies around them stays."""
+    ctx, new, held, table, free, n = case(B, new_hi, ctx_hi, 7, B + shift)
+    new[-1] += 1
+    off, pos, slot, tab, ctx_out, held_out, left = loop(ctx, new, held, table, free, len(free), 7)
+    total = off[-1]
+    full = lambda k: torch.full((k,), -9, dtype=torch.int32, device="cuda")  # noqa: E731
+    wide = [full(total + 8) for _ in range(2)]
+    p, s = (w[shift:shift + total] for w in wide)
+    t, o, c, h, f = P.i32(table), full(B + 1), full(B), full(B), full(1)
+    E.ee_prompt_slots(P.i32(ctx), P.i32(new), P.i32(held), t, P.i32(free), P.i32([len(free)]), n, 7, o, p, s, c, h, f, ws)
+    assert E.ee_read_errors(ws) == 0
+    assert p.tolist() == pos and s.tolist() == slot and o.tolist() == off and f.item() == left
+    assert (t.cpu().numpy() == tab).all() and c.tolist() == ctx_out and h.tolist() == held_out
+    for w in wide:
+        assert (w[:shift] == -9).all() and (w[shift + total:] == -9).all()
