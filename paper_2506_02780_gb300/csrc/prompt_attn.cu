@@ -1125,6 +1125,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         } else if (lane == 0) {
           *cnt = 0;              // for the next launch
         }
+        __syncwarp();            // lane 0 acquired the count: a shuffle hands its value on, not its order
         if (fin && warp_rows) {
           float2 ml[kDirect];
           const float m_own = M;

@@ -97,6 +97,24 @@ def test_the_same_bits_whoever_joins(E, ws):
         assert torch.equal(out, again) and torch.equal(z, za)
 
 
+@pytest.mark.parametrize("heads,lens,ctxs", [CASES[1], CASES[3], CASES[5], CASES[7]])
+def test_a_join_reads_this_calls_partials(E, ws, heads, lens, ctxs):
+    """Two sets of inputs in turn, one workspace, nothing waited for in between: a piece that
+    was read before its writer was done would still hold the other set's partial."""
+    sets = [inputs(heads, lens, ctxs, climb) for climb in (1, -1)]
+    want = [run(E, ws, *x, lens, ctxs) for x in sets]
+    for x, (out, z) in zip(sets, want):
+        check(out, z, *x, lens, ctxs)
+    ctx, off = P.i32(ctxs), P.i32(P.offsets(lens))
+    got = [(torch.empty_like(want[i % 2][0]), torch.empty_like(want[i % 2][1])) for i in range(60)]
+    for i, (out, z) in enumerate(got):
+        q, kc, vc, table = sets[i % 2]
+        E.ee_chunk_attn(q, kc, vc, table, ctx, off, SCALE, out, ws, lse=z)
+    for i, (out, z) in enumerate(got):
+        assert torch.equal(out, want[i % 2][0]) and torch.equal(z, want[i % 2][1]), f"call {i}"
+    assert E.ee_read_errors(ws) == 0
+
+
 @pytest.mark.parametrize("heads,lens,ctxs", [CASES[0], CASES[1], CASES[3], CASES[6], CASES[8]])
 @pytest.mark.parametrize("part", ["first half", "second half", "all"])
 def test_pieces_without_a_key(E, ws, heads, lens, ctxs, part):
