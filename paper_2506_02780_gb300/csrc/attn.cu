@@ -791,7 +791,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmKc, const __grid_constant__
         // node range and context length so that the round trips overlap
         const int split = (int)(blockIdx.x % p.S);
         const int pg = split * (p.chunk / EE_PAGE) + lane;
-        if (pg < p.max_pages) early = ld_nc_pinned(p.block_table + (size_t)blockIdx.z * p.max_pages + pg);
+        if (pg < p.max_pages) early = ld_pinned(p.block_table + (size_t)blockIdx.z * p.max_pages + pg);
         if (!isK && lane == 0 && p.coop && p.S > 1)
           u_count = ld_relaxed64(reinterpret_cast<const unsigned long long*>(
               p.part +
@@ -817,7 +817,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmKc, const __grid_constant__
         const bool need = t < sg.n_tiles && i < sg.n_ctx && pos < sg.k_end;
         if (!kBal && c == 0) return need ? early : INT32_MIN;
         int32_t v = INT32_MIN;
-        if (need) v = ld_nc_pinned(p.block_table + (size_t)sg.b * p.max_pages + pos / EE_PAGE);
+        if (need) v = ld_pinned(p.block_table + (size_t)sg.b * p.max_pages + pos / EE_PAGE);
         return v;
       };
       // balanced, the K producer: the next segment (decoded and published, its first

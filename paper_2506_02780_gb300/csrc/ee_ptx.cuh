@@ -199,11 +199,14 @@ __device__ __forceinline__ void cluster_sync() {
       "barrier.cluster.arrive.release.aligned;\n"
       "barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// Read-only global load that the compiler issues where it is written (volatile:
-// not sunk past branches), so that independent round trips overlap.
-__device__ __forceinline__ int32_t ld_nc_pinned(const int32_t* a) {
+// Global load that the compiler issues where it is written (volatile: neither
+// sunk past branches nor moved before pdl_wait()), so that independent round
+// trips overlap.  Not a non-coherent one: a kernel that writes block tables or
+// lengths (ee_prompt_slots) may still run when its reader's CTAs start, and
+// ld.global.nc takes memory that nobody writes while the reader is alive.
+__device__ __forceinline__ int32_t ld_pinned(const int32_t* a) {
   int32_t v;
-  asm volatile("ld.global.nc.s32 %0, [%1];" : "=r"(v) : "l"(a));
+  asm volatile("ld.global.s32 %0, [%1];" : "=r"(v) : "l"(a));
   return v;
 }
 // gpu-scope acquire load of a global counter

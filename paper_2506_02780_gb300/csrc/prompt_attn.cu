@@ -520,7 +520,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         auto fetch = [&](int j) -> int32_t {
           const int key = (j + (lane >> 3)) * kKT + 16 * (lane & 7);
           const bool need = (j + (lane >> 3)) < s.j1 && key <= last;
-          return need ? max(ld_nc_pinned(p.block_table + (size_t)s.s * p.max_pages + key / EE_PAGE), -1) : INT32_MIN;
+          return need ? max(ld_pinned(p.block_table + (size_t)s.s * p.max_pages + key / EE_PAGE), -1) : INT32_MIN;
         };
         int32_t ids = INT32_MIN, ids_next = INT32_MIN;
         if constexpr (kPaged) ids_next = fetch(s.j0);

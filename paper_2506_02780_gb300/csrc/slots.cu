@@ -18,6 +18,7 @@
 // 8 sequences with a token each 3.7 us; 1024 sequences of up to 2048 new tokens, 2.6 MB in
 // all, 7.2 us.  512 threads: with 256 the latter takes 8.9 us, with 1024 the former 5.6 us.
 #include "ee_common.cuh"
+#include "ee_ptx.cuh"
 
 namespace {
 
@@ -37,9 +38,9 @@ struct SlotParams {
 // One sequence's share: tokens it gets and pages it is given (0 and 0 when its
 // lengths are out of range).
 __device__ __forceinline__ bool seq_share(const SlotParams& p, int s, int& ctx, int& held, int& t, int& give) {
-  ctx = __ldg(p.ctx_len + s);   // (read-only: the loads of neighbouring sequences overlap)
-  held = __ldg(p.held + s);
-  t = __ldg(p.new_len + s);
+  ctx = ee::ld_pinned(p.ctx_len + s);
+  held = ee::ld_pinned(p.held + s);
+  t = ee::ld_pinned(p.new_len + s);
   give = 0;
   const int64_t cap = (int64_t)p.max_pages * EE_PAGE;
   const int64_t end = (int64_t)ctx + t, want = end + p.reserve;

@@ -275,3 +275,55 @@ def test_slots_at_any_alignment(E, ws, shift, B, new_hi, ctx_hi):
     assert (t.cpu().numpy() == tab).all() and c.tolist() == ctx_out and h.tolist() == held_out
     for w in wide:
         assert (w[:shift] == -9).all() and (w[shift + total:] == -9).all()
+
+
+def test_tables_and_lengths_are_read_as_just_written(E, ws):
+    """Slots, then attention over the table that they wrote, then slots of the other
+    sequences into the same table, with nothing in between: each call reads what the one
+    before it wrote, although it may have started earlier."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    B, n_q, n_kv, num_pages, cols = 24, 8, 2, 400, 8
+    kc, vc = P.randn(gen, num_pages, n_kv, 16, D), P.randn(gen, num_pages, n_kv, 16, D)
+    lens = [100 - s for s in range(B)]
+    q = P.randn(gen, B, n_q, D)
+    table = torch.full((B, cols), -1, dtype=torch.int32, device="cuda")
+    zero, ones, off = P.i32([0] * B), P.i32([1] * B), P.i32(list(range(B + 1)))
+    ctx0, free = P.i32([n - 1 for n in lens]), []
+    perm = torch.randperm(num_pages, generator=torch.Generator().manual_seed(5)).to(torch.int32).cuda()
+    need = sum(P.pages(n) for n in lens)
+    free = [perm[:need].contiguous(), perm[-need:].contiguous()]
+    cnt, new = P.i32([need]), P.i32(lens)
+    total = sum(lens)
+    o = dict(tok_off=P.i32([0] * (B + 1)), pos=P.i32([0] * total), slot=P.i32([0] * total), ctx=P.i32([0] * B),
+             held=P.i32([0] * B), left=P.i32([0]))
+    o2 = dict(pos=P.i32([0] * B), slot=P.i32([0] * B), ctx=P.i32([0] * B), held=P.i32([0] * B), left=P.i32([0]),
+              off=P.i32([0] * (B + 1)))
+    got = [(torch.empty_like(q), torch.empty_like(o2["slot"])) for _ in range(40)]
+    scale = 128 ** -0.5
+
+    def once(i, out):
+        # all pages anew, from the one list or the other; then what they hold is attended to
+        E.ee_prompt_slots(zero, new, zero, table, free[i % 2], cnt, num_pages, 0, o["tok_off"], o["pos"], o["slot"],
+                          o["ctx"], o["held"], o["left"], ws)
+        E.ee_chunk_attn(q, kc, vc, table, ctx0, off, scale, out, ws)
+        # one more token each, from the lengths that the first call wrote
+        E.ee_prompt_slots(o["ctx"], ones, o["held"], table, perm, P_ALL, num_pages, 0, o2["off"], o2["pos"],
+                          o2["slot"], o2["ctx"], o2["held"], o2["left"], ws)
+
+    P_ALL = P.i32([num_pages])
+    want = []
+    for i in range(2):
+        out = torch.empty_like(q)
+        once(i, out)
+        torch.cuda.synchronize()
+        for s in range(B):
+            K, V = P.cache_rows(kc, table, s, lens[s]), P.cache_rows(vc, table, s, lens[s])
+            P.assert_attn(out[s:s + 1], None, P.ref_rows(q[s:s + 1], K, V, lens[s] - 1, scale), f"sequence {s}")
+        assert o2["pos"].tolist() == lens
+        want.append((out, o2["slot"].clone()))
+    for i, (out, slot) in enumerate(got):
+        once(i, out)
+        slot.copy_(o2["slot"])
+    for i, (out, slot) in enumerate(got):
+        assert torch.equal(out, want[i % 2][0]) and torch.equal(slot, want[i % 2][1]), f"pass {i}"
+    assert E.ee_read_errors(ws) == 0
