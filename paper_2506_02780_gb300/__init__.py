@@ -447,7 +447,7 @@ def ee_prompt_slots(ctx_len, new_len, held, block_table, free_pages, free_cnt, n
                                _tp(free_pages, i32, "free_pages"), free_pages.numel(), _tp(free_cnt, i32, "free_cnt"),
                                num_pages, _tp(tok_off, i32, "tok_off"), _tp(pos, i32, "pos"), _tp(slot, i32, "slot"),
                                _tp(ctx_out, i32, "ctx_out"), _tp(held_out, i32, "held_out"),
-                               _tp(free_out, i32, "free_out"), ws.data_ptr(), ws.numel(), _stream(stream))
+                               _tp(free_out, i32, "free_out"), _p(ws), ws.numel(), _stream(stream))
     if st:
         raise EEError("ee_prompt_slots", st)
 
@@ -474,7 +474,7 @@ def ee_rope_append(q, k, v, rope, pos, slot, q_out, k_cache, v_cache, ws, k_out=
     st = lib().ee_rope_append(qp, qs, kp, ks, vp, vs, _tp(rope, torch.float32, "rope"), rope.shape[0],
                               _tp(pos, torch.int32, "pos"), _tp(slot, torch.int32, "slot"), total, n_q, n_kv, d, op,
                               os_, rp, rs, _tp(k_cache, bf16, "k_cache"), _tp(v_cache, bf16, "v_cache"), cache[0],
-                              ws.data_ptr(), ws.numel(), _stream(stream))
+                              _p(ws), ws.numel(), _stream(stream))
     if st:
         raise EEError("ee_rope_append", st)
 
@@ -503,7 +503,7 @@ def ee_prompt_attn(q, k, v, tok_off, scale, out, ws, lse=None, stream=None):
     kp, ks = _rows(k, "k")
     vp, vs = _rows(v, "v")
     st = lib().ee_prompt_attn(qp, qs, kp, ks, vp, vs, off, tok_off.numel() - 1, total, n_q, kv[1], d, scale, op, lp,
-                              ws.data_ptr(), ws.numel(), _stream(stream))
+                              _p(ws), ws.numel(), _stream(stream))
     if st:
         raise EEError("ee_prompt_attn", st)
 
@@ -524,7 +524,7 @@ def ee_chunk_attn(q, k_cache, v_cache, block_table, ctx_len, tok_off, scale, out
     lp = None if lse is None else _tp(lse, torch.float32, "lse")
     qp, qs = _rows(q, "q")
     st = lib().ee_chunk_attn(qp, qs, _tp(k_cache, bf16, "k_cache"), _tp(v_cache, bf16, "v_cache"), cache[0],
-                             table, max_pages, ctx, off, B, total, n_q, cache[1], d, scale, op, lp, ws.data_ptr(),
+                             table, max_pages, ctx, off, B, total, n_q, cache[1], d, scale, op, lp, _p(ws),
                              ws.numel(), _stream(stream))
     if st:
         raise EEError("ee_chunk_attn", st)

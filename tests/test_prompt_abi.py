@@ -2,6 +2,7 @@
 on pointers that are never dereferenced, and the binding on wrong tensors."""
 import ctypes
 import os
+import types
 
 import pytest
 import torch
@@ -142,3 +143,58 @@ def test_binding_refuses_wrong_tensors():
         E.ee_rope_append(q, kv, kv, torch.zeros(5, 64), off, off, out, cache, cache, ws)
     with pytest.raises(ValueError, match="entries"):
         E.ee_prompt_slots(off, off, off, table, off, off[:1], 3, 0, off, off, off, off, off, off[:1], ws)
+
+
+class OnDevice(torch.Tensor):
+    """A host tensor that says it is a CUDA tensor: the binding's checks, without a GPU."""
+    is_cuda = property(lambda self: True)
+
+
+NULL = types.SimpleNamespace(cuda_stream=0)
+
+
+def calls(E, ws, kind):
+    """Each prompt-intake call with a workspace of this kind; `kind` makes its other tensors."""
+    def t(*shape, dtype=torch.bfloat16):
+        return kind(torch.zeros(shape, dtype=dtype))
+
+    def i(*shape):
+        return t(*shape, dtype=torch.int32)
+    q, kv, cache = t(4, 8, 128), t(4, 2, 128), t(3, 2, 16, 128)
+    return {
+        "slots": lambda: E.ee_prompt_slots(i(1), i(1), i(1), i(1, 3), i(3), i(1), 3, 0, i(2), i(4), i(4), i(1), i(1),
+                                           i(1), ws, stream=NULL),
+        "rope": lambda: E.ee_rope_append(q, kv, kv, t(5, 128, dtype=torch.float32), i(4), i(4), t(4, 8, 128), cache,
+                                         cache, ws, stream=NULL),
+        "prompt": lambda: E.ee_prompt_attn(q, kv, kv, i(2), 0.1, t(4, 8, 128), ws, stream=NULL),
+        "chunk": lambda: E.ee_chunk_attn(q, cache, cache, i(1, 3), i(1), i(2), 0.1, t(4, 8, 128), ws, stream=NULL),
+    }
+
+
+class Library:
+    """Stands for libee: notes the calls that reach it."""
+    def __init__(self):
+        self.reached = []
+
+    def __getattr__(self, name):
+        return lambda *a: self.reached.append(name) or 0
+
+
+@pytest.mark.parametrize("call", ["slots", "rope", "prompt", "chunk"])
+@pytest.mark.parametrize("ws,error", [("host", ValueError), ("strided", ValueError), ("good", None)])
+def test_binding_looks_at_the_workspace(monkeypatch, call, ws, error):
+    """A workspace in host memory or with gaps never reaches the library."""
+    import paper_2506_02780_gb300 as E
+    on = lambda x: x.as_subclass(OnDevice)  # noqa: E731
+    u8 = torch.zeros(2048, dtype=torch.uint8)
+    w = {"host": u8, "strided": on(u8[::2]), "good": on(u8)}[ws]
+    L = Library()
+    monkeypatch.setattr(E, "lib", lambda: L)
+    go = calls(E, w, on)[call]
+    if error is None:
+        go()
+        assert len(L.reached) == 1
+    else:
+        with pytest.raises(error, match="libee takes"):
+            go()
+        assert not L.reached
