@@ -641,7 +641,7 @@ ee_status ee_rope_append(const ee_bf16* q, int64_t q_stride, const ee_bf16* k, i
  * statistics and sums are fp32; probabilities are rounded to bf16 for the
  * product with V (as their sum is not, the error of an output is about the
  * output's own rounding).  head_dim must be 128, n_q a multiple of n_kv with at
- * most 128 query heads per KV head; arrays 16-byte aligned.
+ * most 128 query heads per KV head, total at most 2^30; arrays 16-byte aligned.
  * Device errors: EE_DEVERR_TREE (a bad tok_off: that sequence is skipped),
  * EE_DEVERR_TIMEOUT (outputs undefined).
  */
@@ -658,7 +658,8 @@ ee_status ee_prompt_attn(const ee_bf16* q, int64_t q_stride, const ee_bf16* k, i
  * prompt (ctx_len 0), mixed in one call; unlike ee_chain_verify_attn there is no
  * limit on the chunk and the output is bf16.
  *   ctx_len int32 [B]: positions BEFORE the chunk; block_table int32
- *   [B][max_pages] with a page for each of a sequence's ctx_len + T positions
+ *   [B][max_pages] with a page for each of a sequence's ctx_len + T positions;
+ *   max_pages at most 2^27 - 256, num_pages * n_kv * EE_PAGE below 2^31
  * Other arguments, precision and errors as ee_prompt_attn.  A missing page sets
  * EE_DEVERR_PAGE and its keys are skipped; a query whose every key is skipped
  * gets out 0 and lse -inf.  EE_DEVERR_CTX: a negative ctx_len or more positions

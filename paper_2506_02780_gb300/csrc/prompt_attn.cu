@@ -1293,7 +1293,7 @@ ee_status check(const ee_bf16* q, int64_t q_stride, const ee_bf16* k, const ee_b
                 int32_t B, int32_t total, int32_t n_q, int32_t n_kv, int32_t head_dim, float scale, const ee_bf16* out,
                 const float* lse, const void* ws, size_t ws_bytes) {
   if (B < 0 || total < 0 || n_q < 1 || n_kv < 1) return EE_ERR_INVALID_ARG;
-  if (head_dim != EE_HEAD_DIM || n_q % n_kv != 0 || n_q / n_kv > kRows) return EE_ERR_UNSUPPORTED;
+  if (head_dim != EE_HEAD_DIM || n_q % n_kv != 0 || n_q / n_kv > kRows || total > (1 << 30)) return EE_ERR_UNSUPPORTED;
   if (!(scale > 0.f) || !std::isfinite(scale)) return EE_ERR_INVALID_ARG;
   if (B == 0 || total == 0) return EE_OK;
   if (!q || !k || !v || !tok_off || !out || !ws) return EE_ERR_INVALID_ARG;
@@ -1407,7 +1407,9 @@ extern "C" ee_status ee_chunk_attn(const ee_bf16* q, int64_t q_stride, const ee_
                              lse_or_null, ws, ws_bytes);
   if (st != EE_OK || B == 0 || total == 0) return st;
   if (!block_table || !ctx_len) return EE_ERR_INVALID_ARG;
-  if ((int64_t)num_pages * n_kv * EE_PAGE >= ((int64_t)1 << 31) || max_pages >= (1 << 27)) return EE_ERR_UNSUPPORTED;
+  // (positions are int32, and what is formed of them runs ahead by a few tiles)
+  if ((int64_t)num_pages * n_kv * EE_PAGE >= ((int64_t)1 << 31) || max_pages > (1 << 27) - 256)
+    return EE_ERR_UNSUPPORTED;
   int dev = 0, ctas = 0;
   ee_status ds = current_device(&dev);
   if (ds == EE_OK) ds = resident_ctas(dev, &ctas);

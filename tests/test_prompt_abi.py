@@ -198,3 +198,15 @@ def test_binding_looks_at_the_workspace(monkeypatch, call, ws, error):
         with pytest.raises(error, match="libee takes"):
             go()
         assert not L.reached
+
+
+@pytest.mark.parametrize("max_pages,total", [((1 << 27) - 1, 9), ((1 << 27) - 255, 9), (4, (1 << 30) + 1)])
+def test_chunk_positions_past_int32_are_refused(L, max_pages, total):
+    """Positions are int32, and the kernel's tile arithmetic rounds them up: a table that
+    reaches to within 4096 of 2^31 is refused, and so are more tokens than memory holds."""
+    over = dict(max_pages=max_pages, total=total)
+    assert L.ee_chunk_attn(*with_(CHUNK, CHUNK_NAMES, **over)) == UNSUPPORTED
+
+
+def test_prompt_positions_past_int32_are_refused(L):
+    assert L.ee_prompt_attn(*with_(PROMPT, PROMPT_NAMES, total=2 ** 31 - 1)) == UNSUPPORTED
