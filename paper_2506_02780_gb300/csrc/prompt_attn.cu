@@ -47,7 +47,7 @@
 //   3      cleans V where the causal edge or the sequence's end lies in a tile: the
 //          MMA multiplies masked rows by P = 0, and 0 times a NaN is a NaN.  Non-finite
 //          values of rows that some query must not see are zeroed, and added at the end
-//          for the queries that do;
+//          (of a split unit: when its pieces are joined) for the queries that do;
 //   4-7    softmax and output of row tile A, one row per thread; 8-11 of row tile B.
 //          (Output by four warps of its own: 214 us instead of 190 for the 16 prompts.)
 // TMEM: S/P of A and B, O of A and B, 128 columns each.
@@ -250,27 +250,38 @@ __device__ __forceinline__ const __nv_bfloat16* v_row(const PromptParams& p, con
   }
 }
 
-// Adds the non-finite values of keys [key0, key1] to one row that sees them: to its
-// output `out`, or (out NULL) to its unnormalised O in the partial slot `part` (column
-// chunks of four, kRows apart).
+// Non-finite values of V that warp 3 took out of the unit's tiles (keys past the first
+// query's): a row that sees some gets them added once, unweighted, on its way out, whoever
+// joins its pieces.  Partials do not hold them; a piece that met one says so by the sign of
+// its l.
+//
+// To one row's output in memory.
 template <bool kPaged>
-__device__ __forceinline__ void add_nonfinite(const PromptParams& p, Seg s, int key0, int key1,
-                                           __nv_bfloat16* out, float* part) {
+__device__ __forceinline__ void add_nonfinite(const PromptParams& p, const Seg& s, int pos, __nv_bfloat16* out) {
 #pragma unroll 1
-  for (int key = key0; key <= key1; ++key) {
+  for (int key = s.ctx + s.tok0 + 1; key <= pos; ++key) {
     const __nv_bfloat16* v = v_row<kPaged>(p, s, key);
     if (!v) continue;
 #pragma unroll 1
     for (int e = 0; e < kD; ++e) {
       const float x = __bfloat162float(v[e]);
       if (isfinite(x)) continue;
-      if (out) {
-        volatile uint16_t* o = reinterpret_cast<volatile uint16_t*>(out) + e;
-        *o = __bfloat16_as_ushort(__float2bfloat16_rn(__bfloat162float(__ushort_as_bfloat16(*o)) + x));
-      } else {
-        volatile float* o = part + (size_t)(e >> 2) * (4 * kRows) + (e & 3);
-        *o = *o + x;
-      }
+      volatile uint16_t* o = reinterpret_cast<volatile uint16_t*>(out) + e;
+      *o = __bfloat16_as_ushort(__float2bfloat16_rn(__bfloat162float(__ushort_as_bfloat16(*o)) + x));
+    }
+  }
+}
+// To eight of one row's columns in registers.
+template <bool kPaged>
+__device__ __forceinline__ void add_nonfinite8(const PromptParams& p, const Seg& s, int pos, int col, float (&y)[8]) {
+#pragma unroll 1
+  for (int key = s.ctx + s.tok0 + 1; key <= pos; ++key) {
+    const __nv_bfloat16* v = v_row<kPaged>(p, s, key);
+    if (!v) continue;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float x = __bfloat162float(v[col + e]);
+      if (!isfinite(x)) y[e] += x;
     }
   }
 }
@@ -280,6 +291,15 @@ __device__ __forceinline__ uint32_t nonfinite2(uint32_t x) {   // 0xffff in each
   const uint32_t hi = (x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
   return lo | hi;
 }
+
+// A partial's (m, l): m is NaN where the piece has no tile of the row tile, and no O then
+// (a row's own maximum is never NaN); l's sign says that values were taken out of V.
+__device__ __forceinline__ float2 pack_ml(bool any, bool bad, float m, float l) {
+  const uint32_t sign = bad ? 0x80000000u : 0u;
+  return make_float2(any ? m : NAN, __uint_as_float((__float_as_uint(l) & 0x7fffffffu) | sign));
+}
+__device__ __forceinline__ bool no_tiles(float m) { return m != m; }
+__device__ __forceinline__ bool took_out(float l) { return (int32_t)__float_as_uint(l) < 0; }
 
 // (m, l, o) of one piece or lane joined to a running one
 struct Joined {
@@ -299,6 +319,7 @@ struct Joined {
 // slot (column-chunk major) are contiguous.  A thread loads from two pieces at a time (a
 // round trip to L2 costs about 1,000 cycles).  With few items and many pieces 2^sub lanes
 // share an item, each over every 2^sub-th piece.
+template <bool kPaged>
 __device__ __forceinline__ void merge_items(const PromptParams& p, const Seg& s, int lo, int hi, int t, int nthr) {
   const int K = s.c1 - s.c0 + 1;
   // (the sum's order depends on it: where any piece's CTA may be the one that joins, it must
@@ -316,6 +337,7 @@ __device__ __forceinline__ void merge_items(const PromptParams& p, const Seg& s,
     const int i = min(i0, hi - 1), cg = i / rows, r = i - cg * rows;
     const int st = r >= rows_a, rr = st ? r - rows_a : r;
     Joined x;
+    bool bad = false;
 #pragma unroll 1
     for (int k = k0; k < K; k += 2 << sub) {
       float2 ml[2];
@@ -331,10 +353,10 @@ __device__ __forceinline__ void merge_items(const PromptParams& p, const Seg& s,
       }
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        // a row without keys in the piece has l = 0 and no O (a sum that is NaN has one)
-        if (k + (q << sub) >= K || ml[q].y == 0.f) continue;
+        if (k + (q << sub) >= K || no_tiles(ml[q].x)) continue;
         const float o[8] = {u[q].x, u[q].y, u[q].z, u[q].w, v[q].x, v[q].y, v[q].z, v[q].w};
-        x.add(ml[q].x, ml[q].y, o);
+        x.add(ml[q].x, fabsf(ml[q].y), o);
+        bad |= took_out(ml[q].y);
       }
     }
 #pragma unroll 1
@@ -344,16 +366,21 @@ __device__ __forceinline__ void merge_items(const PromptParams& p, const Seg& s,
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = __shfl_xor_sync(0xffffffffu, x.a[e], d);
       x.add(Mo, Lo, o);
+      bad |= __shfl_xor_sync(0xffffffffu, (int)bad, d) != 0;
     }
     if (k0 != 0 || i0 >= hi) continue;
     const float il = x.L == 0.f ? 0.f : 1.f / x.L;
     const int tok = rr / p.g, h = rr - tok * p.g;
     const size_t row = (size_t)(s.o + s.tok0 + (st ? p.tpt : 0) + tok) * p.n_q + s.hk * p.g + h;
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = x.a[e] * il;
+    if (bad) add_nonfinite8<kPaged>(p, s, s.ctx + s.tok0 + (st ? p.tpt : 0) + tok, 8 * cg, y);
     uint4 o;
-    o.x = bf16x2_rn(x.a[1] * il, x.a[0] * il);
-    o.y = bf16x2_rn(x.a[3] * il, x.a[2] * il);
-    o.z = bf16x2_rn(x.a[5] * il, x.a[4] * il);
-    o.w = bf16x2_rn(x.a[7] * il, x.a[6] * il);
+    o.x = bf16x2_rn(y[1], y[0]);
+    o.y = bf16x2_rn(y[3], y[2]);
+    o.z = bf16x2_rn(y[5], y[4]);
+    o.w = bf16x2_rn(y[7], y[6]);
     *reinterpret_cast<uint4*>(p.out + row * kD + 8 * cg) = o;
     if (cg == 0 && p.lse) p.lse[row] = x.L == 0.f ? -INFINITY : (x.M + log2f(x.L)) * 0.6931471805599453f;
   }
@@ -1081,8 +1108,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       const size_t row0 = (size_t)(s.o + s.tok0 + st * p.tpt) * p.n_q + s.hk * p.g;
       const uint32_t orow = vrow ? (uint32_t)tok_r * p.n_q + head : UINT32_MAX;
       float M = m == -INFINITY ? m : m * sl2;             // of base-2 exponents
-      const bool bad = any && s_bad[i % kSegs];           // values taken out of V: for the rows that see them
-      const int key0 = max(s.ctx + s.tok0 + 1, s.j0 * kKT), key1 = min(pos, s.j1 * kKT - 1);
+      bool bad = any && s_bad[i % kSegs];                 // values taken out of V: for the rows that see them
       bool fin = whole;
       if (!whole) {
         // Few pieces: a warp that finds its rows' other partials in place joins them to its own
@@ -1114,9 +1140,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                          make_float4(__uint_as_float(ov[4 * e]), __uint_as_float(ov[4 * e + 1]),
                                      __uint_as_float(ov[4 * e + 2]), __uint_as_float(ov[4 * e + 3])));
             }
-            if (bad && vrow) add_nonfinite<kPaged>(p, s, key0, key1, nullptr, reinterpret_cast<float*>(part) + 4 * r);
           }
-          if (vrow) __stcg(reinterpret_cast<float2*>(part + kAttnMlOff) + r, make_float2(M, l));
+          if (vrow) __stcg(reinterpret_cast<float2*>(part + kAttnMlOff) + r, pack_ml(any, bad, M, l));
           __syncwarp();
           if (direct) {
             const uint32_t before = lane == 0 ? atom_inc_acq_rel(cnt, (uint32_t)(K - 1)) : 0u;
@@ -1128,20 +1153,21 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         __syncwarp();            // lane 0 acquired the count: a shuffle hands its value on, not its order
         if (fin && warp_rows) {
           float2 ml[kDirect];
-          const float m_own = M;
+          const float2 ml_own = pack_ml(any, bad, M, l);
 #pragma unroll
           for (int k = 0; k < kDirect; ++k) {
-            ml[k] = k == own ? make_float2(m_own, l) : make_float2(-INFINITY, 0.f);
+            ml[k] = k == own ? ml_own : make_float2(NAN, 0.f);
             if (k < K && k != own && vrow) ml[k] = __ldcg(reinterpret_cast<const float2*>(slot(k) + kAttnMlOff) + r);
             M = fmaxf(M, ml[k].x);
+            bad |= took_out(ml[k].y);
           }
-          float f[kDirect];
+          float f[kDirect];      // NaN: no O (the weight of one that has an O may well be 0)
           l = 0.f;
           static_assert(kDirect == 3, "f by number");
 #pragma unroll
-          for (int k = 0; k < kDirect; ++k) {   // (a row without keys in the piece has l = 0 and no O)
-            f[k] = ml[k].y == 0.f ? 0.f : ml[k].x == M ? 1.f : ex2(ml[k].x - M);
-            l = fmaf(ml[k].y, f[k], l);
+          for (int k = 0; k < kDirect; ++k) {
+            f[k] = ml[k].x == M ? 1.f : ex2(ml[k].x - M);
+            if (!no_tiles(ml[k].x)) l = fmaf(fabsf(ml[k].y), f[k], l);
           }
           // 64 columns of a piece in flight at a time (a round trip to L2 costs about 1,000 cycles)
 #pragma unroll 1
@@ -1168,7 +1194,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                   x[3] = y.w;
                 }
               }
-              if (fk != 0.f) {     // (without keys there is no O)
+              if (fk == fk) {
 #pragma unroll
                 for (int e = 0; e < 64; ++e)
                   acc[e] = fmaf(__uint_as_float(e < 32 ? xa[e] : xb[e - 32]), fk, acc[e]);
@@ -1225,7 +1251,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           __syncwarp();
         }
         if (vrow && p.lse) p.lse[row0 + orow] = l == 0.f ? -INFINITY : (M + log2f(l)) * 0.6931471805599453f;
-        if (bad && vrow) add_nonfinite<kPaged>(p, s, key0, key1, p.out + (row0 + orow) * kD, nullptr);
+        if (bad && vrow) add_nonfinite<kPaged>(p, s, pos, p.out + (row0 + orow) * kD);
       }
       tc_fence_before();
       __syncwarp();
@@ -1265,7 +1291,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     hi = items;
   }
   asm volatile("bar.sync %0, %1;" ::"r"(2 + pi), "r"(nthr) : "memory");
-  if (s_ready[pi]) merge_items(p, s, lo, hi, t, nthr);
+  if (s_ready[pi]) merge_items<kPaged>(p, s, lo, hi, t, nthr);
 }
 
 bool good_stride(int64_t stride, int heads) { return stride % 8 == 0 && stride >= (int64_t)heads * kD; }

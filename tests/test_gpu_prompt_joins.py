@@ -186,3 +186,94 @@ def test_cooperative_launch_in_a_graph(E, ws):
     torch.cuda.synchronize()
     assert all(torch.equal(x[7], w) for x, w in zip(bufs, want))
     assert E.ee_read_errors(ws) == 0
+
+
+# split units of several rows: joined by all, by the last of a few, of many
+EDGE = [((28, 4), [70], [8000]), ((28, 4), [40] * 16, [200 * i for i in range(16)]),
+        ((8, 2), [260, 1, 33], [6000, 9000, 100]), ((7, 1), [90], [1800])]
+
+
+def gapped(heads, lens, ctxs, high):
+    """Inputs whose scores differ by 360 between a sequence's context and its new tokens:
+    `high` says which of the two carries the row's weight."""
+    q, kc, vc, table = inputs(heads, lens, ctxs, 0)
+    q[:] = 4.0
+    for s, (n, c) in enumerate(zip(lens, ctxs)):
+        for p in range(c + n):
+            kc[table[s, p // 16], :, p % 16] = 4.0 if (p < c) == (high == "context") else -4.0
+    return q, kc, vc, table
+
+
+@pytest.mark.parametrize("heads,lens,ctxs", EDGE)
+@pytest.mark.parametrize("high", ["context", "new"])
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+def test_a_seen_value_shows_whatever_its_weight(E, ws, heads, lens, ctxs, high, bad):
+    """A non-finite value among the new tokens of a sequence whose unit is split: the queries
+    from it on show it, also where its weight is below 2^-500 beside another piece's, and
+    whichever piece joins; the others do not.  As it is in the value's own unit (it is kept
+    from the product with V there, and added); in a later unit, all of whose queries see it,
+    it meets its weight, and 0 times an infinity is a NaN."""
+    q, kc, vc, table = gapped(heads, lens, ctxs, high)
+    s = len(lens) - 1 if len(lens) > 3 else 0
+    at, g = min(30, lens[s] // 2), heads[0] // heads[1]
+    clean, zc = run(E, ws, q, kc, vc, table, lens, ctxs)
+    p = ctxs[s] + at
+    vc[table[s, p // 16], 0, p % 16, 77] = bad
+    row0 = sum(lens[:s])
+    hit = torch.zeros_like(clean, dtype=torch.bool)
+    hit[row0 + at:row0 + lens[s], :g, 77] = True
+    unit = 2 * (128 // g)              # tokens of two row tiles of g heads each
+    for i in range(40):
+        out, z = run(E, ws, q, kc, vc, table, lens, ctxs)
+        assert torch.equal(z, zc) and torch.equal(out[~hit], clean[~hit])
+        if i == 0:
+            first = out
+        assert torch.equal(out.view(torch.int16), first.view(torch.int16))
+        assert not torch.isfinite(out[hit]).any()
+        own = out[row0 + at:row0 + min(unit, lens[s]), :g, 77]
+        assert torch.isnan(own).all() if math.isnan(bad) else (own == bad).all()
+    assert E.ee_read_errors(ws) == 0
+
+
+@pytest.mark.parametrize("heads,lens,ctxs", EDGE)
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_a_value_of_the_context_shows_whatever_its_weight(E, ws, heads, lens, ctxs, bad):
+    """The same of a value that every query sees: nowhere finite (0 times it is NaN)."""
+    q, kc, vc, table = gapped(heads, lens, ctxs, "new")
+    s = len(lens) - 1 if len(lens) > 3 else 0
+    g = heads[0] // heads[1]
+    clean, zc = run(E, ws, q, kc, vc, table, lens, ctxs)
+    vc[table[s, 0], 0, 3, 5] = bad
+    rows = slice(sum(lens[:s]), sum(lens[:s + 1]))
+    first = None
+    for _ in range(40):
+        out, z = run(E, ws, q, kc, vc, table, lens, ctxs)
+        first = out.clone() if first is None else first
+        assert torch.equal(z, zc) and not torch.isfinite(out[rows, :g, 5]).any()
+        assert torch.equal(out.view(torch.int16), first.view(torch.int16))
+        out[rows, :g, 5] = clean[rows, :g, 5]
+        assert torch.equal(out, clean)
+
+
+def test_a_seen_value_shows_in_a_split_prompt(E, ws):
+    """The same over packed K/V: one prompt whose last rows hold all the weight."""
+    n_q, n_kv, n = 7, 1, 1700
+    q, k, v = P.packed_qkv(torch.Generator("cuda").manual_seed(3), n, n_q, n_kv, fused=False)
+    q[:] = 4.0
+    k[:] = torch.where(torch.arange(n, device="cuda") % 640 < 320, -4.0, 4.0).to(torch.bfloat16)[:, None, None]
+    off = P.i32([0, n])
+    got = {}
+    for at in (None, 1, 200, 1601):
+        x = v.clone()
+        if at is not None:
+            x[at, 0, 8] = float("inf")
+        for i in range(20):
+            out = torch.empty_like(q)
+            E.ee_prompt_attn(q, k, x, off, SCALE, out, ws)
+            if i == 0:
+                got[at] = out
+            assert torch.equal(out.view(torch.int16), got[at].view(torch.int16))
+        if at is not None:
+            assert not torch.isfinite(out[at:, :, 8]).any()
+            out[at:, :, 8] = got[None][at:, :, 8]
+            assert torch.equal(out, got[None])
