@@ -592,7 +592,8 @@ size_t ee_prompt_workspace_size(void);
  * Device errors: EE_DEVERR_CTX for a negative length or page count, a context
  * that its pages do not hold or a sequence that max_pages do not hold (it gets
  * no tokens and no pages), and for a sum of new_len other than `total` (tokens
- * past `total` are dropped, surplus entries get pos and slot -1).
+ * past `total` are dropped and not counted in ctx_out, surplus entries get pos
+ * and slot -1).
  * EE_DEVERR_PAGE when the free list is too short: then no sequence gets pages,
  * every slot is -1, and ctx_out, held_out and free_out repeat the inputs; and
  * for a free page outside [0, num_pages), whose tokens get slot -1.

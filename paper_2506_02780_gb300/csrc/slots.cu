@@ -123,7 +123,8 @@ __global__ void __launch_bounds__(kThreads) prompt_slots_kernel(const SlotParams
     s_give[s] = enough ? (int)go : 0;
     if (blockIdx.x == 0) {
       p.tok_off[s] = s_tok[s];
-      p.ctx_out[s] = s_ctx[s] + (enough ? t : 0);
+      const int placed = (int)min(to + t, (int64_t)p.total) - s_tok[s];   // tokens past `total` are dropped
+      p.ctx_out[s] = s_ctx[s] + (enough ? placed : 0);
       p.held_out[s] = s_held[s] + (enough ? give : 0);
     }
     to += t;

@@ -327,3 +327,22 @@ def test_tables_and_lengths_are_read_as_just_written(E, ws):
     for i, (out, slot) in enumerate(got):
         assert torch.equal(out, want[i % 2][0]) and torch.equal(slot, want[i % 2][1]), f"pass {i}"
     assert E.ee_read_errors(ws) == 0
+
+
+@pytest.mark.parametrize("total", [0, 1, 10, 30, 33, 35, 50])
+def test_lengths_count_the_tokens_that_got_a_slot(E, ws, total):
+    """More new tokens than were packed: those past `total` are dropped, and the lengths do
+    not claim them (positions that nobody would ever write).  Pages go by the lengths asked for."""
+    ctx, new, held = [0, 4, 7], [30, 5, 0], [0, 1, 1]
+    table = np.full((3, 4), -1)
+    table[1, 0], table[2, 0] = 3, 4
+    free = np.array([0, 1, 2])
+    got, t, bits = call(E, ws, ctx, new, held, table, free, 3, 5, 0, total=total)
+    off, _, _, tr, _, ho, left = loop(ctx, new, held, table, free, 3, 0)
+    assert bits == (0 if total == 35 else CTX)
+    placed = np.diff(np.minimum(off, total))
+    np.testing.assert_array_equal(got["tok_off"], np.minimum(off, total))
+    np.testing.assert_array_equal(got["ctx_out"], ctx + placed)
+    np.testing.assert_array_equal(got["held_out"], ho)
+    np.testing.assert_array_equal(t, tr)
+    assert got["free_out"][0] == left and (got["slot"] >= 0).sum() == placed.sum()
