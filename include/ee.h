@@ -576,7 +576,8 @@ size_t ee_prompt_workspace_size(void);
  * (block_table[s][0 .. held[s]) ) with ctx_len[s] tokens in them and receives
  * new_len[s] >= 0 more.  It needs ceil((ctx + new + reserve) / EE_PAGE) pages
  * (none when ctx + new == 0): `reserve` positions past the new tokens, e.g.
- * for the draft trees of the steps that follow.  Pages it lacks come from the
+ * for the draft trees of the steps that follow, as far as the table has columns
+ * (the step that lacks a page there says so).  Pages it lacks come from the
  * end of the free list: with n counting all pages given in this call, sequence
  * by sequence and in position order, the n-th is free_pages[*free_cnt - 1 - n].
  *   ctx_len, new_len, held int32 [B]; block_table int32 [B][max_pages] in/out:
@@ -590,8 +591,8 @@ size_t ee_prompt_workspace_size(void);
  *     held and free pages afterwards; they must not alias their inputs, which
  *     stay as they are (a call may be repeated)
  * Device errors: EE_DEVERR_CTX for a negative length or page count, a context
- * that its pages do not hold or a sequence that max_pages do not hold (it gets
- * no tokens and no pages), and for a sum of new_len other than `total` (tokens
+ * that its pages do not hold or tokens that max_pages do not hold (the sequence
+ * gets no tokens and no pages), and for a sum of new_len other than `total` (tokens
  * past `total` are dropped and not counted in ctx_out, surplus entries get pos
  * and slot -1).
  * EE_DEVERR_PAGE when the free list is too short: then no sequence gets pages,

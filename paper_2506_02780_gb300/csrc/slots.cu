@@ -2,14 +2,14 @@
 // that live on the device.
 //
 // One launch.  With t_s new tokens and n_s = ceil((ctx + t + reserve) / 16) -
-// held_s pages to give, everything follows from the exclusive sums of t and n
-// over the sequences: token i's sequence is found in the first by bisection, and
-// the k-th given page is the k-th from the end of the free list.  Every CTA forms
-// both sums over all (at most 4096) sequences by itself, in shared memory: a
-// second launch or a grid-wide barrier for one scan would cost more than the
-// repeated reads, which come from L2.  Then the CTAs share the tokens and the new
-// table entries; a token on a page given in this call takes it from the free list
-// directly, so no CTA reads what another writes.
+// held_s pages to give (as far as the table has columns), everything follows from
+// the exclusive sums of t and n over the sequences: token i's sequence is found in
+// the first by bisection, and the k-th given page is the k-th from the end of the
+// free list.  Every CTA forms both sums over all (at most 4096) sequences by
+// itself, in shared memory: a second launch or a grid-wide barrier for one scan
+// would cost more than the repeated reads, which come from L2.  Then the CTAs share
+// the tokens and the new table entries; a token on a page given in this call takes
+// it from the free list directly, so no CTA reads what another writes.
 //
 // Bound by latency: the reads of the lengths, the scan, the bisections in shared memory
 // and the reads of the pages follow one another.  A thread takes four neighbouring tokens,
@@ -43,8 +43,8 @@ __device__ __forceinline__ bool seq_share(const SlotParams& p, int s, int& ctx, 
   t = ee::ld_pinned(p.new_len + s);
   give = 0;
   const int64_t cap = (int64_t)p.max_pages * EE_PAGE;
-  const int64_t end = (int64_t)ctx + t, want = end + p.reserve;
-  if (ctx < 0 || t < 0 || held < 0 || held > p.max_pages || ctx > (int64_t)held * EE_PAGE || want > cap) {
+  const int64_t end = (int64_t)ctx + t, want = min(end + p.reserve, cap);   // the reserve ends with the table
+  if (ctx < 0 || t < 0 || held < 0 || held > p.max_pages || ctx > (int64_t)held * EE_PAGE || end > cap) {
     t = 0;
     return false;
   }

@@ -346,3 +346,36 @@ def test_lengths_count_the_tokens_that_got_a_slot(E, ws, total):
     np.testing.assert_array_equal(got["held_out"], ho)
     np.testing.assert_array_equal(t, tr)
     assert got["free_out"][0] == left and (got["slot"] >= 0).sum() == placed.sum()
+
+
+@pytest.mark.parametrize("reserve", [0, 1, 20, 64, 65, 5000, 1 << 30])
+def test_reserve_ends_where_the_table_ends(E, ws, reserve):
+    """Room for what may follow is given as far as the table's columns go: it refuses no
+    tokens that fit, nor a sequence without new ones, and an empty sequence gets none."""
+    cols = 4
+    ctx, new, held = [50, 60, 0, 33, 64, 0, 1], [10, 0, 0, 31, 0, 64, 1], [4, 4, 0, 3, 4, 0, 1]
+    table, at = np.full((7, cols), -1), 0
+    for s, h in enumerate(held):
+        table[s, :h] = np.arange(at, at + h)
+        at += h
+    free = np.arange(at, at + 30)
+    want = [max(-(-min(c + n + reserve, 16 * cols) // 16) - h, 0) if c + n else 0 for c, n, h in zip(ctx, new, held)]
+    tab, left = table.copy(), len(free)
+    for s, n in enumerate(want):
+        for j in range(n):
+            left -= 1
+            tab[s, held[s] + j] = free[left]
+    got, t, bits = call(E, ws, ctx, new, held, table, free, len(free), at + 30, reserve)
+    assert bits == 0
+    np.testing.assert_array_equal(t, tab)
+    np.testing.assert_array_equal(got["held_out"], np.add(held, want))
+    np.testing.assert_array_equal(got["ctx_out"], np.add(ctx, new))
+    pos = [c + i for c, n in zip(ctx, new) for i in range(n)]
+    slot = [tab[s, p // 16] * 16 + p % 16 for s, (c, n) in enumerate(zip(ctx, new)) for p in range(c, c + n)]
+    np.testing.assert_array_equal(got["pos"], pos)
+    np.testing.assert_array_equal(got["slot"], slot)
+    assert got["free_out"][0] == left
+    new[1] = 5                          # 65 positions do not fit, whatever the reserve
+    got, _, bits = call(E, ws, ctx, new, held, table, free, len(free), at + 30, reserve, total=sum(new) - 5)
+    assert bits == CTX and got["ctx_out"][1] == 60 and got["held_out"][1] == 4
+    np.testing.assert_array_equal(got["slot"], slot)
