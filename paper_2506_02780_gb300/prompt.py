@@ -12,8 +12,10 @@ the lengths of B sequences on the device, and issues, on one stream:
              -> ee_chunk_attn         parts of prompts and single tokens, over the cache
 
 Afterwards ``block_table``, ``ctx_len`` and the cache are what ``VerifyStep`` and
-``EditSession`` take.  The target model's projections, which produce q, k and v,
-are the caller's.  No arithmetic happens here; nothing is read back to the host.
+``EditSession`` take.  Those keep lengths of their own: ``commit`` hands back what
+their steps committed (``EditSession.ctx_len``, ``VerifyStep.ctx_out``) before the
+next ``admit``.  The target model's projections, which produce q, k and v, are the
+caller's.  No arithmetic happens here; nothing is read back to the host.
 """
 from __future__ import annotations
 
@@ -40,12 +42,15 @@ class PromptIntake:
     k_cache / v_cache [L, num_pages, n_kv, 16, 128] bf16; rope fp32 [n_pos, 128]
     (``rope_table``).  max_pages: columns of the block table; max_tokens: new tokens
     of one call at most.  ``reserve`` positions after each sequence's new tokens get
-    pages as well (a draft tree verified in place).  All pages are free at the start
-    (``free_pages`` names others).
+    pages as well, as far as the table goes: room for the draft trees and commits of
+    the steps until the next ``admit``, which gives it anew, also without new tokens.
+    A ``VerifyStep`` in place takes the table itself, rather than a widened copy that
+    later calls do not reach, when it has columns for max_ctx + max_T positions.  All
+    pages are free at the start (``free_pages`` names others).
 
-    ``admit`` and ``attend`` are capturable.  ``admit`` reads one of two sets of
-    lengths and writes the other, so a graph that is to be replayed holds an even
-    number of them."""
+    ``admit``, ``commit`` and ``attend`` are capturable.  ``admit`` reads one of two
+    sets of lengths and writes the other, so ``ctx_len`` is another tensor after each,
+    and a graph that is to be replayed holds an even number of them."""
 
     def __init__(self, *, B, n_q, k_cache, v_cache, rope, max_pages, max_tokens, reserve=0, scale=None,
                  free_pages=None):
@@ -104,6 +109,17 @@ class PromptIntake:
                         self.num_pages, self.reserve, self.tok_off, self.pos, self.slot, self._ctx[b], self._held[b],
                         self._free[b], self.ws, stream=stream)
         self.total, self._now = int(total), b
+
+    def commit(self, ctx_len, stream=None):
+        """The sequences' lengths after verification steps over the cache (device int32
+        [B]): where the next ``admit`` goes on.  Copied; call it after the last admitted
+        tokens' layers, which need the lengths before them."""
+        if ctx_len.dtype is not torch.int32:
+            raise TypeError(f"ctx_len must be {torch.int32}, got {ctx_len.dtype}")
+        if ctx_len.shape != (self.B,) or not ctx_len.is_cuda:
+            raise ValueError("ctx_len must be a CUDA tensor with an entry for each sequence")
+        with torch.cuda.stream(stream):
+            self.ctx_len.copy_(ctx_len)
 
     def attend(self, layer, q, k, v, whole=False, lse=None, stream=None):
         """Attention of the admitted tokens in one layer: q [total, n_q, 128], k and v
