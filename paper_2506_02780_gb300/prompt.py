@@ -14,8 +14,9 @@ the lengths of B sequences on the device, and issues, on one stream:
 Afterwards ``block_table``, ``ctx_len`` and the cache are what ``VerifyStep`` and
 ``EditSession`` take.  Those keep lengths of their own: ``commit`` hands back what
 their steps committed (``EditSession.ctx_len``, ``VerifyStep.ctx_out``) before the
-next ``admit``.  The target model's projections, which produce q, k and v, are the
-caller's.  No arithmetic happens here; nothing is read back to the host.
+next ``admit``.  ``release`` takes a finished sequence's pages back.  The target
+model's projections, which produce q, k and v, are the caller's.  No arithmetic on
+them happens here; nothing is read back to the host.
 """
 from __future__ import annotations
 
@@ -46,9 +47,9 @@ class PromptIntake:
     the steps until the next ``admit``, which gives it anew, also without new tokens.
     A ``VerifyStep`` in place takes the table itself, rather than a widened copy that
     later calls do not reach, when it has columns for max_ctx + max_T positions.  All
-    pages are free at the start (``free_pages`` names others).
+    pages are free at the start (``free_pages`` names others; ``release`` writes it).
 
-    ``admit``, ``commit`` and ``attend`` are capturable.  ``admit`` reads one of two
+    ``admit``, ``commit``, ``release`` and ``attend`` are capturable.  ``admit`` reads one of two
     sets of lengths and writes the other, so ``ctx_len`` is another tensor after each,
     and a graph that is to be replayed holds an even number of them."""
 
@@ -120,6 +121,27 @@ class PromptIntake:
             raise ValueError("ctx_len must be a CUDA tensor with an entry for each sequence")
         with torch.cuda.stream(stream):
             self.ctx_len.copy_(ctx_len)
+
+    def release(self, done, stream=None):
+        """Finished sequences (device bool [B]): their pages go to the end of the free list,
+        in the table's order, their rows of the table to -1 and their lengths to zero; the
+        next ``admit`` may give them a new prompt."""
+        if done.dtype is not torch.bool:
+            raise TypeError(f"done must be {torch.bool}, got {done.dtype}")
+        if done.shape != (self.B,) or not done.is_cuda:
+            raise ValueError("done must be a CUDA tensor with an entry for each sequence")
+        with torch.cuda.stream(stream):
+            n = self.free_pages.numel()
+            gone = (torch.arange(self.block_table.shape[1], device=done.device) < self.held[:, None]) & done[:, None]
+            at = self.free_cnt + gone.flatten().cumsum(0) - 1
+            # an entry past the list takes what is not given back (and pages that never came from it)
+            at = torch.where(gone.flatten(), at, n).clamp(0, n)
+            free = torch.cat((self.free_pages, self.free_pages.new_empty(1)))
+            self.free_pages.copy_(free.scatter_(0, at, self.block_table.flatten())[:n])
+            self.free_cnt.add_(gone.sum()).clamp_(max=n)
+            self.block_table.masked_fill_(done[:, None], -1)
+            self.held.masked_fill_(done, 0)
+            self.ctx_len.masked_fill_(done, 0)
 
     def attend(self, layer, q, k, v, whole=False, lse=None, stream=None):
         """Attention of the admitted tokens in one layer: q [total, n_q, 128], k and v

@@ -157,3 +157,71 @@ def test_committed_lengths_past_the_pages_are_reported(E):
     pi.admit(P.i32([1, 1]), 1)
     assert pi.errors() == 0x08
     assert pi.ctx_len.tolist() == [33, 21] and pi.held.tolist() == [2, 2]
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_released_pages_serve_other_sequences(E, seed):
+    """Sequences come, grow, end and are replaced: a released one has no pages or tokens, the
+    others keep theirs, and no page is lost or held twice (``take`` looks)."""
+    rs = torch.Generator().manual_seed(seed)
+    gen = torch.Generator("cuda").manual_seed(seed)
+    B = 6
+    pi = intake(B, reserve=5, num_pages=60, max_pages=10)
+    now = [0] * B
+    for i in range(12):
+        lens = [0 if n > 100 else int(torch.randint(0, 40, (1,), generator=rs)) for n in now]
+        now = take(pi, gen, lens, now)
+        done = torch.rand(B, generator=rs) < 0.3 if i % 3 else torch.zeros(B, dtype=torch.bool)
+        if i == 7:
+            done[:] = True
+        kept, table, free = rows(pi, now), pi.block_table.clone(), pi.free_pages[:pi.free_cnt.item()].clone()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        pi.release(done.cuda(), stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        back = [p for s in range(B) if done[s] and now[s] for p in table[s, :P.pages(now[s] + 5)].tolist()]
+        assert pi.free_pages[:pi.free_cnt.item()].tolist() == free.tolist() + back
+        for s in range(B):
+            if done[s]:
+                now[s] = 0
+                assert (pi.block_table[s] == -1).all()
+            else:
+                assert torch.equal(pi.block_table[s], table[s])
+        left = [[k if n else k[:0] for k, n in zip(r, now)] for r in kept]
+        assert same(rows(pi, now), left) and pi.ctx_len.tolist() == now
+    assert pi.errors() == 0
+
+
+def test_release_refuses_other_masks(E):
+    pi = intake(3, reserve=0)
+    for bad, error in ((torch.zeros(2, dtype=torch.bool, device="cuda"), ValueError), (P.i32([0, 1, 2]), TypeError),
+                       (torch.zeros(3, dtype=torch.bool), ValueError)):
+        with pytest.raises(error):
+            pi.release(bad)
+
+
+def test_release_in_a_graph(E):
+    """A pass that admits, releases and admits again, captured and replayed."""
+    pi = intake(4, reserve=0, num_pages=40, max_pages=8, max_tokens=64)
+    new, done = P.i32([20, 5, 0, 7]), torch.tensor([True, False, False, True], device="cuda")
+
+    def passes():
+        pi.admit(new, 32)
+        pi.release(done)
+        pi.admit(new, 32)
+        pi.release(done)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        passes()
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        passes()
+    for _ in range(3):
+        g.replay()
+    torch.cuda.synchronize()
+    assert pi.errors() == 0 and pi.ctx_len.tolist() == [0, 40, 0, 0] and pi.held.tolist() == [0, 3, 0, 0]
+    used = pi.block_table[1, :3].tolist() + pi.free_pages[:pi.free_cnt.item()].tolist()
+    assert sorted(used) == list(range(40))
