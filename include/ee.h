@@ -666,6 +666,11 @@ ee_status ee_prompt_attn(const ee_bf16* q, int64_t q_stride, const ee_bf16* k, i
  * EE_DEVERR_PAGE and its keys are skipped; a query whose every key is skipped
  * gets out 0 and lse -inf.  EE_DEVERR_CTX: a negative ctx_len or more positions
  * than max_pages hold (the sequence is skipped).
+ * Which of the two for new tokens in the cache: ee_chain_verify_attn (at most 2048
+ * a sequence, a host bound on the context, fp32 output, probabilities in two bf16
+ * words) is the faster one for up to some 64 tokens a sequence, this one for more
+ * (64 tokens after 8000: 15.8 and 24.8 us; 2048 after 30720: 1680 and 1205).  Their
+ * outputs round differently, so a greedy choice near a tie may differ between them.
  */
 ee_status ee_chunk_attn(const ee_bf16* q, int64_t q_stride, const ee_bf16* k_cache, const ee_bf16* v_cache,
                         int32_t num_pages, const int32_t* block_table, int32_t max_pages,

@@ -25,18 +25,20 @@
 // launched cooperatively, so that the wait ends).  Every length follows from the device's
 // offsets: long prompts, ragged batches and single tokens over long contexts are one case.
 //
-// Bound, and measured (one call, captured).  Long rows: the tensor core, as far as the
-// chain S -> P -> P V -> next S of the two row tiles keeps it busy: 128 keys of both take
-// 2,700 cycles, of which the MMAs need 2,048 (S and P of both and both O fill tensor
-// memory, so S of the next tile waits for P V of this one).  One prompt of 16384 tokens,
-// 28 heads over 4: 1158 us, 1,660 TFLOP/s; a chunk of 2048 after 30720, 56 heads over 8:
-// 1135 us, 1,640.  Ragged batches: also a segment's start and end, about 4,500 cycles that
-// no product covers (mostly code that is not in the instruction cache), and the CTAs'
-// imbalance (5%): 16 prompts of 33 to 4097 tokens 182 us, 1,260 TFLOP/s.  Single tokens:
-// the cache, 64 sequences of 1024 to 16384 keys 139 us, 5.7 TB/s, where loads of random
-// pages alone reach 6.2.  One token over 4096 keys: latency, 12.0 us (4,000 cycles until
-// the roles start, 5,000 until the first page is asked for, 7,000 for its tile, 6,000 to
-// meet and join); a prompt of 37 tokens, 8 heads over 2: 7.6 us.
+// Bound, and measured (captured / calls one after another, where the long ones run at the
+// power cap).  Long rows: the tensor core, as far as the chain S -> P -> P V -> next S of
+// the two row tiles keeps it busy: 128 keys of both take 2,700 cycles, of which the MMAs
+// need 2,048 (S and P of both and both O fill tensor memory, so S of the next tile waits
+// for P V of this one).  One prompt of 16384 tokens, 28 heads over 4: 1,156 / 1,250 us
+// (1,660 / 1,540 TFLOP/s); a chunk of 2048 after 30720, 56 heads over 8: 1,135 / 1,230 us
+// (1,640 / 1,515).  Ragged batches: also a segment's start and end, about 4,500 cycles that
+// no product covers (the next segment's receipt, its first S, the last P V and the output
+// follow one another), and the CTAs' imbalance (5%): 16 prompts of 33 to 4097 tokens 184 /
+// 197 us, 1,250 / 1,165 TFLOP/s.  Single tokens: the cache, 64 sequences of 1024 to 16384
+// keys 140 / 141 us, 5.6 TB/s, where loads of random pages alone reach 6.2.  One token over
+// 4096 keys: latency, 12.0 / 14.4 us (4,000 cycles until the roles start, 5,000 until the
+// first page is asked for, 7,000 for its tile, 6,000 to meet and join); a prompt of 37
+// tokens, 8 heads over 2: 7.8 / 9.3 us.
 //
 // Roles of a CTA's twelve warps; all walk the share's segments (tile ranges of units)
 // by themselves, from a ring the scheduler fills:
@@ -109,8 +111,9 @@ struct PromptParams {
 };
 
 // The code that a CTA runs over and over is kept small (loops over the two row tiles
-// and over column blocks stay rolled): warps of six kinds share one instruction cache,
-// and a segment's start and end run all of it.
+// and over column blocks stay rolled): warps of six kinds share one instruction cache, and
+// a segment's start and end run all of it (of its requests 4.5% miss in 16 packed prompts,
+// 0.9% in a long one).
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -138,7 +141,11 @@ __device__ __forceinline__ float max32(const uint32_t (&x)[32], float m) {
   return fmax3(a, b, __uint_as_float(x[31]));
 }
 // P = 2^(S sl2 + nms) of 32 scores, rounded to bf16 and packed; the fp32 values are added
-// to ls.  Scale and shift and the sums take one packed instruction a pair.
+// to ls.  Scale and shift and the sums take one packed instruction a pair.  P V takes P in
+// one bf16 word (in two, as the verification attention has it, P V would take twice the
+// tensor time and P all of S's columns): a probability is off by 2^-9 of itself at most,
+// either way, and l is not, so that outputs are 1.05 to 1.4 times as far from 64 bits as
+// with P in 32 bits, most of which is the output's own rounding to bf16.
 __device__ __forceinline__ void exp32(const uint32_t (&x)[32], uint64_t sl2x2, uint64_t nmsx2, uint64_t (&ls)[2],
                                       uint32_t (&pw)[16]) {
 #pragma unroll
@@ -1029,8 +1036,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           }
           // Two rolled passes over the tile's scores, 32 at a time with the next 32 on their
           // way: the tile's maximum, then the exponentials.  (All 128 in registers and the
-          // passes unrolled is 7 KB of code, more than a scheduler's instruction cache keeps
-          // beside its other warps' code: 3 cycles an instruction instead of 1.5.  A maximum
+          // passes unrolled is 7 KB of code: 3 cycles an instruction instead of 1.5.  A maximum
           // for each half instead, with the exponentials from the same registers: no faster
           // rolled, and unrolled 2% faster for long rows, 4% slower for short ones.)
           uint32_t xa[32], xb[32];
@@ -1375,8 +1381,10 @@ PromptParams params(const int32_t* tok_off, int B, int total, int64_t max_keys, 
   p.tpt = kRows / p.g;
   p.scale = scale;
   p.scale_log2 = scale * 1.4426950408889634f;
-  // Units of the call, at most (a sequence's last one may be partial).  Where they are
-  // fewer than a third of the SMs and long, they are split among many CTAs, whose partials
+  // Units of the call, at most (a sequence's last one may be partial; one without tokens has
+  // none, which the host does not know: its lengths are on the device).  Where they are fewer
+  // than a third of the SMs and may be long (for chunks, by the block table's width), they
+  // are split among many CTAs, whose partials
   // all of them join, which needs a cooperative launch.  Measured with and without, captured
   // / back to back: one token over 4096 keys 12.0 / 14.4 us and 17.3 / 17.4, 100 tokens after
   // 8000 27 / 30 and 66 / 66; but 16 tokens over 1024 to 16384 keys (64 units) 49.9 / 52.8 and
@@ -1384,8 +1392,8 @@ PromptParams params(const int32_t* tok_off, int B, int total, int64_t max_keys, 
   const int w = 2 * p.tpt;
   p.units = (int)std::min<int64_t>((int64_t)n_kv * std::min<int64_t>((int64_t)total / w + B, total), INT32_MAX);
   p.coop = p.units < kNumSMs / 3 && max_keys > kDirect * kShareMany ? 1 : 0;
-  // Few rows a sequence: their partials cost little to leave and to join.  With the shares
-  // of few and of many rows: one token over 4096 keys 12.0 and 17.7 us, 4 tokens 12.7 and 17.8;
+  // Few rows a sequence, idle ones counted: their partials cost little to leave and to join.
+  // With the shares of few and of many rows: one token over 4096 keys 12.0 and 17.7 us, 4 tokens 12.7 and 17.8;
   // 100 tokens after 8000 28.4 and 27.0, a prompt of 300 15.2 and 12.2.
   const bool few = (int64_t)total * p.g <= 32 * (int64_t)B;
   p.min_share = few ? kShareFew : kShareMany;

@@ -15,8 +15,8 @@
 // and the reads of the pages follow one another.  A thread takes four neighbouring tokens,
 // mostly of one sequence and page, and all its reads precede its writes (four tokens a
 // grid apart, each written before the next is read: 9.7 us for 1024 sequences).  Measured:
-// 8 sequences with a token each 3.7 us; 1024 sequences of up to 2048 new tokens, 2.6 MB in
-// all, 7.2 us.  512 threads: with 256 the latter takes 8.9 us, with 1024 the former 5.6 us.
+// 8 sequences with a token each 3.8 us; 1024 sequences of up to 2048 new tokens, 2.6 MB in
+// all, 7.3 us.  512 threads: with 256 the latter takes 8.9 us, with 1024 the former 5.6 us.
 #include "ee_common.cuh"
 #include "ee_ptx.cuh"
 

@@ -30,7 +30,8 @@ from . import (EE_HEAD_DIM, EE_PAGE, ee_chunk_attn, ee_prompt_attn, ee_prompt_sl
 
 def rope_table(n_pos, base=1e6, device="cuda"):
     """ee_rope_append's table: [n_pos, 128] fp32, cosines of a position's 64 angles
-    p base^(-i / 64), then sines; formed in 64 bits, once, at model load."""
+    p base^(-i / 64), then sines; formed in 64 bits, once, at model load.  A model whose
+    angles follow another rule (scaled positions, say) brings a table of that form."""
     half = EE_HEAD_DIM // 2
     inv = base ** (-torch.arange(half, dtype=torch.float64, device=device) / half)
     a = torch.arange(n_pos, dtype=torch.float64, device=device)[:, None] * inv[None, :]
