@@ -303,8 +303,8 @@ def run(state):
 
 def _nearest_e4m3(v):
     """The nearest multiple of the step at |v|, an even one where two are as near: 4 significant bits, no step below 2^-9."""
-    _, ex = torch.frexp(v)
-    step = torch.ldexp(torch.ones_like(v), (ex - 4).clamp(min=-9))
+    m = torch.frexp(v).mantissa                            # v / m is a power of two, exactly
+    step = torch.where(v == 0, 0.0, v / m * 2.0 ** -4).clamp(min=2.0 ** -9)
     return (v / step).round() * step
 
 
