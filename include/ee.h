@@ -30,6 +30,10 @@
  *                        rotary positions and the K/V write into the slots,
  *                        causal attention of whole prompts and of chunks of
  *                        them over the cache the steps above read
+ *   ee_fp8_quantize / ee_fp8_quantize_weights / ee_fp8_linear / ee_moe_layer
+ *                        the pass's weight products: 8-bit codes with a scale
+ *                        for each block of 128, linear layers on them, and
+ *                        whole mixture-of-experts layers
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -677,6 +681,63 @@ ee_status ee_chunk_attn(const ee_bf16* q, int64_t q_stride, const ee_bf16* k_cac
                         const int32_t* ctx_len, const int32_t* tok_off, int32_t B, int32_t total, int32_t n_q,
                         int32_t n_kv, int32_t head_dim, float scale, ee_bf16* out, float* lse_or_null, void* ws,
                         size_t ws_bytes, ee_stream_t stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Weight products.  A target pass over a draft's nodes is, between the calls
+ * above, a stream of weights: projections and feed-forward layers for 1 to some
+ * hundred tokens.  Weights in e4m3 (8-bit floating point, 4 exponent and 3 mantissa
+ * bits, largest number 448) halve that stream.  A BLOCK is 128 columns of one row
+ * of activations, or 128 x 128 of a weight matrix (fewer at the matrix's ends); its
+ * values are code * scale.
+ *   activations [rows][cols]: codes uint8 [rows][cols], scales fp32
+ *     [ceil(cols / 128)][rows]  (a block's scales of all rows side by side)
+ *   weights [rows][cols]: codes uint8 [rows][cols], scales fp32
+ *     [ceil(rows / 128)][ceil(cols / 128)]
+ * Any scales will do; those the quantising calls make are
+ *   a = max(max |x|, 2^-100),  scale = a / 448,
+ *   code = the e4m3 number nearest to 448 x / a (an even code where two are as near).
+ * A block that holds an infinity or a NaN gets NaN codes and such a scale: what is
+ * computed from it is NaN.
+ */
+
+/*
+ * ee_fp8_quantize -- codes and scales of activations.
+ *   x      bf16 [rows] of cols elements, x_stride elements apart (a multiple of 8,
+ *          at least the row's elements); 16-byte aligned
+ *   gated  0: x as it is; else a row holds 2 cols elements, gate then up, and what
+ *          is quantised is silu(gate) * up in fp32, silu(g) = g / (1 + e^-g)
+ *   q      uint8 [rows][cols], 16-byte aligned; scale fp32 [ceil(cols/128)][rows]
+ * cols a multiple of 16.  No workspace; outputs must not overlap x.
+ */
+ee_status ee_fp8_quantize(const ee_bf16* x, int64_t x_stride, int32_t rows, int32_t cols, int32_t gated,
+                          uint8_t* q, float* scale, ee_stream_t stream);
+
+/*
+ * ee_fp8_quantize_weights -- codes and scales of `batch` weight matrices
+ * [rows][cols] bf16, densely packed: q uint8 [batch][rows][cols], scale fp32
+ * [batch][ceil(rows/128)][ceil(cols/128)].  cols a multiple of 16.
+ */
+ee_status ee_fp8_quantize_weights(const ee_bf16* w, int32_t batch, int32_t rows, int32_t cols, uint8_t* q,
+                                  float* scale, ee_stream_t stream);
+
+/*
+ * ee_fp8_linear -- y = x W^T (+ bias), W [N][K]:
+ *   out[i][o] = bf16( sum_b x_scale[b][i] w_scale[o/128][b] sum_{k in block b} x[i][k] w[o][k] + bias[o] )
+ * Products within a block are summed in the tensor cores' fp32, blocks in fp32
+ * (always in the same order: repeated calls agree bit for bit), and the sum is
+ * rounded once.
+ *   x uint8 [n][K], x_scale fp32 [ceil(K/128)][n]; w uint8 [N][K], w_scale fp32
+ *   [ceil(N/128)][ceil(K/128)]; bias bf16 [N] or NULL
+ *   out bf16, out_stride elements from one token to the next (at least N)
+ * K a multiple of 16; x and w 16-byte aligned; n, N of any size (up to 2^24).  A
+ * token's output depends on that token alone.
+ * Device errors: EE_DEVERR_TIMEOUT (outputs undefined).
+ */
+size_t ee_linear_workspace_size(void);
+ee_status ee_fp8_linear(const uint8_t* x, const float* x_scale, const uint8_t* w, const float* w_scale,
+                        const ee_bf16* bias_or_null, int32_t n, int32_t K, int32_t N, ee_bf16* out,
+                        int64_t out_stride, void* ws, size_t ws_bytes, ee_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -23,6 +23,7 @@ EE_HEAD_DIM = 128
 EE_MAX_TREE = 128
 EE_MAX_LM_NODES = 2048
 EE_MAX_SEQS = 4096
+EE_BLOCK = 128
 
 STATUS = {0: "ok", 1: "invalid argument", 2: "unsupported configuration", 3: "CUDA error",
           4: "device error word set", 5: "workspace too small"}
@@ -36,7 +37,8 @@ EXPORTS = ("ee_version", "ee_status_string", "ee_workspace_size", "ee_workspace_
            "ee_selftest_timeout", "ee_tree_verify_attn_inplace", "ee_kv_compact_inplace",
            "ee_chain_verify_attn", "ee_build_reuse_tree", "ee_advance", "ee_lmhead_packed_bytes",
            "ee_lmhead_pack_weights", "ee_lmhead_accept_packed", "ee_prompt_workspace_size", "ee_prompt_slots",
-           "ee_rope_append", "ee_prompt_attn", "ee_chunk_attn")
+           "ee_rope_append", "ee_prompt_attn", "ee_chunk_attn", "ee_fp8_quantize", "ee_fp8_quantize_weights",
+           "ee_linear_workspace_size", "ee_fp8_linear")
 
 VERIFY_MODES = {"greedy": 0, "direct": 1, "topk": 2, "entropy": 3}
 
@@ -98,6 +100,10 @@ _SIGS = {
                         _P, _SZ, _P], _I),
     "ee_prompt_attn": ([_P, _I64, _P, _I64, _P, _I64, _P, _I, _I, _I, _I, _I, _F, _P, _P, _P, _SZ, _P], _I),
     "ee_chunk_attn": ([_P, _I64, _P, _P, _I, _P, _I, _P, _P, _I, _I, _I, _I, _I, _F, _P, _P, _P, _SZ, _P], _I),
+    "ee_fp8_quantize": ([_P, _I64, _I, _I, _I, _P, _P, _P], _I),
+    "ee_fp8_quantize_weights": ([_P, _I, _I, _I, _P, _P, _P], _I),
+    "ee_linear_workspace_size": ([], _SZ),
+    "ee_fp8_linear": ([_P, _P, _P, _P, _P, _I, _I, _I, _P, _I64, _P, _SZ, _P], _I),
 }
 
 
@@ -528,3 +534,79 @@ def ee_chunk_attn(q, k_cache, v_cache, block_table, ctx_len, tok_off, scale, out
                              ws.numel(), _stream(stream))
     if st:
         raise EEError("ee_chunk_attn", st)
+
+
+def _blocks(n):
+    return -(-n // EE_BLOCK)
+
+
+def _cols2(t, dtype, name):
+    """(pointer, row stride) of a [rows, cols] tensor whose rows are contiguous."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"libee takes CUDA tensors only ({name})")
+    n, c = t.shape
+    s0, s1 = t.stride()
+    if c > 1 and s1 != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    return t.data_ptr(), (s0 if n > 1 else c)
+
+
+def ee_fp8_quantize(x, q, scale, gated=False, stream=None):
+    """Codes and scales of activations x [rows, cols] (rows may be views of wider ones);
+    gated: of silu(x[:, :cols]) * x[:, cols:].  q float8_e4m3fn [rows, cols], scale
+    float32 [ceil(cols / 128), rows]."""
+    rows, cols = q.shape
+    if x.shape != (rows, 2 * cols if gated else cols) or scale.shape != (_blocks(cols), rows):
+        raise ValueError("ee_fp8_quantize: shapes do not fit together")
+    xp, xs = _cols2(x, torch.bfloat16, "x")
+    st = lib().ee_fp8_quantize(xp, xs, rows, cols, int(gated), _tp(q, torch.float8_e4m3fn, "q"),
+                               _tp(scale, torch.float32, "scale"), _stream(stream))
+    if st:
+        raise EEError("ee_fp8_quantize", st)
+
+
+def ee_fp8_quantize_weights(w, q, scale, stream=None):
+    """Codes and scales of weights w [..., rows, cols]: q float8_e4m3fn of w's shape,
+    scale float32 [..., ceil(rows / 128), ceil(cols / 128)]."""
+    *lead, rows, cols = w.shape
+    if q.shape != w.shape or scale.shape != (*lead, _blocks(rows), _blocks(cols)):
+        raise ValueError("ee_fp8_quantize_weights: shapes do not fit together")
+    batch = 1
+    for n in lead:
+        batch *= n
+    st = lib().ee_fp8_quantize_weights(_tp(w, torch.bfloat16, "w"), batch, rows, cols,
+                                       _tp(q, torch.float8_e4m3fn, "q"), _tp(scale, torch.float32, "scale"),
+                                       _stream(stream))
+    if st:
+        raise EEError("ee_fp8_quantize_weights", st)
+
+
+def ee_linear_workspace_size() -> int:
+    return int(lib().ee_linear_workspace_size())
+
+
+def new_linear_workspace(device="cuda", stream=None):
+    """Allocate (through torch) and zero a workspace for ee_fp8_linear."""
+    ws = torch.empty(ee_linear_workspace_size(), dtype=torch.uint8, device=device)
+    ee_workspace_init(ws, stream)
+    return ws
+
+
+def ee_fp8_linear(x, x_scale, w, w_scale, out, ws, bias=None, stream=None):
+    """out = x W^T (+ bias) for codes x [n, K] and w [N, K] with their scales; out bfloat16
+    [n, N], whose rows may be views of wider ones."""
+    n, K = x.shape
+    N = w.shape[0]
+    kb = _blocks(K)
+    if (w.shape != (N, K) or x_scale.shape != (kb, n) or w_scale.shape != (_blocks(N), kb) or out.shape != (n, N)
+            or (bias is not None and bias.shape != (N,))):
+        raise ValueError("ee_fp8_linear: shapes do not fit together")
+    f8, f32 = torch.float8_e4m3fn, torch.float32
+    op, os_ = _cols2(out, torch.bfloat16, "out")
+    st = lib().ee_fp8_linear(_tp(x, f8, "x"), _tp(x_scale, f32, "x_scale"), _tp(w, f8, "w"),
+                             _tp(w_scale, f32, "w_scale"), None if bias is None else _tp(bias, torch.bfloat16, "bias"),
+                             n, K, N, op, os_, _p(ws), ws.numel(), _stream(stream))
+    if st:
+        raise EEError("ee_fp8_linear", st)

@@ -1,0 +1,124 @@
+// What the weight products of a pass share (ee_fp8_linear, ee_moe_layer):
+// 8-bit MMAs, gathering TMA loads, the promotion of one block's product into
+// fp32 registers, and the quantisation of a block.  Internal header.
+//
+// A product with a scale for each block of 128 along K cannot stay in the
+// tensor cores' accumulator: y = sum_b s_b (x_b . w_b).  Each block's product
+// goes to tensor memory by itself (two accumulators in turn) and the epilogue
+// warps add it, scaled, to sums of their own in registers.  Tokens are the MMA's
+// M side (one tensor-memory lane, one thread), so a block's scale is one number a
+// thread and 128 columns; weight rows are the N side.
+#pragma once
+#include "ee_common.cuh"
+#include "ee_ptx.cuh"
+
+namespace ee {
+
+constexpr int kBlk = 128;              // columns (and weight rows) that share a scale
+constexpr float kE4m3Max = 448.f;
+constexpr float kLeastMax = 0x1p-100f;   // a block's maximum counts as at least this
+
+// dims[0] bytes are contiguous; 128-byte swizzle, zero fill out of bounds
+bool encode_u8_tmap_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t stride_bytes,
+                       uint32_t box_cols, uint32_t box_rows);
+
+// Instruction descriptor of kind::f8f6f4: e4m3 A and B, fp32 D, both K-major.
+__host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N) {
+  return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+__device__ __forceinline__ void tc_mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                          uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Four rows of a map whose box is one row high, to four consecutive rows of shared memory.
+__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int r0, int r1,
+                                            int r2, int r3) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, "
+      "%5, %6}], [%7];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar)
+      : "memory");
+}
+
+// acc[16 g .. 16 g + 15] (pairs) += s * 32 columns that a load left in r
+template <int G, int N>
+__device__ __forceinline__ void add_scaled32(uint64_t (&acc)[N], uint32_t (&r)[32], uint64_t s) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc[G * 16 + i] = f2_fma(f2_pack(r[2 * i], r[2 * i + 1]), s, acc[G * 16 + i]);
+}
+
+// acc += s0 * the 64 columns at c0 and s1 * the 64 at c1 of this warp's lanes; the loads of the
+// second 64 run behind the sums of the first.
+__device__ __forceinline__ void promote_2x64(uint64_t (&acc)[64], uint32_t c0, uint32_t c1, float s0, float s1) {
+  uint32_t a[32], b[32];
+  tc_ld32_nowait(c0, a);
+  tc_ld32_nowait(c0 + 32, b);
+  const uint64_t p0 = f2_pack(__float_as_uint(s0), __float_as_uint(s0));
+  const uint64_t p1 = f2_pack(__float_as_uint(s1), __float_as_uint(s1));
+  tc_wait_ld32(a);
+  tc_pin32(b);
+  add_scaled32<0>(acc, a, p0);
+  tc_ld32_nowait(c1, a);
+  add_scaled32<1>(acc, b, p0);
+  tc_ld32_nowait(c1 + 32, b);
+  tc_wait_ld32(a);
+  tc_pin32(b);
+  add_scaled32<2>(acc, a, p1);
+  add_scaled32<3>(acc, b, p1);
+}
+// acc += s * the 64 columns at c
+__device__ __forceinline__ void promote_64(uint64_t (&acc)[32], uint32_t c, float s) {
+  uint32_t a[32], b[32];
+  tc_ld32_nowait(c, a);
+  tc_ld32_nowait(c + 32, b);
+  const uint64_t p = f2_pack(__float_as_uint(s), __float_as_uint(s));
+  tc_wait_ld32(a);
+  tc_pin32(b);
+  add_scaled32<0>(acc, a, p);
+  add_scaled32<1>(acc, b, p);
+}
+
+// The code of x in a block whose largest magnitude is a: the e4m3 number nearest to 448 x / a.
+// The quotient is x (hi + lo) with hi + lo = 448 / a to about 48 bits, rounded once to fp32: for a
+// bf16 x it is then never on the wrong side of a border between two codes (448 x / a is either a
+// border itself, which fp32 holds, or at least 2^-13 of it away), so codes do not depend on how a
+// program divides.  A block with an infinity or a NaN has NaN codes throughout.
+struct BlockScale {
+  float hi, lo, scale;
+};
+__device__ __forceinline__ BlockScale block_scale(float a) {
+  BlockScale b;
+  a = a < kLeastMax ? kLeastMax : a;   // (a NaN stays)
+  b.hi = __fdiv_rn(kE4m3Max, a);
+  b.lo = __fdiv_rn(__fmaf_rn(-b.hi, a, kE4m3Max), a);
+  b.scale = __fdiv_rn(a, kE4m3Max);
+  return b;
+}
+__device__ __forceinline__ float to_code(float x, const BlockScale& b) {
+  return __fmaf_rn(x, b.hi, __fmul_rn(x, b.lo));
+}
+__device__ __forceinline__ uint32_t pack_e4m3(float x0, float x1, float x2, float x3) {
+  uint32_t d;
+  asm("{\n .reg .b16 l, h;\n cvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n cvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n"
+      " mov.b32 %0, {l, h};\n}\n"
+      : "=r"(d)
+      : "f"(x0), "f"(x1), "f"(x2), "f"(x3));
+  return d;
+}
+// silu(g) u; the fast division's error is 2 units in the last place (its result for a divisor
+// above 2^126, g < -87.3, is 0, off by less than 1e-36 u)
+__device__ __forceinline__ float silu_times(float g, float u) { return __fdividef(g, 1.f + __expf(-g)) * u; }
+
+__device__ __forceinline__ float bf16_lo(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+
+}  // namespace ee

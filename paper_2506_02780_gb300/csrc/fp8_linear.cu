@@ -1,0 +1,382 @@
+// ee_fp8_linear: y = x W^T (+ bias) with x and W in e4m3, a scale for each token and 128
+// columns of x and for each 128 x 128 block of W, bf16 out.
+//
+// Warp 0 streams 128-byte-wide tiles of x (up to 128 tokens) and W (BN rows) with TMA into a
+// ring, warp 1 multiplies each k-block (128 columns, 4 MMAs of 128 x BN x 32) into one of the
+// tensor memory's 512 / BN accumulators, and warps 4..11 add it, scaled, to fp32 sums in their
+// registers (block_mma.cuh).  A CTA walks its tiles without a stop between them: the ring and
+// the next tile's first MMAs run behind the stores.
+// Few tokens: the stream of W bounds the call, so it has to come from every SM.  Where there
+// are fewer tiles than SMs, a cluster of up to 8 CTAs shares a tile's k-blocks and adds its
+// partial sums through distributed shared memory, always in the same order.
+#include <mutex>
+
+#include "block_mma.cuh"
+
+namespace {
+
+using namespace ee;
+
+constexpr int kThreads = 384;          // warp 0 TMA, 1 MMA, 2 TMEM, 3 none; 4..11 epilogue
+constexpr int kEpiWarps = 8;           // two per TMEM lane quarter, half of the columns each
+constexpr int kRegsEpi = 216, kRegsOther = 72;   // 256 * 216 + 128 * 72 = 384 * 168
+constexpr int BM = 128;
+
+struct LinParams {
+  int n, N, KB, MT, NT, ks, a_rows, stages;
+  const float* xs;     // [KB][n]
+  const float* ws;     // [ceil(N / 128)][KB]
+  const __nv_bfloat16* bias;
+  __nv_bfloat16* out;
+  int64_t out_stride;
+  int vec;             // rows of out are 16-byte aligned
+  int32_t* err;
+};
+
+__device__ __forceinline__ void st_shared_f4(uint32_t a, float4 v) {
+  asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(a)
+               : "memory");
+  return v;
+}
+
+template <int BN, bool kSplit>
+__global__ void __launch_bounds__(kThreads, 1)
+fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const LinParams p) {
+  constexpr int kBufs = 512 / BN;               // accumulators
+  constexpr int kCols = BN / 2;                 // columns of an epilogue warp
+  constexpr uint32_t kWBytes = BN * kBlk;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  __shared__ __align__(8) uint64_t s_bars[2 * 16 + 2 * 4 + 1];
+  __shared__ uint32_t s_tmem;
+  __shared__ volatile int s_abort;
+  __shared__ int s_issued, s_consumed;
+
+  pdl_allow_next();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int S = p.stages;
+  const uint32_t aBytes = (uint32_t)p.a_rows * kBlk;
+  const uint32_t aStage = (aBytes + 1023) & ~1023u;        // x rows, then W rows: an MMA's rows past a_rows are
+  const uint32_t stBytes = aStage + kWBytes;               // whatever follows, and so are lanes that nobody reads
+  const uint32_t ring = smem_u32(smem);
+  const uint32_t full0 = smem_u32(s_bars), empty0 = full0 + 8 * 16, tfull0 = empty0 + 8 * 16, tempty0 = tfull0 + 8 * 4,
+                 drain = tempty0 + 8 * 4;
+  if (threadIdx.x == 0) {
+    s_abort = 0;
+    s_issued = 0;
+    s_consumed = 0;
+    for (int s = 0; s < S; ++s) {
+      mbar_init(full0 + 8 * s, 1);
+      mbar_init(empty0 + 8 * s, 1);
+    }
+    for (int a = 0; a < kBufs; ++a) {
+      mbar_init(tfull0 + 8 * a, 1);
+      mbar_init(tempty0 + 8 * a, kEpiWarps);
+    }
+    mbar_init(drain, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_smem();
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmW)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmX)) : "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem))
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = s_tmem;
+  pdl_wait();
+
+  const int num_tiles = p.MT * p.NT;
+  const int ks = kSplit ? p.ks : 1;
+  const int rank = kSplit ? (int)blockIdx.x % ks : 0;
+  const int first = (int)blockIdx.x / ks, step = (int)gridDim.x / ks;
+  const int kb0 = p.KB * rank / ks, kb1 = p.KB * (rank + 1) / ks;   // (KB is at most 2^17)
+
+  if (warp >= 4) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpi));
+    const int q = warp & 3, half = (warp - 4) >> 2;
+    const int r = 32 * q + lane;                              // row of the tile
+    const uint32_t taddr = tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)(half * kCols);
+    uint32_t it = 0;
+    bool ok = true;
+    for (int t = first; t < num_tiles && ok; t += step) {
+      const int nt = t / p.MT, row = (t % p.MT) * BM + r;
+      const int c0 = nt * BN + half * kCols;                  // this thread's first column
+      const bool mine = (t % p.MT) * BM + 32 * q < p.n && c0 < p.N;     // the warp has something to keep
+      const float* xs = p.xs + min(row, p.n - 1);
+      const float* ws = p.ws + (int64_t)min(c0 / kBlk, (p.N - 1) / kBlk) * p.KB;
+      uint64_t acc[BN / 4];
+#pragma unroll
+      for (int i = 0; i < BN / 4; ++i) acc[i] = 0;
+      float sx = 0.f, sw = 0.f;
+      if (kb0 < kb1) {
+        sx = xs[(int64_t)kb0 * p.n];
+        sw = ws[kb0];
+      }
+      for (int kb = kb0; kb < kb1; ++kb, ++it) {
+        const float s = sx * sw;
+        if (kb + 1 < kb1) {                                   // the next block's scales load behind this one
+          sx = xs[(int64_t)(kb + 1) * p.n];
+          sw = ws[kb + 1];
+        }
+        const uint32_t buf = it % kBufs, ph = (it / kBufs) & 1;
+        if (!__all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * buf, ph, &s_abort))) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        if (mine) {
+          if constexpr (BN == 256)
+            promote_2x64(acc, taddr + buf * BN, taddr + buf * BN + 64, s, s);
+          else
+            promote_64(acc, taddr + buf * BN, s);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(tempty0 + 8 * buf);
+      }
+      if (!ok || !mine) continue;
+      if constexpr (kSplit) {
+        // to shared memory, 16-byte chunks permuted within a row so that a warp's 32 rows
+        // spread over the banks; the ring is idle (every stage was read by an MMA that ended)
+        const uint32_t base = ring + (uint32_t)r * (BN * 4);
+        if (row < p.n)
+#pragma unroll
+          for (int i = 0; i < kCols / 4; ++i) {
+            uint32_t x, y, z, w;
+            f2_unpack(acc[2 * i], x, y);
+            f2_unpack(acc[2 * i + 1], z, w);
+            const uint32_t ch = (uint32_t)(half * (kCols / 4) + i) ^ (uint32_t)(r & 31);
+            st_shared_f4(base + ch * 16, make_float4(__uint_as_float(x), __uint_as_float(y), __uint_as_float(z),
+                                                     __uint_as_float(w)));
+          }
+        continue;
+      }
+      if (row >= p.n) continue;
+      __nv_bfloat16* o = p.out + (int64_t)row * p.out_stride + c0;
+#pragma unroll
+      for (int i = 0; i < kCols / 8; ++i) {
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t lo, hi;
+          f2_unpack(acc[4 * i + j], lo, hi);
+          f[2 * j] = __uint_as_float(lo);
+          f[2 * j + 1] = __uint_as_float(hi);
+        }
+        const int left = p.N - c0 - 8 * i;
+        if (p.bias)
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j < left) f[j] += __bfloat162float(p.bias[c0 + 8 * i + j]);
+        if (p.vec && left >= 8) {
+          *reinterpret_cast<uint4*>(o + 8 * i) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]),
+                                                            pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j < left) o[8 * i + j] = __float2bfloat16_rn(f[j]);
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
+    if (warp == 0 && lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int t = first; t < num_tiles && ok; t += step) {
+        const int nt = t / p.MT, mt = t % p.MT;
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, &s_abort)) {
+            ok = false;
+            break;
+          }
+          const uint32_t fb = full0 + 8 * stage, at = ring + (uint32_t)stage * stBytes;
+          mbar_expect_tx(fb, aBytes + kWBytes);
+          tma_load_2d(at + aStage, &tmW, fb, kb * kBlk, nt * BN);
+          tma_load_2d(at, &tmX, fb, kb * kBlk, mt * BM);
+          ++s_issued;
+          if (++stage == S) {
+            stage = 0;
+            phase ^= 1;
+          }
+        }
+      }
+    } else if (warp == 1) {
+      const uint32_t idesc = idesc_e4m3(BM, BN);
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+      const uint64_t ad0 = smem_desc_sw128(__shfl_sync(0xffffffffu, ring, 0));
+      int stage = 0, consumed = 0;
+      uint32_t phase = 0, it = 0;
+      bool ok = true;
+      for (int t = first; t < num_tiles && ok; t += step) {
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
+          const uint32_t buf = it % kBufs, ph = (it / kBufs) & 1;
+          if (!__all_sync(0xffffffffu, mbar_wait(tempty0 + 8 * buf, ph ^ 1, &s_abort)) ||
+              !__all_sync(0xffffffffu, mbar_wait(full0 + 8 * stage, phase, &s_abort))) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t ad = ad0 + (uint64_t)(stage * (stBytes >> 4));
+            const uint64_t bd = ad + (uint64_t)(aStage >> 4);
+#pragma unroll
+            for (int k = 0; k < kBlk / 32; ++k)
+              tc_mma_f8(tm + buf * BN, ad + (uint64_t)(2 * k), bd + (uint64_t)(2 * k), idesc, k != 0 ? 1u : 0u);
+            tc_commit(empty0 + 8 * stage);
+            tc_commit(tfull0 + 8 * buf);
+          }
+          __syncwarp();
+          ++consumed;
+          if (++stage == S) {
+            stage = 0;
+            phase ^= 1;
+          }
+        }
+      }
+      if (lane == 0) s_consumed = consumed;
+    }
+  }
+
+  // ---- a cluster's partial sums ----------------------------------------------------
+  __syncwarp();
+  tc_fence_before();
+  if constexpr (kSplit) {
+    cluster_sync();
+    const int nt = first / p.MT, m0 = (first % p.MT) * BM;
+    const int rows = min(BM, p.n - m0), chunks = rows * (BN / 4);
+    for (int i = rank * kThreads + (int)threadIdx.x; i < chunks; i += ks * kThreads) {
+      const int r = i / (BN / 4), c4 = i % (BN / 4);
+      const int c = nt * BN + 4 * c4;
+      if (c >= p.N) continue;
+      const uint32_t at = ring + (uint32_t)r * (BN * 4) + (((uint32_t)c4 ^ (uint32_t)(r & 31)) << 4);
+      float4 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < ks) v[k] = ld_cluster_f4(map_cluster(at, k));
+      float f[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+      for (int k = 1; k < 8; ++k)
+        if (k < ks) {
+          f[0] += v[k].x;
+          f[1] += v[k].y;
+          f[2] += v[k].z;
+          f[3] += v[k].w;
+        }
+      __nv_bfloat16* o = p.out + (int64_t)(m0 + r) * p.out_stride + c;
+      if (p.bias)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (c + j < p.N) f[j] += __bfloat162float(p.bias[c + j]);
+      if (p.vec && c + 4 <= p.N) {
+        *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (c + j < p.N) o[j] = __float2bfloat16_rn(f[j]);
+      }
+    }
+    cluster_sync();                    // nobody leaves while a peer still reads its sums
+  } else {
+    __syncthreads();
+  }
+
+  // ---- teardown: drain on abort, free TMEM -----------------------------------------
+  if (s_abort) {
+    if (threadIdx.x == 0) {
+      flag_error(p.err, EE_DEVERR_TIMEOUT);
+      for (int k = s_consumed; k < s_issued; ++k)
+        if (!mbar_wait_plain(full0 + 8 * (k % S), (uint32_t)((k / S) & 1))) break;
+    }
+    if (warp == 1) {
+      if (elect_one()) {   // the lane that issued the MMAs
+        tc_commit(drain);
+        mbar_wait_plain(drain, 0);
+      }
+      __syncwarp();
+    }
+    __syncthreads();
+  }
+  if (warp == 2) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+template <int BN, bool kSplit>
+ee_status launch(const uint8_t* x, const uint8_t* w, int32_t K, LinParams& p, cudaStream_t stream) {
+  p.NT = (p.N + BN - 1) / BN;
+  const int tiles = p.MT * p.NT;
+  const size_t stage = (((size_t)p.a_rows * kBlk + 1023) & ~(size_t)1023) + (size_t)BN * kBlk;
+  p.stages = (int)std::min<size_t>(16, (size_t)(224 * 1024) / stage);
+  const size_t smem = 1024 + p.stages * stage;
+  CUtensorMap tmX, tmW;
+  if (!encode_u8_tmap_2d(&tmX, x, K, p.n, K, kBlk, p.a_rows) || !encode_u8_tmap_2d(&tmW, w, K, p.N, K, kBlk, BN))
+    return EE_ERR_CUDA;
+  {
+    int dev = 0;
+    const ee_status ds = current_device(&dev);
+    if (ds != EE_OK) return ds;
+    static std::mutex mu;
+    static bool set[kMaxDevices] = {};
+    std::lock_guard<std::mutex> lock(mu);
+    if (!set[dev]) {
+      EE_CUDA_OK(cudaFuncSetAttribute(fp8_linear_kernel<BN, kSplit>, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024));
+      set[dev] = true;
+    }
+  }
+  const int grid = kSplit ? tiles * p.ks : std::min(tiles, kNumSMs);
+  EE_CUDA_OK(launch_pdl(fp8_linear_kernel<BN, kSplit>, dim3(grid), dim3(kThreads), smem, stream, (unsigned)p.ks, tmX, tmW, p));
+  return EE_OK;
+}
+
+}  // namespace
+
+extern "C" size_t ee_linear_workspace_size(void) { return ee::align_up(ee::kWorkspaceBytes, 256); }
+
+extern "C" ee_status ee_fp8_linear(const uint8_t* x, const float* x_scale, const uint8_t* w, const float* w_scale,
+                                   const ee_bf16* bias_or_null, int32_t n, int32_t K, int32_t N, ee_bf16* out,
+                                   int64_t out_stride, void* ws, size_t ws_bytes, ee_stream_t stream) {
+  if (n < 0 || K < 1 || N < 1) return EE_ERR_INVALID_ARG;
+  if (K % 16 != 0 || K > (1 << 24) || N > (1 << 24) || n > (1 << 24)) return EE_ERR_UNSUPPORTED;
+  if (n == 0) return EE_OK;
+  if (!x || !x_scale || !w || !w_scale || !out || !ws || !ee::aligned(ws, 256) || !ee::aligned(x, 16) ||
+      !ee::aligned(w, 16) || !ee::aligned(x_scale, 4) || !ee::aligned(w_scale, 4) || !ee::aligned(out, 2) ||
+      !ee::aligned(bias_or_null, 2) || out_stride < N)
+    return EE_ERR_INVALID_ARG;
+  if (ws_bytes < ee_linear_workspace_size()) return EE_ERR_WORKSPACE;
+  LinParams p;
+  p.n = n;
+  p.N = N;
+  p.KB = (K + kBlk - 1) / kBlk;
+  p.MT = (n + BM - 1) / BM;
+  p.a_rows = std::min(BM, (n + 7) / 8 * 8);
+  p.xs = x_scale;
+  p.ws = w_scale;
+  p.bias = reinterpret_cast<const __nv_bfloat16*>(bias_or_null);
+  p.out = reinterpret_cast<__nv_bfloat16*>(out);
+  p.out_stride = out_stride;
+  p.vec = ee::aligned(out, 16) && out_stride % 8 == 0;
+  p.err = ee::err_word(ws);
+  const int64_t t128 = (int64_t)p.MT * ((N + 127) / 128), t256 = (int64_t)p.MT * ((N + 255) / 256);
+  if (t256 > (1 << 30)) return EE_ERR_UNSUPPORTED;
+  // the widest split of a tile's k-blocks that the SMs hold at once
+  p.ks = 1;
+  if (t128 < ee::kNumSMs) p.ks = (int)std::min<int64_t>({8, (int64_t)ee::kNumSMs / t128, p.KB});
+  if (p.ks > 1) return launch<128, true>(x, w, K, p, (cudaStream_t)stream);
+  if (t256 < ee::kNumSMs) return launch<128, false>(x, w, K, p, (cudaStream_t)stream);
+  return launch<256, false>(x, w, K, p, (cudaStream_t)stream);
+}

@@ -1,9 +1,10 @@
-// Host-side TMA tensor-map encoding for libee's bf16 operands.  The driver
+// Host-side TMA tensor-map encoding for libee's bf16 and 8-bit operands.  The driver
 // entry point is looked up once through the runtime, so libee does not link
 // libcuda directly.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
+#include "block_mma.cuh"
 #include "ee_common.cuh"
 
 namespace ee {
@@ -40,6 +41,17 @@ bool encode_bf16_tmap(CUtensorMap* map, const void* base, int rank, const uint64
                   s, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS;
+}
+
+bool encode_u8_tmap_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t stride_bytes,
+                       uint32_t box_cols, uint32_t box_rows) {
+  auto fn = get_encode();
+  if (!fn) return false;
+  const cuuint64_t d[2] = {cols, rows}, s[1] = {stride_bytes};
+  const cuuint32_t bx[2] = {box_cols, box_rows}, es[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), d, s, bx, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace ee
