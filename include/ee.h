@@ -739,6 +739,35 @@ ee_status ee_fp8_linear(const uint8_t* x, const float* x_scale, const uint8_t* w
                         const ee_bf16* bias_or_null, int32_t n, int32_t K, int32_t N, ee_bf16* out,
                         int64_t out_stride, void* ws, size_t ws_bytes, ee_stream_t stream);
 
+/*
+ * ee_moe_layer -- a mixture-of-experts feed-forward layer for the tokens of a pass (T <= 4096).
+ *   logits   l = x router^T in fp32, router bf16 [E][H]
+ *   choice   the k experts with the largest logits (of equal ones the lowest; a NaN
+ *            counts as less than any number), in ascending order of their number
+ *   weights  p = e^l / sum e^l, the sum over all experts, or with renorm != 0 over the k chosen ones
+ *   expert e h = silu(x Wg[e]^T) * (x Wu[e]^T),  y_e = h Wd[e]^T
+ *   out[t]   = bf16( sum_j p[t][j] y_{ids[t][j]} ), experts in ascending order, fp32
+ * w1 [E][2 I][H] holds an expert's gate rows, then its up rows; w2 [E][H][I] is Wd.  Both are
+ *   bf16 (scales NULL): h is rounded to bf16 between the products; or
+ *   e4m3 codes with block scales: w1_scale [E][2][ceil(I/128)][ceil(H/128)] (gate and up each in
+ *   blocks of their own), w2_scale [E][ceil(H/128)][ceil(I/128)]: x and h are then quantised as by
+ *   ee_fp8_quantize, h from fp32.
+ *   x bf16 [T] rows of H elements, x_stride apart (a multiple of 8); out likewise, out_stride apart
+ *   live     int32[1] or NULL: only the first min(max(*live, 0), T) tokens are computed; rows of out, ids and
+ *            probs behind them are left as they are
+ *   ids int32 [T][k], probs fp32 [T][k] or NULL: the choice and its weights
+ * H and I multiples of 16, up to 65536; E up to 256, k up to 16; x, router, w1 and w2 16-byte aligned.
+ * Always summed in the same order: repeated calls agree bit for bit.
+ * ws: ee_moe_workspace_size(...) bytes for these sizes (a larger one serves too), zeroed once with ee_workspace_init().
+ * Device errors: EE_DEVERR_TIMEOUT (outputs undefined).
+ */
+size_t ee_moe_workspace_size(int32_t T, int32_t H, int32_t I, int32_t E, int32_t k);
+ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_bf16* router, const void* w1,
+                       const float* w1_scale_or_null, const void* w2, const float* w2_scale_or_null, int32_t T,
+                       int32_t H, int32_t I, int32_t E, int32_t k, int32_t renorm, const int32_t* live_or_null,
+                       ee_bf16* out, int64_t out_stride, int32_t* ids_or_null, float* probs_or_null, void* ws,
+                       size_t ws_bytes, ee_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -38,7 +38,7 @@ EXPORTS = ("ee_version", "ee_status_string", "ee_workspace_size", "ee_workspace_
            "ee_chain_verify_attn", "ee_build_reuse_tree", "ee_advance", "ee_lmhead_packed_bytes",
            "ee_lmhead_pack_weights", "ee_lmhead_accept_packed", "ee_prompt_workspace_size", "ee_prompt_slots",
            "ee_rope_append", "ee_prompt_attn", "ee_chunk_attn", "ee_fp8_quantize", "ee_fp8_quantize_weights",
-           "ee_linear_workspace_size", "ee_fp8_linear")
+           "ee_linear_workspace_size", "ee_fp8_linear", "ee_moe_workspace_size", "ee_moe_layer")
 
 VERIFY_MODES = {"greedy": 0, "direct": 1, "topk": 2, "entropy": 3}
 
@@ -104,6 +104,8 @@ _SIGS = {
     "ee_fp8_quantize_weights": ([_P, _I, _I, _I, _P, _P, _P], _I),
     "ee_linear_workspace_size": ([], _SZ),
     "ee_fp8_linear": ([_P, _P, _P, _P, _P, _I, _I, _I, _P, _I64, _P, _SZ, _P], _I),
+    "ee_moe_workspace_size": ([_I, _I, _I, _I, _I], _SZ),
+    "ee_moe_layer": ([_P, _I64, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _P, _P, _I64, _P, _P, _P, _SZ, _P], _I),
 }
 
 
@@ -610,3 +612,45 @@ def ee_fp8_linear(x, x_scale, w, w_scale, out, ws, bias=None, stream=None):
                              n, K, N, op, os_, _p(ws), ws.numel(), _stream(stream))
     if st:
         raise EEError("ee_fp8_linear", st)
+
+
+def ee_moe_workspace_size(T, H, I, E, k) -> int:
+    return int(lib().ee_moe_workspace_size(T, H, I, E, k))
+
+
+def new_moe_workspace(T, H, I, E, k, device="cuda", stream=None):
+    """Allocate (through torch) and zero a workspace for ee_moe_layer calls of up to these sizes."""
+    ws = torch.empty(ee_moe_workspace_size(T, H, I, E, k), dtype=torch.uint8, device=device)
+    ee_workspace_init(ws, stream)
+    return ws
+
+
+def ee_moe_layer(x, router, w1, w2, k, out, ws, w1_scale=None, w2_scale=None, renorm=False, live=None, ids=None,
+                 probs=None, stream=None):
+    """A mixture-of-experts layer: x, out bfloat16 [T, H] (rows may be views of wider ones), router
+    bfloat16 [E, H], w1 [E, 2 I, H] (gate rows, then up rows) and w2 [E, H, I], both bfloat16 or both
+    float8_e4m3fn with w1_scale [E, 2, ceil(I / 128), ceil(H / 128)] and w2_scale [E, ceil(H / 128),
+    ceil(I / 128)].  live int32 [1]: tokens to compute; ids int32 and probs float32 [T, k]: the choice."""
+    T, H = x.shape
+    E, I = router.shape[0], w2.shape[2]
+    if (router.shape != (E, H) or w1.shape != (E, 2 * I, H) or w2.shape != (E, H, I) or out.shape != (T, H)
+            or (live is not None and live.numel() != 1) or (ids is not None and ids.shape != (T, k))
+            or (probs is not None and probs.shape != (T, k))):
+        raise ValueError("ee_moe_layer: shapes do not fit together")
+    bf16, f32 = torch.bfloat16, torch.float32
+    s1 = s2 = None
+    if w1_scale is not None or w2_scale is not None:
+        if w1_scale is None or w2_scale is None:
+            raise ValueError("ee_moe_layer: w1_scale and w2_scale belong together")
+        if w1_scale.shape != (E, 2, _blocks(I), _blocks(H)) or w2_scale.shape != (E, _blocks(H), _blocks(I)):
+            raise ValueError("ee_moe_layer: shapes do not fit together")
+        s1, s2 = _tp(w1_scale, f32, "w1_scale"), _tp(w2_scale, f32, "w2_scale")
+    wt = bf16 if s1 is None else torch.float8_e4m3fn
+    xp, xs = _cols2(x, bf16, "x")
+    op, os_ = _cols2(out, bf16, "out")
+    st = lib().ee_moe_layer(xp, xs, _tp(router, bf16, "router"), _tp(w1, wt, "w1"), s1, _tp(w2, wt, "w2"), s2, T, H, I, E,
+                            k, int(renorm), None if live is None else _tp(live, torch.int32, "live"), op, os_,
+                            None if ids is None else _tp(ids, torch.int32, "ids"),
+                            None if probs is None else _tp(probs, f32, "probs"), _p(ws), ws.numel(), _stream(stream))
+    if st:
+        raise EEError("ee_moe_layer", st)

@@ -19,7 +19,7 @@ using namespace ee;
 
 constexpr int kThreads = 384;          // warp 0 TMA, 1 MMA, 2 TMEM, 3 none; 4..11 epilogue
 constexpr int kEpiWarps = 8;           // two per TMEM lane quarter, half of the columns each
-constexpr int kRegsEpi = 216, kRegsOther = 72;   // 256 * 216 + 128 * 72 = 384 * 168
+constexpr int kRegsAll = 168, kRegsEpi = 216, kRegsOther = 72;   // 256 * 216 + 128 * 72 = 384 * 168
 constexpr int BM = 128;
 
 struct LinParams {
@@ -253,6 +253,9 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
 
   // ---- a cluster's partial sums ----------------------------------------------------
   __syncwarp();
+  // one code for all warps from here: as many registers as it was compiled for
+  if (warp >= 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsAll));
+  else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsAll));
   tc_fence_before();
   if constexpr (kSplit) {
     cluster_sync();

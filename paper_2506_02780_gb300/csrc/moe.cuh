@@ -1,0 +1,79 @@
+// ee_moe_layer's workspace and the launch of its first kernel (moe_route.cu).  Internal header.
+//
+// An ENTRY is a token at one of its experts; entries are numbered by expert, then by token.
+// A token TILE is up to 128 entries of one expert.
+#pragma once
+#include "block_mma.cuh"
+
+namespace ee {
+
+constexpr int kMoeMaxTopK = 16;
+constexpr int kMoeMaxExperts = 256;
+constexpr int kMoeMaxTokens = 4096;
+constexpr int kMoeTile = 128;
+
+// counters in front of the workspace's arrays, set by the routing kernel
+struct MoeCtl {
+  uint32_t route_ticket;     // zero between calls
+  uint32_t queue;            // next task of the experts' kernel
+  uint32_t down_done;        // warps that stored their part of a down tile
+  uint32_t tiles;            // token tiles
+  uint32_t quarters;         // groups of 32 entries in them (a warp's rows)
+  uint32_t pad[3];
+  uint32_t gate_done[1];     // per token tile: warps that stored their part of a gate tile
+};
+struct __align__(32) MoeTile {   // a token tile's expert
+  int expert, entry0, count;   // its first entry and their number
+  int first, tiles;            // its first tile and their number
+  int pad[3];
+};
+
+struct MoeLayout {
+  size_t ctl, tile, ids, prob, list, inv, xq, xs, h, hs, y, total;
+  int max_tiles;             // token tiles of all experts, at most
+};
+inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t k) {
+  MoeLayout l;
+  const int64_t n = T * k;
+  l.max_tiles = (int)(std::min(E, n) + n / kMoeTile);
+  size_t at = align_up(kWorkspaceBytes, 256);
+  const auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at = align_up(at + bytes, 256);
+    return here;
+  };
+  l.ctl = take(sizeof(MoeCtl) + 4 * (size_t)l.max_tiles);
+  l.tile = take(sizeof(MoeTile) * (size_t)l.max_tiles);
+  l.ids = take(4 * (size_t)n);
+  l.prob = take(4 * (size_t)n);
+  l.list = take(4 * (size_t)n);
+  l.inv = take(4 * (size_t)n);
+  l.xq = take((size_t)(T * H));
+  l.xs = take(4 * (size_t)(T * ((H + kBlk - 1) / kBlk)));
+  l.h = take(2 * (size_t)(n * I));
+  l.hs = take(4 * (size_t)(n * ((I + kBlk - 1) / kBlk)));
+  l.y = take(4 * (size_t)(n * H));
+  l.total = at;
+  return l;
+}
+
+struct RouteParams {
+  const __nv_bfloat16* x;
+  int64_t x_stride;
+  const __nv_bfloat16* router;
+  const int32_t* live;       // or NULL
+  int T, H, E, k, renorm, cl, max_tiles;
+  MoeCtl* ctl;
+  MoeTile* tile;
+  int32_t* ids;              // [T][k] experts of a token, ascending
+  float* prob;               // [T][k]
+  int32_t* list;             // [T k] token of an entry
+  int32_t* inv;              // [T][k] entry of a token's j-th expert
+  uint8_t* xq;               // [T][H] codes of x (NULL: not wanted)
+  float* xs;                 // [blocks][T]
+  int32_t* ids_out;          // the caller's copies, or NULL
+  float* prob_out;
+};
+ee_status launch_moe_route(const RouteParams& p, cudaStream_t stream);
+
+}  // namespace ee

@@ -1,0 +1,284 @@
+// First kernel of ee_moe_layer: the router's product, each token's experts and their
+// probabilities, x as e4m3 codes (for 8-bit weights), and the tokens grouped by expert.
+//
+// A cluster of up to 8 CTAs takes 16 tokens and shares the hidden dimension: an m16n8k16 MMA
+// of bf16 a warp and 16 columns, operands straight from global memory (a lane takes 8
+// neighbouring columns of its row of x and of the router; the order of the columns within
+// a sum is free, so x's and the router's fragments need only agree).  2 T E H operations are too few for
+// the tensor memory's set-up; what counts is that the router's rows are read by many
+// SMs at once.  Warps' sums are added in shared memory, CTAs' in distributed shared memory, in a
+// fixed order.  The last CTA to finish groups the tokens: a bit for each expert and token, so
+// that an entry's place is a count of bits and does not depend on who comes first.
+#include <mutex>
+
+#include "moe.cuh"
+
+namespace {
+
+using namespace ee;
+
+constexpr int kThreads = 256, kWarps = 8, kTok = 16;
+
+__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                          uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, "
+      "%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float ld_cluster_f(uint32_t a) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+// larger key, better logit; at least 1: a NaN is the worst
+__device__ __forceinline__ uint32_t logit_key(float f) {
+  const uint32_t u = __float_as_uint(f);
+  return f != f ? 1u : (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+// NT: groups of 8 experts (E <= 8 NT)
+template <int NT>
+__global__ void __launch_bounds__(kThreads) moe_route_kernel(const RouteParams p) {
+  constexpr int EP = 8 * NT;
+  extern __shared__ float s_red[];                 // [kWarps][kTok][EP], the first becomes the CTA's sums
+  __shared__ int s_last;
+  __shared__ uint64_t s_scan[kWarps];
+  pdl_allow_next();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)blockIdx.x % p.cl, t0 = (int)blockIdx.x / p.cl * kTok;
+  pdl_wait();
+  const int live = p.live ? max(0, min(p.T, ld_pinned(p.live))) : p.T;
+  if (t0 < live) {                                 // (the same in the whole cluster)
+    const int nb = (p.H + kBlk - 1) / kBlk;
+    const int b0 = nb * rank / p.cl, b1 = nb * (rank + 1) / p.cl;
+    const int g = lane >> 2, tq = lane & 3;
+    float acc[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    for (int c = b0 * 4 + warp; c < b1 * 4; c += kWarps) {
+      const int col = c * 32 + tq * 8;
+      const bool in = col < p.H;
+      uint4 xa = zero, xb = zero;
+      if (in && t0 + g < live) xa = *reinterpret_cast<const uint4*>(p.x + (t0 + g) * p.x_stride + col);
+      if (in && t0 + g + 8 < live) xb = *reinterpret_cast<const uint4*>(p.x + (t0 + g + 8) * p.x_stride + col);
+      constexpr int kStep = NT < 8 ? NT : 8;
+#pragma unroll
+      for (int n0 = 0; n0 < NT; n0 += kStep) {
+        uint4 w[kStep];
+#pragma unroll
+        for (int n = 0; n < kStep; ++n) {
+          const int e = (n0 + n) * 8 + g;
+          w[n] = in && e < p.E ? *reinterpret_cast<const uint4*>(p.router + (size_t)e * p.H + col) : zero;
+        }
+#pragma unroll
+        for (int n = 0; n < kStep; ++n) {
+          mma_16816(acc[n0 + n], xa.x, xb.x, xa.y, xb.y, w[n].x, w[n].y);
+          mma_16816(acc[n0 + n], xa.z, xb.z, xa.w, xb.w, w[n].z, w[n].w);
+        }
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float* r = s_red + ((size_t)warp * kTok + g) * EP + n * 8 + 2 * tq;
+      *reinterpret_cast<float2*>(r) = make_float2(acc[n][0], acc[n][1]);
+      *reinterpret_cast<float2*>(r + 8 * EP) = make_float2(acc[n][2], acc[n][3]);
+    }
+    if (p.xq) {                                    // a warp and a block of one token at a time
+      for (int i = warp; i < kTok * (b1 - b0); i += kWarps) {
+        const int t = t0 + i % kTok, b = b0 + i / kTok, col = b * kBlk + lane * 4;
+        if (t >= live) continue;
+        uint2 v = make_uint2(0, 0);
+        if (col < p.H) v = *reinterpret_cast<const uint2*>(p.x + t * p.x_stride + col);
+        const uint32_t a = __vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu);
+        const uint32_t top = __reduce_max_sync(0xffffffffu, max(a & 0xffffu, a >> 16));
+        const BlockScale s = block_scale(__uint_as_float(top << 16));
+        if (col < p.H)
+          *reinterpret_cast<uint32_t*>(p.xq + (size_t)t * p.H + col) = pack_e4m3(
+              to_code(bf16_lo(v.x), s), to_code(bf16_hi(v.x), s), to_code(bf16_lo(v.y), s), to_code(bf16_hi(v.y), s));
+        if (lane == 0) p.xs[(size_t)b * p.T + t] = s.scale;
+      }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kTok * EP; i += kThreads) {
+      float s = s_red[i];
+#pragma unroll
+      for (int w = 1; w < kWarps; ++w) s += s_red[w * kTok * EP + i];
+      s_red[i] = s;
+    }
+    if (p.cl > 1) cluster_sync();
+    else __syncthreads();
+    // the CTAs of the cluster take the tokens in turn, a warp each
+    for (int row = rank + p.cl * warp; row < kTok && t0 + row < live; row += p.cl * kWarps) {
+      constexpr int kPer = (EP + 31) / 32;
+      float l[kPer];
+      uint32_t key[kPer];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int e = lane + 32 * i;
+        l[i] = 0.f;
+        key[i] = 0;
+        if (e < p.E) {
+          const uint32_t at = smem_u32(s_red + row * EP + e);
+          float part[8];
+#pragma unroll
+          for (int r = 0; r < 8; ++r)
+            if (r < p.cl) part[r] = p.cl > 1 ? ld_cluster_f(map_cluster(at, r)) : s_red[row * EP + e];
+          l[i] = part[0];
+#pragma unroll
+          for (int r = 1; r < 8; ++r)
+            if (r < p.cl) l[i] += part[r];
+          key[i] = logit_key(l[i]);
+        }
+      }
+      int my_e = 0x7fffffff;                       // lane j: the j-th choice and its logit
+      float my_l = 0.f, top = 0.f;
+      for (int j = 0; j < p.k; ++j) {
+        uint32_t best = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) best = max(best, key[i]);
+        const uint32_t all = __reduce_max_sync(0xffffffffu, best);
+        uint32_t e = 0xffffffffu;
+#pragma unroll
+        for (int i = kPer - 1; i >= 0; --i)
+          if (key[i] == all) e = lane + 32 * i;
+        e = __reduce_min_sync(0xffffffffu, e);     // of equal logits the lowest expert
+        float le = 0.f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (e == (uint32_t)(lane + 32 * i)) {
+            le = l[i];
+            key[i] = 0;
+          }
+        le = __shfl_sync(0xffffffffu, le, e & 31);
+        if (j == 0) top = le;
+        if (lane == j) {
+          my_e = (int)e;
+          my_l = le;
+        }
+      }
+      float sum = 0.f;
+      const float pe = lane < p.k ? expf(my_l - top) : 0.f;
+      if (p.renorm) {
+        sum = pe;
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (lane + 32 * i < p.E) sum += expf(l[i] - top);
+      }
+#pragma unroll
+      for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      int before = 0;
+      for (int j = 0; j < p.k; ++j) before += __shfl_sync(0xffffffffu, my_e, j) < my_e;
+      if (lane < p.k) {
+        const size_t at = (size_t)(t0 + row) * p.k + before;
+        const float pr = __fdiv_rn(pe, sum);
+        p.ids[at] = my_e;
+        p.prob[at] = pr;
+        if (p.ids_out) p.ids_out[at] = my_e;
+        if (p.prob_out) p.prob_out[at] = pr;
+      }
+    }
+    if (p.cl > 1) cluster_sync();                  // nobody leaves while a peer reads its sums
+  }
+
+  // ---- the last CTA groups the tokens by expert --------------------------------------
+  __syncthreads();
+  if (threadIdx.x == 0) s_last = atom_add_acq_rel(&p.ctl->route_ticket, 1u) == gridDim.x - 1;
+  __syncthreads();
+  if (!s_last) return;
+  const int words = (live + 31) >> 5, n = live * p.k;
+  uint32_t* mask = reinterpret_cast<uint32_t*>(s_red);          // [E][words]
+  uint16_t* pre = reinterpret_cast<uint16_t*>(mask + p.E * words);   // bits in an expert's earlier words
+  int* s_off = reinterpret_cast<int*>(pre + ((p.E * words + 1) & ~1));
+  for (int i = threadIdx.x; i < p.E * words; i += kThreads) mask[i] = 0;
+  for (int i = threadIdx.x; i < p.max_tiles; i += kThreads) p.ctl->gate_done[i] = 0;
+  if (threadIdx.x == 0) {
+    p.ctl->route_ticket = 0;
+    p.ctl->queue = 0;
+    p.ctl->down_done = 0;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const int t = i / p.k;
+    atomicOr(&mask[__ldcg(p.ids + i) * words + (t >> 5)], 1u << (t & 31));
+  }
+  __syncthreads();
+  int cnt = 0;                                     // (E <= kThreads: thread e counts expert e's)
+  if ((int)threadIdx.x < p.E)
+    for (int w = 0; w < words; ++w) {
+      pre[threadIdx.x * words + w] = (uint16_t)cnt;
+      cnt += __popc(mask[threadIdx.x * words + w]);
+    }
+  // running numbers of entries, tiles and quarters in one scan (20 bits each: at most 2^16 entries)
+  const int tiles = (cnt + kMoeTile - 1) / kMoeTile;
+  const uint64_t own = (uint64_t)cnt | (uint64_t)tiles << 20 | (uint64_t)((cnt + 31) / 32) << 40;
+  uint64_t incl = own;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const uint64_t o = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += o;
+  }
+  if (lane == 31) s_scan[warp] = incl;
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) incl += s_scan[w];
+  if ((int)threadIdx.x < p.E) {
+    const uint64_t before = incl - own;
+    MoeTile m;
+    m.expert = (int)threadIdx.x;
+    m.entry0 = (int)(before & 0xfffffu);
+    m.count = cnt;
+    m.first = (int)(before >> 20 & 0xfffffu);
+    m.tiles = tiles;
+    m.pad[0] = m.pad[1] = m.pad[2] = 0;
+    s_off[threadIdx.x] = m.entry0;
+    for (int i = 0; i < tiles; ++i) p.tile[m.first + i] = m;
+    if ((int)threadIdx.x == p.E - 1) {
+      p.ctl->tiles = (uint32_t)(incl >> 20 & 0xfffffu);
+      p.ctl->quarters = (uint32_t)(incl >> 40);
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const int t = i / p.k, e = __ldcg(p.ids + i), at = e * words + (t >> 5);
+    const int pos = s_off[e] + pre[at] + __popc(mask[at] & ((1u << (t & 31)) - 1u));
+    p.list[pos] = t;
+    p.inv[i] = pos;
+  }
+}
+
+template <int NT>
+ee_status launch(const RouteParams& p, cudaStream_t stream) {
+  const size_t sums = (size_t)kWarps * kTok * 8 * NT * 4;
+  const size_t words = ((size_t)p.T + 31) / 32;
+  const size_t group = p.E * words * 6 + 4 + 4 * (size_t)p.E;
+  const size_t smem = std::max(sums, group);
+  {
+    int dev = 0;
+    const ee_status ds = current_device(&dev);
+    if (ds != EE_OK) return ds;
+    static std::mutex mu;
+    static size_t have[kMaxDevices] = {};
+    std::lock_guard<std::mutex> lock(mu);
+    if (have[dev] < smem) {
+      EE_CUDA_OK(cudaFuncSetAttribute(moe_route_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+      have[dev] = smem;
+    }
+  }
+  const unsigned grid = (unsigned)((p.T + kTok - 1) / kTok * p.cl);
+  EE_CUDA_OK(launch_pdl(moe_route_kernel<NT>, dim3(grid), dim3(kThreads), smem, stream, (unsigned)p.cl, p));
+  return EE_OK;
+}
+
+}  // namespace
+
+namespace ee {
+ee_status launch_moe_route(const RouteParams& p, cudaStream_t stream) {
+  if (p.E <= 8) return launch<1>(p, stream);
+  if (p.E <= 64) return launch<8>(p, stream);
+  if (p.E <= 128) return launch<16>(p, stream);
+  return launch<32>(p, stream);
+}
+}  // namespace ee
