@@ -252,8 +252,9 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
   }
 
   // ---- a cluster's partial sums ----------------------------------------------------
-  __syncwarp();
-  // one code for all warps from here: as many registers as it was compiled for
+  // one code for all warps from here: as many registers as it was compiled for (a warpgroup has to
+  // meet between two changes of its registers)
+  __syncthreads();
   if (warp >= 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsAll));
   else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsAll));
   tc_fence_before();

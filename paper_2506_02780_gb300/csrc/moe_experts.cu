@@ -63,9 +63,9 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
-  __shared__ __align__(8) uint64_t s_bars[2 * 8 + 2 * kBufs + 2 * kRing + 1];
+  __shared__ __align__(8) uint64_t s_bars[2 * 8 + 2 * kBufs + 2 * kRing + 4 + 1];
   __shared__ Task s_task[kRing];
-  __shared__ uint32_t s_top[2][128];
+  __shared__ uint32_t s_top[2][2][128];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
   __shared__ int s_issued, s_consumed;
@@ -77,7 +77,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
   const uint32_t stBytes = aStage + 2 * kBoxBytes;
   const uint32_t ring = smem_u32(smem);
   const uint32_t full0 = smem_u32(s_bars), empty0 = full0 + 8 * 8, tfull0 = empty0 + 8 * 8, tempty0 = tfull0 + 8 * kBufs,
-                 qfull0 = tempty0 + 8 * kBufs, qempty0 = qfull0 + 8 * kRing, drain = qempty0 + 8 * kRing;
+                 qfull0 = tempty0 + 8 * kBufs, qempty0 = qfull0 + 8 * kRing, pair0 = qempty0 + 8 * kRing, drain = pair0 + 8 * 4;
   if (threadIdx.x == 0) {
     s_abort = 0;
     s_issued = 0;
@@ -94,6 +94,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
       mbar_init(qfull0 + 8 * a, 1);
       mbar_init(qempty0 + 8 * a, 1 + kEpiWarps);
     }
+    for (int a = 0; a < 4; ++a) mbar_init(pair0 + 8 * a, 2);
     mbar_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
@@ -118,7 +119,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
     const int q = warp & 3, half = (warp - 4) >> 2;
     const int r = 32 * q + lane;                              // row of the tile
     const uint32_t tq = tmem + ((uint32_t)(32 * q) << 16);
-    uint32_t it = 0;                                          // accumulators taken
+    uint32_t it = 0, pairs = 0;                               // accumulators taken, meetings with the neighbour
     for (uint32_t nt = 0;; ++nt) {
       const uint32_t slot = nt % kRing;
       if (!__all_sync(0xffffffffu, mbar_wait(qfull0 + 8 * slot, (nt / kRing) & 1, &s_abort))) break;
@@ -210,10 +211,14 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
 #pragma unroll
           for (int i = 0; i < 64; ++i)
             if (i0 + i < p.I) top = max(top, __float_as_uint(h[i]) & 0x7fffffffu);
-          s_top[half][r] = top;
-          asm volatile("bar.sync %0, 64;" ::"r"(1 + q) : "memory");
-          top = max(top, s_top[half ^ 1][r]);
-          asm volatile("bar.sync %0, 64;" ::"r"(1 + q) : "memory");
+          // the block's other 64 columns are the neighbour warp's; two places in turn, so that one meeting
+          // a task is enough
+          s_top[pairs & 1][half][r] = top;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(pair0 + 8 * q);
+          if (!__all_sync(0xffffffffu, mbar_wait(pair0 + 8 * q, pairs & 1, &s_abort))) break;
+          top = max(top, s_top[pairs & 1][half ^ 1][r]);
+          ++pairs;
           const BlockScale b = block_scale(__uint_as_float(top));
           if (r < t.rows) {
             uint8_t* o = static_cast<uint8_t*>(p.h) + (size_t)entry * p.I + i0;
@@ -394,8 +399,9 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
   }
 
   // ---- the sum over a token's experts, all warps ------------------------------------
-  __syncwarp();
-  // one code for all warps from here: as many registers as it was compiled for
+  // one code for all warps from here: as many registers as it was compiled for (a warpgroup has to
+  // meet between two changes of its registers)
+  __syncthreads();
   if (warp >= 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsAll));
   else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsAll));
   tc_fence_before();
