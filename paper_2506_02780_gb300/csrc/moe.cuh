@@ -16,11 +16,10 @@ constexpr int kMoeTile = 128;
 struct MoeCtl {
   uint32_t route_ticket;     // zero between calls
   uint32_t queue;            // next task of the experts' kernel
-  uint32_t down_done;        // warps that stored their part of a down tile
+  uint32_t down_done;        // down tasks that stored their part of y
   uint32_t tiles;            // token tiles
-  uint32_t quarters;         // groups of 32 entries in them (a warp's rows)
-  uint32_t pad[3];
-  uint32_t gate_done[1];     // per token tile: warps that stored their part of a gate tile
+  uint32_t pad[4];
+  uint32_t gate_done[1];     // per token tile: gate tasks (8-bit weights: blocks of h) that are there
 };
 struct __align__(32) MoeTile {   // a token tile's expert
   int expert, entry0, count;   // its first entry and their number
@@ -29,7 +28,7 @@ struct __align__(32) MoeTile {   // a token tile's expert
 };
 
 struct MoeLayout {
-  size_t ctl, tile, ids, prob, list, inv, xq, xs, h, hs, y, total;
+  size_t ctl, sub, tile, ids, prob, list, inv, xq, xs, h, hf, hs, y, total;
   int max_tiles;             // token tiles of all experts, at most
 };
 inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t k) {
@@ -43,6 +42,7 @@ inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t 
     return here;
   };
   l.ctl = take(sizeof(MoeCtl) + 4 * (size_t)l.max_tiles);
+  l.sub = take(4 * (size_t)l.max_tiles * (size_t)((I + kBlk - 1) / kBlk));
   l.tile = take(sizeof(MoeTile) * (size_t)l.max_tiles);
   l.ids = take(4 * (size_t)n);
   l.prob = take(4 * (size_t)n);
@@ -51,6 +51,7 @@ inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t 
   l.xq = take((size_t)(T * H));
   l.xs = take(4 * (size_t)(T * ((H + kBlk - 1) / kBlk)));
   l.h = take(2 * (size_t)(n * I));
+  l.hf = take(4 * (size_t)(n * I));
   l.hs = take(4 * (size_t)(n * ((I + kBlk - 1) / kBlk)));
   l.y = take(4 * (size_t)(n * H));
   l.total = at;
@@ -64,6 +65,8 @@ struct RouteParams {
   const int32_t* live;       // or NULL
   int T, H, E, k, renorm, cl, max_tiles;
   MoeCtl* ctl;
+  uint32_t* sub;             // or NULL: [n_sub] counters to zero
+  int n_sub;
   MoeTile* tile;
   int32_t* ids;              // [T][k] experts of a token, ascending
   float* prob;               // [T][k]

@@ -1,16 +1,21 @@
 // ee_moe_layer: a mixture-of-experts layer for the few tokens of a pass.  After the router (moe_route.cu)
 // one persistent kernel runs the chosen experts:
-//   gate tasks   h = silu(x Wg^T) * (x Wu^T)   128 columns of h for one token tile
-//   down tasks   y = h Wd^T                    256 columns of y
+//   gate tasks   h = silu(x Wg^T) * (x Wu^T)   w columns of h for one token tile
+//   down tasks   y = h Wd^T                    2 w columns of y
 //   the sum      out[t] = sum_j p[t][j] y[entry of t's j-th expert]
-// The experts' weights are read once and bound the call; tokens are the MMA's M side, so that a
-// few of them cost no more than 128 (block_mma.cuh).
+// The experts' weights are read once and bound the call.  Weight rows are the MMA's M side (two tiles of
+// up to 128: gate and up, or two of down), tokens its N side: a few tokens then cost the epilogue a few
+// columns of every lane, where with tokens on the lanes two warps of eight would do all of its work (a draft
+// tree's layer of 64 experts of 1280 x 3584: 194 us against %TREE%).
 //
 // CTAs draw tasks from one queue, gate tasks first.  A down task waits for the gate tasks of its
 // token tile; those were drawn before it by CTAs that are running, so no wait depends on
 // a CTA that has not started.  Warp 0 draws, publishes the task to the other roles in a ring of
-// shared memory and streams the operands (x's rows gathered by TMA); it runs ahead of the others across tasks, so
-// that the stream does not stop between them.
+// shared memory and streams the operands (x's rows gathered by TMA); it runs ahead of the others across
+// tasks, so that the stream does not stop between them.  Warp 2 puts products of scales into shared memory,
+// warp 3 tells other CTAs what the epilogue warps 4..11 have stored (a release waits for the stores: it would hold them up
+// for 2 us a task) and quantises h: a block of 128 columns of h may be several tasks', whoever completes it
+// reads it back.
 #include <mutex>
 
 #include "moe.cuh"
@@ -19,19 +24,22 @@ namespace {
 
 using namespace ee;
 
-constexpr int kThreads = 384;          // warp 0 tasks and TMA, 1 MMA, 2 TMEM, 3 none; 4..11 epilogue
-constexpr int kEpiWarps = 8;           // two per TMEM lane quarter, half of the columns each
+constexpr int kThreads = 384;          // warp 0 tasks and TMA, 1 MMA, 2 TMEM and scales, 3 publishing; 4..11 epilogue
+constexpr int kEpiWarps = 8;           // two per TMEM lane quarter, every other 16 tokens each
 constexpr int kRegsAll = 168, kRegsEpi = 216, kRegsOther = 72;   // 256 * 216 + 128 * 72 = 384 * 168
-constexpr int BN = 256, kHalf = 128;   // weight rows of a task: 128 of gate and up each, or 256 of down
-constexpr int kBufs = 512 / BN;
-constexpr int kRing = 4;               // tasks published and not yet taken by every role
+constexpr int kRing = 4;               // tasks published and not yet done with by every role
+constexpr int kScRing = 8;             // k-blocks' scales
+constexpr int kMaxStages = 12;
 
 struct MoeParams {
   int T, H, I, E, k, n;                // n = T k
   int KB1, KB2;                        // 128-byte blocks along H and I
-  int IB, HT, HB;                      // gate tasks, down tasks of a token tile; scale blocks along H
-  int a_rows, stages;
+  int wg, wd;                          // rows of a tile of gate and up, of down
+  int IT, HT;                          // gate tasks, down tasks of a token tile
+  int IB, HB;                          // scale blocks along I and H
+  int b_rows, stages;
   MoeCtl* ctl;
+  uint32_t* sub;                       // [tile][IB] gate tasks of a block of h that are there (wg < 128)
   const MoeTile* tile;
   const int32_t* list;
   const int32_t* inv;
@@ -40,6 +48,7 @@ struct MoeParams {
   const float* s1;                     // [E][2][IB][blocks of H]
   const float* s2;                     // [E][HB][blocks of I]
   void* h;                             // [n][I] codes or bf16
+  float* hf;                           // [n][I] h before it is quantised
   float* hs;                           // [IB][n]
   float* y;                            // [n][H]
   __nv_bfloat16* out;
@@ -54,18 +63,34 @@ struct Task {
   int kind, blk, expert, tile, entry, rows;   // column block; token tile, its first entry and their number
 };
 
-template <bool kFp8>
+__device__ __forceinline__ void lds_2u64(uint32_t a, uint64_t& x, uint64_t& y) {
+  asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(x), "=l"(y) : "r"(a) : "memory");
+}
+// acc += scale * 16 columns; scales of the columns at shared address a
+__device__ __forceinline__ void add_scaled16(uint64_t (&acc)[8], const uint32_t (&r)[16], uint32_t a) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint64_t s0, s1;
+    lds_2u64(a + 16 * i, s0, s1);
+    acc[2 * i] = f2_fma(f2_pack(r[4 * i], r[4 * i + 1]), s0, acc[2 * i]);
+    acc[2 * i + 1] = f2_fma(f2_pack(r[4 * i + 2], r[4 * i + 3]), s1, acc[2 * i + 1]);
+  }
+}
+
+// NT: most tokens of a tile
+template <bool kFp8, int NT>
 __global__ void __launch_bounds__(kThreads, 1)
 moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW1,
                    const __grid_constant__ CUtensorMap tmH, const __grid_constant__ CUtensorMap tmW2, const MoeParams p) {
   constexpr int kCols = kFp8 ? 128 : 64;        // elements in 128 bytes
-  constexpr uint32_t kBoxBytes = 128 * 128;     // 128 weight rows
+  constexpr int kBufs = 512 / (2 * NT) < 8 ? 512 / (2 * NT) : 8;   // accumulators of two tiles
+  constexpr int kChunks = NT / 32;              // groups of 16 tokens of an epilogue warp
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
-  __shared__ __align__(8) uint64_t s_bars[2 * 8 + 2 * kBufs + 2 * kRing + 4 + 1];
+  __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 2 * 8 + 3 * kRing + 2 * kScRing + 1];
+  __shared__ __align__(16) float s_scale[kFp8 ? kScRing : 1][2][NT];
   __shared__ Task s_task[kRing];
-  __shared__ uint32_t s_top[2][2][128];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
   __shared__ int s_issued, s_consumed;
@@ -73,11 +98,13 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
   pdl_allow_next();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int S = p.stages;
-  const uint32_t aStage = ((uint32_t)p.a_rows * 128 + 1023) & ~1023u;
-  const uint32_t stBytes = aStage + 2 * kBoxBytes;
+  const uint32_t bStage = (uint32_t)p.b_rows * 128;            // tokens, then the weights' two tiles
+  const uint32_t stBytes = bStage + 2u * (uint32_t)max(p.wg, p.wd) * 128;
   const uint32_t ring = smem_u32(smem);
-  const uint32_t full0 = smem_u32(s_bars), empty0 = full0 + 8 * 8, tfull0 = empty0 + 8 * 8, tempty0 = tfull0 + 8 * kBufs,
-                 qfull0 = tempty0 + 8 * kBufs, qempty0 = qfull0 + 8 * kRing, pair0 = qempty0 + 8 * kRing, drain = pair0 + 8 * 4;
+  const uint32_t full0 = smem_u32(s_bars), empty0 = full0 + 8 * kMaxStages, tfull0 = empty0 + 8 * kMaxStages,
+                 tempty0 = tfull0 + 8 * 8, qfull0 = tempty0 + 8 * 8, qempty0 = qfull0 + 8 * kRing,
+                 edone0 = qempty0 + 8 * kRing, sfull0 = edone0 + 8 * kRing, sempty0 = sfull0 + 8 * kScRing,
+                 drain = sempty0 + 8 * kScRing;
   if (threadIdx.x == 0) {
     s_abort = 0;
     s_issued = 0;
@@ -92,9 +119,13 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
     }
     for (int a = 0; a < kRing; ++a) {
       mbar_init(qfull0 + 8 * a, 1);
-      mbar_init(qempty0 + 8 * a, 1 + kEpiWarps);
+      mbar_init(qempty0 + 8 * a, kEpiWarps + (kFp8 ? 3 : 2));
+      mbar_init(edone0 + 8 * a, kEpiWarps);
     }
-    for (int a = 0; a < 4; ++a) mbar_init(pair0 + 8 * a, 2);
+    for (int a = 0; a < kScRing; ++a) {
+      mbar_init(sfull0 + 8 * a, 1);
+      mbar_init(sempty0 + 8 * a, kEpiWarps);
+    }
     mbar_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
@@ -117,9 +148,9 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
   if (warp >= 4) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpi));
     const int q = warp & 3, half = (warp - 4) >> 2;
-    const int r = 32 * q + lane;                              // row of the tile
+    const int r = 32 * q + lane;                              // row of both weight tiles
     const uint32_t tq = tmem + ((uint32_t)(32 * q) << 16);
-    uint32_t it = 0, pairs = 0;                               // accumulators taken, meetings with the neighbour
+    uint32_t it = 0, sc = 0;                                  // accumulators and scales taken
     for (uint32_t nt = 0;; ++nt) {
       const uint32_t slot = nt % kRing;
       if (!__all_sync(0xffffffffu, mbar_wait(qfull0 + 8 * slot, (nt / kRing) & 1, &s_abort))) break;
@@ -128,140 +159,91 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
       if (lane == 0) mbar_arrive(qempty0 + 8 * slot);
       if (t.kind == kEnd) break;
       const bool gate = t.kind == kGate;
-      const bool mine = 32 * q < t.rows;                      // the warp has something to keep
-      const int entry = t.entry + min(r, t.rows - 1);
-      // accumulator columns of this warp: 64 of gate and 64 of up, or 128 of down
-      const uint32_t c0 = gate ? half * 64 : half * 128, c1 = gate ? 128 + half * 64 : half * 128 + 64;
-      uint64_t acc[64];
-      if constexpr (kFp8) {
-        const int KB = gate ? p.KB1 : p.KB2;
-        const int hb = min(t.blk * 2 + half, p.HB - 1);
-        const float* ws0 = gate ? p.s1 + ((int64_t)(2 * t.expert) * p.IB + t.blk) * KB : p.s2 + ((int64_t)t.expert * p.HB + hb) * KB;
-        const float* ws1 = gate ? ws0 + (int64_t)p.IB * KB : ws0;
-        const int xstep = gate ? p.T : p.n;
-        const float* xs = gate ? p.xs + p.list[entry] : p.hs + entry;
+      const int w = gate ? p.wg : p.wd;
+      const bool mine = 32 * q < w && half * 16 < t.rows;     // the warp has something to keep
+      uint64_t acc0[kChunks][8], acc1[kChunks][8];            // tokens (2 j + half) 16 .. + 15 of the two tiles
 #pragma unroll
-        for (int i = 0; i < 64; ++i) acc[i] = 0;
-        bool ok = true;
-        float sx = __ldcg(xs), sw0 = ws0[0], sw1 = ws1[0];
-        for (int kb = 0; kb < KB; ++kb, ++it) {
-          const uint32_t buf = it % kBufs, ph = (it / kBufs) & 1;
-          const float f0 = sx * sw0, f1 = sx * sw1;
-          if (kb + 1 < KB) {                                  // the next block's scales load behind this one
-            sx = __ldcg(xs + (int64_t)(kb + 1) * xstep);
-            sw0 = ws0[kb + 1];
-            sw1 = ws1[kb + 1];
-          }
-          if (!__all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * buf, ph, &s_abort))) {
-            ok = false;
-            break;
-          }
-          tc_fence_after();
-          if (mine) promote_2x64(acc, tq + buf * BN + c0, tq + buf * BN + c1, f0, f1);
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(tempty0 + 8 * buf);
-        }
-        if (!ok) break;
-      } else {
+      for (int j = 0; j < kChunks; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc0[j][i] = acc1[j][i] = 0;
+      const int KB = kFp8 ? (gate ? p.KB1 : p.KB2) : 1;
+      bool ok = true;
+      for (int kb = 0; kb < KB; ++kb, ++it) {
         const uint32_t buf = it % kBufs, ph = (it / kBufs) & 1;
-        ++it;
-        if (!__all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * buf, ph, &s_abort))) break;
+        if constexpr (kFp8)
+          ok = __all_sync(0xffffffffu, mbar_wait(sfull0 + 8 * (sc % kScRing), (sc / kScRing) & 1, &s_abort));
+        if (!ok || !__all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * buf, ph, &s_abort))) {
+          ok = false;
+          break;
+        }
         tc_fence_after();
         if (mine) {
-          uint32_t a[32], b[32];
-          const uint32_t at0 = tq + buf * BN + c0, at1 = tq + buf * BN + c1;
-          tc_ld32_nowait(at0, a);
-          tc_ld32_nowait(at0 + 32, b);
-          tc_wait_ld32(a);
-          tc_pin32(b);
+          const uint32_t sa = smem_u32(&s_scale[kFp8 ? sc % kScRing : 0][0][0]);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            acc[i] = f2_pack(a[2 * i], a[2 * i + 1]);
-            acc[16 + i] = f2_pack(b[2 * i], b[2 * i + 1]);
-          }
-          tc_ld32_nowait(at1, a);
-          tc_ld32_nowait(at1 + 32, b);
-          tc_wait_ld32(a);
-          tc_pin32(b);
+          for (int j = 0; j < kChunks; ++j) {
+            const int c = (2 * j + half) * 16;
+            if (c < t.rows) {
+              uint32_t a[16], b[16];
+              tc_ld16_nowait(tq + buf * (2 * NT) + c, a);
+              tc_ld16_nowait(tq + buf * (2 * NT) + NT + c, b);
+              tc_wait_ld16x2(a, b);
+              if constexpr (kFp8) {
+                add_scaled16(acc0[j], a, sa + 4 * c);
+                add_scaled16(acc1[j], b, sa + 4 * (NT + c));
+              } else {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            acc[32 + i] = f2_pack(a[2 * i], a[2 * i + 1]);
-            acc[48 + i] = f2_pack(b[2 * i], b[2 * i + 1]);
+                for (int i = 0; i < 8; ++i) {
+                  acc0[j][i] = f2_pack(a[2 * i], a[2 * i + 1]);
+                  acc1[j][i] = f2_pack(b[2 * i], b[2 * i + 1]);
+                }
+              }
+            }
           }
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(tempty0 + 8 * buf);
-      }
-      if (!mine) continue;
-      if (gate) {
-        const int i0 = t.blk * 128 + half * 64;               // first of 64 columns of h
-        float h[64];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          uint32_t g0, g1, u0, u1;
-          f2_unpack(acc[i], g0, g1);
-          f2_unpack(acc[32 + i], u0, u1);
-          h[2 * i] = silu_times(__uint_as_float(g0), __uint_as_float(u0));
-          h[2 * i + 1] = silu_times(__uint_as_float(g1), __uint_as_float(u1));
+        if (lane == 0) {
+          mbar_arrive(tempty0 + 8 * buf);
+          if constexpr (kFp8) mbar_arrive(sempty0 + 8 * (sc % kScRing));
         }
-        if constexpr (kFp8) {
-          uint32_t top = 0;
+        ++sc;
+      }
+      if (!ok) break;
+      if (mine && r < w) {
+        const int col = gate ? t.blk * w + r : t.blk * 2 * w + r;
 #pragma unroll
-          for (int i = 0; i < 64; ++i)
-            if (i0 + i < p.I) top = max(top, __float_as_uint(h[i]) & 0x7fffffffu);
-          // the block's other 64 columns are the neighbour warp's; two places in turn, so that one meeting
-          // a task is enough
-          s_top[pairs & 1][half][r] = top;
-          __syncwarp();
-          if (lane == 0) mbar_arrive(pair0 + 8 * q);
-          if (!__all_sync(0xffffffffu, mbar_wait(pair0 + 8 * q, pairs & 1, &s_abort))) break;
-          top = max(top, s_top[pairs & 1][half ^ 1][r]);
-          ++pairs;
-          const BlockScale b = block_scale(__uint_as_float(top));
-          if (r < t.rows) {
-            uint8_t* o = static_cast<uint8_t*>(p.h) + (size_t)entry * p.I + i0;
+        for (int j = 0; j < kChunks; ++j) {
+          const int c = (2 * j + half) * 16;
+          if (c >= t.rows) break;
+          const size_t e0 = (size_t)t.entry + c;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t w[4];
+          for (int i = 0; i < 8; ++i) {
+            uint32_t a[2], b[2];
+            f2_unpack(acc0[j][i], a[0], a[1]);
+            f2_unpack(acc1[j][i], b[0], b[1]);
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const float* v = h + 16 * i + 4 * j;
-                w[j] = pack_e4m3(to_code(v[0], b), to_code(v[1], b), to_code(v[2], b), to_code(v[3], b));
+            for (int d = 0; d < 2; ++d) {
+              const int tok = 2 * i + d;
+              if (c + tok >= t.rows) continue;
+              if (gate) {
+                const float h = silu_times(__uint_as_float(a[d]), __uint_as_float(b[d]));
+                if (col < p.I) {
+                  if constexpr (kFp8)
+                    __stcg(p.hf + (e0 + tok) * p.I + col, h);
+                  else
+                    static_cast<__nv_bfloat16*>(p.h)[(e0 + tok) * p.I + col] = __float2bfloat16_rn(h);
+                }
+              } else {
+                float* o = p.y + (e0 + tok) * p.H + col;
+                if (col < p.H) __stcg(o, __uint_as_float(a[d]));
+                if (col + w < p.H) __stcg(o + w, __uint_as_float(b[d]));
               }
-              if (i0 + 16 * i < p.I) *reinterpret_cast<uint4*>(o + 16 * i) = make_uint4(w[0], w[1], w[2], w[3]);
             }
-            if (half == 0) p.hs[(size_t)t.blk * p.n + entry] = b.scale;
-          }
-        } else if (r < t.rows) {
-          __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.h) + (size_t)entry * p.I + i0;
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (i0 + 8 * i < p.I)
-              *reinterpret_cast<uint4*>(o + 8 * i) =
-                  make_uint4(pack_bf16(h[8 * i], h[8 * i + 1]), pack_bf16(h[8 * i + 2], h[8 * i + 3]),
-                             pack_bf16(h[8 * i + 4], h[8 * i + 5]), pack_bf16(h[8 * i + 6], h[8 * i + 7]));
-        }
-        // the down tasks read h by TMA
-        asm volatile("fence.proxy.async;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) red_inc_release(p.ctl->gate_done + t.tile, 0xffffffffu);
-      } else {
-        const int o0 = t.blk * BN + half * 128;
-        if (r < t.rows) {
-          float* o = p.y + (size_t)entry * p.H + o0;
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            uint32_t x, y, z, w;
-            f2_unpack(acc[2 * i], x, y);
-            f2_unpack(acc[2 * i + 1], z, w);
-            if (o0 + 4 * i < p.H) __stcg(reinterpret_cast<uint4*>(o + 4 * i), make_uint4(x, y, z, w));
           }
         }
-        __syncwarp();
-        if (lane == 0) red_inc_release(&p.ctl->down_done, 0xffffffffu);
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(edone0 + 8 * slot);
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
@@ -269,7 +251,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true;
-      const int tiles = (int)p.ctl->tiles, gates = tiles * p.IB, total = gates + tiles * p.HT;
+      const int tiles = (int)p.ctl->tiles, gates = tiles * p.IT, total = gates + tiles * p.HT;
       int g = 0;
       if (lane == 0) g = (int)atomicAdd(&p.ctl->queue, 1u);
       g = __shfl_sync(0xffffffffu, g, 0);
@@ -284,22 +266,21 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
           break;
         }
         const bool gate = g < gates;
-        const int per = gate ? p.IB : p.HT, at = gate ? g : g - gates;
+        const int per = gate ? p.IT : p.HT, at = gate ? g : g - gates, w = gate ? p.wg : p.wd;
         const MoeTile e = p.tile[at / per];
         const int local = at - e.first * per, mt = local % e.tiles, blk = local / e.tiles;
         const int entry = e.entry0 + mt * kMoeTile, rows = min(kMoeTile, e.count - mt * kMoeTile);
         int tok[4] = {0, 0, 0, 0};
-        int wy0, wy1;                                         // the two boxes' first weight rows
+        int wy0, wy1;                                         // the two tiles' first weight rows
         if (gate) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) tok[j] = p.list[entry + min(4 * lane + j, rows - 1)];
-          wy0 = e.expert * 2 * p.I + blk * 128;
+          wy0 = e.expert * 2 * p.I + blk * w;
           wy1 = wy0 + p.I;
         } else {
-          wy0 = e.expert * p.H + blk * BN;
-          wy1 = wy0 + 128;
-          const uint32_t want = (uint32_t)(p.IB * 2 * ((rows + 31) / 32));
-          if (!__all_sync(0xffffffffu, wait_count_geq(p.ctl->gate_done + e.first + mt, want))) {
+          wy0 = e.expert * p.H + blk * 2 * w;
+          wy1 = wy0 + w;
+          if (!__all_sync(0xffffffffu, wait_count_geq(p.ctl->gate_done + e.first + mt, (uint32_t)(kFp8 ? p.IB : p.IT)))) {
             s_abort = 1;
             break;
           }
@@ -317,7 +298,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
           mbar_arrive(qfull0 + 8 * slot);
         }
         const int copies = gate ? (rows + 3) / 4 : (rows + 7) / 8;
-        const uint32_t bytes = 2 * kBoxBytes + (uint32_t)copies * (gate ? 512u : 1024u);
+        const uint32_t boxBytes = (uint32_t)w * 128, bytes = 2 * boxBytes + (uint32_t)copies * (gate ? 512u : 1024u);
         const int KB = gate ? p.KB1 : p.KB2;
         int next = 0;
         for (int kb = 0; kb < KB; ++kb) {
@@ -325,19 +306,19 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
             ok = false;
             break;
           }
-          const uint32_t fb = full0 + 8 * stage, sa = ring + (uint32_t)stage * stBytes, sw = sa + aStage;
+          const uint32_t fb = full0 + 8 * stage, sb = ring + (uint32_t)stage * stBytes, sw = sb + bStage;
           if (lane == 0) {
             mbar_expect_tx(fb, bytes);
             tma_load_2d(sw, gate ? &tmW1 : &tmW2, fb, kb * kCols, wy0);
-            tma_load_2d(sw + kBoxBytes, gate ? &tmW1 : &tmW2, fb, kb * kCols, wy1);
+            tma_load_2d(sw + boxBytes, gate ? &tmW1 : &tmW2, fb, kb * kCols, wy1);
             ++s_issued;
           }
           __syncwarp();
           if (lane < copies) {
             if (gate)
-              tma_gather4(sa + lane * 512, &tmX, fb, kb * kCols, tok[0], tok[1], tok[2], tok[3]);
+              tma_gather4(sb + lane * 512, &tmX, fb, kb * kCols, tok[0], tok[1], tok[2], tok[3]);
             else
-              tma_load_2d(sa + lane * 1024, &tmH, fb, kb * kCols, entry + 8 * lane);
+              tma_load_2d(sb + lane * 1024, &tmH, fb, kb * kCols, entry + 8 * lane);
           }
           __syncwarp();
           if (kb == KB - 1 - min(KB - 1, 3) && lane == 0) next = (int)atomicAdd(&p.ctl->queue, 1u);
@@ -349,20 +330,22 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
         g = __shfl_sync(0xffffffffu, next, 0);
       }
     } else if (warp == 1) {
-      constexpr uint32_t idesc = kFp8 ? idesc_e4m3(128, BN) : idesc_bf16(128, BN);
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
-      const uint64_t ad0 = smem_desc_sw128(__shfl_sync(0xffffffffu, ring, 0));
+      const uint64_t bd0 = smem_desc_sw128(__shfl_sync(0xffffffffu, ring, 0));
       int stage = 0, consumed = 0;
       uint32_t phase = 0, it = 0;
       bool ok = true;
       for (uint32_t nt = 0; ok; ++nt) {
         const uint32_t slot = nt % kRing;
         if (!__all_sync(0xffffffffu, mbar_wait(qfull0 + 8 * slot, (nt / kRing) & 1, &s_abort))) break;
-        const int kind = s_task[slot].kind;
-        __syncwarp();
+        const int kind = __shfl_sync(0xffffffffu, s_task[slot].kind, 0);
+        const int rows = __shfl_sync(0xffffffffu, s_task[slot].rows, 0);
         if (lane == 0) mbar_arrive(qempty0 + 8 * slot);
         if (kind == kEnd) break;
         const int KB = kind == kGate ? p.KB1 : p.KB2;
+        const uint64_t tile2 = (uint64_t)((kind == kGate ? p.wg : p.wd) * 128 >> 4);
+        const int N = (rows + 15) & ~15;
+        const uint32_t idesc = kFp8 ? idesc_e4m3(128, N) : idesc_bf16(128, N);
         for (int kb = 0; kb < KB; ++kb) {
           const uint32_t buf = it % kBufs, ph = (it / kBufs) & 1;
           if (((kFp8 || kb == 0) && !__all_sync(0xffffffffu, mbar_wait(tempty0 + 8 * buf, ph ^ 1, &s_abort))) ||
@@ -372,14 +355,19 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
           }
           tc_fence_after();
           if (elect_one()) {
-            const uint64_t ad = ad0 + (uint64_t)(stage * (stBytes >> 4));
-            const uint64_t bd = ad + (uint64_t)(aStage >> 4);
+            const uint64_t bd = bd0 + (uint64_t)(stage * (stBytes >> 4));
+            const uint64_t ad = bd + (uint64_t)(bStage >> 4);
+            const uint32_t d = tm + buf * (2 * NT);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {                     // 32 bytes along K each
-              if constexpr (kFp8)
-                tc_mma_f8(tm + buf * BN, ad + (uint64_t)(2 * k), bd + (uint64_t)(2 * k), idesc, k != 0 ? 1u : 0u);
-              else
-                tc_mma(tm + buf * BN, ad + (uint64_t)(2 * k), bd + (uint64_t)(2 * k), idesc, kb + k != 0 ? 1u : 0u);
+              const uint32_t add = (kFp8 ? k : kb + k) != 0 ? 1u : 0u;
+              if constexpr (kFp8) {
+                tc_mma_f8(d, ad + (uint64_t)(2 * k), bd + (uint64_t)(2 * k), idesc, add);
+                tc_mma_f8(d + NT, ad + tile2 + (uint64_t)(2 * k), bd + (uint64_t)(2 * k), idesc, add);
+              } else {
+                tc_mma(d, ad + (uint64_t)(2 * k), bd + (uint64_t)(2 * k), idesc, add);
+                tc_mma(d + NT, ad + tile2 + (uint64_t)(2 * k), bd + (uint64_t)(2 * k), idesc, add);
+              }
             }
             tc_commit(empty0 + 8 * stage);
             if (kFp8 || kb == KB - 1) tc_commit(tfull0 + 8 * buf);
@@ -395,8 +383,127 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
         if (!kFp8) ++it;
       }
       if (lane == 0) s_consumed = consumed;
+    } else if (warp == 2) {
+      if constexpr (kFp8) {
+        // scale of (k-block, token, weight tile): four tokens a lane, four k-blocks' loads at once
+        uint32_t sc = 0;
+        bool ok = true;
+        for (uint32_t nt = 0; ok; ++nt) {
+          const uint32_t slot = nt % kRing;
+          if (!__all_sync(0xffffffffu, mbar_wait(qfull0 + 8 * slot, (nt / kRing) & 1, &s_abort))) break;
+          const Task t = s_task[slot];
+          __syncwarp();
+          if (lane == 0) mbar_arrive(qempty0 + 8 * slot);
+          if (t.kind == kEnd) break;
+          const bool gate = t.kind == kGate;
+          const int KB = gate ? p.KB1 : p.KB2;
+          const float *ws0, *ws1;
+          if (gate) {
+            ws0 = p.s1 + ((int64_t)(2 * t.expert) * p.IB + t.blk * p.wg / kBlk) * KB;
+            ws1 = ws0 + (int64_t)p.IB * KB;
+          } else {
+            ws0 = p.s2 + ((int64_t)t.expert * p.HB + min(t.blk * 2 * p.wd / kBlk, p.HB - 1)) * KB;
+            ws1 = p.s2 + ((int64_t)t.expert * p.HB + min((t.blk * 2 + 1) * p.wd / kBlk, p.HB - 1)) * KB;
+          }
+          const float* xs = gate ? p.xs : p.hs;
+          const int xstep = gate ? p.T : p.n;
+          int at[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int e = t.entry + min(4 * lane + j, t.rows - 1);
+            at[j] = gate ? p.list[e] : e;
+          }
+          for (int kb = 0; kb < KB && ok; kb += 4) {
+            float f[4][4], w0[4], w1[4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+              if (kb + b < KB) {
+                const float* row = xs + (int64_t)(kb + b) * xstep;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f[b][j] = __ldcg(row + at[j]);
+                w0[b] = ws0[kb + b];
+                w1[b] = ws1[kb + b];
+              }
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+              if (kb + b < KB && ok) {
+                const uint32_t e = sc % kScRing;
+                ok = __all_sync(0xffffffffu, mbar_wait(sempty0 + 8 * e, ((sc / kScRing) & 1) ^ 1, &s_abort));
+                if (ok && 4 * lane < NT) {
+                  *reinterpret_cast<float4*>(&s_scale[e][0][4 * lane]) =
+                      make_float4(f[b][0] * w0[b], f[b][1] * w0[b], f[b][2] * w0[b], f[b][3] * w0[b]);
+                  *reinterpret_cast<float4*>(&s_scale[e][1][4 * lane]) =
+                      make_float4(f[b][0] * w1[b], f[b][1] * w1[b], f[b][2] * w1[b], f[b][3] * w1[b]);
+                }
+                __syncwarp();
+                if (ok && lane == 0) mbar_arrive(sfull0 + 8 * e);
+                ++sc;
+              }
+          }
+        }
+      }
+    } else {
+      for (uint32_t nt = 0;; ++nt) {
+        const uint32_t slot = nt % kRing;
+        if (!__all_sync(0xffffffffu, mbar_wait(qfull0 + 8 * slot, (nt / kRing) & 1, &s_abort))) break;
+        const Task t = s_task[slot];
+        if (t.kind == kEnd) break;
+        if (!__all_sync(0xffffffffu, mbar_wait(edone0 + 8 * slot, (nt / kRing) & 1, &s_abort))) break;
+        if (lane == 0) mbar_arrive(qempty0 + 8 * slot);
+        if (t.kind == kDown) {
+          if (lane == 0) red_inc_release(&p.ctl->down_done, 0xffffffffu);
+          continue;
+        }
+        if constexpr (kFp8) {
+          const int b = t.blk * p.wg / kBlk;                  // the block of h
+          if (p.wg < kBlk) {
+            uint32_t last = 0;
+            if (lane == 0) {
+              const uint32_t parts = (uint32_t)((min(kBlk, p.I - b * kBlk) + p.wg - 1) / p.wg);
+              last = atom_inc_acq_rel(p.sub + t.tile * p.IB + b, parts - 1) == parts - 1;
+            }
+            if (!__shfl_sync(0xffffffffu, last, 0)) continue;
+          }
+          const int col = b * kBlk + 4 * lane;
+          const bool in = col < p.I;
+          for (int r0 = 0; r0 < t.rows; r0 += 8) {            // a token's block a warp, eight loads in flight
+            float4 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (in && r0 + i < t.rows)
+                v[i] = __ldcg(reinterpret_cast<const float4*>(p.hf + (size_t)(t.entry + r0 + i) * p.I + col));
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (r0 + i < t.rows) {
+                const uint32_t m = 0x7fffffffu;
+                const uint32_t top = __reduce_max_sync(
+                    0xffffffffu, max(max(__float_as_uint(v[i].x) & m, __float_as_uint(v[i].y) & m),
+                                     max(__float_as_uint(v[i].z) & m, __float_as_uint(v[i].w) & m)));
+                const BlockScale s = block_scale(__uint_as_float(top));
+                const size_t e = (size_t)(t.entry + r0 + i);
+                if (in)
+                  *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(p.h) + e * p.I + col) =
+                      pack_e4m3(to_code(v[i].x, s), to_code(v[i].y, s), to_code(v[i].z, s), to_code(v[i].w, s));
+                if (lane == 0) p.hs[(size_t)b * p.n + e] = s.scale;
+              }
+          }
+        }
+        asm volatile("fence.proxy.async;" ::: "memory");      // down tasks read h by TMA
+        __syncwarp();
+        if (lane == 0) red_inc_release(p.ctl->gate_done + t.tile, 0xffffffffu);
+      }
     }
   }
+
+  // one code for all warps from here: as many registers as it was compiled for (a warpgroup has to
+  // meet between two changes of its registers)
+  __syncthreads();
+  if (warp >= 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsAll));
+  else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsAll));
+  tc_fence_before();
+  __syncthreads();
 
   // ---- the sum over a token's experts, all warps ------------------------------------
   // one code for all warps from here: as many registers as it was compiled for (a warpgroup has to
@@ -407,7 +514,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
   tc_fence_before();
   __syncthreads();
   if (!s_abort) {
-    if (threadIdx.x == 0 && !wait_count_geq(&p.ctl->down_done, p.ctl->quarters * 2u * (uint32_t)p.HT)) s_abort = 1;
+    if (threadIdx.x == 0 && !wait_count_geq(&p.ctl->down_done, p.ctl->tiles * (uint32_t)p.HT)) s_abort = 1;
     __syncthreads();
   }
   if (!s_abort) {
@@ -468,12 +575,14 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
   }
 }
 
-template <bool kFp8>
+template <bool kFp8, int NT>
 ee_status launch(const void* x, int64_t x_stride, const void* w1, const void* w2, MoeParams& p, cudaStream_t stream) {
   const uint64_t es = kFp8 ? 1 : 2;
-  const size_t stage = (((size_t)p.a_rows * 128 + 1023) & ~(size_t)1023) + 2 * 128 * 128;
-  p.stages = (int)std::min<size_t>(8, (size_t)(222 * 1024) / stage);
-  const size_t smem = 1024 + p.stages * stage;
+  const size_t wide = (size_t)std::max(p.wg, p.wd), stage = (size_t)p.b_rows * 128 + 2 * wide * 128;
+  // an MMA takes 128 rows of a tile of fewer: what follows, and the lanes are not looked at
+  const size_t slack = 1024 + (128 - (size_t)std::min(p.wg, p.wd)) * 128;
+  p.stages = (int)std::min<size_t>(kMaxStages, ((size_t)(214 * 1024) - slack) / stage);
+  const size_t smem = slack + p.stages * stage;
   CUtensorMap tmX, tmW1, tmH, tmW2;
   const auto encode = [](CUtensorMap* m, const void* base, uint64_t cols, uint64_t rows, uint64_t stride, uint32_t box) {
     if constexpr (kFp8) return encode_u8_tmap_2d(m, base, cols, rows, stride, 128, box);
@@ -481,8 +590,8 @@ ee_status launch(const void* x, int64_t x_stride, const void* w1, const void* w2
     const uint32_t boxes[2] = {64, box};
     return encode_bf16_tmap(m, base, 2, dims, strides, boxes);
   };
-  if (!encode(&tmX, x, p.H, p.T, x_stride, 1) || !encode(&tmW1, w1, p.H, (uint64_t)p.E * 2 * p.I, p.H, 128) ||
-      !encode(&tmH, p.h, p.I, p.n, p.I, 8) || !encode(&tmW2, w2, p.I, (uint64_t)p.E * p.H, p.I, 128))
+  if (!encode(&tmX, x, p.H, p.T, x_stride, 1) || !encode(&tmW1, w1, p.H, (uint64_t)p.E * 2 * p.I, p.H, p.wg) ||
+      !encode(&tmH, p.h, p.I, p.n, p.I, 8) || !encode(&tmW2, w2, p.I, (uint64_t)p.E * p.H, p.I, p.wd))
     return EE_ERR_CUDA;
   p.KB1 = (int)((p.H * es + 127) / 128);
   p.KB2 = (int)((p.I * es + 127) / 128);
@@ -494,11 +603,11 @@ ee_status launch(const void* x, int64_t x_stride, const void* w1, const void* w2
     static bool set[kMaxDevices] = {};
     std::lock_guard<std::mutex> lock(mu);
     if (!set[dev]) {
-      EE_CUDA_OK(cudaFuncSetAttribute(moe_experts_kernel<kFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024));
+      EE_CUDA_OK(cudaFuncSetAttribute(moe_experts_kernel<kFp8, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 214 * 1024));
       set[dev] = true;
     }
   }
-  EE_CUDA_OK(launch_pdl(moe_experts_kernel<kFp8>, dim3(kNumSMs), dim3(kThreads), smem, stream, 1, tmX, tmW1, tmH, tmW2, p));
+  EE_CUDA_OK(launch_pdl(moe_experts_kernel<kFp8, NT>, dim3(kNumSMs), dim3(kThreads), smem, stream, 1, tmX, tmW1, tmH, tmW2, p));
   return EE_OK;
 }
 
@@ -562,11 +671,21 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   p.E = E;
   p.k = k;
   p.n = T * k;
-  p.IB = (I + 127) / 128;
-  p.HT = (H + BN - 1) / BN;
+  // the widest tiles of which the tiles in use at most make a task for nearly every SM
+  const int64_t most = std::min<int64_t>(E, p.n);
+  p.wg = p.wd = 128;
+  while (p.wg > 32 && most * ((I + p.wg - 1) / p.wg) < 100) p.wg /= 2;
+  while (p.wd > 32 && most * ((H + 2 * p.wd - 1) / (2 * p.wd)) < 2 * ee::kNumSMs) p.wd /= 2;
+  p.IT = (I + p.wg - 1) / p.wg;
+  p.HT = (H + 2 * p.wd - 1) / (2 * p.wd);
+  p.IB = (I + kBlk - 1) / kBlk;
   p.HB = blocks;
-  p.a_rows = std::min(128, (T + 7) / 8 * 8);
+  const int nt = T <= 32 ? 32 : 128;
+  p.b_rows = std::min(nt, (T + 15) / 16 * 16);
   p.ctl = r.ctl;
+  p.sub = reinterpret_cast<uint32_t*>(base + l.sub);
+  r.sub = fp8 && p.wg < kBlk ? p.sub : nullptr;
+  r.n_sub = l.max_tiles * p.IB;
   p.tile = r.tile;
   p.list = r.list;
   p.inv = r.inv;
@@ -575,6 +694,7 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   p.s1 = w1_scale_or_null;
   p.s2 = w2_scale_or_null;
   p.h = base + l.h;
+  p.hf = reinterpret_cast<float*>(base + l.hf);
   p.hs = reinterpret_cast<float*>(base + l.hs);
   p.y = reinterpret_cast<float*>(base + l.y);
   p.out = reinterpret_cast<__nv_bfloat16*>(out);
@@ -584,6 +704,7 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   p.err = ee::err_word(ws);
   const ee_status st = ee::launch_moe_route(r, (cudaStream_t)stream);
   if (st != EE_OK) return st;
-  return fp8 ? launch<true>(r.xq, H, w1, w2, p, (cudaStream_t)stream)
-             : launch<false>(x, x_stride, w1, w2, p, (cudaStream_t)stream);
+  const cudaStream_t s = (cudaStream_t)stream;
+  if (fp8) return nt == 32 ? launch<true, 32>(r.xq, H, w1, w2, p, s) : launch<true, 128>(r.xq, H, w1, w2, p, s);
+  return nt == 32 ? launch<false, 32>(x, x_stride, w1, w2, p, s) : launch<false, 128>(x, x_stride, w1, w2, p, s);
 }

@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(kThreads) moe_route_kernel(const RouteParams p
   constexpr int EP = 8 * NT;
   extern __shared__ float s_red[];                 // [kWarps][kTok][EP], the first becomes the CTA's sums
   __shared__ int s_last;
-  __shared__ uint64_t s_scan[kWarps];
+  __shared__ uint32_t s_scan[kWarps];
   pdl_allow_next();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)blockIdx.x % p.cl, t0 = (int)blockIdx.x / p.cl * kTok;
@@ -195,6 +195,8 @@ __global__ void __launch_bounds__(kThreads) moe_route_kernel(const RouteParams p
   int* s_off = reinterpret_cast<int*>(pre + ((p.E * words + 1) & ~1));
   for (int i = threadIdx.x; i < p.E * words; i += kThreads) mask[i] = 0;
   for (int i = threadIdx.x; i < p.max_tiles; i += kThreads) p.ctl->gate_done[i] = 0;
+  if (p.sub)
+    for (int i = threadIdx.x; i < p.n_sub; i += kThreads) p.sub[i] = 0;
   if (threadIdx.x == 0) {
     p.ctl->route_ticket = 0;
     p.ctl->queue = 0;
@@ -212,33 +214,30 @@ __global__ void __launch_bounds__(kThreads) moe_route_kernel(const RouteParams p
       pre[threadIdx.x * words + w] = (uint16_t)cnt;
       cnt += __popc(mask[threadIdx.x * words + w]);
     }
-  // running numbers of entries, tiles and quarters in one scan (20 bits each: at most 2^16 entries)
+  // running numbers of entries and tiles in one scan (at most 2^16 entries, 2^10 tiles)
   const int tiles = (cnt + kMoeTile - 1) / kMoeTile;
-  const uint64_t own = (uint64_t)cnt | (uint64_t)tiles << 20 | (uint64_t)((cnt + 31) / 32) << 40;
-  uint64_t incl = own;
+  const uint32_t own = (uint32_t)cnt | (uint32_t)tiles << 20;
+  uint32_t incl = own;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const uint64_t o = __shfl_up_sync(0xffffffffu, incl, d);
+    const uint32_t o = __shfl_up_sync(0xffffffffu, incl, d);
     if (lane >= d) incl += o;
   }
   if (lane == 31) s_scan[warp] = incl;
   __syncthreads();
   for (int w = 0; w < warp; ++w) incl += s_scan[w];
   if ((int)threadIdx.x < p.E) {
-    const uint64_t before = incl - own;
+    const uint32_t before = incl - own;
     MoeTile m;
     m.expert = (int)threadIdx.x;
     m.entry0 = (int)(before & 0xfffffu);
     m.count = cnt;
-    m.first = (int)(before >> 20 & 0xfffffu);
+    m.first = (int)(before >> 20);
     m.tiles = tiles;
     m.pad[0] = m.pad[1] = m.pad[2] = 0;
     s_off[threadIdx.x] = m.entry0;
     for (int i = 0; i < tiles; ++i) p.tile[m.first + i] = m;
-    if ((int)threadIdx.x == p.E - 1) {
-      p.ctl->tiles = (uint32_t)(incl >> 20 & 0xfffffu);
-      p.ctl->quarters = (uint32_t)(incl >> 40);
-    }
+    if ((int)threadIdx.x == p.E - 1) p.ctl->tiles = incl >> 20;
   }
   __syncthreads();
   for (int i = threadIdx.x; i < n; i += kThreads) {
