@@ -11,7 +11,7 @@
 // partial sums through distributed shared memory, always in the same order.
 #include <mutex>
 
-#include "block_mma.cuh"
+#include "few.cuh"
 
 namespace {
 
@@ -320,6 +320,57 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
   }
 }
 
+// Up to 8 tokens: a CTA takes 16 weight rows, its warps every eighth block of them.
+__global__ void __launch_bounds__(kFewWarps * 32, 2) fp8_linear_few_kernel(const uint8_t* x, const uint8_t* w, int K, const LinParams p) {
+  constexpr int kFlight = 4;                      // blocks of a warp whose loads are under way together
+  __shared__ float s_part[kFewWarps][16][kFewTokens];
+  pdl_allow_next();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, tq = lane & 3;
+  const int o0 = (int)blockIdx.x * 16;
+  const int64_t r0 = o0 + g, r1 = r0 + 8;
+  const float* ws = p.ws + (int64_t)(o0 / kBlk) * p.KB;
+  const int t0 = min(2 * tq, p.n - 1), t1 = min(2 * tq + 1, p.n - 1);
+  float acc[4] = {0.f, 0.f, 0.f, 0.f};
+  pdl_wait();
+  for (int k0 = warp; k0 < p.KB; k0 += kFewWarps * kFlight) {
+    FewFrag a[kFlight], b[kFlight], v[kFlight];
+    float s[kFlight][3];
+#pragma unroll
+    for (int j = 0; j < kFlight; ++j) {
+      const int kb = k0 + j * kFewWarps, left = K - kb * kBlk;
+      const bool in = kb < p.KB;
+      a[j] = few_load(w + r0 * K + (int64_t)kb * kBlk, left, tq, in && r0 < p.N);
+      b[j] = few_load(w + r1 * K + (int64_t)kb * kBlk, left, tq, in && r1 < p.N);
+      v[j] = few_load(x + (int64_t)g * K + (int64_t)kb * kBlk, left, tq, in && g < p.n);
+      s[j][0] = in ? p.xs[(int64_t)kb * p.n + t0] : 0.f;
+      s[j][1] = in ? p.xs[(int64_t)kb * p.n + t1] : 0.f;
+      s[j][2] = in ? ws[kb] : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < kFlight; ++j)
+      if (k0 + j * kFewWarps < p.KB) {
+        float c[4] = {0.f, 0.f, 0.f, 0.f};
+        few_block<true>(c, a[j], b[j], v[j]);
+        const float f0 = s[j][0] * s[j][2], f1 = s[j][1] * s[j][2];
+        acc[0] = __fmaf_rn(c[0], f0, acc[0]);
+        acc[1] = __fmaf_rn(c[1], f1, acc[1]);
+        acc[2] = __fmaf_rn(c[2], f0, acc[2]);
+        acc[3] = __fmaf_rn(c[3], f1, acc[3]);
+      }
+  }
+  *reinterpret_cast<float2*>(&s_part[warp][g][2 * tq]) = make_float2(acc[0], acc[1]);
+  *reinterpret_cast<float2*>(&s_part[warp][g + 8][2 * tq]) = make_float2(acc[2], acc[3]);
+  __syncthreads();
+  const int t = threadIdx.x >> 4, o = threadIdx.x & 15;
+  if (t < p.n && o0 + o < p.N) {
+    float f = s_part[0][o][t];
+#pragma unroll
+    for (int i = 1; i < kFewWarps; ++i) f += s_part[i][o][t];
+    if (p.bias) f += __bfloat162float(p.bias[o0 + o]);
+    p.out[(int64_t)t * p.out_stride + o0 + o] = __float2bfloat16_rn(f);
+  }
+}
+
 template <int BN, bool kSplit>
 ee_status launch(const uint8_t* x, const uint8_t* w, int32_t K, LinParams& p, cudaStream_t stream) {
   p.NT = (p.N + BN - 1) / BN;
@@ -377,6 +428,11 @@ extern "C" ee_status ee_fp8_linear(const uint8_t* x, const float* x_scale, const
   p.err = ee::err_word(ws);
   const int64_t t128 = (int64_t)p.MT * ((N + 127) / 128), t256 = (int64_t)p.MT * ((N + 255) / 256);
   if (t256 > (1 << 30)) return EE_ERR_UNSUPPORTED;
+  if (n <= kFewTokens) {
+    EE_CUDA_OK(ee::launch_pdl(fp8_linear_few_kernel, dim3((unsigned)((N + 15) / 16)), dim3(kFewWarps * 32), 0,
+                              (cudaStream_t)stream, 1, x, w, K, p));
+    return EE_OK;
+  }
   // the widest split of a tile's k-blocks that the SMs hold at once
   p.ks = 1;
   if (t128 < ee::kNumSMs) p.ks = (int)std::min<int64_t>({8, (int64_t)ee::kNumSMs / t128, p.KB});

@@ -3,7 +3,7 @@
 // An ENTRY is a token at one of its experts; entries are numbered by expert, then by token.
 // A token TILE is up to 128 entries of one expert.
 #pragma once
-#include "block_mma.cuh"
+#include "few.cuh"
 
 namespace ee {
 
@@ -16,7 +16,7 @@ constexpr int kMoeTile = 128;
 struct MoeCtl {
   uint32_t route_ticket;     // zero between calls
   uint32_t queue;            // next task of the experts' kernel
-  uint32_t down_done;        // down tasks that stored their part of y
+  uint32_t down_done;        // down tasks that stored their part of y (few tokens: gate tasks, of h)
   uint32_t tiles;            // token tiles
   uint32_t pad[4];
   uint32_t gate_done[1];     // per token tile: gate tasks (8-bit weights: blocks of h) that are there
@@ -28,7 +28,7 @@ struct __align__(32) MoeTile {   // a token tile's expert
 };
 
 struct MoeLayout {
-  size_t ctl, sub, tile, ids, prob, list, inv, xq, xs, h, hf, hs, y, total;
+  size_t ctl, sub, tile, ids, prob, pe, list, inv, xq, xs, h, hf, hs, y, total;
   int max_tiles;             // token tiles of all experts, at most
 };
 inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t k) {
@@ -46,6 +46,7 @@ inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t 
   l.tile = take(sizeof(MoeTile) * (size_t)l.max_tiles);
   l.ids = take(4 * (size_t)n);
   l.prob = take(4 * (size_t)n);
+  l.pe = take(4 * (size_t)n);
   l.list = take(4 * (size_t)n);
   l.inv = take(4 * (size_t)n);
   l.xq = take((size_t)(T * H));
@@ -70,6 +71,7 @@ struct RouteParams {
   MoeTile* tile;
   int32_t* ids;              // [T][k] experts of a token, ascending
   float* prob;               // [T][k]
+  float* pe;                 // [T k] of an entry
   int32_t* list;             // [T k] token of an entry
   int32_t* inv;              // [T][k] entry of a token's j-th expert
   uint8_t* xq;               // [T][H] codes of x (NULL: not wanted)
@@ -78,5 +80,41 @@ struct RouteParams {
   float* prob_out;
 };
 ee_status launch_moe_route(const RouteParams& p, cudaStream_t stream);
+
+struct MoeParams {
+  int T, H, I, E, k, n;                // n = T k
+  int KB1, KB2;                        // 128-byte blocks along H and I
+  int wg, wd;                          // rows of a tile of gate and up, of down
+  int IT, HT;                          // gate tasks, down tasks of a token tile
+  int IB, HB;                          // scale blocks along I and H
+  int b_rows, stages;
+  const void* w1;
+  const void* w2;
+  const void* x;                       // codes or bf16
+  int64_t x_stride;
+  MoeCtl* ctl;
+  uint32_t* sub;                       // [tile][IB] gate tasks of a block of h that are there (wg < 128)
+  const MoeTile* tile;
+  const int32_t* list;
+  const int32_t* inv;
+  const float* prob;
+  const float* pe;                     // [n] of an entry
+  const float* xs;                     // [blocks of H][T]
+  const float* s1;                     // [E][2][IB][blocks of H]
+  const float* s2;                     // [E][HB][blocks of I]
+  void* h;                             // [n][I] codes or bf16
+  float* hf;                           // [n][I] h before it is quantised
+  float* hs;                           // [IB][n]
+  float* y;                            // [n][H]
+  __nv_bfloat16* out;
+  int64_t out_stride;
+  int vec;                             // rows of out are 8-byte aligned
+  const int32_t* live;
+  int32_t* err;
+};
+// For up to 8 tokens whose h fits beside another CTA's in shared memory (moe_few.cu): its bytes, or 0.
+size_t moe_few_smem(int T, int I, int k, bool fp8);
+ee_status launch_moe_few(const MoeParams& p, bool fp8, cudaStream_t stream);
+
 
 }  // namespace ee

@@ -31,33 +31,6 @@ constexpr int kRing = 4;               // tasks published and not yet done with 
 constexpr int kScRing = 8;             // k-blocks' scales
 constexpr int kMaxStages = 12;
 
-struct MoeParams {
-  int T, H, I, E, k, n;                // n = T k
-  int KB1, KB2;                        // 128-byte blocks along H and I
-  int wg, wd;                          // rows of a tile of gate and up, of down
-  int IT, HT;                          // gate tasks, down tasks of a token tile
-  int IB, HB;                          // scale blocks along I and H
-  int b_rows, stages;
-  MoeCtl* ctl;
-  uint32_t* sub;                       // [tile][IB] gate tasks of a block of h that are there (wg < 128)
-  const MoeTile* tile;
-  const int32_t* list;
-  const int32_t* inv;
-  const float* prob;
-  const float* xs;                     // [blocks of H][T]
-  const float* s1;                     // [E][2][IB][blocks of H]
-  const float* s2;                     // [E][HB][blocks of I]
-  void* h;                             // [n][I] codes or bf16
-  float* hf;                           // [n][I] h before it is quantised
-  float* hs;                           // [IB][n]
-  float* y;                            // [n][H]
-  __nv_bfloat16* out;
-  int64_t out_stride;
-  int vec;                             // rows of out are 8-byte aligned
-  const int32_t* live;
-  int32_t* err;
-};
-
 enum { kGate = 0, kDown = 1, kEnd = 2 };
 struct Task {
   int kind, blk, expert, tile, entry, rows;   // column block; token tile, its first entry and their number
@@ -576,7 +549,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
 }
 
 template <bool kFp8, int NT>
-ee_status launch(const void* x, int64_t x_stride, const void* w1, const void* w2, MoeParams& p, cudaStream_t stream) {
+ee_status launch(MoeParams& p, cudaStream_t stream) {
   const uint64_t es = kFp8 ? 1 : 2;
   const size_t wide = (size_t)std::max(p.wg, p.wd), stage = (size_t)p.b_rows * 128 + 2 * wide * 128;
   // an MMA takes 128 rows of a tile of fewer: what follows, and the lanes are not looked at
@@ -590,11 +563,9 @@ ee_status launch(const void* x, int64_t x_stride, const void* w1, const void* w2
     const uint32_t boxes[2] = {64, box};
     return encode_bf16_tmap(m, base, 2, dims, strides, boxes);
   };
-  if (!encode(&tmX, x, p.H, p.T, x_stride, 1) || !encode(&tmW1, w1, p.H, (uint64_t)p.E * 2 * p.I, p.H, p.wg) ||
-      !encode(&tmH, p.h, p.I, p.n, p.I, 8) || !encode(&tmW2, w2, p.I, (uint64_t)p.E * p.H, p.I, p.wd))
+  if (!encode(&tmX, p.x, p.H, p.T, p.x_stride, 1) || !encode(&tmW1, p.w1, p.H, (uint64_t)p.E * 2 * p.I, p.H, p.wg) ||
+      !encode(&tmH, p.h, p.I, p.n, p.I, 8) || !encode(&tmW2, p.w2, p.I, (uint64_t)p.E * p.H, p.I, p.wd))
     return EE_ERR_CUDA;
-  p.KB1 = (int)((p.H * es + 127) / 128);
-  p.KB2 = (int)((p.I * es + 127) / 128);
   {
     int dev = 0;
     const ee_status ds = current_device(&dev);
@@ -654,6 +625,7 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   r.tile = reinterpret_cast<ee::MoeTile*>(base + l.tile);
   r.ids = reinterpret_cast<int32_t*>(base + l.ids);
   r.prob = reinterpret_cast<float*>(base + l.prob);
+  r.pe = reinterpret_cast<float*>(base + l.pe);
   r.list = reinterpret_cast<int32_t*>(base + l.list);
   r.inv = reinterpret_cast<int32_t*>(base + l.inv);
   r.xq = fp8 ? reinterpret_cast<uint8_t*>(base + l.xq) : nullptr;
@@ -678,10 +650,16 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   while (p.wd > 32 && most * ((H + 2 * p.wd - 1) / (2 * p.wd)) < 2 * ee::kNumSMs) p.wd /= 2;
   p.IT = (I + p.wg - 1) / p.wg;
   p.HT = (H + 2 * p.wd - 1) / (2 * p.wd);
+  p.KB1 = (H * (fp8 ? 1 : 2) + 127) / 128;
+  p.KB2 = (I * (fp8 ? 1 : 2) + 127) / 128;
   p.IB = (I + kBlk - 1) / kBlk;
   p.HB = blocks;
   const int nt = T <= 32 ? 32 : 128;
   p.b_rows = std::min(nt, (T + 15) / 16 * 16);
+  p.w1 = w1;
+  p.w2 = w2;
+  p.x = fp8 ? static_cast<const void*>(r.xq) : x;
+  p.x_stride = fp8 ? H : x_stride;
   p.ctl = r.ctl;
   p.sub = reinterpret_cast<uint32_t*>(base + l.sub);
   r.sub = fp8 && p.wg < kBlk ? p.sub : nullptr;
@@ -690,6 +668,7 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   p.list = r.list;
   p.inv = r.inv;
   p.prob = r.prob;
+  p.pe = r.pe;
   p.xs = r.xs;
   p.s1 = w1_scale_or_null;
   p.s2 = w2_scale_or_null;
@@ -705,6 +684,7 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   const ee_status st = ee::launch_moe_route(r, (cudaStream_t)stream);
   if (st != EE_OK) return st;
   const cudaStream_t s = (cudaStream_t)stream;
-  if (fp8) return nt == 32 ? launch<true, 32>(r.xq, H, w1, w2, p, s) : launch<true, 128>(r.xq, H, w1, w2, p, s);
-  return nt == 32 ? launch<false, 32>(x, x_stride, w1, w2, p, s) : launch<false, 128>(x, x_stride, w1, w2, p, s);
+  if (ee::moe_few_smem(T, I, k, fp8)) return ee::launch_moe_few(p, fp8, s);
+  if (fp8) return nt == 32 ? launch<true, 32>(p, s) : launch<true, 128>(p, s);
+  return nt == 32 ? launch<false, 32>(p, s) : launch<false, 128>(p, s);
 }

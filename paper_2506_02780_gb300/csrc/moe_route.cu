@@ -244,6 +244,7 @@ __global__ void __launch_bounds__(kThreads) moe_route_kernel(const RouteParams p
     const int t = i / p.k, e = __ldcg(p.ids + i), at = e * words + (t >> 5);
     const int pos = s_off[e] + pre[at] + __popc(mask[at] & ((1u << (t & 31)) - 1u));
     p.list[pos] = t;
+    p.pe[pos] = __ldcg(p.prob + i);
     p.inv[i] = pos;
   }
 }
