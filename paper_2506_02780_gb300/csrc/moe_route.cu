@@ -5,10 +5,12 @@
 // of bf16 a warp and 16 columns, operands straight from global memory (a lane takes 8
 // neighbouring columns of its row of x and of the router; the order of the columns within
 // a sum is free, so x's and the router's fragments need only agree).  2 T E H operations are too few for
-// the tensor memory's set-up; what counts is that the router's rows are read by many
-// SMs at once.  Warps' sums are added in shared memory, CTAs' in distributed shared memory, in a
-// fixed order.  The last CTA to finish groups the tokens: a bit for each expert and token, so
-// that an entry's place is a count of bits and does not depend on who comes first.
+// the tensor memory's set-up; what bounds the kernel is the chain of waits for memory, so every warp's loads are
+// under way at once and the router's rows are read by many SMs.  Warps' sums are added in shared memory, CTAs' in
+// distributed shared memory, in a fixed order.  The last CTA to finish groups the tokens: a bit for
+// each expert and token, so that an entry's place is a count of bits and does not depend on who comes first.
+// Up to 16 tokens are one cluster's: its first CTA then chooses and groups without a way through global memory.
+// CTAs of their own quantise x.
 #include <mutex>
 
 #include "moe.cuh"
@@ -17,7 +19,9 @@ namespace {
 
 using namespace ee;
 
-constexpr int kThreads = 256, kWarps = 8, kTok = 16;
+constexpr int kTok = 16, kQuantUnits = 4;
+// more warps where their sums fit in shared memory
+__host__ __device__ constexpr int warps_of(int NT) { return NT <= 16 ? 16 : 8; }
 
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                           uint32_t b0, uint32_t b1) {
@@ -40,16 +44,45 @@ __device__ __forceinline__ uint32_t logit_key(float f) {
 
 // NT: groups of 8 experts (E <= 8 NT)
 template <int NT>
-__global__ void __launch_bounds__(kThreads) moe_route_kernel(const RouteParams p) {
-  constexpr int EP = 8 * NT;
+__global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const RouteParams p) {
+  constexpr int EP = 8 * NT, kWarps = warps_of(NT), kThreads = 32 * kWarps;
   extern __shared__ float s_red[];                 // [kWarps][kTok][EP], the first becomes the CTA's sums
   __shared__ int s_last;
+  __shared__ int s_ids[kTok * kMoeMaxTopK];        // of a single cluster's tokens
+  __shared__ float s_prob[kTok * kMoeMaxTopK];
   __shared__ uint32_t s_scan[kWarps];
   pdl_allow_next();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)blockIdx.x % p.cl, t0 = (int)blockIdx.x / p.cl * kTok;
+  const int groups = (p.T + kTok - 1) / kTok, routers = groups * p.cl;
+  const bool alone = groups == 1;
   pdl_wait();
   const int live = p.live ? max(0, min(p.T, ld_pinned(p.live))) : p.T;
+  if ((int)blockIdx.x >= routers) {                // x as codes: a warp and a block of one token, four at once
+    const int blocks = (p.H + kBlk - 1) / kBlk, units = live * blocks;
+    const int u0 = (((int)blockIdx.x - routers) * kWarps + warp) * kQuantUnits;
+    uint2 v[kQuantUnits];
+#pragma unroll
+    for (int j = 0; j < kQuantUnits; ++j) {
+      const int u = u0 + j, t = u / blocks, col = u % blocks * kBlk + lane * 4;
+      v[j] = make_uint2(0, 0);
+      if (u < units && col < p.H) v[j] = *reinterpret_cast<const uint2*>(p.x + t * p.x_stride + col);
+    }
+#pragma unroll
+    for (int j = 0; j < kQuantUnits; ++j) {
+      const int u = u0 + j, t = u / blocks, b = u % blocks, col = b * kBlk + lane * 4;
+      if (u >= units) break;
+      const uint32_t a = __vmaxu2(v[j].x & 0x7fff7fffu, v[j].y & 0x7fff7fffu);
+      const uint32_t top = __reduce_max_sync(0xffffffffu, max(a & 0xffffu, a >> 16));
+      const BlockScale s = block_scale(__uint_as_float(top << 16));
+      if (col < p.H)
+        *reinterpret_cast<uint32_t*>(p.xq + (size_t)t * p.H + col) =
+            pack_e4m3(to_code(bf16_lo(v[j].x), s), to_code(bf16_hi(v[j].x), s), to_code(bf16_lo(v[j].y), s),
+                      to_code(bf16_hi(v[j].y), s));
+      if (lane == 0) p.xs[(size_t)b * p.T + t] = s.scale;
+    }
+    return;                                        // (all CTAs of a cluster)
+  }
   if (t0 < live) {                                 // (the same in the whole cluster)
     const int nb = (p.H + kBlk - 1) / kBlk;
     const int b0 = nb * rank / p.cl, b1 = nb * (rank + 1) / p.cl;
@@ -86,21 +119,6 @@ __global__ void __launch_bounds__(kThreads) moe_route_kernel(const RouteParams p
       *reinterpret_cast<float2*>(r) = make_float2(acc[n][0], acc[n][1]);
       *reinterpret_cast<float2*>(r + 8 * EP) = make_float2(acc[n][2], acc[n][3]);
     }
-    if (p.xq) {                                    // a warp and a block of one token at a time
-      for (int i = warp; i < kTok * (b1 - b0); i += kWarps) {
-        const int t = t0 + i % kTok, b = b0 + i / kTok, col = b * kBlk + lane * 4;
-        if (t >= live) continue;
-        uint2 v = make_uint2(0, 0);
-        if (col < p.H) v = *reinterpret_cast<const uint2*>(p.x + t * p.x_stride + col);
-        const uint32_t a = __vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu);
-        const uint32_t top = __reduce_max_sync(0xffffffffu, max(a & 0xffffu, a >> 16));
-        const BlockScale s = block_scale(__uint_as_float(top << 16));
-        if (col < p.H)
-          *reinterpret_cast<uint32_t*>(p.xq + (size_t)t * p.H + col) = pack_e4m3(
-              to_code(bf16_lo(v.x), s), to_code(bf16_hi(v.x), s), to_code(bf16_lo(v.y), s), to_code(bf16_hi(v.y), s));
-        if (lane == 0) p.xs[(size_t)b * p.T + t] = s.scale;
-      }
-    }
     __syncthreads();
     for (int i = threadIdx.x; i < kTok * EP; i += kThreads) {
       float s = s_red[i];
@@ -110,8 +128,9 @@ __global__ void __launch_bounds__(kThreads) moe_route_kernel(const RouteParams p
     }
     if (p.cl > 1) cluster_sync();
     else __syncthreads();
-    // the CTAs of the cluster take the tokens in turn, a warp each
-    for (int row = rank + p.cl * warp; row < kTok && t0 + row < live; row += p.cl * kWarps) {
+    // the CTAs of the cluster take the tokens in turn, a warp each (a single cluster's first CTA all of them)
+    const int step = alone ? kWarps : p.cl * kWarps;
+    for (int row = alone ? (rank == 0 ? warp : kTok) : rank + p.cl * warp; row < kTok && t0 + row < live; row += step) {
       constexpr int kPer = (EP + 31) / 32;
       float l[kPer];
       uint32_t key[kPer];
@@ -175,8 +194,13 @@ __global__ void __launch_bounds__(kThreads) moe_route_kernel(const RouteParams p
       if (lane < p.k) {
         const size_t at = (size_t)(t0 + row) * p.k + before;
         const float pr = __fdiv_rn(pe, sum);
-        p.ids[at] = my_e;
-        p.prob[at] = pr;
+        if (alone) {
+          s_ids[at] = my_e;
+          s_prob[at] = pr;
+        } else {
+          p.ids[at] = my_e;
+          p.prob[at] = pr;
+        }
         if (p.ids_out) p.ids_out[at] = my_e;
         if (p.prob_out) p.prob_out[at] = pr;
       }
@@ -185,10 +209,15 @@ __global__ void __launch_bounds__(kThreads) moe_route_kernel(const RouteParams p
   }
 
   // ---- the last CTA groups the tokens by expert --------------------------------------
-  __syncthreads();
-  if (threadIdx.x == 0) s_last = atom_add_acq_rel(&p.ctl->route_ticket, 1u) == gridDim.x - 1;
-  __syncthreads();
-  if (!s_last) return;
+  if (alone) {
+    if (rank != 0) return;
+    __syncthreads();
+  } else {
+    __syncthreads();
+    if (threadIdx.x == 0) s_last = atom_add_acq_rel(&p.ctl->route_ticket, 1u) == (uint32_t)routers - 1;
+    __syncthreads();
+    if (!s_last) return;
+  }
   const int words = (live + 31) >> 5, n = live * p.k;
   uint32_t* mask = reinterpret_cast<uint32_t*>(s_red);          // [E][words]
   uint16_t* pre = reinterpret_cast<uint16_t*>(mask + p.E * words);   // bits in an expert's earlier words
@@ -203,12 +232,22 @@ __global__ void __launch_bounds__(kThreads) moe_route_kernel(const RouteParams p
     p.ctl->down_done = 0;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    const int t = i / p.k;
-    atomicOr(&mask[__ldcg(p.ids + i) * words + (t >> 5)], 1u << (t & 31));
+  constexpr int kAhead = 4;                        // entries of a thread whose loads are under way together
+  for (int i0 = threadIdx.x; i0 < n; i0 += kThreads * kAhead) {
+    int e[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = i0 + j * kThreads;
+      if (i < n) e[j] = alone ? s_ids[i] : __ldcg(p.ids + i);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = i0 + j * kThreads, t = i / p.k;
+      if (i < n) atomicOr(&mask[e[j] * words + (t >> 5)], 1u << (t & 31));
+    }
   }
   __syncthreads();
-  int cnt = 0;                                     // (E <= kThreads: thread e counts expert e's)
+  int cnt = 0;                                     // (at most 256 experts: thread e counts expert e's)
   if ((int)threadIdx.x < p.E)
     for (int w = 0; w < words; ++w) {
       pre[threadIdx.x * words + w] = (uint16_t)cnt;
@@ -240,17 +279,34 @@ __global__ void __launch_bounds__(kThreads) moe_route_kernel(const RouteParams p
     if ((int)threadIdx.x == p.E - 1) p.ctl->tiles = incl >> 20;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    const int t = i / p.k, e = __ldcg(p.ids + i), at = e * words + (t >> 5);
-    const int pos = s_off[e] + pre[at] + __popc(mask[at] & ((1u << (t & 31)) - 1u));
-    p.list[pos] = t;
-    p.pe[pos] = __ldcg(p.prob + i);
-    p.inv[i] = pos;
+  for (int i0 = threadIdx.x; i0 < n; i0 += kThreads * kAhead) {
+    int e[kAhead];
+    float pr[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = i0 + j * kThreads;
+      if (i < n) {
+        e[j] = alone ? s_ids[i] : __ldcg(p.ids + i);
+        pr[j] = alone ? s_prob[i] : __ldcg(p.prob + i);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = i0 + j * kThreads;
+      if (i >= n) break;
+      const int t = i / p.k, at = e[j] * words + (t >> 5);
+      const int pos = s_off[e[j]] + pre[at] + __popc(mask[at] & ((1u << (t & 31)) - 1u));
+      p.list[pos] = t;
+      p.pe[pos] = pr[j];
+      p.inv[i] = pos;
+      if (alone) p.prob[i] = pr[j];
+    }
   }
 }
 
 template <int NT>
 ee_status launch(const RouteParams& p, cudaStream_t stream) {
+  constexpr int kWarps = warps_of(NT);
   const size_t sums = (size_t)kWarps * kTok * 8 * NT * 4;
   const size_t words = ((size_t)p.T + 31) / 32;
   const size_t group = p.E * words * 6 + 4 + 4 * (size_t)p.E;
@@ -267,8 +323,10 @@ ee_status launch(const RouteParams& p, cudaStream_t stream) {
       have[dev] = smem;
     }
   }
-  const unsigned grid = (unsigned)((p.T + kTok - 1) / kTok * p.cl);
-  EE_CUDA_OK(launch_pdl(moe_route_kernel<NT>, dim3(grid), dim3(kThreads), smem, stream, (unsigned)p.cl, p));
+  const int routers = (p.T + kTok - 1) / kTok * p.cl, per = kWarps * kQuantUnits;
+  const int quants = p.xq ? (p.T * ((p.H + kBlk - 1) / kBlk) + per - 1) / per : 0;
+  const unsigned grid = (unsigned)(routers + (quants + p.cl - 1) / p.cl * p.cl);
+  EE_CUDA_OK(launch_pdl(moe_route_kernel<NT>, dim3(grid), dim3(32 * kWarps), smem, stream, (unsigned)p.cl, p));
   return EE_OK;
 }
 
