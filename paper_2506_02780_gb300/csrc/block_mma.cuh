@@ -21,6 +21,9 @@ constexpr float kLeastMax = 0x1p-100f;   // a block's maximum counts as at least
 // dims[0] bytes are contiguous; 128-byte swizzle, zero fill out of bounds
 bool encode_u8_tmap_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t stride_bytes,
                        uint32_t box_cols, uint32_t box_rows);
+// the same in 4-byte elements without a swizzle: rows of a box lie behind one another
+bool encode_u32_tmap_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t stride_bytes,
+                        uint32_t box_cols, uint32_t box_rows);
 
 // Instruction descriptor of kind::f8f6f4: e4m3 A and B, fp32 D, both K-major.
 __host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N) {

@@ -248,6 +248,9 @@ __device__ __forceinline__ bool wait_count_geq(const uint32_t* cnt, uint32_t tar
 __device__ __forceinline__ void red_inc_release(uint32_t* a, uint32_t last) {
   asm volatile("red.release.gpu.global.inc.u32 [%0], %1;" ::"l"(a), "r"(last) : "memory");
 }
+__device__ __forceinline__ void red_add_release(uint32_t* a, uint32_t v) {
+  asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(a), "r"(v) : "memory");
+}
 // the same with the count before it, and acquiring
 __device__ __forceinline__ uint32_t atom_inc_acq_rel(uint32_t* a, uint32_t last) {
   uint32_t old;

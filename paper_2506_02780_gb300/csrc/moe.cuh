@@ -26,9 +26,13 @@ struct __align__(32) MoeTile {   // a token tile's expert
   int first, tiles;            // its first tile and their number
   int pad[3];
 };
+struct FewEntry {            // of up to 8 tokens: an active expert's entry of a token, or -1, and its weight
+  int entry;
+  float p;
+};
 
 struct MoeLayout {
-  size_t ctl, sub, tile, ids, prob, pe, list, inv, xq, xs, h, hf, hs, y, total;
+  size_t ctl, sub, tile, few, ids, prob, list, inv, xq, xs, h, hf, hs, y, total;
   int max_tiles;             // token tiles of all experts, at most
 };
 inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t k) {
@@ -44,9 +48,9 @@ inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t 
   l.ctl = take(sizeof(MoeCtl) + 4 * (size_t)l.max_tiles);
   l.sub = take(4 * (size_t)l.max_tiles * (size_t)((I + kBlk - 1) / kBlk));
   l.tile = take(sizeof(MoeTile) * (size_t)l.max_tiles);
+  l.few = take(sizeof(FewEntry) * kFewTokens * kFewTokens * kMoeMaxTopK);
   l.ids = take(4 * (size_t)n);
   l.prob = take(4 * (size_t)n);
-  l.pe = take(4 * (size_t)n);
   l.list = take(4 * (size_t)n);
   l.inv = take(4 * (size_t)n);
   l.xq = take((size_t)(T * H));
@@ -69,9 +73,9 @@ struct RouteParams {
   uint32_t* sub;             // or NULL: [n_sub] counters to zero
   int n_sub;
   MoeTile* tile;
+  FewEntry* few;             // or NULL (more than 8 tokens): [active expert][8]
   int32_t* ids;              // [T][k] experts of a token, ascending
   float* prob;               // [T][k]
-  float* pe;                 // [T k] of an entry
   int32_t* list;             // [T k] token of an entry
   int32_t* inv;              // [T][k] entry of a token's j-th expert
   uint8_t* xq;               // [T][H] codes of x (NULL: not wanted)
@@ -95,10 +99,10 @@ struct MoeParams {
   MoeCtl* ctl;
   uint32_t* sub;                       // [tile][IB] gate tasks of a block of h that are there (wg < 128)
   const MoeTile* tile;
+  const FewEntry* few;
   const int32_t* list;
   const int32_t* inv;
   const float* prob;
-  const float* pe;                     // [n] of an entry
   const float* xs;                     // [blocks of H][T]
   const float* s1;                     // [E][2][IB][blocks of H]
   const float* s2;                     // [E][HB][blocks of I]
@@ -112,9 +116,8 @@ struct MoeParams {
   const int32_t* live;
   int32_t* err;
 };
-// For up to 8 tokens whose h fits beside another CTA's in shared memory (moe_few.cu): its bytes, or 0.
-size_t moe_few_smem(int T, int I, int k, bool fp8);
-ee_status launch_moe_few(const MoeParams& p, bool fp8, cudaStream_t stream);
-
+// Up to 8 tokens whose x and h fit in shared memory beside the rings (moe_few.cu): their depth and the bytes, or 0.
+int moe_few_stages(int T, int H, int I, int k, bool fp8, size_t* smem);
+ee_status launch_moe_few(MoeParams& p, bool fp8, cudaStream_t stream);
 
 }  // namespace ee

@@ -623,9 +623,9 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   r.max_tiles = l.max_tiles;
   r.ctl = reinterpret_cast<ee::MoeCtl*>(base + l.ctl);
   r.tile = reinterpret_cast<ee::MoeTile*>(base + l.tile);
+  r.few = T <= ee::kFewTokens ? reinterpret_cast<ee::FewEntry*>(base + l.few) : nullptr;
   r.ids = reinterpret_cast<int32_t*>(base + l.ids);
   r.prob = reinterpret_cast<float*>(base + l.prob);
-  r.pe = reinterpret_cast<float*>(base + l.pe);
   r.list = reinterpret_cast<int32_t*>(base + l.list);
   r.inv = reinterpret_cast<int32_t*>(base + l.inv);
   r.xq = fp8 ? reinterpret_cast<uint8_t*>(base + l.xq) : nullptr;
@@ -665,10 +665,10 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   r.sub = fp8 && p.wg < kBlk ? p.sub : nullptr;
   r.n_sub = l.max_tiles * p.IB;
   p.tile = r.tile;
+  p.few = r.few;
   p.list = r.list;
   p.inv = r.inv;
   p.prob = r.prob;
-  p.pe = r.pe;
   p.xs = r.xs;
   p.s1 = w1_scale_or_null;
   p.s2 = w2_scale_or_null;
@@ -684,7 +684,8 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   const ee_status st = ee::launch_moe_route(r, (cudaStream_t)stream);
   if (st != EE_OK) return st;
   const cudaStream_t s = (cudaStream_t)stream;
-  if (ee::moe_few_smem(T, I, k, fp8)) return ee::launch_moe_few(p, fp8, s);
+  size_t few = 0;
+  if (ee::moe_few_stages(T, H, I, k, fp8, &few)) return ee::launch_moe_few(p, fp8, s);
   if (fp8) return nt == 32 ? launch<true, 32>(p, s) : launch<true, 128>(p, s);
   return nt == 32 ? launch<false, 32>(p, s) : launch<false, 128>(p, s);
 }

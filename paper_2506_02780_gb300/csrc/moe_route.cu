@@ -36,6 +36,12 @@ __device__ __forceinline__ float ld_cluster_f(uint32_t a) {
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
   return v;
 }
+// (in the order in which they are written, so that all of a warp's loads are under way together)
+__device__ __forceinline__ uint4 ld_pinned16(const __nv_bfloat16* a) {
+  uint4 v;
+  asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(a));
+  return v;
+}
 // larger key, better logit; at least 1: a NaN is the worst
 __device__ __forceinline__ uint32_t logit_key(float f) {
   const uint32_t u = __float_as_uint(f);
@@ -50,12 +56,16 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
   __shared__ int s_last;
   __shared__ int s_ids[kTok * kMoeMaxTopK];        // of a single cluster's tokens
   __shared__ float s_prob[kTok * kMoeMaxTopK];
+  __shared__ uint32_t s_bits[kMoeMaxExperts];      // ... a bit for each expert and token
+  __shared__ int s_tile[kMoeMaxExperts];           // an expert's first tile
   __shared__ uint32_t s_scan[kWarps];
   pdl_allow_next();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)blockIdx.x % p.cl, t0 = (int)blockIdx.x / p.cl * kTok;
   const int groups = (p.T + kTok - 1) / kTok, routers = groups * p.cl;
   const bool alone = groups == 1;
+  if (alone)
+    for (int i = threadIdx.x; i < kMoeMaxExperts; i += kThreads) s_bits[i] = 0;
   pdl_wait();
   const int live = p.live ? max(0, min(p.T, ld_pinned(p.live))) : p.T;
   if ((int)blockIdx.x >= routers) {                // x as codes: a warp and a block of one token, four at once
@@ -95,8 +105,8 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
       const int col = c * 32 + tq * 8;
       const bool in = col < p.H;
       uint4 xa = zero, xb = zero;
-      if (in && t0 + g < live) xa = *reinterpret_cast<const uint4*>(p.x + (t0 + g) * p.x_stride + col);
-      if (in && t0 + g + 8 < live) xb = *reinterpret_cast<const uint4*>(p.x + (t0 + g + 8) * p.x_stride + col);
+      if (in && t0 + g < live) xa = ld_pinned16(p.x + (t0 + g) * p.x_stride + col);
+      if (in && t0 + g + 8 < live) xb = ld_pinned16(p.x + (t0 + g + 8) * p.x_stride + col);
       constexpr int kStep = NT < 8 ? NT : 8;
 #pragma unroll
       for (int n0 = 0; n0 < NT; n0 += kStep) {
@@ -104,7 +114,8 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
 #pragma unroll
         for (int n = 0; n < kStep; ++n) {
           const int e = (n0 + n) * 8 + g;
-          w[n] = in && e < p.E ? *reinterpret_cast<const uint4*>(p.router + (size_t)e * p.H + col) : zero;
+          w[n] = zero;
+          if (in && e < p.E) w[n] = ld_pinned16(p.router + (size_t)e * p.H + col);
         }
 #pragma unroll
         for (int n = 0; n < kStep; ++n) {
@@ -195,6 +206,7 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
         const size_t at = (size_t)(t0 + row) * p.k + before;
         const float pr = __fdiv_rn(pe, sum);
         if (alone) {
+          atomicOr(&s_bits[my_e], 1u << row);
           s_ids[at] = my_e;
           s_prob[at] = pr;
         } else {
@@ -205,7 +217,11 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
         if (p.prob_out) p.prob_out[at] = pr;
       }
     }
-    if (p.cl > 1) cluster_sync();                  // nobody leaves while a peer reads its sums
+    // nobody leaves while a peer reads its sums; who groups a single cluster's tokens waits at its end
+    if (p.cl > 1) {
+      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+      if (!alone || rank != 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
   }
 
   // ---- the last CTA groups the tokens by expert --------------------------------------
@@ -219,10 +235,11 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
     if (!s_last) return;
   }
   const int words = (live + 31) >> 5, n = live * p.k;
-  uint32_t* mask = reinterpret_cast<uint32_t*>(s_red);          // [E][words]
-  uint16_t* pre = reinterpret_cast<uint16_t*>(mask + p.E * words);   // bits in an expert's earlier words
+  uint32_t* mask = alone ? s_bits : reinterpret_cast<uint32_t*>(s_red);   // [E][words]
+  uint16_t* pre = reinterpret_cast<uint16_t*>(reinterpret_cast<uint32_t*>(s_red) + p.E * words);   // bits in an expert's earlier words
   int* s_off = reinterpret_cast<int*>(pre + ((p.E * words + 1) & ~1));
-  for (int i = threadIdx.x; i < p.E * words; i += kThreads) mask[i] = 0;
+  if (!alone)
+    for (int i = threadIdx.x; i < p.E * words; i += kThreads) mask[i] = 0;
   for (int i = threadIdx.x; i < p.max_tiles; i += kThreads) p.ctl->gate_done[i] = 0;
   if (p.sub)
     for (int i = threadIdx.x; i < p.n_sub; i += kThreads) p.sub[i] = 0;
@@ -231,14 +248,14 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
     p.ctl->queue = 0;
     p.ctl->down_done = 0;
   }
-  __syncthreads();
   constexpr int kAhead = 4;                        // entries of a thread whose loads are under way together
-  for (int i0 = threadIdx.x; i0 < n; i0 += kThreads * kAhead) {
+  if (!alone) __syncthreads();
+  for (int i0 = threadIdx.x; i0 < n && !alone; i0 += kThreads * kAhead) {
     int e[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const int i = i0 + j * kThreads;
-      if (i < n) e[j] = alone ? s_ids[i] : __ldcg(p.ids + i);
+      if (i < n) e[j] = __ldcg(p.ids + i);
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
@@ -246,7 +263,7 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
       if (i < n) atomicOr(&mask[e[j] * words + (t >> 5)], 1u << (t & 31));
     }
   }
-  __syncthreads();
+  if (!alone) __syncthreads();
   int cnt = 0;                                     // (at most 256 experts: thread e counts expert e's)
   if ((int)threadIdx.x < p.E)
     for (int w = 0; w < words; ++w) {
@@ -275,6 +292,10 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
     m.tiles = tiles;
     m.pad[0] = m.pad[1] = m.pad[2] = 0;
     s_off[threadIdx.x] = m.entry0;
+    s_tile[threadIdx.x] = m.first;
+    if (p.few && tiles)                            // (the entries' own are written behind the next barrier)
+      for (int t = 0; t < kFewTokens; ++t)
+        if (!(mask[threadIdx.x] >> t & 1u)) p.few[m.first * kFewTokens + t] = FewEntry{-1, 0.f};
     for (int i = 0; i < tiles; ++i) p.tile[m.first + i] = m;
     if ((int)threadIdx.x == p.E - 1) p.ctl->tiles = incl >> 20;
   }
@@ -297,11 +318,12 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
       const int t = i / p.k, at = e[j] * words + (t >> 5);
       const int pos = s_off[e[j]] + pre[at] + __popc(mask[at] & ((1u << (t & 31)) - 1u));
       p.list[pos] = t;
-      p.pe[pos] = pr[j];
+      if (p.few) p.few[s_tile[e[j]] * kFewTokens + t] = FewEntry{pos, pr[j]};
       p.inv[i] = pos;
       if (alone) p.prob[i] = pr[j];
     }
   }
+  if (alone && p.cl > 1 && live > 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 template <int NT>

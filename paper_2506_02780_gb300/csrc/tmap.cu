@@ -43,15 +43,25 @@ bool encode_bf16_tmap(CUtensorMap* map, const void* base, int rank, const uint64
   return r == CUDA_SUCCESS;
 }
 
-bool encode_u8_tmap_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t stride_bytes,
-                       uint32_t box_cols, uint32_t box_rows) {
+static bool encode_2d(CUtensorMap* map, CUtensorMapDataType type, CUtensorMapSwizzle swizzle, const void* base, uint64_t cols,
+                      uint64_t rows, uint64_t stride_bytes, uint32_t box_cols, uint32_t box_rows) {
   auto fn = get_encode();
   if (!fn) return false;
   const cuuint64_t d[2] = {cols, rows}, s[1] = {stride_bytes};
   const cuuint32_t bx[2] = {box_cols, box_rows}, es[2] = {1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), d, s, bx, es,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return fn(map, type, 2, const_cast<void*>(base), d, s, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool encode_u8_tmap_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t stride_bytes,
+                       uint32_t box_cols, uint32_t box_rows) {
+  return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_128B, base, cols, rows, stride_bytes, box_cols,
+                   box_rows);
+}
+bool encode_u32_tmap_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t stride_bytes,
+                        uint32_t box_cols, uint32_t box_rows) {
+  return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, CU_TENSOR_MAP_SWIZZLE_NONE, base, cols, rows, stride_bytes, box_cols,
+                   box_rows);
 }
 
 }  // namespace ee
