@@ -54,35 +54,26 @@ __device__ __forceinline__ void add_scaled32(uint64_t (&acc)[N], uint32_t (&r)[3
   for (int i = 0; i < 16; ++i) acc[G * 16 + i] = f2_fma(f2_pack(r[2 * i], r[2 * i + 1]), s, acc[G * 16 + i]);
 }
 
-// acc += s0 * the 64 columns at c0 and s1 * the 64 at c1 of this warp's lanes; the loads of the
-// second 64 run behind the sums of the first.
-__device__ __forceinline__ void promote_2x64(uint64_t (&acc)[64], uint32_t c0, uint32_t c1, float s0, float s1) {
-  uint32_t a[32], b[32];
-  tc_ld32_nowait(c0, a);
-  tc_ld32_nowait(c0 + 32, b);
-  const uint64_t p0 = f2_pack(__float_as_uint(s0), __float_as_uint(s0));
-  const uint64_t p1 = f2_pack(__float_as_uint(s1), __float_as_uint(s1));
-  tc_wait_ld32(a);
-  tc_pin32(b);
-  add_scaled32<0>(acc, a, p0);
-  tc_ld32_nowait(c1, a);
-  add_scaled32<1>(acc, b, p0);
-  tc_ld32_nowait(c1 + 32, b);
-  tc_wait_ld32(a);
-  tc_pin32(b);
-  add_scaled32<2>(acc, a, p1);
-  add_scaled32<3>(acc, b, p1);
-}
-// acc += s * the 64 columns at c
-__device__ __forceinline__ void promote_64(uint64_t (&acc)[32], uint32_t c, float s) {
+// acc += f * the 64 or 128 columns (G groups of 32) from c on of this warp's lanes; the loads of the
+// second 64 run behind the sums of the first
+template <int G>
+__device__ __forceinline__ void promote(uint64_t (&acc)[16 * G], uint32_t c, float f) {
   uint32_t a[32], b[32];
   tc_ld32_nowait(c, a);
   tc_ld32_nowait(c + 32, b);
-  const uint64_t p = f2_pack(__float_as_uint(s), __float_as_uint(s));
+  const uint64_t p = f2_pack(__float_as_uint(f), __float_as_uint(f));
   tc_wait_ld32(a);
   tc_pin32(b);
   add_scaled32<0>(acc, a, p);
+  if constexpr (G == 4) tc_ld32_nowait(c + 64, a);
   add_scaled32<1>(acc, b, p);
+  if constexpr (G == 4) {
+    tc_ld32_nowait(c + 96, b);
+    tc_wait_ld32(a);
+    tc_pin32(b);
+    add_scaled32<2>(acc, a, p);
+    add_scaled32<3>(acc, b, p);
+  }
 }
 
 // The code of x in a block whose largest magnitude is a: the e4m3 number nearest to 448 x / a.

@@ -5,7 +5,9 @@
 // ring, warp 1 multiplies each k-block (128 columns, 4 MMAs of 128 x BN x 32) into one of the
 // tensor memory's 512 / BN accumulators, and warps 4..11 add it, scaled, to fp32 sums in their
 // registers (block_mma.cuh).  A CTA walks its tiles without a stop between them: the ring and
-// the next tile's first MMAs run behind the stores.
+// the next tile's first MMAs run behind the stores, which go through shared memory (as 16-byte pieces
+// of 32 rows straight from the registers they hold the next tile up for 2 us; TMA would take them behind the loads it
+// has queued).
 // Few tokens: the stream of W bounds the call, so it has to come from every SM.  Where there
 // are fewer tiles than SMs, a cluster of up to 8 CTAs shares a tile's k-blocks and adds its
 // partial sums through distributed shared memory, always in the same order.
@@ -19,7 +21,7 @@ using namespace ee;
 
 constexpr int kThreads = 384;          // warp 0 TMA, 1 MMA, 2 TMEM, 3 none; 4..11 epilogue
 constexpr int kEpiWarps = 8;           // two per TMEM lane quarter, half of the columns each
-constexpr int kRegsAll = 168, kRegsEpi = 216, kRegsOther = 72;   // 256 * 216 + 128 * 72 = 384 * 168
+constexpr int kRegsAll = 168;          // a warp's at launch; the epilogue's take some of the others', kRegsEpi
 constexpr int BM = 128;
 
 struct LinParams {
@@ -36,6 +38,14 @@ struct LinParams {
 __device__ __forceinline__ void st_shared_f4(uint32_t a, float4 v) {
   asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
+__device__ __forceinline__ void st_shared_u4(uint32_t a, uint4 v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared_u4(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
 __device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
@@ -45,10 +55,16 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {
   return v;
 }
 
+constexpr uint32_t kOutBytes = 32 * 32 * 2;   // of an epilogue warp: 32 rows of 32 columns on their way out
+
 template <int BN, bool kSplit>
 __global__ void __launch_bounds__(kThreads, 1)
 fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const LinParams p) {
+  // what spills least
+  constexpr int kRegsEpi = BN < 256 ? 208 : kSplit ? 232 : 224, kRegsOther = 3 * kRegsAll - 2 * kRegsEpi;
+  constexpr bool kAllPromote = BN == 256;   // (also warps that have nothing to keep)
   constexpr int kBufs = 512 / BN;               // accumulators
+  constexpr int kGroups = BN / 64;              // groups of 32 columns of an epilogue warp
   constexpr int kCols = BN / 2;                 // columns of an epilogue warp
   constexpr uint32_t kWBytes = BN * kBlk;
   extern __shared__ uint8_t smem_raw[];
@@ -65,7 +81,7 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
   const uint32_t aBytes = (uint32_t)p.a_rows * kBlk;
   const uint32_t aStage = (aBytes + 1023) & ~1023u;        // x rows, then W rows: an MMA's rows past a_rows are
   const uint32_t stBytes = aStage + kWBytes;               // whatever follows, and so are lanes that nobody reads
-  const uint32_t ring = smem_u32(smem);
+  const uint32_t ring = smem_u32(smem), out0 = ring + (uint32_t)S * stBytes;
   const uint32_t full0 = smem_u32(s_bars), empty0 = full0 + 8 * 16, tfull0 = empty0 + 8 * 16, tempty0 = tfull0 + 8 * 4,
                  drain = tempty0 + 8 * 4;
   if (threadIdx.x == 0) {
@@ -91,17 +107,25 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  const int num_tiles = p.MT * p.NT;
+  const int ks = kSplit ? p.ks : 1;
+  const int rank = kSplit ? (int)blockIdx.x % ks : 0;
+  const int first = (int)blockIdx.x / ks, step = (int)gridDim.x / ks;
+  const int kb0 = p.KB * rank / ks, kb1 = p.KB * (rank + 1) / ks;   // (KB is at most 2^17)
+  if (warp == 3) {                              // the first weights on their way while the kernel in front still runs
+    const int n0 = first / p.MT * BN;
+    if (lane < kb1 - kb0 && lane < 2 * S) prefetch_l2_box(&tmW, (kb0 + lane) * kBlk, n0);
+    for (int i = 32 * lane; i < kb1 - kb0; i += 32 * 32) {
+      prefetch_l2_line(p.ws + (int64_t)(n0 / kBlk) * p.KB + kb0 + i);
+      if (n0 + kBlk < p.N) prefetch_l2_line(p.ws + (int64_t)(n0 / kBlk + 1) * p.KB + kb0 + i);
+    }
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
   pdl_wait();
 
-  const int num_tiles = p.MT * p.NT;
-  const int ks = kSplit ? p.ks : 1;
-  const int rank = kSplit ? (int)blockIdx.x % ks : 0;
-  const int first = (int)blockIdx.x / ks, step = (int)gridDim.x / ks;
-  const int kb0 = p.KB * rank / ks, kb1 = p.KB * (rank + 1) / ks;   // (KB is at most 2^17)
 
   if (warp >= 4) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpi));
@@ -115,36 +139,44 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
       const int c0 = nt * BN + half * kCols;                  // this thread's first column
       const bool mine = (t % p.MT) * BM + 32 * q < p.n && c0 < p.N;     // the warp has something to keep
       const float* xs = p.xs + min(row, p.n - 1);
-      const float* ws = p.ws + (int64_t)min(c0 / kBlk, (p.N - 1) / kBlk) * p.KB;
+      const float* ws = p.ws + (int64_t)min(c0 / kBlk, (p.N - 1) / kBlk) * p.KB;   // (a warp's columns have one block)
       uint64_t acc[BN / 4];
 #pragma unroll
       for (int i = 0; i < BN / 4; ++i) acc[i] = 0;
-      float sx = 0.f, sw = 0.f;
-      if (kb0 < kb1) {
-        sx = xs[(int64_t)kb0 * p.n];
-        sw = ws[kb0];
+      // scales load kAhead blocks ahead (two, where there are registers: those of W come from HBM); turns of kAhead
+      // blocks, for a load under way cannot move to another register
+      constexpr int kAhead = BN == 256 ? 1 : 2;
+      float sx[kAhead], sw[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        sx[j] = sw[j] = 0.f;
+        if (kb0 + j < kb1) {
+          sx[j] = xs[(int64_t)(kb0 + j) * p.n];
+          sw[j] = ws[kb0 + j];
+        }
       }
-      for (int kb = kb0; kb < kb1; ++kb, ++it) {
-        const float s = sx * sw;
-        if (kb + 1 < kb1) {                                   // the next block's scales load behind this one
-          sx = xs[(int64_t)(kb + 1) * p.n];
-          sw = ws[kb + 1];
+      for (int kb1st = kb0; kb1st < kb1 && ok; kb1st += kAhead) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const int kb = kb1st + j;
+          if (kb >= kb1) break;
+          const float f = sx[j] * sw[j];
+          if (kb + kAhead < kb1) {
+            sx[j] = xs[(int64_t)(kb + kAhead) * p.n];
+            sw[j] = ws[kb + kAhead];
+          }
+          const uint32_t buf = it % kBufs, ph = (it / kBufs) & 1;
+          ++it;
+          if (!__all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * buf, ph, &s_abort))) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          if (kAllPromote || mine) promote<kGroups>(acc, taddr + buf * BN, f);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(tempty0 + 8 * buf);
         }
-        const uint32_t buf = it % kBufs, ph = (it / kBufs) & 1;
-        if (!__all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * buf, ph, &s_abort))) {
-          ok = false;
-          break;
-        }
-        tc_fence_after();
-        if (mine) {
-          if constexpr (BN == 256)
-            promote_2x64(acc, taddr + buf * BN, taddr + buf * BN + 64, s, s);
-          else
-            promote_64(acc, taddr + buf * BN, s);
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(tempty0 + 8 * buf);
       }
       if (!ok || !mine) continue;
       if constexpr (kSplit) {
@@ -163,31 +195,50 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
           }
         continue;
       }
-      if (row >= p.n) continue;
-      __nv_bfloat16* o = p.out + (int64_t)row * p.out_stride + c0;
+      // 32 columns at a time through shared memory, so that a store is eight rows' 64 bytes
+      // (addresses from values that the compiler cannot follow: it would keep them through the k-blocks, and spill)
+      uint32_t ln = (uint32_t)lane, tile = (uint32_t)t;
+      asm volatile("" : "+r"(ln), "+r"(tile));
+      const int o0 = (int)(tile / (uint32_t)p.MT) * BN + half * kCols;
+      const uint32_t buf = out0 + (uint32_t)(warp - 4) * kOutBytes;
 #pragma unroll
-      for (int i = 0; i < kCols / 8; ++i) {
-        float f[8];
+      for (int h = 0; h < kGroups; ++h) {
+        if (o0 + 32 * h >= p.N) break;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          uint32_t lo, hi;
-          f2_unpack(acc[4 * i + j], lo, hi);
-          f[2 * j] = __uint_as_float(lo);
-          f[2 * j + 1] = __uint_as_float(hi);
+        for (int i = 0; i < 4; ++i) {
+          float f[8];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t lo, hi;
+            f2_unpack(acc[16 * h + 4 * i + j], lo, hi);
+            f[2 * j] = __uint_as_float(lo);
+            f[2 * j + 1] = __uint_as_float(hi);
+          }
+          if (p.bias)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] += __bfloat162float(p.bias[min(o0 + 32 * h + 8 * i + j, p.N - 1)]);
+          // pieces permuted within two rows: eight rows' pieces on different banks
+          st_shared_u4(buf + ln * 64 + (uint32_t)((i ^ (ln >> 1 & 3)) << 4),
+                       make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])));
         }
-        const int left = p.N - c0 - 8 * i;
-        if (p.bias)
+        __syncwarp();
+        const int c = o0 + 32 * h + 8 * (int)(ln & 3), left = p.N - c;
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (j < left) f[j] += __bfloat162float(p.bias[c0 + 8 * i + j]);
-        if (p.vec && left >= 8) {
-          *reinterpret_cast<uint4*>(o + 8 * i) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]),
-                                                            pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-        } else {
+        for (int i = 0; i < 4; ++i) {
+          const int rr = 8 * i + (int)(ln >> 2), orow = (int)(tile % (uint32_t)p.MT) * BM + 32 * q + rr;
+          const uint4 v = ld_shared_u4(buf + (uint32_t)rr * 64 + (uint32_t)(((int)(ln & 3) ^ (rr >> 1 & 3)) << 4));
+          if (orow >= p.n) continue;
+          __nv_bfloat16* o = p.out + (int64_t)orow * p.out_stride + c;
+          if (p.vec && left >= 8) {
+            *reinterpret_cast<uint4*>(o) = v;
+          } else {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (j < left) o[8 * i + j] = __float2bfloat16_rn(f[j]);
+            for (int j = 0; j < 8; ++j)
+              if (j < left) reinterpret_cast<uint16_t*>(o)[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+          }
         }
+        __syncwarp();
       }
     }
   } else {
@@ -251,7 +302,6 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
     }
   }
 
-  // ---- a cluster's partial sums ----------------------------------------------------
   // one code for all warps from here: as many registers as it was compiled for (a warpgroup has to
   // meet between two changes of its registers)
   __syncthreads();
@@ -331,6 +381,8 @@ __global__ void __launch_bounds__(kFewWarps * 32, 2) fp8_linear_few_kernel(const
   const float* ws = p.ws + (int64_t)(o0 / kBlk) * p.KB;
   const int t0 = min(2 * tq, p.n - 1), t1 = min(2 * tq + 1, p.n - 1);
   float acc[4] = {0.f, 0.f, 0.f, 0.f};
+  if (threadIdx.x == 0) prefetch_l2(w + (int64_t)o0 * K, (uint32_t)(min(16, p.N - o0) * K));   // (K is at most 2^24)
+  if (threadIdx.x >= 32 && (int)threadIdx.x - 32 < (p.KB + 31) / 32) prefetch_l2_line(ws + ((int)threadIdx.x - 32) * 32);
   pdl_wait();
   for (int k0 = warp; k0 < p.KB; k0 += kFewWarps * kFlight) {
     FewFrag a[kFlight], b[kFlight], v[kFlight];
@@ -376,8 +428,9 @@ ee_status launch(const uint8_t* x, const uint8_t* w, int32_t K, LinParams& p, cu
   p.NT = (p.N + BN - 1) / BN;
   const int tiles = p.MT * p.NT;
   const size_t stage = (((size_t)p.a_rows * kBlk + 1023) & ~(size_t)1023) + (size_t)BN * kBlk;
-  p.stages = (int)std::min<size_t>(16, (size_t)(224 * 1024) / stage);
-  const size_t smem = 1024 + p.stages * stage;
+  const size_t outs = kSplit ? 0 : kEpiWarps * kOutBytes;
+  p.stages = (int)std::min<size_t>(16, ((size_t)(224 * 1024) - outs) / stage);
+  const size_t smem = 1024 + p.stages * stage + outs;
   CUtensorMap tmX, tmW;
   if (!encode_u8_tmap_2d(&tmX, x, K, p.n, K, kBlk, p.a_rows) || !encode_u8_tmap_2d(&tmW, w, K, p.N, K, kBlk, BN))
     return EE_ERR_CUDA;
@@ -433,10 +486,30 @@ extern "C" ee_status ee_fp8_linear(const uint8_t* x, const float* x_scale, const
                               (cudaStream_t)stream, 1, x, w, K, p));
     return EE_OK;
   }
-  // the widest split of a tile's k-blocks that the SMs hold at once
-  p.ks = 1;
-  if (t128 < ee::kNumSMs) p.ks = (int)std::min<int64_t>({8, (int64_t)ee::kNumSMs / t128, p.KB});
-  if (p.ks > 1) return launch<128, true>(x, w, K, p, (cudaStream_t)stream);
-  if (t256 < ee::kNumSMs) return launch<128, false>(x, w, K, p, (cudaStream_t)stream);
-  return launch<256, false>(x, w, K, p, (cudaStream_t)stream);
+  const cudaStream_t s = (cudaStream_t)stream;
+  // Tiles of 128 or 256 weight rows, a tile's k-blocks split over ks CTAs.  What a call takes, in units of 0.12 us: 3 or 4
+  // for a k-block (a wider tile brings x fewer times: 0.48 us for twice the 0.36), for a split
+  // the way of its sums through the cluster.  (us, 28 blocks, 64 tokens: 3,584 rows as 28 tiles x 4 7.7, as 14 x 6 9.0,
+  // unsplit 13.9; 10,752 rows as 42 x 3 11.6, as 84 14.4; 28,672 rows as 112 23.8, as 224 27.8.)
+  const int rows = std::min(n, 128);
+  int64_t best = INT64_MAX;
+  bool wide = false;
+  for (int ks = 1; ks <= 8; ++ks) {
+    // a cluster's CTAs are on one GPC: of 5 and more fewer than the SMs would hold (18 clusters of 8 took two turns)
+    if (ks == 7 || ks > p.KB) continue;
+    const int64_t room = ks <= 4 ? ee::kNumSMs : ks == 5 ? 145 : 128;
+    for (int w2 = 0; w2 < 2; ++w2) {
+      const int64_t tiles = w2 ? t256 : t128;
+      if (ks > 1 && tiles * ks > room) continue;
+      const int64_t turns = ks > 1 ? 1 : (tiles + ee::kNumSMs - 1) / ee::kNumSMs;
+      const int64_t cost = turns * ((p.KB + ks - 1) / ks) * (w2 ? 4 : 3) + (ks == 1 ? 0 : w2 ? 10 + rows / 7 : 4 + rows / 10);
+      if (cost < best) {
+        best = cost;
+        p.ks = ks;
+        wide = w2 != 0;
+      }
+    }
+  }
+  if (p.ks > 1) return wide ? launch<256, true>(x, w, K, p, s) : launch<128, true>(x, w, K, p, s);
+  return wide ? launch<256, false>(x, w, K, p, s) : launch<128, false>(x, w, K, p, s);
 }

@@ -492,36 +492,52 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
   }
   if (!s_abort) {
     const int live = p.live ? max(0, min(p.T, ld_pinned(p.live))) : p.T;
-    const int per = (p.H + 4 * kThreads - 1) / (4 * kThreads);
-    for (int i = (int)blockIdx.x; i < live * per; i += (int)gridDim.x) {
-      const int t = i / per, c = (i % per) * 4 * kThreads + 4 * (int)threadIdx.x;
-      if (c >= p.H) continue;
-      float f[4] = {0.f, 0.f, 0.f, 0.f};
-      for (int j0 = 0; j0 < p.k; j0 += 4) {                   // four entries in flight
-        float4 v[4];
-        float pr[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (j0 + j < p.k) {
-            const int64_t at = (int64_t)t * p.k + j0 + j;
-            pr[j] = p.prob[at];
-            v[j] = __ldcg(reinterpret_cast<const float4*>(p.y + (size_t)p.inv[at] * p.H + c));
-          }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (j0 + j < p.k) {
-            f[0] += pr[j] * v[j].x;
-            f[1] += pr[j] * v[j].y;
-            f[2] += pr[j] * v[j].z;
-            f[3] += pr[j] * v[j].w;
-          }
+    // a warp takes 256 columns of a token: a round trip for the entries' numbers, one for 8 entries
+    const int per = (p.H + 255) / 256, step = (int)gridDim.x * (kThreads / 32);
+    for (int u = (int)blockIdx.x * (kThreads / 32) + warp; u < live * per; u += step) {
+      const int t = u / per, c = u % per * 256 + 4 * lane;
+      const bool in0 = c < p.H, in1 = c + 128 < p.H;
+      int my_at = 0;
+      float my_p = 0.f;
+      if (lane < p.k) {
+        my_at = p.inv[(int64_t)t * p.k + lane];
+        my_p = p.prob[(int64_t)t * p.k + lane];
       }
-      __nv_bfloat16* o = p.out + (int64_t)t * p.out_stride + c;
-      if (p.vec) {
-        *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
-      } else {
+      float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      for (int j0 = 0; j0 < p.k; j0 += 8) {
+        float4 v[8][2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = __float2bfloat16_rn(f[j]);
+        for (int j = 0; j < 8; ++j) {
+          const float* y = p.y + (size_t)__shfl_sync(0xffffffffu, my_at, (j0 + j) & 31) * p.H + c;
+          v[j][0] = v[j][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (j0 + j < p.k) {
+            if (in0) v[j][0] = __ldcg(reinterpret_cast<const float4*>(y));
+            if (in1) v[j][1] = __ldcg(reinterpret_cast<const float4*>(y + 128));
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float pr = __shfl_sync(0xffffffffu, my_p, (j0 + j) & 31);
+          if (j0 + j < p.k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              f[4 * i] += pr * v[j][i].x;
+              f[4 * i + 1] += pr * v[j][i].y;
+              f[4 * i + 2] += pr * v[j][i].z;
+              f[4 * i + 3] += pr * v[j][i].w;
+            }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (!(i ? in1 : in0)) continue;
+        __nv_bfloat16* o = p.out + (int64_t)t * p.out_stride + c + 128 * i;
+        if (p.vec) {
+          *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(f[4 * i], f[4 * i + 1]), pack_bf16(f[4 * i + 2], f[4 * i + 3]));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[j] = __float2bfloat16_rn(f[4 * i + j]);
+        }
       }
     }
   }

@@ -66,6 +66,11 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
   const bool alone = groups == 1;
   if (alone)
     for (int i = threadIdx.x; i < kMoeMaxExperts; i += kThreads) s_bits[i] = 0;
+  if ((int)blockIdx.x < routers && t0 == 0) {      // this CTA's columns of the router, while the kernel in front still runs
+    const int blocks = (p.H + kBlk - 1) / kBlk, c0 = blocks * rank / p.cl * kBlk, c1 = min(p.H, blocks * (rank + 1) / p.cl * kBlk);
+    if (c0 < c1)
+      for (int e = threadIdx.x; e < p.E; e += kThreads) prefetch_l2(p.router + (size_t)e * p.H + c0, (uint32_t)(c1 - c0) * 2);
+  }
   pdl_wait();
   const int live = p.live ? max(0, min(p.T, ld_pinned(p.live))) : p.T;
   if ((int)blockIdx.x >= routers) {                // x as codes: a warp and a block of one token, four at once
