@@ -1,4 +1,4 @@
-// Weight products for up to 8 tokens (ee_fp8_linear, ee_moe_layer): a warp takes 16 weight rows
+// Weight products for a few tokens (ee_fp8_linear up to 8, ee_moe_layer up to 16): a warp takes 16 weight rows
 // and some of their 128-byte blocks, straight from global memory into the fragments of an m16n8 MMA (weights the
 // 16 side, tokens the 8 side).  So few tokens leave nothing to share between warps but the
 // sums, and without rings, tensor memory and barriers a call costs little more than its one wait for memory.
@@ -12,7 +12,6 @@
 
 namespace ee {
 
-constexpr int kFewTokens = 8;
 constexpr int kFewWarps = 8;           // warps that share the blocks of 16 rows
 
 struct FewFrag {

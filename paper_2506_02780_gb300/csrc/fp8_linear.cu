@@ -23,6 +23,7 @@ constexpr int kThreads = 384;          // warp 0 TMA, 1 MMA, 2 TMEM, 3 none; 4..
 constexpr int kEpiWarps = 8;           // two per TMEM lane quarter, half of the columns each
 constexpr int kRegsAll = 168;          // a warp's at launch; the epilogue's take some of the others', kRegsEpi
 constexpr int BM = 128;
+constexpr int kFewRows = 8;            // tokens that a kernel of their own takes
 
 struct LinParams {
   int n, N, KB, MT, NT, ks, a_rows, stages;
@@ -373,7 +374,7 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
 // Up to 8 tokens: a CTA takes 16 weight rows, its warps every eighth block of them.
 __global__ void __launch_bounds__(kFewWarps * 32, 2) fp8_linear_few_kernel(const uint8_t* x, const uint8_t* w, int K, const LinParams p) {
   constexpr int kFlight = 4;                      // blocks of a warp whose loads are under way together
-  __shared__ float s_part[kFewWarps][16][kFewTokens];
+  __shared__ float s_part[kFewWarps][16][kFewRows];
   pdl_allow_next();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, tq = lane & 3;
   const int o0 = (int)blockIdx.x * 16;
@@ -481,7 +482,7 @@ extern "C" ee_status ee_fp8_linear(const uint8_t* x, const float* x_scale, const
   p.err = ee::err_word(ws);
   const int64_t t128 = (int64_t)p.MT * ((N + 127) / 128), t256 = (int64_t)p.MT * ((N + 255) / 256);
   if (t256 > (1 << 30)) return EE_ERR_UNSUPPORTED;
-  if (n <= kFewTokens) {
+  if (n <= kFewRows) {
     EE_CUDA_OK(ee::launch_pdl(fp8_linear_few_kernel, dim3((unsigned)((N + 15) / 16)), dim3(kFewWarps * 32), 0,
                               (cudaStream_t)stream, 1, x, w, K, p));
     return EE_OK;

@@ -26,7 +26,8 @@ struct __align__(32) MoeTile {   // a token tile's expert
   int first, tiles;            // its first tile and their number
   int pad[3];
 };
-struct FewEntry {            // of up to 8 tokens: an active expert's entry of a token, or -1, and its weight
+constexpr int kFewTokens = 16;
+struct FewEntry {            // of up to 16 tokens: an active expert's entry of a token, or -1, and its weight
   int entry;
   float p;
 };
@@ -73,7 +74,7 @@ struct RouteParams {
   uint32_t* sub;             // or NULL: [n_sub] counters to zero
   int n_sub;
   MoeTile* tile;
-  FewEntry* few;             // or NULL (more than 8 tokens): [active expert][8]
+  FewEntry* few;             // or NULL (more than 16 tokens): [active expert][16]
   int32_t* ids;              // [T][k] experts of a token, ascending
   float* prob;               // [T][k]
   int32_t* list;             // [T k] token of an entry
@@ -116,7 +117,7 @@ struct MoeParams {
   const int32_t* live;
   int32_t* err;
 };
-// Up to 8 tokens whose x and h fit in shared memory beside the rings (moe_few.cu): their depth and the bytes, or 0.
+// Up to 16 tokens whose x and h fit in shared memory beside the rings (moe_few.cu): their depth and the bytes, or 0.
 int moe_few_stages(int T, int H, int I, int k, bool fp8, size_t* smem);
 ee_status launch_moe_few(MoeParams& p, bool fp8, cudaStream_t stream);
 
