@@ -1,7 +1,7 @@
 // ee_moe_layer's workspace and the launch of its first kernel (moe_route.cu).  Internal header.
 //
 // An ENTRY is a token at one of its experts; entries are numbered by expert, then by token.
-// A token TILE is up to 128 entries of one expert.
+// A token TILE is up to 32, 64 or 128 entries of one expert.
 #pragma once
 #include "few.cuh"
 
@@ -10,7 +10,10 @@ namespace ee {
 constexpr int kMoeMaxTopK = 16;
 constexpr int kMoeMaxExperts = 256;
 constexpr int kMoeMaxTokens = 4096;
-constexpr int kMoeTile = 128;
+// entries of a tile (moe_experts.cu)
+inline int moe_tile_rows(int64_t T, int64_t E, int64_t k, bool fp8) {
+  return T <= 32 ? 32 : T <= 64 || (fp8 && T * k <= 64 * E) ? 64 : 128;
+}
 
 // counters in front of the workspace's arrays, set by the routing kernel
 struct MoeCtl {
@@ -39,7 +42,7 @@ struct MoeLayout {
 inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t k) {
   MoeLayout l;
   const int64_t n = T * k;
-  l.max_tiles = (int)(std::min(E, n) + n / kMoeTile);
+  l.max_tiles = (int)(std::min(E, n) + n / 64);   // (32 only where no expert can have more)
   size_t at = align_up(kWorkspaceBytes, 256);
   const auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -69,7 +72,7 @@ struct RouteParams {
   int64_t x_stride;
   const __nv_bfloat16* router;
   const int32_t* live;       // or NULL
-  int T, H, E, k, renorm, cl, max_tiles;
+  int T, H, E, k, renorm, cl, max_tiles, tile_rows;
   MoeCtl* ctl;
   uint32_t* sub;             // or NULL: [n_sub] counters to zero
   int n_sub;

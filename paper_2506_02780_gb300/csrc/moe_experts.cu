@@ -11,7 +11,7 @@
 // CTAs draw tasks from one queue, gate tasks first.  A down task waits for the gate tasks of its
 // token tile; those were drawn before it by CTAs that are running, so no wait depends on
 // a CTA that has not started.  Warp 0 draws, publishes the task to the other roles in a ring of
-// shared memory and streams the operands (x's rows gathered by TMA); it runs ahead of the others across
+// shared memory and streams the operands (x's rows: warps 12..15); it runs ahead of the others across
 // tasks, so that the stream does not stop between them.  Warp 2 puts products of scales into shared memory,
 // warp 3 tells other CTAs what the epilogue warps 4..11 have stored (a release waits for the stores: it would hold them up
 // for 2 us a task) and quantises h: a block of 128 columns of h may be several tasks', whoever completes it
@@ -24,9 +24,10 @@ namespace {
 
 using namespace ee;
 
-constexpr int kThreads = 384;          // warp 0 tasks and TMA, 1 MMA, 2 TMEM and scales, 3 publishing; 4..11 epilogue
+constexpr int kThreads = 512;          // warp 0 tasks and TMA, 1 MMA, 2 TMEM and scales, 3 publishing; 4..11 epilogue; 12..15 x
 constexpr int kEpiWarps = 8;           // two per TMEM lane quarter, every other 16 tokens each
-constexpr int kRegsAll = 168, kRegsEpi = 216, kRegsOther = 72;   // 256 * 216 + 128 * 72 = 384 * 168
+constexpr int kRegsAll = 128;          // a warp's at launch; the epilogue's take some of the others'
+constexpr int kGatherWarps = 4;
 constexpr int kRing = 4;               // tasks published and not yet done with by every role
 constexpr int kScRing = 8;             // k-blocks' scales
 constexpr int kMaxStages = 12;
@@ -53,9 +54,11 @@ __device__ __forceinline__ void add_scaled16(uint64_t (&acc)[8], const uint32_t 
 // NT: most tokens of a tile
 template <bool kFp8, int NT>
 __global__ void __launch_bounds__(kThreads, 1)
-moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW1,
-                   const __grid_constant__ CUtensorMap tmH, const __grid_constant__ CUtensorMap tmW2, const MoeParams p) {
+moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__ CUtensorMap tmH8,
+                   const __grid_constant__ CUtensorMap tmH32, const __grid_constant__ CUtensorMap tmW2, const MoeParams p) {
   constexpr int kCols = kFp8 ? 128 : 64;        // elements in 128 bytes
+  constexpr int kRegsEpi = NT == 128 ? 200 : 152, kRegsOther = 2 * kRegsAll - kRegsEpi;
+  constexpr int kScBatch = NT == 128 ? 2 : 4, kQuBatch = NT == 128 ? 4 : 8;   // k-blocks' scales, tokens' h: loads in flight
   constexpr int kBufs = 512 / (2 * NT) < 8 ? 512 / (2 * NT) : 8;   // accumulators of two tiles
   constexpr int kChunks = NT / 32;              // groups of 16 tokens of an epilogue warp
   extern __shared__ uint8_t smem_raw[];
@@ -83,7 +86,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
     s_issued = 0;
     s_consumed = 0;
     for (int s = 0; s < S; ++s) {
-      mbar_init(full0 + 8 * s, 1);
+      mbar_init(full0 + 8 * s, 1 + kGatherWarps);
       mbar_init(empty0 + 8 * s, 1);
     }
     for (int a = 0; a < kBufs; ++a) {
@@ -92,7 +95,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
     }
     for (int a = 0; a < kRing; ++a) {
       mbar_init(qfull0 + 8 * a, 1);
-      mbar_init(qempty0 + 8 * a, kEpiWarps + (kFp8 ? 3 : 2));
+      mbar_init(qempty0 + 8 * a, kEpiWarps + kGatherWarps + (kFp8 ? 3 : 2));
       mbar_init(edone0 + 8 * a, kEpiWarps);
     }
     for (int a = 0; a < kScRing; ++a) {
@@ -102,9 +105,9 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
     mbar_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmX)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmH32)) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmW1)) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmH)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmH8)) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmW2)) : "memory");
   }
   if (warp == 2) {
@@ -118,7 +121,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
   const uint32_t tmem = s_tmem;
   pdl_wait();
 
-  if (warp >= 4) {
+  if (warp >= 4 && warp < 4 + kEpiWarps) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpi));
     const int q = warp & 3, half = (warp - 4) >> 2;
     const int r = 32 * q + lane;                              // row of both weight tiles
@@ -225,9 +228,33 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
       uint32_t phase = 0;
       bool ok = true;
       const int tiles = (int)p.ctl->tiles, gates = tiles * p.IT, total = gates + tiles * p.HT;
-      int g = 0;
-      if (lane == 0) g = (int)atomicAdd(&p.ctl->queue, 1u);
-      g = __shfl_sync(0xffffffffu, g, 0);
+      // a task, worked out while the loads of the one before it wait for room in the ring: drawn at kDraw k-blocks
+      // before that one's end, its tile looked up at kLook, whether h is there at kList
+      constexpr int kDraw = 10, kLook = 7, kList = 4;
+      int g = 0, blk = 0, entry = 0, rows = 0;
+      uint32_t have = 0;
+      MoeTile e;
+      const auto draw = [&]() {
+        if (lane == 0) g = (int)atomicAdd(&p.ctl->queue, 1u);
+      };
+      const auto look = [&]() {
+        g = __shfl_sync(0xffffffffu, g, 0);
+        if (g < total) e = p.tile[(g < gates ? g : g - gates) / (g < gates ? p.IT : p.HT)];
+      };
+      int tile = 0;
+      const auto list = [&]() {
+        if (g >= total) return;
+        const bool gate = g < gates;
+        const int local = (gate ? g : g - gates) - e.first * (gate ? p.IT : p.HT), mt = local % e.tiles;
+        blk = local / e.tiles;
+        tile = e.first + mt;
+        entry = e.entry0 + mt * NT;
+        rows = min(NT, e.count - mt * NT);
+        if (!gate) have = ld_acquire(p.ctl->gate_done + tile);
+      };
+      draw();
+      look();
+      list();
       for (uint32_t nt = 0; ok; ++nt) {
         const uint32_t slot = nt % kRing;
         if (!__all_sync(0xffffffffu, mbar_wait(qempty0 + 8 * slot, ((nt / kRing) & 1) ^ 1, &s_abort))) break;
@@ -239,21 +266,17 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
           break;
         }
         const bool gate = g < gates;
-        const int per = gate ? p.IT : p.HT, at = gate ? g : g - gates, w = gate ? p.wg : p.wd;
-        const MoeTile e = p.tile[at / per];
-        const int local = at - e.first * per, mt = local % e.tiles, blk = local / e.tiles;
-        const int entry = e.entry0 + mt * kMoeTile, rows = min(kMoeTile, e.count - mt * kMoeTile);
-        int tok[4] = {0, 0, 0, 0};
+        const int w = gate ? p.wg : p.wd;
+        const int at_entry = entry, h32 = gate ? 0 : rows / 32, h8 = gate ? 0 : (rows % 32 + 7) / 8;   // boxes of h
         int wy0, wy1;                                         // the two tiles' first weight rows
         if (gate) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) tok[j] = p.list[entry + min(4 * lane + j, rows - 1)];
           wy0 = e.expert * 2 * p.I + blk * w;
           wy1 = wy0 + p.I;
         } else {
           wy0 = e.expert * p.H + blk * 2 * w;
           wy1 = wy0 + w;
-          if (!__all_sync(0xffffffffu, wait_count_geq(p.ctl->gate_done + e.first + mt, (uint32_t)(kFp8 ? p.IB : p.IT)))) {
+          const uint32_t want = (uint32_t)(kFp8 ? p.IB : p.IT);
+          if (!__all_sync(0xffffffffu, have >= want || wait_count_geq(p.ctl->gate_done + tile, want))) {
             s_abort = 1;
             break;
           }
@@ -264,16 +287,14 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
           t.kind = gate ? kGate : kDown;
           t.blk = blk;
           t.expert = e.expert;
-          t.tile = e.first + mt;
+          t.tile = tile;
           t.entry = entry;
           t.rows = rows;
           s_task[slot] = t;
           mbar_arrive(qfull0 + 8 * slot);
         }
-        const int copies = gate ? (rows + 3) / 4 : (rows + 7) / 8;
-        const uint32_t boxBytes = (uint32_t)w * 128, bytes = 2 * boxBytes + (uint32_t)copies * (gate ? 512u : 1024u);
+        const uint32_t boxBytes = (uint32_t)w * 128, bytes = 2 * boxBytes + (uint32_t)(4 * h32 + h8) * 1024u;
         const int KB = gate ? p.KB1 : p.KB2;
-        int next = 0;
         for (int kb = 0; kb < KB; ++kb) {
           if (!__all_sync(0xffffffffu, mbar_wait(empty0 + 8 * stage, phase ^ 1, &s_abort))) {
             ok = false;
@@ -287,20 +308,18 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
             ++s_issued;
           }
           __syncwarp();
-          if (lane < copies) {
-            if (gate)
-              tma_gather4(sb + lane * 512, &tmX, fb, kb * kCols, tok[0], tok[1], tok[2], tok[3]);
-            else
-              tma_load_2d(sb + lane * 1024, &tmH, fb, kb * kCols, entry + 8 * lane);
-          }
+          if (lane < h32) tma_load_2d(sb + lane * 4096, &tmH32, fb, kb * kCols, at_entry + 32 * lane);
+          else if (lane - h32 < h8)
+            tma_load_2d(sb + h32 * 4096 + (lane - h32) * 1024, &tmH8, fb, kb * kCols, at_entry + 32 * h32 + 8 * (lane - h32));
           __syncwarp();
-          if (kb == KB - 1 - min(KB - 1, 3) && lane == 0) next = (int)atomicAdd(&p.ctl->queue, 1u);
+          if (kb == max(0, KB - kDraw)) draw();
+          if (kb == max(0, KB - kLook)) look();
+          if (kb == max(0, KB - kList)) list();
           if (++stage == S) {
             stage = 0;
             phase ^= 1;
           }
         }
-        g = __shfl_sync(0xffffffffu, next, 0);
       }
     } else if (warp == 1) {
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
@@ -358,7 +377,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
       if (lane == 0) s_consumed = consumed;
     } else if (warp == 2) {
       if constexpr (kFp8) {
-        // scale of (k-block, token, weight tile): four tokens a lane, four k-blocks' loads at once
+        // scale of (k-block, token, weight tile): four tokens a lane, some k-blocks' loads at once
         uint32_t sc = 0;
         bool ok = true;
         for (uint32_t nt = 0; ok; ++nt) {
@@ -386,10 +405,10 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
             const int e = t.entry + min(4 * lane + j, t.rows - 1);
             at[j] = gate ? p.list[e] : e;
           }
-          for (int kb = 0; kb < KB && ok; kb += 4) {
-            float f[4][4], w0[4], w1[4];
+          for (int kb = 0; kb < KB && ok; kb += kScBatch) {
+            float f[kScBatch][4], w0[kScBatch], w1[kScBatch];
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
+            for (int b = 0; b < kScBatch; ++b)
               if (kb + b < KB) {
                 const float* row = xs + (int64_t)(kb + b) * xstep;
 #pragma unroll
@@ -398,7 +417,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
                 w1[b] = ws1[kb + b];
               }
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
+            for (int b = 0; b < kScBatch; ++b)
               if (kb + b < KB && ok) {
                 const uint32_t e = sc % kScRing;
                 ok = __all_sync(0xffffffffu, mbar_wait(sempty0 + 8 * e, ((sc / kScRing) & 1) ^ 1, &s_abort));
@@ -415,6 +434,65 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
           }
         }
       }
+    } else if (warp >= 4 + kEpiWarps) {
+      // x's rows of a tile, 16 bytes a copy, to where TMA's 128-byte swizzle would put them (gathered by TMA, four rows an
+      // operation of 55 ns, they took longer than everything else for 40 tokens and more); a stage is
+      // signalled kLag stages later, when its copies have landed, and at a task's end at once: the next
+      // task may wait for this one
+      constexpr int kLag = 2, kMine = NT / 16;
+      const int gw = warp - 4 - kEpiWarps, ch = lane & 7, row0 = gw * 4 + (lane >> 3);
+      const uint32_t to = (uint32_t)row0 * 128 + (uint32_t)((ch ^ (row0 & 7)) << 4);   // (16 rows on: the same place in a group of 8)
+      const int x_bytes = p.H * (kFp8 ? 1 : 2);
+      int stage = 0, sig = 0;                                 // stages filled and signalled
+      uint32_t phase = 0;
+      bool ok = true;
+      const auto signal = [&]() {
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(full0 + 8 * sig);
+        if (++sig == S) sig = 0;
+      };
+      for (uint32_t nt = 0; ok; ++nt) {
+        const uint32_t slot = nt % kRing;
+        if (!__all_sync(0xffffffffu, mbar_wait(qfull0 + 8 * slot, (nt / kRing) & 1, &s_abort))) break;
+        const Task t = s_task[slot];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(qempty0 + 8 * slot);
+        if (t.kind == kEnd) break;
+        const bool gate = t.kind == kGate;
+        const int KB = gate ? p.KB1 : p.KB2;
+        const uint8_t* src[kMine];
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+          src[i] = nullptr;
+          if (gate && row0 + 16 * i < t.rows)
+            src[i] = static_cast<const uint8_t*>(p.x) + (int64_t)p.list[t.entry + row0 + 16 * i] * p.x_stride * (kFp8 ? 1 : 2) + ch * 16;
+        }
+        for (int kb = 0; kb < KB; ++kb) {
+          if (!__all_sync(0xffffffffu, mbar_wait(empty0 + 8 * stage, phase ^ 1, &s_abort))) {
+            ok = false;
+            break;
+          }
+          const uint32_t at = ring + (uint32_t)stage * stBytes + to;
+          const uint32_t in = kb * 128 + ch * 16 < x_bytes ? 16u : 0u;   // (nothing is read where 0 bytes are)
+#pragma unroll
+          for (int i = 0; i < kMine; ++i)
+            if (src[i]) cp_async16(at + i * 2048, src[i] + (in ? kb * 128 : 0), in);
+          asm volatile("cp.async.commit_group;" ::: "memory");
+          if (kb >= kLag) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
+            signal();
+          }
+          if (++stage == S) {
+            stage = 0;
+            phase ^= 1;
+          }
+        }
+        cp_async_wait_all();
+        if (ok)
+          for (int i = 0; i < min(KB, kLag); ++i) signal();
+      }
+      cp_async_wait_all();
     } else {
       for (uint32_t nt = 0;; ++nt) {
         const uint32_t slot = nt % kRing;
@@ -439,28 +517,34 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
           }
           const int col = b * kBlk + 4 * lane;
           const bool in = col < p.I;
-          for (int r0 = 0; r0 < t.rows; r0 += 8) {            // a token's block a warp, eight loads in flight
-            float4 v[8];
+          for (int r0 = 0; r0 < t.rows; r0 += kQuBatch) {            // a token's block at a time
+            float4 v[kQuBatch];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < kQuBatch; ++i) {
               v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
               if (in && r0 + i < t.rows)
                 v[i] = __ldcg(reinterpret_cast<const float4*>(p.hf + (size_t)(t.entry + r0 + i) * p.I + col));
             }
+            uint32_t my_top = 0;                              // lane i: of the i-th token
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (r0 + i < t.rows) {
-                const uint32_t m = 0x7fffffffu;
-                const uint32_t top = __reduce_max_sync(
-                    0xffffffffu, max(max(__float_as_uint(v[i].x) & m, __float_as_uint(v[i].y) & m),
-                                     max(__float_as_uint(v[i].z) & m, __float_as_uint(v[i].w) & m)));
-                const BlockScale s = block_scale(__uint_as_float(top));
-                const size_t e = (size_t)(t.entry + r0 + i);
-                if (in)
-                  *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(p.h) + e * p.I + col) =
-                      pack_e4m3(to_code(v[i].x, s), to_code(v[i].y, s), to_code(v[i].z, s), to_code(v[i].w, s));
-                if (lane == 0) p.hs[(size_t)b * p.n + e] = s.scale;
-              }
+            for (int i = 0; i < kQuBatch; ++i) {
+              const uint32_t m = 0x7fffffffu;
+              const uint32_t top = __reduce_max_sync(
+                  0xffffffffu, max(max(__float_as_uint(v[i].x) & m, __float_as_uint(v[i].y) & m),
+                                   max(__float_as_uint(v[i].z) & m, __float_as_uint(v[i].w) & m)));
+              if (lane == i) my_top = top;
+            }
+            const BlockScale mine = block_scale(__uint_as_float(my_top));
+            if (lane < kQuBatch && r0 + lane < t.rows) p.hs[(size_t)b * p.n + t.entry + r0 + lane] = mine.scale;
+#pragma unroll
+            for (int i = 0; i < kQuBatch; ++i) {
+              BlockScale s;
+              s.hi = __shfl_sync(0xffffffffu, mine.hi, i);
+              s.lo = __shfl_sync(0xffffffffu, mine.lo, i);
+              if (in && r0 + i < t.rows)
+                *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(p.h) + (size_t)(t.entry + r0 + i) * p.I + col) =
+                    pack_e4m3(to_code(v[i].x, s), to_code(v[i].y, s), to_code(v[i].z, s), to_code(v[i].w, s));
+            }
           }
         }
         asm volatile("fence.proxy.async;" ::: "memory");      // down tasks read h by TMA
@@ -473,7 +557,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
   // one code for all warps from here: as many registers as it was compiled for (a warpgroup has to
   // meet between two changes of its registers)
   __syncthreads();
-  if (warp >= 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsAll));
+  if (warp >= 4 && warp < 4 + kEpiWarps) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsAll));
   else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsAll));
   tc_fence_before();
   __syncthreads();
@@ -572,15 +656,15 @@ ee_status launch(MoeParams& p, cudaStream_t stream) {
   const size_t slack = 1024 + (128 - (size_t)std::min(p.wg, p.wd)) * 128;
   p.stages = (int)std::min<size_t>(kMaxStages, ((size_t)(214 * 1024) - slack) / stage);
   const size_t smem = slack + p.stages * stage;
-  CUtensorMap tmX, tmW1, tmH, tmW2;
+  CUtensorMap tmW1, tmH8, tmH32, tmW2;
   const auto encode = [](CUtensorMap* m, const void* base, uint64_t cols, uint64_t rows, uint64_t stride, uint32_t box) {
     if constexpr (kFp8) return encode_u8_tmap_2d(m, base, cols, rows, stride, 128, box);
     const uint64_t dims[2] = {cols, rows}, strides[1] = {2 * stride};
     const uint32_t boxes[2] = {64, box};
     return encode_bf16_tmap(m, base, 2, dims, strides, boxes);
   };
-  if (!encode(&tmX, p.x, p.H, p.T, p.x_stride, 1) || !encode(&tmW1, p.w1, p.H, (uint64_t)p.E * 2 * p.I, p.H, p.wg) ||
-      !encode(&tmH, p.h, p.I, p.n, p.I, 8) || !encode(&tmW2, p.w2, p.I, (uint64_t)p.E * p.H, p.I, p.wd))
+  if (!encode(&tmW1, p.w1, p.H, (uint64_t)p.E * 2 * p.I, p.H, p.wg) ||
+      !encode(&tmH8, p.h, p.I, p.n, p.I, 8) || !encode(&tmH32, p.h, p.I, p.n, p.I, 32) || !encode(&tmW2, p.w2, p.I, (uint64_t)p.E * p.H, p.I, p.wd))
     return EE_ERR_CUDA;
   {
     int dev = 0;
@@ -594,7 +678,7 @@ ee_status launch(MoeParams& p, cudaStream_t stream) {
       set[dev] = true;
     }
   }
-  EE_CUDA_OK(launch_pdl(moe_experts_kernel<kFp8, NT>, dim3(kNumSMs), dim3(kThreads), smem, stream, 1, tmX, tmW1, tmH, tmW2, p));
+  EE_CUDA_OK(launch_pdl(moe_experts_kernel<kFp8, NT>, dim3(kNumSMs), dim3(kThreads), smem, stream, 1, tmW1, tmH8, tmH32, tmW2, p));
   return EE_OK;
 }
 
@@ -637,6 +721,7 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   r.k = k;
   r.renorm = renorm != 0;
   r.max_tiles = l.max_tiles;
+  r.tile_rows = ee::moe_tile_rows(T, E, k, fp8);
   r.ctl = reinterpret_cast<ee::MoeCtl*>(base + l.ctl);
   r.tile = reinterpret_cast<ee::MoeTile*>(base + l.tile);
   r.few = T <= ee::kFewTokens ? reinterpret_cast<ee::FewEntry*>(base + l.few) : nullptr;
@@ -670,7 +755,7 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   p.KB2 = (I * (fp8 ? 1 : 2) + 127) / 128;
   p.IB = (I + kBlk - 1) / kBlk;
   p.HB = blocks;
-  const int nt = T <= 32 ? 32 : 128;
+  const int nt = ee::moe_tile_rows(T, E, k, fp8);
   p.b_rows = std::min(nt, (T + 15) / 16 * 16);
   p.w1 = w1;
   p.w2 = w2;
@@ -702,6 +787,6 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   const cudaStream_t s = (cudaStream_t)stream;
   size_t few = 0;
   if (ee::moe_few_stages(T, H, I, k, fp8, &few)) return ee::launch_moe_few(p, fp8, s);
-  if (fp8) return nt == 32 ? launch<true, 32>(p, s) : launch<true, 128>(p, s);
-  return nt == 32 ? launch<false, 32>(p, s) : launch<false, 128>(p, s);
+  if (fp8) return nt == 32 ? launch<true, 32>(p, s) : nt == 64 ? launch<true, 64>(p, s) : launch<true, 128>(p, s);
+  return nt == 32 ? launch<false, 32>(p, s) : nt == 64 ? launch<false, 64>(p, s) : launch<false, 128>(p, s);
 }

@@ -275,8 +275,8 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
       pre[threadIdx.x * words + w] = (uint16_t)cnt;
       cnt += __popc(mask[threadIdx.x * words + w]);
     }
-  // running numbers of entries and tiles in one scan (at most 2^16 entries, 2^10 tiles)
-  const int tiles = (cnt + kMoeTile - 1) / kMoeTile;
+  // running numbers of entries and tiles in one scan (at most 2^16 entries, 2^11 tiles)
+  const int tiles = (cnt + p.tile_rows - 1) / p.tile_rows;
   const uint32_t own = (uint32_t)cnt | (uint32_t)tiles << 20;
   uint32_t incl = own;
 #pragma unroll
