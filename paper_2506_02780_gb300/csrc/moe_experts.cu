@@ -14,8 +14,8 @@
 // shared memory and streams the operands (x's rows: warps 12..15); it runs ahead of the others across
 // tasks, so that the stream does not stop between them.  Warp 2 puts products of scales into shared memory,
 // warp 3 tells other CTAs what the epilogue warps 4..11 have stored (a release waits for the stores: it would hold them up
-// for 2 us a task) and quantises h: a block of 128 columns of h may be several tasks', whoever completes it
-// reads it back.
+// for 2 us a task).  A block of 128 columns of h is quantised by the epilogue where it is one task's; where
+// tasks are narrower, warp 3 of the CTA that completes it reads it back.
 #include <mutex>
 
 #include "moe.cuh"
@@ -64,7 +64,8 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
-  __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 2 * 8 + 3 * kRing + 2 * kScRing + 1];
+  __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 2 * 8 + 3 * kRing + 2 * kScRing + 2 + 1];
+  __shared__ uint32_t s_top[kFp8 ? 2 : 1][4][NT];
   __shared__ __align__(16) float s_scale[kFp8 ? kScRing : 1][2][NT];
   __shared__ Task s_task[kRing];
   __shared__ uint32_t s_tmem;
@@ -80,7 +81,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
   const uint32_t full0 = smem_u32(s_bars), empty0 = full0 + 8 * kMaxStages, tfull0 = empty0 + 8 * kMaxStages,
                  tempty0 = tfull0 + 8 * 8, qfull0 = tempty0 + 8 * 8, qempty0 = qfull0 + 8 * kRing,
                  edone0 = qempty0 + 8 * kRing, sfull0 = edone0 + 8 * kRing, sempty0 = sfull0 + 8 * kScRing,
-                 drain = sempty0 + 8 * kScRing;
+                 meet0 = sempty0 + 8 * kScRing, drain = meet0 + 8 * 2;
   if (threadIdx.x == 0) {
     s_abort = 0;
     s_issued = 0;
@@ -102,6 +103,8 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
       mbar_init(sfull0 + 8 * a, 1);
       mbar_init(sempty0 + 8 * a, kEpiWarps);
     }
+    mbar_init(meet0, 4);
+    mbar_init(meet0 + 8, 4);
     mbar_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
@@ -126,7 +129,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
     const int q = warp & 3, half = (warp - 4) >> 2;
     const int r = 32 * q + lane;                              // row of both weight tiles
     const uint32_t tq = tmem + ((uint32_t)(32 * q) << 16);
-    uint32_t it = 0, sc = 0;                                  // accumulators and scales taken
+    uint32_t it = 0, sc = 0, meets = 0;                       // accumulators and scales taken, blocks of h shared
     for (uint32_t nt = 0;; ++nt) {
       const uint32_t slot = nt % kRing;
       if (!__all_sync(0xffffffffu, mbar_wait(qfull0 + 8 * slot, (nt / kRing) & 1, &s_abort))) break;
@@ -185,36 +188,85 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
         ++sc;
       }
       if (!ok) break;
-      if (mine && r < w) {
-        const int col = gate ? t.blk * w + r : t.blk * 2 * w + r;
+      if (mine && gate) {
+        const int col = t.blk * w + r;
+        const bool in = r < w && col < p.I;
+        const bool whole = kFp8 && p.wg == kBlk;              // the task has its block of h to itself
+        uint32_t top[kChunks];                                // lane i: the largest |h| of token i in these 32 columns
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) {
+          const int c = (2 * j + half) * 16;
+          top[j] = 0;
+          if (c >= t.rows) break;
+          const size_t at = (size_t)(t.entry + c) * p.I + col;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            uint32_t g[2], u[2];
+            f2_unpack(acc0[j][i / 2], g[0], g[1]);
+            f2_unpack(acc1[j][i / 2], u[0], u[1]);
+            const float h = silu_times(__uint_as_float(g[i & 1]), __uint_as_float(u[i & 1]));
+            if (whole) {
+              const uint32_t m = __reduce_max_sync(0xffffffffu, in ? __float_as_uint(h) & 0x7fffffffu : 0u);
+              if (lane == i) top[j] = m;
+              acc0[j][i / 2] = i & 1 ? f2_pack(g[0], __float_as_uint(h)) : f2_pack(__float_as_uint(h), g[1]);
+            } else if (in && c + i < t.rows) {
+              if constexpr (kFp8) __stcg(p.hf + at + (size_t)i * p.I, h);
+              else static_cast<__nv_bfloat16*>(p.h)[at + (size_t)i * p.I] = __float2bfloat16_rn(h);
+            }
+          }
+          if (kFp8 && whole && lane < 16) s_top[meets & 1][q][c + lane] = top[j];
+        }
+        if constexpr (kFp8) {
+          if (whole) {
+            // the block's other columns are the three warps' of the same tokens
+            __syncwarp();
+            if (lane == 0) mbar_arrive(meet0 + 8 * half);
+            if (!__all_sync(0xffffffffu, mbar_wait(meet0 + 8 * half, meets & 1, &s_abort))) break;
+#pragma unroll
+            for (int j = 0; j < kChunks; ++j) {
+              const int c = (2 * j + half) * 16;
+              if (c >= t.rows) break;
+              uint32_t m = 0;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) m = max(m, s_top[meets & 1][i][c + (lane & 15)]);
+              const BlockScale mine_s = block_scale(__uint_as_float(m));
+              if (q == 0 && lane < 16 && c + lane < t.rows) p.hs[(size_t)t.blk * p.n + t.entry + c + lane] = mine_s.scale;
+              uint8_t* o = static_cast<uint8_t*>(p.h) + (size_t)(t.entry + c) * p.I + col;
+#pragma unroll
+              for (int i = 0; i < 16; i += 2) {
+                uint32_t h[2];
+                f2_unpack(acc0[j][i / 2], h[0], h[1]);
+                float v[2];
+#pragma unroll
+                for (int d = 0; d < 2; ++d) {
+                  BlockScale s;
+                  s.hi = __shfl_sync(0xffffffffu, mine_s.hi, i + d);
+                  s.lo = __shfl_sync(0xffffffffu, mine_s.lo, i + d);
+                  v[d] = to_code(__uint_as_float(h[d]), s);
+                }
+                const uint32_t code = pack_e4m3(v[0], v[1], 0.f, 0.f);
+                if (in && c + i < t.rows) o[(size_t)i * p.I] = (uint8_t)code;
+                if (in && c + i + 1 < t.rows) o[(size_t)(i + 1) * p.I] = (uint8_t)(code >> 8);
+              }
+            }
+            ++meets;
+          }
+        }
+      } else if (mine) {
+        const int col = t.blk * 2 * w + r;
+        const bool in0 = r < w && col < p.H, in1 = r < w && col + w < p.H;
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
           const int c = (2 * j + half) * 16;
           if (c >= t.rows) break;
-          const size_t e0 = (size_t)t.entry + c;
+          float* o = p.y + (size_t)(t.entry + c) * p.H + col;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
+          for (int i = 0; i < 16; ++i, o += p.H) {
             uint32_t a[2], b[2];
-            f2_unpack(acc0[j][i], a[0], a[1]);
-            f2_unpack(acc1[j][i], b[0], b[1]);
-#pragma unroll
-            for (int d = 0; d < 2; ++d) {
-              const int tok = 2 * i + d;
-              if (c + tok >= t.rows) continue;
-              if (gate) {
-                const float h = silu_times(__uint_as_float(a[d]), __uint_as_float(b[d]));
-                if (col < p.I) {
-                  if constexpr (kFp8)
-                    __stcg(p.hf + (e0 + tok) * p.I + col, h);
-                  else
-                    static_cast<__nv_bfloat16*>(p.h)[(e0 + tok) * p.I + col] = __float2bfloat16_rn(h);
-                }
-              } else {
-                float* o = p.y + (e0 + tok) * p.H + col;
-                if (col < p.H) __stcg(o, __uint_as_float(a[d]));
-                if (col + w < p.H) __stcg(o + w, __uint_as_float(b[d]));
-              }
-            }
+            f2_unpack(acc0[j][i / 2], a[0], a[1]);
+            f2_unpack(acc1[j][i / 2], b[0], b[1]);
+            if (in0 && c + i < t.rows) __stcg(o, __uint_as_float(a[i & 1]));
+            if (in1 && c + i < t.rows) __stcg(o + w, __uint_as_float(b[i & 1]));
           }
         }
       }
@@ -233,6 +285,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
       constexpr int kDraw = 10, kLook = 7, kList = 4;
       int g = 0, blk = 0, entry = 0, rows = 0;
       uint32_t have = 0;
+      const uint64_t policy = policy_evict_first();           // (h and y stay in L2)
       MoeTile e;
       const auto draw = [&]() {
         if (lane == 0) g = (int)atomicAdd(&p.ctl->queue, 1u);
@@ -303,8 +356,8 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
           const uint32_t fb = full0 + 8 * stage, sb = ring + (uint32_t)stage * stBytes, sw = sb + bStage;
           if (lane == 0) {
             mbar_expect_tx(fb, bytes);
-            tma_load_2d(sw, gate ? &tmW1 : &tmW2, fb, kb * kCols, wy0);
-            tma_load_2d(sw + boxBytes, gate ? &tmW1 : &tmW2, fb, kb * kCols, wy1);
+            tma_load_2d_hint(sw, gate ? &tmW1 : &tmW2, fb, kb * kCols, wy0, policy);
+            tma_load_2d_hint(sw + boxBytes, gate ? &tmW1 : &tmW2, fb, kb * kCols, wy1, policy);
             ++s_issued;
           }
           __syncwarp();
@@ -507,7 +560,12 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
         }
         if constexpr (kFp8) {
           const int b = t.blk * p.wg / kBlk;                  // the block of h
-          if (p.wg < kBlk) {
+          if (p.wg == kBlk) {
+            asm volatile("fence.proxy.async;" ::: "memory");
+            if (lane == 0) red_inc_release(p.ctl->gate_done + t.tile, 0xffffffffu);
+            continue;
+          }
+          {
             uint32_t last = 0;
             if (lane == 0) {
               const uint32_t parts = (uint32_t)((min(kBlk, p.I - b * kBlk) + p.wg - 1) / p.wg);
