@@ -244,28 +244,34 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
-    if (warp == 0 && lane == 0) {
-      int stage = 0;
+    if (warp == 0) {
+      // (the whole warp and an elected lane: the copies' operands stay in uniform registers)
+      const uint32_t u_ring = __shfl_sync(0xffffffffu, ring, 0), u_full = __shfl_sync(0xffffffffu, full0, 0);
+      int stage = 0, issued = 0;
       uint32_t phase = 0;
       bool ok = true;
       for (int t = first; t < num_tiles && ok; t += step) {
         const int nt = t / p.MT, mt = t % p.MT;
         for (int kb = kb0; kb < kb1; ++kb) {
-          if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, &s_abort)) {
+          if (!__all_sync(0xffffffffu, mbar_wait(empty0 + 8 * stage, phase ^ 1, &s_abort))) {
             ok = false;
             break;
           }
-          const uint32_t fb = full0 + 8 * stage, at = ring + (uint32_t)stage * stBytes;
-          mbar_expect_tx(fb, aBytes + kWBytes);
-          tma_load_2d(at + aStage, &tmW, fb, kb * kBlk, nt * BN);
-          tma_load_2d(at, &tmX, fb, kb * kBlk, mt * BM);
-          ++s_issued;
+          if (elect_one()) {
+            const uint32_t fb = u_full + 8 * stage, at = u_ring + (uint32_t)stage * stBytes;
+            mbar_expect_tx(fb, aBytes + kWBytes);
+            tma_load_2d(at + aStage, &tmW, fb, kb * kBlk, nt * BN);
+            tma_load_2d(at, &tmX, fb, kb * kBlk, mt * BM);
+          }
+          __syncwarp();
+          ++issued;
           if (++stage == S) {
             stage = 0;
             phase ^= 1;
           }
         }
       }
+      if (lane == 0) s_issued = issued;
     } else if (warp == 1) {
       const uint32_t idesc = idesc_e4m3(BM, BN);
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);

@@ -276,9 +276,10 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
     if (warp == 0) {
-      int stage = 0;
+      int stage = 0, issued = 0;
       uint32_t phase = 0;
       bool ok = true;
+      const uint32_t u_full = __shfl_sync(0xffffffffu, full0, 0), u_ring = __shfl_sync(0xffffffffu, ring, 0);
       const int tiles = (int)p.ctl->tiles, gates = tiles * p.IT, total = gates + tiles * p.HT;
       // a task, worked out while the loads of the one before it wait for room in the ring: drawn at kDraw k-blocks
       // before that one's end, its tile looked up at kLook, whether h is there at kList
@@ -318,9 +319,10 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
           }
           break;
         }
-        const bool gate = g < gates;
+        const bool gate = __shfl_sync(0xffffffffu, (int)(g < gates), 0) != 0;
         const int w = gate ? p.wg : p.wd;
-        const int at_entry = entry, h32 = gate ? 0 : rows / 32, h8 = gate ? 0 : (rows % 32 + 7) / 8;   // boxes of h
+        const int at_entry = __shfl_sync(0xffffffffu, entry, 0), urows = __shfl_sync(0xffffffffu, rows, 0);
+        const int h32 = gate ? 0 : urows / 32, h8 = gate ? 0 : (urows % 32 + 7) / 8;   // boxes of h
         int wy0, wy1;                                         // the two tiles' first weight rows
         if (gate) {
           wy0 = e.expert * 2 * p.I + blk * w;
@@ -346,6 +348,10 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
           s_task[slot] = t;
           mbar_arrive(qfull0 + 8 * slot);
         }
+        // (uniform values and an elected lane: copies whose operands the compiler has to move to uniform registers one by one
+        // take 100 ns each to issue)
+        wy0 = __shfl_sync(0xffffffffu, wy0, 0);
+        wy1 = __shfl_sync(0xffffffffu, wy1, 0);
         const uint32_t boxBytes = (uint32_t)w * 128, bytes = 2 * boxBytes + (uint32_t)(4 * h32 + h8) * 1024u;
         const int KB = gate ? p.KB1 : p.KB2;
         for (int kb = 0; kb < KB; ++kb) {
@@ -353,18 +359,21 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
             ok = false;
             break;
           }
-          const uint32_t fb = full0 + 8 * stage, sb = ring + (uint32_t)stage * stBytes, sw = sb + bStage;
-          if (lane == 0) {
+          const uint32_t fb = u_full + 8 * stage, sb = u_ring + (uint32_t)stage * stBytes, sw = sb + bStage;
+          if (elect_one()) {
             mbar_expect_tx(fb, bytes);
-            tma_load_2d_hint(sw, gate ? &tmW1 : &tmW2, fb, kb * kCols, wy0, policy);
-            tma_load_2d_hint(sw + boxBytes, gate ? &tmW1 : &tmW2, fb, kb * kCols, wy1, policy);
-            ++s_issued;
+            if (gate) {
+              tma_load_2d_hint(sw, &tmW1, fb, kb * kCols, wy0, policy);
+              tma_load_2d_hint(sw + boxBytes, &tmW1, fb, kb * kCols, wy1, policy);
+            } else {
+              tma_load_2d_hint(sw, &tmW2, fb, kb * kCols, wy0, policy);
+              tma_load_2d_hint(sw + boxBytes, &tmW2, fb, kb * kCols, wy1, policy);
+              for (int i = 0; i < h32; ++i) tma_load_2d(sb + i * 4096, &tmH32, fb, kb * kCols, at_entry + 32 * i);
+              for (int i = 0; i < h8; ++i) tma_load_2d(sb + h32 * 4096 + i * 1024, &tmH8, fb, kb * kCols, at_entry + 32 * h32 + 8 * i);
+            }
           }
           __syncwarp();
-          if (lane < h32) tma_load_2d(sb + lane * 4096, &tmH32, fb, kb * kCols, at_entry + 32 * lane);
-          else if (lane - h32 < h8)
-            tma_load_2d(sb + h32 * 4096 + (lane - h32) * 1024, &tmH8, fb, kb * kCols, at_entry + 32 * h32 + 8 * (lane - h32));
-          __syncwarp();
+          ++issued;
           if (kb == max(0, KB - kDraw)) draw();
           if (kb == max(0, KB - kLook)) look();
           if (kb == max(0, KB - kList)) list();
@@ -374,6 +383,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
           }
         }
       }
+      if (lane == 0) s_issued = issued;
     } else if (warp == 1) {
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
       const uint64_t bd0 = smem_desc_sw128(__shfl_sync(0xffffffffu, ring, 0));

@@ -121,7 +121,8 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
           break;
         }
         const uint32_t fb = full0 + 8 * slot, at = ring + (uint32_t)slot * stBytes;
-        if (lane == 0) {
+        const int w2row = (end || gate ? 0 : s_tab.expert[a] * p.H) + col;
+        if (elect_one()) {                                     // (operands in uniform registers)
           s_unit[grp][slot] = u;
           if (end) {
             mbar_arrive(fb);
@@ -132,7 +133,7 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
             tma_load_2d(at + 8u * 128u * (uint32_t)c1, &tmW1, fb, ch * c1 * 32, y + p.I);
           } else {
             mbar_expect_tx(fb, 16u * 128u * (uint32_t)c2);
-            tma_load_2d(at, &tmW2, fb, ch * c2 * 32, s_tab.expert[a] * p.H + col);
+            tma_load_2d(at, &tmW2, fb, ch * c2 * 32, w2row);
           }
         }
         if (kFp8 && lane < 2 * kFewWarps) {
