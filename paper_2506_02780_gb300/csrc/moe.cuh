@@ -22,7 +22,7 @@ struct MoeCtl {
   uint32_t down_done;        // down tasks that stored their part of y (few tokens: gate tasks, of h)
   uint32_t tiles;            // token tiles
   uint32_t pad[4];
-  uint32_t gate_done[1];     // per token tile: gate tasks (8-bit weights: blocks of h) that are there
+  uint32_t gate_done[1];     // per token tile: gate tasks that stored their part of h (few tokens, the first: down units)
 };
 struct __align__(32) MoeTile {   // a token tile's expert
   int expert, entry0, count;   // its first entry and their number
@@ -30,18 +30,19 @@ struct __align__(32) MoeTile {   // a token tile's expert
   int pad[3];
 };
 constexpr int kFewTokens = 16;
+constexpr int kFewParts = 4;  // of the chosen experts, whose sums for a column are units of their own
 struct FewEntry {            // of up to 16 tokens: an active expert's entry of a token, or -1, and its weight
   int entry;
   float p;
 };
 
 struct MoeLayout {
-  size_t ctl, sub, tile, few, ids, prob, list, inv, xq, xs, h, hf, hs, y, total;
+  size_t ctl, tile, few, ids, prob, list, inv, xq, xs, h, hf, hs, y, total;
   int max_tiles;             // token tiles of all experts, at most
 };
 inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t k) {
   MoeLayout l;
-  const int64_t n = T * k;
+  const int64_t n = T * k, few = std::min<int64_t>(T, kFewTokens);
   l.max_tiles = (int)(std::min(E, n) + n / 64);   // (32 only where no expert can have more)
   size_t at = align_up(kWorkspaceBytes, 256);
   const auto take = [&](size_t bytes) {
@@ -50,7 +51,6 @@ inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t 
     return here;
   };
   l.ctl = take(sizeof(MoeCtl) + 4 * (size_t)l.max_tiles);
-  l.sub = take(4 * (size_t)l.max_tiles * (size_t)((I + kBlk - 1) / kBlk));
   l.tile = take(sizeof(MoeTile) * (size_t)l.max_tiles);
   l.few = take(sizeof(FewEntry) * kFewTokens * kFewTokens * kMoeMaxTopK);
   l.ids = take(4 * (size_t)n);
@@ -60,9 +60,9 @@ inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t 
   l.xq = take((size_t)(T * H));
   l.xs = take(4 * (size_t)(T * ((H + kBlk - 1) / kBlk)));
   l.h = take(2 * (size_t)(n * I));
-  l.hf = take(4 * (size_t)(n * I));
+  l.hf = take(4 * (size_t)(few * k * I));
   l.hs = take(4 * (size_t)(n * ((I + kBlk - 1) / kBlk)));
-  l.y = take(4 * (size_t)(n * H));
+  l.y = take(4 * (size_t)(std::max(n, few * kFewParts) * H));
   l.total = at;
   return l;
 }
@@ -74,8 +74,6 @@ struct RouteParams {
   const int32_t* live;       // or NULL
   int T, H, E, k, renorm, cl, max_tiles, tile_rows;
   MoeCtl* ctl;
-  uint32_t* sub;             // or NULL: [n_sub] counters to zero
-  int n_sub;
   MoeTile* tile;
   FewEntry* few;             // or NULL (more than 16 tokens): [active expert][16]
   int32_t* ids;              // [T][k] experts of a token, ascending
@@ -92,16 +90,14 @@ ee_status launch_moe_route(const RouteParams& p, cudaStream_t stream);
 struct MoeParams {
   int T, H, I, E, k, n;                // n = T k
   int KB1, KB2;                        // 128-byte blocks along H and I
-  int wg, wd;                          // rows of a tile of gate and up, of down
-  int IT, HT;                          // gate tasks, down tasks of a token tile
-  int IB, HB;                          // scale blocks along I and H
+  int HT;                              // down tasks of a token tile
+  int IB, HB;                          // blocks of 128 along I (gate tasks, too) and H
   int b_rows, stages;
   const void* w1;
   const void* w2;
   const void* x;                       // codes or bf16
   int64_t x_stride;
   MoeCtl* ctl;
-  uint32_t* sub;                       // [tile][IB] gate tasks of a block of h that are there (wg < 128)
   const MoeTile* tile;
   const FewEntry* few;
   const int32_t* list;
@@ -111,7 +107,7 @@ struct MoeParams {
   const float* s1;                     // [E][2][IB][blocks of H]
   const float* s2;                     // [E][HB][blocks of I]
   void* h;                             // [n][I] codes or bf16
-  float* hf;                           // [n][I] h before it is quantised
+  float* hf;                           // [n][I] h before it is quantised (few tokens)
   float* hs;                           // [IB][n]
   float* y;                            // [n][H]
   __nv_bfloat16* out;

@@ -1,12 +1,14 @@
 // ee_moe_layer: a mixture-of-experts layer for the few tokens of a pass.  After the router (moe_route.cu)
 // one persistent kernel runs the chosen experts:
-//   gate tasks   h = silu(x Wg^T) * (x Wu^T)   w columns of h for one token tile
-//   down tasks   y = h Wd^T                    2 w columns of y
+//   gate tasks   h = silu(x Wg^T) * (x Wu^T)   128 columns of h for one token tile
+//   down tasks   y = h Wd^T                    256 columns of y
 //   the sum      out[t] = sum_j p[t][j] y[entry of t's j-th expert]
 // The experts' weights are read once and bound the call.  Weight rows are the MMA's M side (two tiles of
-// up to 128: gate and up, or two of down), tokens its N side: a few tokens then cost the epilogue a few
+// 128: gate and up, or two of down), tokens its N side: a few tokens then cost the epilogue a few
 // columns of every lane, where with tokens on the lanes two warps of eight would do all of its work (a draft
-// tree's layer of 64 experts of 1280 x 3584: 194 us against %TREE%).
+// tree's layer of 64 experts of 1280 x 3584 took 194 us so).  Narrower tiles make more tasks, but a k-block takes
+// its 0.4 us with half the rows, too (the same layer with 64 rows 177 us, with 128 141; 8 experts of 2560 for 20
+// tokens 63 and 67).
 //
 // CTAs draw tasks from one queue, gate tasks first.  A down task waits for the gate tasks of its
 // token tile; those were drawn before it by CTAs that are running, so no wait depends on
@@ -14,8 +16,7 @@
 // shared memory and streams the operands (x's rows: warps 12..15); it runs ahead of the others across
 // tasks, so that the stream does not stop between them.  Warp 2 puts products of scales into shared memory,
 // warp 3 tells other CTAs what the epilogue warps 4..11 have stored (a release waits for the stores: it would hold them up
-// for 2 us a task).  A block of 128 columns of h is quantised by the epilogue where it is one task's; where
-// tasks are narrower, warp 3 of the CTA that completes it reads it back.
+// for 2 us a task).
 #include <mutex>
 
 #include "moe.cuh"
@@ -28,9 +29,10 @@ constexpr int kThreads = 512;          // warp 0 tasks and TMA, 1 MMA, 2 TMEM an
 constexpr int kEpiWarps = 8;           // two per TMEM lane quarter, every other 16 tokens each
 constexpr int kRegsAll = 128;          // a warp's at launch; the epilogue's take some of the others'
 constexpr int kGatherWarps = 4;
+constexpr int kTile = 128;             // rows of a weight tile
 constexpr int kRing = 4;               // tasks published and not yet done with by every role
 constexpr int kScRing = 8;             // k-blocks' scales
-constexpr int kMaxStages = 12;
+constexpr int kMaxStages = 6;
 
 enum { kGate = 0, kDown = 1, kEnd = 2 };
 struct Task {
@@ -58,7 +60,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
                    const __grid_constant__ CUtensorMap tmH32, const __grid_constant__ CUtensorMap tmW2, const MoeParams p) {
   constexpr int kCols = kFp8 ? 128 : 64;        // elements in 128 bytes
   constexpr int kRegsEpi = NT == 128 ? 200 : 152, kRegsOther = 2 * kRegsAll - kRegsEpi;
-  constexpr int kScBatch = NT == 128 ? 2 : 4, kQuBatch = NT == 128 ? 4 : 8;   // k-blocks' scales, tokens' h: loads in flight
+  constexpr int kScBatch = NT == 128 ? 2 : 4;   // k-blocks whose scales' loads are in flight
   constexpr int kBufs = 512 / (2 * NT) < 8 ? 512 / (2 * NT) : 8;   // accumulators of two tiles
   constexpr int kChunks = NT / 32;              // groups of 16 tokens of an epilogue warp
   extern __shared__ uint8_t smem_raw[];
@@ -76,7 +78,8 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int S = p.stages;
   const uint32_t bStage = (uint32_t)p.b_rows * 128;            // tokens, then the weights' two tiles
-  const uint32_t stBytes = bStage + 2u * (uint32_t)max(p.wg, p.wd) * 128;
+  constexpr uint32_t kBoxBytes = kTile * 128;
+  const uint32_t stBytes = bStage + 2 * kBoxBytes;
   const uint32_t ring = smem_u32(smem);
   const uint32_t full0 = smem_u32(s_bars), empty0 = full0 + 8 * kMaxStages, tfull0 = empty0 + 8 * kMaxStages,
                  tempty0 = tfull0 + 8 * 8, qfull0 = tempty0 + 8 * 8, qempty0 = qfull0 + 8 * kRing,
@@ -138,8 +141,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
       if (lane == 0) mbar_arrive(qempty0 + 8 * slot);
       if (t.kind == kEnd) break;
       const bool gate = t.kind == kGate;
-      const int w = gate ? p.wg : p.wd;
-      const bool mine = 32 * q < w && half * 16 < t.rows;     // the warp has something to keep
+      const bool mine = half * 16 < t.rows;                   // the warp has something to keep
       uint64_t acc0[kChunks][8], acc1[kChunks][8];            // tokens (2 j + half) 16 .. + 15 of the two tiles
 #pragma unroll
       for (int j = 0; j < kChunks; ++j)
@@ -189,72 +191,68 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
       }
       if (!ok) break;
       if (mine && gate) {
-        const int col = t.blk * w + r;
-        const bool in = r < w && col < p.I;
-        const bool whole = kFp8 && p.wg == kBlk;              // the task has its block of h to itself
+        const int col = t.blk * kTile + r;
+        const bool in = col < p.I;
         uint32_t top[kChunks];                                // lane i: the largest |h| of token i in these 32 columns
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
           const int c = (2 * j + half) * 16;
           top[j] = 0;
           if (c >= t.rows) break;
-          const size_t at = (size_t)(t.entry + c) * p.I + col;
+          __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.h) + (size_t)(t.entry + c) * p.I + col;
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             uint32_t g[2], u[2];
             f2_unpack(acc0[j][i / 2], g[0], g[1]);
             f2_unpack(acc1[j][i / 2], u[0], u[1]);
             const float h = silu_times(__uint_as_float(g[i & 1]), __uint_as_float(u[i & 1]));
-            if (whole) {
+            if constexpr (kFp8) {
               const uint32_t m = __reduce_max_sync(0xffffffffu, in ? __float_as_uint(h) & 0x7fffffffu : 0u);
               if (lane == i) top[j] = m;
               acc0[j][i / 2] = i & 1 ? f2_pack(g[0], __float_as_uint(h)) : f2_pack(__float_as_uint(h), g[1]);
             } else if (in && c + i < t.rows) {
-              if constexpr (kFp8) __stcg(p.hf + at + (size_t)i * p.I, h);
-              else static_cast<__nv_bfloat16*>(p.h)[at + (size_t)i * p.I] = __float2bfloat16_rn(h);
+              o[(size_t)i * p.I] = __float2bfloat16_rn(h);
             }
           }
-          if (kFp8 && whole && lane < 16) s_top[meets & 1][q][c + lane] = top[j];
+          if (kFp8 && lane < 16) s_top[meets & 1][q][c + lane] = top[j];
         }
         if constexpr (kFp8) {
-          if (whole) {
-            // the block's other columns are the three warps' of the same tokens
-            __syncwarp();
-            if (lane == 0) mbar_arrive(meet0 + 8 * half);
-            if (!__all_sync(0xffffffffu, mbar_wait(meet0 + 8 * half, meets & 1, &s_abort))) break;
+          // the block's other columns are the three warps' of the same tokens
+          __syncwarp();
+          if (lane == 0) mbar_arrive(meet0 + 8 * half);
+          if (!__all_sync(0xffffffffu, mbar_wait(meet0 + 8 * half, meets & 1, &s_abort))) break;
 #pragma unroll
-            for (int j = 0; j < kChunks; ++j) {
-              const int c = (2 * j + half) * 16;
-              if (c >= t.rows) break;
-              uint32_t m = 0;
+          for (int j = 0; j < kChunks; ++j) {
+            const int c = (2 * j + half) * 16;
+            if (c >= t.rows) break;
+            uint32_t m = 0;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) m = max(m, s_top[meets & 1][i][c + (lane & 15)]);
-              const BlockScale mine_s = block_scale(__uint_as_float(m));
-              if (q == 0 && lane < 16 && c + lane < t.rows) p.hs[(size_t)t.blk * p.n + t.entry + c + lane] = mine_s.scale;
-              uint8_t* o = static_cast<uint8_t*>(p.h) + (size_t)(t.entry + c) * p.I + col;
+            for (int i = 0; i < 4; ++i) m = max(m, s_top[meets & 1][i][c + (lane & 15)]);
+            const BlockScale mine_s = block_scale(__uint_as_float(m));
+            if (q == 0 && lane < 16 && c + lane < t.rows) p.hs[(size_t)t.blk * p.n + t.entry + c + lane] = mine_s.scale;
+            uint8_t* o = static_cast<uint8_t*>(p.h) + (size_t)(t.entry + c) * p.I + col;
 #pragma unroll
-              for (int i = 0; i < 16; i += 2) {
-                uint32_t h[2];
-                f2_unpack(acc0[j][i / 2], h[0], h[1]);
-                float v[2];
+            for (int i = 0; i < 16; i += 2) {
+              uint32_t h[2];
+              f2_unpack(acc0[j][i / 2], h[0], h[1]);
+              float v[2];
 #pragma unroll
-                for (int d = 0; d < 2; ++d) {
-                  BlockScale s;
-                  s.hi = __shfl_sync(0xffffffffu, mine_s.hi, i + d);
-                  s.lo = __shfl_sync(0xffffffffu, mine_s.lo, i + d);
-                  v[d] = to_code(__uint_as_float(h[d]), s);
-                }
-                const uint32_t code = pack_e4m3(v[0], v[1], 0.f, 0.f);
-                if (in && c + i < t.rows) o[(size_t)i * p.I] = (uint8_t)code;
-                if (in && c + i + 1 < t.rows) o[(size_t)(i + 1) * p.I] = (uint8_t)(code >> 8);
+              for (int d = 0; d < 2; ++d) {
+                BlockScale s;
+                s.hi = __shfl_sync(0xffffffffu, mine_s.hi, i + d);
+                s.lo = __shfl_sync(0xffffffffu, mine_s.lo, i + d);
+                v[d] = to_code(__uint_as_float(h[d]), s);
               }
+              const uint32_t code = pack_e4m3(v[0], v[1], 0.f, 0.f);
+              if (in && c + i < t.rows) o[(size_t)i * p.I] = (uint8_t)code;
+              if (in && c + i + 1 < t.rows) o[(size_t)(i + 1) * p.I] = (uint8_t)(code >> 8);
             }
-            ++meets;
           }
+          ++meets;
         }
       } else if (mine) {
-        const int col = t.blk * 2 * w + r;
-        const bool in0 = r < w && col < p.H, in1 = r < w && col + w < p.H;
+        const int col = t.blk * 2 * kTile + r;
+        const bool in0 = col < p.H, in1 = col + kTile < p.H;
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
           const int c = (2 * j + half) * 16;
@@ -266,7 +264,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
             f2_unpack(acc0[j][i / 2], a[0], a[1]);
             f2_unpack(acc1[j][i / 2], b[0], b[1]);
             if (in0 && c + i < t.rows) __stcg(o, __uint_as_float(a[i & 1]));
-            if (in1 && c + i < t.rows) __stcg(o + w, __uint_as_float(b[i & 1]));
+            if (in1 && c + i < t.rows) __stcg(o + kTile, __uint_as_float(b[i & 1]));
           }
         }
       }
@@ -280,7 +278,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
       uint32_t phase = 0;
       bool ok = true;
       const uint32_t u_full = __shfl_sync(0xffffffffu, full0, 0), u_ring = __shfl_sync(0xffffffffu, ring, 0);
-      const int tiles = (int)p.ctl->tiles, gates = tiles * p.IT, total = gates + tiles * p.HT;
+      const int tiles = (int)p.ctl->tiles, gates = tiles * p.IB, total = gates + tiles * p.HT;
       // a task, worked out while the loads of the one before it wait for room in the ring: drawn at kDraw k-blocks
       // before that one's end, its tile looked up at kLook, whether h is there at kList
       constexpr int kDraw = 10, kLook = 7, kList = 4;
@@ -293,13 +291,13 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
       };
       const auto look = [&]() {
         g = __shfl_sync(0xffffffffu, g, 0);
-        if (g < total) e = p.tile[(g < gates ? g : g - gates) / (g < gates ? p.IT : p.HT)];
+        if (g < total) e = p.tile[(g < gates ? g : g - gates) / (g < gates ? p.IB : p.HT)];
       };
       int tile = 0;
       const auto list = [&]() {
         if (g >= total) return;
         const bool gate = g < gates;
-        const int local = (gate ? g : g - gates) - e.first * (gate ? p.IT : p.HT), mt = local % e.tiles;
+        const int local = (gate ? g : g - gates) - e.first * (gate ? p.IB : p.HT), mt = local % e.tiles;
         blk = local / e.tiles;
         tile = e.first + mt;
         entry = e.entry0 + mt * NT;
@@ -320,17 +318,16 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
           break;
         }
         const bool gate = __shfl_sync(0xffffffffu, (int)(g < gates), 0) != 0;
-        const int w = gate ? p.wg : p.wd;
         const int at_entry = __shfl_sync(0xffffffffu, entry, 0), urows = __shfl_sync(0xffffffffu, rows, 0);
         const int h32 = gate ? 0 : urows / 32, h8 = gate ? 0 : (urows % 32 + 7) / 8;   // boxes of h
         int wy0, wy1;                                         // the two tiles' first weight rows
         if (gate) {
-          wy0 = e.expert * 2 * p.I + blk * w;
+          wy0 = e.expert * 2 * p.I + blk * kTile;
           wy1 = wy0 + p.I;
         } else {
-          wy0 = e.expert * p.H + blk * 2 * w;
-          wy1 = wy0 + w;
-          const uint32_t want = (uint32_t)(kFp8 ? p.IB : p.IT);
+          wy0 = e.expert * p.H + blk * 2 * kTile;
+          wy1 = wy0 + kTile;
+          const uint32_t want = (uint32_t)p.IB;
           if (!__all_sync(0xffffffffu, have >= want || wait_count_geq(p.ctl->gate_done + tile, want))) {
             s_abort = 1;
             break;
@@ -352,7 +349,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
         // take 100 ns each to issue)
         wy0 = __shfl_sync(0xffffffffu, wy0, 0);
         wy1 = __shfl_sync(0xffffffffu, wy1, 0);
-        const uint32_t boxBytes = (uint32_t)w * 128, bytes = 2 * boxBytes + (uint32_t)(4 * h32 + h8) * 1024u;
+        const uint32_t bytes = 2 * kBoxBytes + (uint32_t)(4 * h32 + h8) * 1024u;
         const int KB = gate ? p.KB1 : p.KB2;
         for (int kb = 0; kb < KB; ++kb) {
           if (!__all_sync(0xffffffffu, mbar_wait(empty0 + 8 * stage, phase ^ 1, &s_abort))) {
@@ -364,10 +361,10 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
             mbar_expect_tx(fb, bytes);
             if (gate) {
               tma_load_2d_hint(sw, &tmW1, fb, kb * kCols, wy0, policy);
-              tma_load_2d_hint(sw + boxBytes, &tmW1, fb, kb * kCols, wy1, policy);
+              tma_load_2d_hint(sw + kBoxBytes, &tmW1, fb, kb * kCols, wy1, policy);
             } else {
               tma_load_2d_hint(sw, &tmW2, fb, kb * kCols, wy0, policy);
-              tma_load_2d_hint(sw + boxBytes, &tmW2, fb, kb * kCols, wy1, policy);
+              tma_load_2d_hint(sw + kBoxBytes, &tmW2, fb, kb * kCols, wy1, policy);
               for (int i = 0; i < h32; ++i) tma_load_2d(sb + i * 4096, &tmH32, fb, kb * kCols, at_entry + 32 * i);
               for (int i = 0; i < h8; ++i) tma_load_2d(sb + h32 * 4096 + i * 1024, &tmH8, fb, kb * kCols, at_entry + 32 * h32 + 8 * i);
             }
@@ -398,7 +395,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
         if (lane == 0) mbar_arrive(qempty0 + 8 * slot);
         if (kind == kEnd) break;
         const int KB = kind == kGate ? p.KB1 : p.KB2;
-        const uint64_t tile2 = (uint64_t)((kind == kGate ? p.wg : p.wd) * 128 >> 4);
+        constexpr uint64_t tile2 = kBoxBytes >> 4;
         const int N = (rows + 15) & ~15;
         const uint32_t idesc = kFp8 ? idesc_e4m3(128, N) : idesc_bf16(128, N);
         for (int kb = 0; kb < KB; ++kb) {
@@ -454,11 +451,11 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
           const int KB = gate ? p.KB1 : p.KB2;
           const float *ws0, *ws1;
           if (gate) {
-            ws0 = p.s1 + ((int64_t)(2 * t.expert) * p.IB + t.blk * p.wg / kBlk) * KB;
+            ws0 = p.s1 + ((int64_t)(2 * t.expert) * p.IB + t.blk) * KB;
             ws1 = ws0 + (int64_t)p.IB * KB;
           } else {
-            ws0 = p.s2 + ((int64_t)t.expert * p.HB + min(t.blk * 2 * p.wd / kBlk, p.HB - 1)) * KB;
-            ws1 = p.s2 + ((int64_t)t.expert * p.HB + min((t.blk * 2 + 1) * p.wd / kBlk, p.HB - 1)) * KB;
+            ws0 = p.s2 + ((int64_t)t.expert * p.HB + min(t.blk * 2, p.HB - 1)) * KB;
+            ws1 = p.s2 + ((int64_t)t.expert * p.HB + min(t.blk * 2 + 1, p.HB - 1)) * KB;
           }
           const float* xs = gate ? p.xs : p.hs;
           const int xstep = gate ? p.T : p.n;
@@ -568,53 +565,6 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
           if (lane == 0) red_inc_release(&p.ctl->down_done, 0xffffffffu);
           continue;
         }
-        if constexpr (kFp8) {
-          const int b = t.blk * p.wg / kBlk;                  // the block of h
-          if (p.wg == kBlk) {
-            asm volatile("fence.proxy.async;" ::: "memory");
-            if (lane == 0) red_inc_release(p.ctl->gate_done + t.tile, 0xffffffffu);
-            continue;
-          }
-          {
-            uint32_t last = 0;
-            if (lane == 0) {
-              const uint32_t parts = (uint32_t)((min(kBlk, p.I - b * kBlk) + p.wg - 1) / p.wg);
-              last = atom_inc_acq_rel(p.sub + t.tile * p.IB + b, parts - 1) == parts - 1;
-            }
-            if (!__shfl_sync(0xffffffffu, last, 0)) continue;
-          }
-          const int col = b * kBlk + 4 * lane;
-          const bool in = col < p.I;
-          for (int r0 = 0; r0 < t.rows; r0 += kQuBatch) {            // a token's block at a time
-            float4 v[kQuBatch];
-#pragma unroll
-            for (int i = 0; i < kQuBatch; ++i) {
-              v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-              if (in && r0 + i < t.rows)
-                v[i] = __ldcg(reinterpret_cast<const float4*>(p.hf + (size_t)(t.entry + r0 + i) * p.I + col));
-            }
-            uint32_t my_top = 0;                              // lane i: of the i-th token
-#pragma unroll
-            for (int i = 0; i < kQuBatch; ++i) {
-              const uint32_t m = 0x7fffffffu;
-              const uint32_t top = __reduce_max_sync(
-                  0xffffffffu, max(max(__float_as_uint(v[i].x) & m, __float_as_uint(v[i].y) & m),
-                                   max(__float_as_uint(v[i].z) & m, __float_as_uint(v[i].w) & m)));
-              if (lane == i) my_top = top;
-            }
-            const BlockScale mine = block_scale(__uint_as_float(my_top));
-            if (lane < kQuBatch && r0 + lane < t.rows) p.hs[(size_t)b * p.n + t.entry + r0 + lane] = mine.scale;
-#pragma unroll
-            for (int i = 0; i < kQuBatch; ++i) {
-              BlockScale s;
-              s.hi = __shfl_sync(0xffffffffu, mine.hi, i);
-              s.lo = __shfl_sync(0xffffffffu, mine.lo, i);
-              if (in && r0 + i < t.rows)
-                *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(p.h) + (size_t)(t.entry + r0 + i) * p.I + col) =
-                    pack_e4m3(to_code(v[i].x, s), to_code(v[i].y, s), to_code(v[i].z, s), to_code(v[i].w, s));
-            }
-          }
-        }
         asm volatile("fence.proxy.async;" ::: "memory");      // down tasks read h by TMA
         __syncwarp();
         if (lane == 0) red_inc_release(p.ctl->gate_done + t.tile, 0xffffffffu);
@@ -719,11 +669,9 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
 template <bool kFp8, int NT>
 ee_status launch(MoeParams& p, cudaStream_t stream) {
   const uint64_t es = kFp8 ? 1 : 2;
-  const size_t wide = (size_t)std::max(p.wg, p.wd), stage = (size_t)p.b_rows * 128 + 2 * wide * 128;
-  // an MMA takes 128 rows of a tile of fewer: what follows, and the lanes are not looked at
-  const size_t slack = 1024 + (128 - (size_t)std::min(p.wg, p.wd)) * 128;
-  p.stages = (int)std::min<size_t>(kMaxStages, ((size_t)(214 * 1024) - slack) / stage);
-  const size_t smem = slack + p.stages * stage;
+  const size_t stage = (size_t)p.b_rows * 128 + 2 * kTile * 128;
+  p.stages = (int)std::min<size_t>(kMaxStages, (size_t)(213 * 1024) / stage);
+  const size_t smem = 1024 + p.stages * stage;
   CUtensorMap tmW1, tmH8, tmH32, tmW2;
   const auto encode = [](CUtensorMap* m, const void* base, uint64_t cols, uint64_t rows, uint64_t stride, uint32_t box) {
     if constexpr (kFp8) return encode_u8_tmap_2d(m, base, cols, rows, stride, 128, box);
@@ -731,8 +679,8 @@ ee_status launch(MoeParams& p, cudaStream_t stream) {
     const uint32_t boxes[2] = {64, box};
     return encode_bf16_tmap(m, base, 2, dims, strides, boxes);
   };
-  if (!encode(&tmW1, p.w1, p.H, (uint64_t)p.E * 2 * p.I, p.H, p.wg) ||
-      !encode(&tmH8, p.h, p.I, p.n, p.I, 8) || !encode(&tmH32, p.h, p.I, p.n, p.I, 32) || !encode(&tmW2, p.w2, p.I, (uint64_t)p.E * p.H, p.I, p.wd))
+  if (!encode(&tmW1, p.w1, p.H, (uint64_t)p.E * 2 * p.I, p.H, kTile) ||
+      !encode(&tmH8, p.h, p.I, p.n, p.I, 8) || !encode(&tmH32, p.h, p.I, p.n, p.I, 32) || !encode(&tmW2, p.w2, p.I, (uint64_t)p.E * p.H, p.I, kTile))
     return EE_ERR_CUDA;
   {
     int dev = 0;
@@ -812,16 +760,10 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   p.E = E;
   p.k = k;
   p.n = T * k;
-  // the widest tiles of which the tiles in use at most make a task for nearly every SM
-  const int64_t most = std::min<int64_t>(E, p.n);
-  p.wg = p.wd = 128;
-  while (p.wg > 32 && most * ((I + p.wg - 1) / p.wg) < 100) p.wg /= 2;
-  while (p.wd > 32 && most * ((H + 2 * p.wd - 1) / (2 * p.wd)) < 2 * ee::kNumSMs) p.wd /= 2;
-  p.IT = (I + p.wg - 1) / p.wg;
-  p.HT = (H + 2 * p.wd - 1) / (2 * p.wd);
   p.KB1 = (H * (fp8 ? 1 : 2) + 127) / 128;
   p.KB2 = (I * (fp8 ? 1 : 2) + 127) / 128;
   p.IB = (I + kBlk - 1) / kBlk;
+  p.HT = (H + 2 * kTile - 1) / (2 * kTile);
   p.HB = blocks;
   const int nt = ee::moe_tile_rows(T, E, k, fp8);
   p.b_rows = std::min(nt, (T + 15) / 16 * 16);
@@ -830,9 +772,6 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   p.x = fp8 ? static_cast<const void*>(r.xq) : x;
   p.x_stride = fp8 ? H : x_stride;
   p.ctl = r.ctl;
-  p.sub = reinterpret_cast<uint32_t*>(base + l.sub);
-  r.sub = fp8 && p.wg < kBlk ? p.sub : nullptr;
-  r.n_sub = l.max_tiles * p.IB;
   p.tile = r.tile;
   p.few = r.few;
   p.list = r.list;

@@ -2,13 +2,14 @@
 // Two groups of a producer warp and 8 consumer warps draw units from a queue:
 //   gate unit    8 columns of h of one expert: a warp's MMAs take its 8 gate rows and its 8 up rows, so that a
 //                lane holds both halves of silu(g) u
-//   down unit    16 columns of out, over all chosen experts: their sums are weighted on the way, and no y is stored
+//   down unit    16 columns of out, over all chosen experts or a part of them: their sums are weighted on the way, and
+//                y of single experts is not stored
 // A group's producer streams its units' 16 weight rows in stages of up to 8 blocks of 128 bytes, one for
 // each consumer (few.cuh), and runs ahead across units; the consumers add their sums at a unit's end.
 // (Consumers that load their own weights spend more instructions on addresses than on products and reach 3 to
 // 4.3 TB/s.)  Between gate and down units lies one wait for the gate units of the other CTAs (all drawn before,
 // by CTAs that are running), during which the first down units' weights are under way; then
-// every CTA brings h into its own shared memory, as e4m3 codes for 8-bit weights.
+// every CTA brings h into its own shared memory, as e4m3 codes for 8-bit weights.  Parts' sums are added at the end.
 #include <mutex>
 
 #include "moe.cuh"
@@ -86,7 +87,18 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
     s_tab.p[i / NT][i % NT] = e.p;
   }
   const int live = p.live ? max(0, min(p.T, ld_pinned(p.live))) : p.T;
-  const int per = p.I / 8, gates = na * per, total = gates + (na ? (p.H + 15) / 16 : 0);
+  const int per = p.I / 8, gates = na * per, cols = (p.H + 15) / 16;
+  // the experts of a down unit: in as few parts as give the busiest group the least to do (8 tokens at 6 of 64 experts
+  // of 1280 x 3584, about 36 in use: down units of all of them, 224 for 304 groups, took 35 us)
+  int parts = 1;
+  for (int s = 2, best = (cols + kGroups * (int)gridDim.x - 1) / (kGroups * (int)gridDim.x) * na; s <= kFewParts; s *= 2) {
+    const int turns = (cols * s + kGroups * (int)gridDim.x - 1) / (kGroups * (int)gridDim.x), cost = turns * ((na + s - 1) / s) + 1;
+    if (cost < best) {
+      best = cost;
+      parts = s;
+    }
+  }
+  const int total = gates + (na ? cols * parts : 0);
   const int nst1 = stages_of(p.KB1), nst2 = stages_of(p.KB2), c1 = blocks_of(p.KB1), c2 = blocks_of(p.KB2);
   const uint32_t stBytes = 16u * 128u * (uint32_t)max(c1, c2);
   const int grp = warp < kGroups ? warp : (warp - kGroups) / kFewWarps;
@@ -112,9 +124,10 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
       const bool end = u >= total, gate = u < gates;
       int next = 0;
       if (!end && lane == 0) next = (int)atomicAdd(&p.ctl->queue, 1u);
-      const int stages = end ? 1 : gate ? nst1 : na * nst2;
-      const int ge = gate && !end ? s_tab.expert[u / per] : 0, col = gate ? u % per * 8 : (u - gates) * 16;
-      int a = 0, ch = 0;
+      const int part = (u - gates) % parts, a0 = na * part / parts, a1 = na * (part + 1) / parts;
+      const int stages = end ? 1 : gate ? nst1 : (a1 - a0) * nst2;
+      const int ge = gate && !end ? s_tab.expert[u / per] : 0, col = gate ? u % per * 8 : (u - gates) / parts * 16;
+      int a = gate || end ? 0 : a0, ch = 0;
       for (int i = 0; i < stages; ++i) {
         if (!__all_sync(0xffffffffu, mbar_wait(empty0 + 8 * slot, phase ^ 1, &s_abort))) {
           ok = false;
@@ -270,6 +283,7 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
         }
       }
     }
+    const int gates_done = done;
     if (gt == 0) s_done[grp] = done;
 
     // ---- h, once it is there: one release for all of this CTA's gate units --------------
@@ -285,25 +299,33 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
     if (ok) {
       if constexpr (kFp8) {
         constexpr int kAll = kGroups * kFewWarps;
-        for (int i0 = ct >> 5; i0 < n * p.IB; i0 += kAll * 4) {   // a block a warp, four loads in flight
-          float4 v[4];
+        for (int i0 = ct >> 5; i0 < n * p.IB; i0 += kAll * 8) {   // a block a warp, eight loads in flight
+          float4 v[8];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+          for (int j = 0; j < 8; ++j) {
             const int i = i0 + j * kAll, m = i / p.IB, col = i % p.IB * kBlk + 4 * lane;
             v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (i < n * p.IB && col < p.I) v[j] = __ldcg(reinterpret_cast<const float4*>(p.hf + (size_t)m * p.I + col));
           }
+          uint32_t my_top = 0;                                 // lane j: of the j-th block
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int i = i0 + j * kAll, m = i / p.IB, b = i % p.IB;
-            if (i >= n * p.IB) continue;
+          for (int j = 0; j < 8; ++j) {
             const uint32_t k = 0x7fffffffu;
             const uint32_t top = __reduce_max_sync(0xffffffffu, max(max(__float_as_uint(v[j].x) & k, __float_as_uint(v[j].y) & k),
                                                                     max(__float_as_uint(v[j].z) & k, __float_as_uint(v[j].w) & k)));
-            const BlockScale s = block_scale(__uint_as_float(top));
-            *reinterpret_cast<uint32_t*>(s_rows + (size_t)m * hs + b * kBlk + 4 * lane) =
-                pack_e4m3(to_code(v[j].x, s), to_code(v[j].y, s), to_code(v[j].z, s), to_code(v[j].w, s));
-            if (lane == 0) s_hs[m * p.IB + b] = s.scale;
+            if (lane == j) my_top = top;
+          }
+          const BlockScale mine = block_scale(__uint_as_float(my_top));
+          if (lane < 8 && i0 + lane * kAll < n * p.IB) s_hs[i0 + lane * kAll] = mine.scale;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int i = i0 + j * kAll, m = i / p.IB, b = i % p.IB;
+            BlockScale s;
+            s.hi = __shfl_sync(0xffffffffu, mine.hi, j);
+            s.lo = __shfl_sync(0xffffffffu, mine.lo, j);
+            if (i < n * p.IB)
+              *reinterpret_cast<uint32_t*>(s_rows + (size_t)m * hs + b * kBlk + 4 * lane) =
+                  pack_e4m3(to_code(v[j].x, s), to_code(v[j].y, s), to_code(v[j].z, s), to_code(v[j].w, s));
           }
         }
       } else {
@@ -333,10 +355,11 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
       if (!ok) break;
       u = s_unit[grp][slot];
       if (u >= total) break;
-      const int o0 = (u - gates) * 16, turn = done & 1;
+      const int o0 = (u - gates) / parts * 16, pt = (u - gates) % parts, turn = done & 1;
+      const int a0 = na * pt / parts, a1 = na * (pt + 1) / parts;
       float acc[NG][4] = {};
-      int a = 0, ch = 0;
-      for (int i = 0; i < na * nst2; ++i) {
+      int a = a0, ch = 0;
+      for (int i = 0; i < (a1 - a0) * nst2; ++i) {
         if (i > 0 && !__all_sync(0xffffffffu, mbar_wait(full0 + 8 * slot, phase, &s_abort))) {
           ok = false;
           break;
@@ -398,8 +421,43 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
         float f = part[0][o][t];
 #pragma unroll
         for (int i = 1; i < kFewWarps; ++i) f += part[i][o][t];
-        p.out[(int64_t)t * p.out_stride + o0 + o] = __float2bfloat16_rn(f);
+        if (parts == 1) p.out[(int64_t)t * p.out_stride + o0 + o] = __float2bfloat16_rn(f);
+        else __stcg(p.y + ((size_t)pt * p.T + t) * p.H + o0 + o, f);
       }
+    }
+
+    // ---- the parts' sums -----------------------------------------------------------------
+    if (parts > 1) {
+      if (gt == 0) s_done[grp] = done - gates_done;
+      ok = ok && meet_at(meet_all, met_all);
+      if (ok && ct == 0) {
+        int k = 0;
+        for (int i = 0; i < kGroups; ++i) k += s_done[i];
+        red_add_release(p.ctl->gate_done, (uint32_t)k);
+        if (!wait_count_geq(p.ctl->gate_done, (uint32_t)(cols * parts))) s_abort = 1;
+      }
+      ok = ok && meet_at(meet_all, met_all);
+      const int quads = p.H / 4;
+      if (ok)
+        for (int i = (int)blockIdx.x * 32 * kGroups * kFewWarps + ct; i < live * quads;
+             i += (int)gridDim.x * 32 * kGroups * kFewWarps) {
+          const int t = i / quads, o = i % quads * 4;
+          float4 v[kFewParts];
+#pragma unroll
+          for (int j = 0; j < kFewParts; ++j)
+            if (j < parts) v[j] = __ldcg(reinterpret_cast<const float4*>(p.y + ((size_t)j * p.T + t) * p.H + o));
+          float f[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+          for (int j = 1; j < kFewParts; ++j)
+            if (j < parts) {
+              f[0] += v[j].x;
+              f[1] += v[j].y;
+              f[2] += v[j].z;
+              f[3] += v[j].w;
+            }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) p.out[(int64_t)t * p.out_stride + o + j] = __float2bfloat16_rn(f[j]);
+        }
     }
     if (!ok && lane == 0) flag_error(p.err, EE_DEVERR_TIMEOUT);
   }

@@ -246,8 +246,6 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
   if (!alone)
     for (int i = threadIdx.x; i < p.E * words; i += kThreads) mask[i] = 0;
   for (int i = threadIdx.x; i < p.max_tiles; i += kThreads) p.ctl->gate_done[i] = 0;
-  if (p.sub)
-    for (int i = threadIdx.x; i < p.n_sub; i += kThreads) p.sub[i] = 0;
   if (threadIdx.x == 0) {
     p.ctl->route_ticket = 0;
     p.ctl->queue = 0;
