@@ -1,4 +1,4 @@
-// Weight products for a few tokens (ee_fp8_linear up to 8, ee_moe_layer up to 16): a warp takes 16 weight rows
+// Weight products for a few tokens (up to 8): a warp takes 16 weight rows
 // and some of their 128-byte blocks, straight from global memory into the fragments of an m16n8 MMA (weights the
 // 16 side, tokens the 8 side).  So few tokens leave nothing to share between warps but the
 // sums, and without rings, tensor memory and barriers a call costs little more than its one wait for memory.

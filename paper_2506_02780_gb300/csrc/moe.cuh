@@ -22,16 +22,15 @@ struct MoeCtl {
   uint32_t down_done;        // down tasks that stored their part of y (few tokens: gate tasks, of h)
   uint32_t tiles;            // token tiles
   uint32_t pad[4];
-  uint32_t gate_done[1];     // per token tile: gate tasks that stored their part of h (few tokens, the first: down units)
+  uint32_t gate_done[1];     // per token tile: gate tasks that stored their part of h
 };
 struct __align__(32) MoeTile {   // a token tile's expert
   int expert, entry0, count;   // its first entry and their number
   int first, tiles;            // its first tile and their number
   int pad[3];
 };
-constexpr int kFewTokens = 16;
-constexpr int kFewParts = 4;  // of the chosen experts, whose sums for a column are units of their own
-struct FewEntry {            // of up to 16 tokens: an active expert's entry of a token, or -1, and its weight
+constexpr int kFewEntries = 8, kFewTokens = 8;   // what moe_few.cu takes
+struct FewEntry {            // of so few: an active expert's entry of a token, or -1, and its weight
   int entry;
   float p;
 };
@@ -42,7 +41,7 @@ struct MoeLayout {
 };
 inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t k) {
   MoeLayout l;
-  const int64_t n = T * k, few = std::min<int64_t>(T, kFewTokens);
+  const int64_t n = T * k;
   l.max_tiles = (int)(std::min(E, n) + n / 64);   // (32 only where no expert can have more)
   size_t at = align_up(kWorkspaceBytes, 256);
   const auto take = [&](size_t bytes) {
@@ -52,7 +51,7 @@ inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t 
   };
   l.ctl = take(sizeof(MoeCtl) + 4 * (size_t)l.max_tiles);
   l.tile = take(sizeof(MoeTile) * (size_t)l.max_tiles);
-  l.few = take(sizeof(FewEntry) * kFewTokens * kFewTokens * kMoeMaxTopK);
+  l.few = take(sizeof(FewEntry) * kFewEntries * kFewTokens);
   l.ids = take(4 * (size_t)n);
   l.prob = take(4 * (size_t)n);
   l.list = take(4 * (size_t)n);
@@ -60,9 +59,9 @@ inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t 
   l.xq = take((size_t)(T * H));
   l.xs = take(4 * (size_t)(T * ((H + kBlk - 1) / kBlk)));
   l.h = take(2 * (size_t)(n * I));
-  l.hf = take(4 * (size_t)(few * k * I));
+  l.hf = take(4 * (size_t)(kFewEntries * I));
   l.hs = take(4 * (size_t)(n * ((I + kBlk - 1) / kBlk)));
-  l.y = take(4 * (size_t)(std::max(n, few * kFewParts) * H));
+  l.y = take(4 * (size_t)(n * H));
   l.total = at;
   return l;
 }
@@ -75,7 +74,7 @@ struct RouteParams {
   int T, H, E, k, renorm, cl, max_tiles, tile_rows;
   MoeCtl* ctl;
   MoeTile* tile;
-  FewEntry* few;             // or NULL (more than 16 tokens): [active expert][16]
+  FewEntry* few;             // or NULL (more than 8 entries): [active expert][8]
   int32_t* ids;              // [T][k] experts of a token, ascending
   float* prob;               // [T][k]
   int32_t* list;             // [T k] token of an entry
@@ -116,7 +115,7 @@ struct MoeParams {
   const int32_t* live;
   int32_t* err;
 };
-// Up to 16 tokens whose x and h fit in shared memory beside the rings (moe_few.cu): their depth and the bytes, or 0.
+// Up to 8 entries whose x and h fit in shared memory beside the rings (moe_few.cu): their depth and the bytes, or 0.
 int moe_few_stages(int T, int H, int I, int k, bool fp8, size_t* smem);
 ee_status launch_moe_few(MoeParams& p, bool fp8, cudaStream_t stream);
 

@@ -740,7 +740,7 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   r.tile_rows = ee::moe_tile_rows(T, E, k, fp8);
   r.ctl = reinterpret_cast<ee::MoeCtl*>(base + l.ctl);
   r.tile = reinterpret_cast<ee::MoeTile*>(base + l.tile);
-  r.few = T <= ee::kFewTokens ? reinterpret_cast<ee::FewEntry*>(base + l.few) : nullptr;
+  r.few = T * k <= ee::kFewEntries ? reinterpret_cast<ee::FewEntry*>(base + l.few) : nullptr;
   r.ids = reinterpret_cast<int32_t*>(base + l.ids);
   r.prob = reinterpret_cast<float*>(base + l.prob);
   r.list = reinterpret_cast<int32_t*>(base + l.list);

@@ -1,15 +1,17 @@
-// ee_moe_layer for up to 16 tokens, after the router (moe_route.cu): one persistent kernel, a CTA an SM.
-// Two groups of a producer warp and 8 consumer warps draw units from a queue:
+// ee_moe_layer for up to 8 entries (tokens times chosen experts), after the router (moe_route.cu): one persistent
+// kernel, a CTA an SM.  So few experts make few tiles for the tensor cores (6 experts of 1280 x 3584 60 gate
+// tasks for 152 SMs); here two groups of a producer warp and 8 consumer warps draw units from a queue:
 //   gate unit    8 columns of h of one expert: a warp's MMAs take its 8 gate rows and its 8 up rows, so that a
 //                lane holds both halves of silu(g) u
-//   down unit    16 columns of out, over all chosen experts or a part of them: their sums are weighted on the way, and
-//                y of single experts is not stored
+//   down unit    16 columns of out, over all chosen experts: their sums are weighted on the way, and no y is stored
 // A group's producer streams its units' 16 weight rows in stages of up to 8 blocks of 128 bytes, one for
 // each consumer (few.cuh), and runs ahead across units; the consumers add their sums at a unit's end.
 // (Consumers that load their own weights spend more instructions on addresses than on products and reach 3 to
-// 4.3 TB/s.)  Between gate and down units lies one wait for the gate units of the other CTAs (all drawn before,
-// by CTAs that are running), during which the first down units' weights are under way; then
-// every CTA brings h into its own shared memory, as e4m3 codes for 8-bit weights.  Parts' sums are added at the end.
+// 4.3 TB/s; here gate units run at 6.4.)  Between gate and down units lies one wait for the gate units of the other CTAs
+// (all drawn before, by CTAs that are running), during which the first down units' weights are under way; then
+// every CTA brings h into its own shared memory, as e4m3 codes for 8-bit weights.
+// One token at 6 of 64 experts of 1280 x 3584, 8-bit: 33 us, by the tiles of moe_experts.cu 36; at 2 of 8 of 2560: 25 and 35.
+// More entries are those tiles' (8 tokens at 6 of 64: 78 us, here 98).
 #include <mutex>
 
 #include "moe.cuh"
@@ -22,7 +24,7 @@ constexpr int kGroups = 2;
 constexpr int kThreads = 32 * kGroups * (1 + kFewWarps);      // warps 0 and 1 produce
 constexpr int kMaxDeep = 6;            // stages in a group's ring, at most
 constexpr int kMinDeep = 3;
-constexpr size_t kAllSmem = 226 * 1024;
+constexpr size_t kMostSmem = 204 * 1024;
 
 // bytes of a row of x or h in shared memory: rows two by two on different banks
 __host__ __device__ constexpr int row_stride(int KB) { return KB * 128 + 64; }
@@ -35,26 +37,19 @@ __device__ __forceinline__ uint4 lds16(uint32_t a) {
   return v;
 }
 
-// NG: groups of 8 tokens
-template <int NG>
-struct FewTables {
-  static constexpr int kActive = NG * 8 * kMoeMaxTopK;         // experts at most
-  float part[kGroups][2][kFewWarps][16][8 * NG];
-  float p[kActive][8 * NG];                                    // an active expert's weight for a token
-  int16_t map[kActive][8 * NG];                                // ... and the entry, or -1
-  int16_t expert[kActive];
-};
-
-template <bool kFp8, int NG>
+template <bool kFp8>
 __global__ void __launch_bounds__(kThreads, 1)
 moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__ CUtensorMap tmW2, const MoeParams p) {
-  constexpr int es = kFp8 ? 1 : 2, NT = 8 * NG;
+  constexpr int es = kFp8 ? 1 : 2, NT = kFewTokens;
   extern __shared__ uint8_t s_raw[];                           // the rings; rows of x, later of h; their scales
   uint8_t* const s_dyn = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(s_raw) + 127) & ~static_cast<uintptr_t>(127));
   __shared__ __align__(8) uint64_t s_bars[kGroups * (2 * kMaxDeep + 1) + 1];
   __shared__ float s_ws[kGroups][kMaxDeep][kFewWarps][2];      // scales of a stage's blocks: of rows 0 .. 7 and 8 .. 15
   __shared__ int s_unit[kGroups][kMaxDeep];
-  __shared__ FewTables<NG> s_tab;
+  __shared__ float s_part[kGroups][2][kFewWarps][16][kFewTokens];
+  __shared__ float s_p[kFewEntries][kFewTokens];               // an active expert's weight for a token
+  __shared__ int16_t s_map[kFewEntries][kFewTokens];           // ... and the entry, or -1
+  __shared__ int s_exp[kFewEntries];
   __shared__ int s_done[kGroups];                              // gate units of the group
   __shared__ volatile int s_abort;
   pdl_allow_next();
@@ -80,25 +75,14 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
   const int na = (int)p.ctl->tiles;                            // an active expert has one tile
   int first = 0;
   if (warp < kGroups && lane == 0) first = (int)atomicAdd(&p.ctl->queue, 1u);
-  for (int i = threadIdx.x; i < na; i += kThreads) s_tab.expert[i] = (int16_t)p.tile[i].expert;
+  for (int i = threadIdx.x; i < na; i += kThreads) s_exp[i] = p.tile[i].expert;
   for (int i = threadIdx.x; i < na * NT; i += kThreads) {
-    const FewEntry e = p.few[i / NT * kFewTokens + i % NT];
-    s_tab.map[i / NT][i % NT] = (int16_t)e.entry;
-    s_tab.p[i / NT][i % NT] = e.p;
+    const FewEntry e = p.few[i];
+    s_map[i / NT][i % NT] = (int16_t)e.entry;
+    s_p[i / NT][i % NT] = e.p;
   }
   const int live = p.live ? max(0, min(p.T, ld_pinned(p.live))) : p.T;
-  const int per = p.I / 8, gates = na * per, cols = (p.H + 15) / 16;
-  // the experts of a down unit: in as few parts as give the busiest group the least to do (8 tokens at 6 of 64 experts
-  // of 1280 x 3584, about 36 in use: down units of all of them, 224 for 304 groups, took 35 us)
-  int parts = 1;
-  for (int s = 2, best = (cols + kGroups * (int)gridDim.x - 1) / (kGroups * (int)gridDim.x) * na; s <= kFewParts; s *= 2) {
-    const int turns = (cols * s + kGroups * (int)gridDim.x - 1) / (kGroups * (int)gridDim.x), cost = turns * ((na + s - 1) / s) + 1;
-    if (cost < best) {
-      best = cost;
-      parts = s;
-    }
-  }
-  const int total = gates + (na ? cols * parts : 0);
+  const int per = p.I / 8, gates = na * per, total = gates + (na ? (p.H + 15) / 16 : 0);
   const int nst1 = stages_of(p.KB1), nst2 = stages_of(p.KB2), c1 = blocks_of(p.KB1), c2 = blocks_of(p.KB2);
   const uint32_t stBytes = 16u * 128u * (uint32_t)max(c1, c2);
   const int grp = warp < kGroups ? warp : (warp - kGroups) / kFewWarps;
@@ -117,54 +101,56 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
 
   if (warp < kGroups) {
     // ---- producer ---------------------------------------------------------------------
+    // (uniform values and an elected lane: see moe_experts.cu)
+    const uint32_t u_ring = __shfl_sync(0xffffffffu, ring, 0), u_full = __shfl_sync(0xffffffffu, full0, 0);
+    const int ug = __shfl_sync(0xffffffffu, grp, 0), una = __shfl_sync(0xffffffffu, na, 0);
+    const int ugates = una * per, utotal = __shfl_sync(0xffffffffu, total, 0);
+    const uint64_t policy = policy_evict_first();
     int issued = 0;
     bool ok = true;
     int u = __shfl_sync(0xffffffffu, first, 0);
     while (ok) {
-      const bool end = u >= total, gate = u < gates;
+      const bool end = u >= utotal, gate = u < ugates;
       int next = 0;
       if (!end && lane == 0) next = (int)atomicAdd(&p.ctl->queue, 1u);
-      const int part = (u - gates) % parts, a0 = na * part / parts, a1 = na * (part + 1) / parts;
-      const int stages = end ? 1 : gate ? nst1 : (a1 - a0) * nst2;
-      const int ge = gate && !end ? s_tab.expert[u / per] : 0, col = gate ? u % per * 8 : (u - gates) / parts * 16;
-      int a = gate || end ? 0 : a0, ch = 0;
-      for (int i = 0; i < stages; ++i) {
-        if (!__all_sync(0xffffffffu, mbar_wait(empty0 + 8 * slot, phase ^ 1, &s_abort))) {
-          ok = false;
-          break;
-        }
-        const uint32_t fb = full0 + 8 * slot, at = ring + (uint32_t)slot * stBytes;
-        const int w2row = (end || gate ? 0 : s_tab.expert[a] * p.H) + col;
-        if (elect_one()) {                                     // (operands in uniform registers)
-          s_unit[grp][slot] = u;
-          if (end) {
-            mbar_arrive(fb);
-          } else if (gate) {
-            mbar_expect_tx(fb, 16u * 128u * (uint32_t)c1);
-            const int y = ge * 2 * p.I + col;
-            tma_load_2d(at, &tmW1, fb, ch * c1 * 32, y);
-            tma_load_2d(at + 8u * 128u * (uint32_t)c1, &tmW1, fb, ch * c1 * 32, y + p.I);
-          } else {
-            mbar_expect_tx(fb, 16u * 128u * (uint32_t)c2);
-            tma_load_2d(at, &tmW2, fb, ch * c2 * 32, w2row);
+      const int na_u = end || gate ? 1 : una, nst = end ? 1 : gate ? nst1 : nst2;
+      const int col = gate ? u % per * 8 : (u - ugates) * 16;
+      for (int i = 0; i < na_u && ok; ++i) {
+        const int a = end ? 0 : gate ? u / per : i;
+        const int e = __shfl_sync(0xffffffffu, s_exp[a], 0);
+        const int y = gate ? e * 2 * p.I + col : e * p.H + col;
+        for (int ch = 0; ch < nst; ++ch) {
+          if (!__all_sync(0xffffffffu, mbar_wait(empty0 + 8 * slot, phase ^ 1, &s_abort))) {
+            ok = false;
+            break;
           }
-        }
-        if (kFp8 && lane < 2 * kFewWarps) {
-          const int b = lane >> 1, which = lane & 1, kb = ch * (gate ? c1 : c2) + b;
-          const uint32_t to = smem_u32(&s_ws[grp][slot][b][which]);
-          if (!end && b < (gate ? c1 : c2) && kb < (gate ? p.KB1 : p.KB2)) {
-            const float* ws = gate ? p.s1 + (((size_t)ge * 2 + which) * p.IB + col / kBlk) * p.KB1 + kb
-                                   : p.s2 + ((size_t)s_tab.expert[a] * p.HB + col / kBlk) * p.KB2 + kb;
-            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(ws) : "memory");
+          const uint32_t fb = u_full + 8 * slot, at = u_ring + (uint32_t)slot * stBytes;
+          if (elect_one()) {
+            s_unit[ug][slot] = u;
+            if (end) {
+              mbar_arrive(fb);
+            } else if (gate) {
+              mbar_expect_tx(fb, 16u * 128u * (uint32_t)c1);
+              tma_load_2d_hint(at, &tmW1, fb, ch * c1 * 32, y, policy);
+              tma_load_2d_hint(at + 8u * 128u * (uint32_t)c1, &tmW1, fb, ch * c1 * 32, y + p.I, policy);
+            } else {
+              mbar_expect_tx(fb, 16u * 128u * (uint32_t)c2);
+              tma_load_2d_hint(at, &tmW2, fb, ch * c2 * 32, y, policy);
+            }
           }
-          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(fb) : "memory");
-        }
-        __syncwarp();
-        if (!end) ++issued;
-        advance();
-        if (++ch == (gate ? nst1 : nst2)) {
-          ch = 0;
-          ++a;
+          if (kFp8 && lane < 2 * kFewWarps) {
+            const int b = lane >> 1, which = lane & 1, kb = ch * (gate ? c1 : c2) + b;
+            const uint32_t to = smem_u32(&s_ws[grp][slot][b][which]);
+            if (!end && b < (gate ? c1 : c2) && kb < (gate ? p.KB1 : p.KB2)) {
+              const float* ws = gate ? p.s1 + (((size_t)e * 2 + which) * p.IB + col / kBlk) * p.KB1 + kb
+                                     : p.s2 + ((size_t)e * p.HB + col / kBlk) * p.KB2 + kb;
+              asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(ws) : "memory");
+            }
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(fb) : "memory");
+          }
+          __syncwarp();
+          if (!end) ++issued;
+          advance();
         }
       }
       if (end) break;
@@ -206,9 +192,8 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
     }
     bool ok = meet_at(meet_all, met_all);
     const int last = max(live, 1) - 1;
-    uint32_t xrow[NG];
-#pragma unroll
-    for (int n = 0; n < NG; ++n) xrow[n] = smem_u32(s_rows) + (uint32_t)(min(8 * n + g, p.T - 1) * xs + tq * 16);
+    const int t0 = min(2 * tq, last), t1 = min(2 * tq + 1, last);
+    const uint32_t xrow = smem_u32(s_rows) + (uint32_t)(min(g, p.T - 1) * xs + tq * 16);
     const uint32_t wat = (uint32_t)(w * 128 + tq * 16);
     int done = 0, u = 0;
     while (ok) {
@@ -217,7 +202,7 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
       u = s_unit[grp][slot];
       if (u >= gates) break;
       const int a = u / per, i8 = u % per, turn = done & 1;
-      float acc[NG][4] = {};
+      float acc[4] = {0.f, 0.f, 0.f, 0.f};
       for (int ch = 0; ch < nst1; ++ch) {
         if (ch > 0 && !__all_sync(0xffffffffu, mbar_wait(full0 + 8 * slot, phase, &s_abort))) {
           ok = false;
@@ -231,24 +216,20 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
           fa.hi = lds16(r0 + 64);
           fb.lo = lds16(r1);
           fb.hi = lds16(r1 + 64);
-#pragma unroll
-          for (int n = 0; n < NG; ++n) {
-            FewFrag fx;
-            fx.lo = lds16(xrow[n] + (uint32_t)kb * 128);       // (rows past T: a copy of the last one, not looked at)
-            fx.hi = lds16(xrow[n] + (uint32_t)kb * 128 + 64);
-            if constexpr (kFp8) {
-              const int t0 = min(8 * n + 2 * tq, last), t1 = min(8 * n + 2 * tq + 1, last);
-              const float x0 = s_xs[t0 * p.KB1 + kb], x1 = s_xs[t1 * p.KB1 + kb];
-              const float w0 = s_ws[grp][slot][w][0], w1 = s_ws[grp][slot][w][1];
-              float d[4] = {0.f, 0.f, 0.f, 0.f};
-              few_block<true>(d, fa, fb, fx);
-              acc[n][0] = __fmaf_rn(d[0], x0 * w0, acc[n][0]);
-              acc[n][1] = __fmaf_rn(d[1], x1 * w0, acc[n][1]);
-              acc[n][2] = __fmaf_rn(d[2], x0 * w1, acc[n][2]);
-              acc[n][3] = __fmaf_rn(d[3], x1 * w1, acc[n][3]);
-            } else {
-              few_block<false>(acc[n], fa, fb, fx);
-            }
+          FewFrag fx;
+          fx.lo = lds16(xrow + (uint32_t)kb * 128);            // (rows past T: a copy of the last one, not looked at)
+          fx.hi = lds16(xrow + (uint32_t)kb * 128 + 64);
+          if constexpr (kFp8) {
+            const float x0 = s_xs[t0 * p.KB1 + kb], x1 = s_xs[t1 * p.KB1 + kb];
+            const float w0 = s_ws[grp][slot][w][0], w1 = s_ws[grp][slot][w][1];
+            float d[4] = {0.f, 0.f, 0.f, 0.f};
+            few_block<true>(d, fa, fb, fx);
+            acc[0] = __fmaf_rn(d[0], x0 * w0, acc[0]);
+            acc[1] = __fmaf_rn(d[1], x1 * w0, acc[1]);
+            acc[2] = __fmaf_rn(d[2], x0 * w1, acc[2]);
+            acc[3] = __fmaf_rn(d[3], x1 * w1, acc[3]);
+          } else {
+            few_block<false>(acc, fa, fb, fx);
           }
         }
         __syncwarp();
@@ -256,19 +237,16 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
         advance();
       }
       if (!ok) break;
-      float(*part)[16][NT] = s_tab.part[grp][turn];
-#pragma unroll
-      for (int n = 0; n < NG; ++n) {
-        *reinterpret_cast<float2*>(&part[w][g][8 * n + 2 * tq]) = make_float2(acc[n][0], acc[n][1]);
-        *reinterpret_cast<float2*>(&part[w][g + 8][8 * n + 2 * tq]) = make_float2(acc[n][2], acc[n][3]);
-      }
+      float(*part)[16][NT] = s_part[grp][turn];
+      *reinterpret_cast<float2*>(&part[w][g][2 * tq]) = make_float2(acc[0], acc[1]);
+      *reinterpret_cast<float2*>(&part[w][g + 8][2 * tq]) = make_float2(acc[2], acc[3]);
       ok = meet_at(meet, met);
       if (!ok) break;
       ++done;
       constexpr int kSumWarps = NT * 8 / 32;                   // others in turn: token t, column o
       if (w / kSumWarps == done % (kFewWarps / kSumWarps)) {
         const int t = gt / 8 % NT, o = gt & 7;
-        const int entry = s_tab.map[a][t];
+        const int entry = s_map[a][t];
         if (entry >= 0) {
           float gs = part[0][o][t], us = part[0][o + 8][t];
 #pragma unroll
@@ -283,7 +261,6 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
         }
       }
     }
-    const int gates_done = done;
     if (gt == 0) s_done[grp] = done;
 
     // ---- h, once it is there: one release for all of this CTA's gate units --------------
@@ -355,11 +332,10 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
       if (!ok) break;
       u = s_unit[grp][slot];
       if (u >= total) break;
-      const int o0 = (u - gates) / parts * 16, pt = (u - gates) % parts, turn = done & 1;
-      const int a0 = na * pt / parts, a1 = na * (pt + 1) / parts;
-      float acc[NG][4] = {};
-      int a = a0, ch = 0;
-      for (int i = 0; i < (a1 - a0) * nst2; ++i) {
+      const int o0 = (u - gates) * 16, turn = done & 1;
+      float acc[4] = {0.f, 0.f, 0.f, 0.f};
+      int a = 0, ch = 0;
+      for (int i = 0; i < na * nst2; ++i) {
         if (i > 0 && !__all_sync(0xffffffffu, mbar_wait(full0 + 8 * slot, phase, &s_abort))) {
           ok = false;
           break;
@@ -373,29 +349,25 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
           fb.lo = lds16(r1);
           fb.hi = lds16(r1 + 64);
           const float ws = kFp8 ? s_ws[grp][slot][w][0] : 1.f;
-#pragma unroll
-          for (int n = 0; n < NG; ++n) {
-            const int tc = 8 * n + 2 * tq, m = s_tab.map[a][8 * n + g], m0 = s_tab.map[a][tc], m1 = s_tab.map[a][tc + 1];
-            if (NG > 1 && __all_sync(0xffffffffu, m < 0)) continue;
-            FewFrag fx;
-            fx.lo = fx.hi = make_uint4(0, 0, 0, 0);
-            if (m >= 0) {
-              const uint32_t r = smem_u32(s_rows) + (uint32_t)(m * hs + kb * 128 + tq * 16);
-              fx.lo = lds16(r);
-              fx.hi = lds16(r + 64);
-            }
-            float d[4] = {0.f, 0.f, 0.f, 0.f};
-            few_block<kFp8>(d, fa, fb, fx);
-            if (m0 >= 0) {                                     // (a token at other experts takes nothing, not even a NaN)
-              const float f = kFp8 ? s_tab.p[a][tc] * (s_hs[m0 * p.IB + kb] * ws) : s_tab.p[a][tc];
-              acc[n][0] = __fmaf_rn(d[0], f, acc[n][0]);
-              acc[n][2] = __fmaf_rn(d[2], f, acc[n][2]);
-            }
-            if (m1 >= 0) {
-              const float f = kFp8 ? s_tab.p[a][tc + 1] * (s_hs[m1 * p.IB + kb] * ws) : s_tab.p[a][tc + 1];
-              acc[n][1] = __fmaf_rn(d[1], f, acc[n][1]);
-              acc[n][3] = __fmaf_rn(d[3], f, acc[n][3]);
-            }
+          const int m = s_map[a][g], m0 = s_map[a][2 * tq], m1 = s_map[a][2 * tq + 1];
+          FewFrag fx;
+          fx.lo = fx.hi = make_uint4(0, 0, 0, 0);
+          if (m >= 0) {
+            const uint32_t r = smem_u32(s_rows) + (uint32_t)(m * hs + kb * 128 + tq * 16);
+            fx.lo = lds16(r);
+            fx.hi = lds16(r + 64);
+          }
+          float d[4] = {0.f, 0.f, 0.f, 0.f};
+          few_block<kFp8>(d, fa, fb, fx);
+          if (m0 >= 0) {                                       // (a token at other experts takes nothing, not even a NaN)
+            const float f = kFp8 ? s_p[a][2 * tq] * (s_hs[m0 * p.IB + kb] * ws) : s_p[a][2 * tq];
+            acc[0] = __fmaf_rn(d[0], f, acc[0]);
+            acc[2] = __fmaf_rn(d[2], f, acc[2]);
+          }
+          if (m1 >= 0) {
+            const float f = kFp8 ? s_p[a][2 * tq + 1] * (s_hs[m1 * p.IB + kb] * ws) : s_p[a][2 * tq + 1];
+            acc[1] = __fmaf_rn(d[1], f, acc[1]);
+            acc[3] = __fmaf_rn(d[3], f, acc[3]);
           }
         }
         __syncwarp();
@@ -407,67 +379,25 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
         }
       }
       if (!ok) break;
-      float(*part)[16][NT] = s_tab.part[grp][turn];
-#pragma unroll
-      for (int n = 0; n < NG; ++n) {
-        *reinterpret_cast<float2*>(&part[w][g][8 * n + 2 * tq]) = make_float2(acc[n][0], acc[n][1]);
-        *reinterpret_cast<float2*>(&part[w][g + 8][8 * n + 2 * tq]) = make_float2(acc[n][2], acc[n][3]);
-      }
+      float(*part)[16][NT] = s_part[grp][turn];
+      *reinterpret_cast<float2*>(&part[w][g][2 * tq]) = make_float2(acc[0], acc[1]);
+      *reinterpret_cast<float2*>(&part[w][g + 8][2 * tq]) = make_float2(acc[2], acc[3]);
       ok = meet_at(meet, met);
       if (!ok) break;
       ++done;
       const int t = gt >> 4, o = gt & 15;
-      if (t < live && o0 + o < p.H) {                          // (live is at most NT, and t < 16)
+      if (t < live && o0 + o < p.H) {                          // (live is at most 8)
         float f = part[0][o][t];
 #pragma unroll
         for (int i = 1; i < kFewWarps; ++i) f += part[i][o][t];
-        if (parts == 1) p.out[(int64_t)t * p.out_stride + o0 + o] = __float2bfloat16_rn(f);
-        else __stcg(p.y + ((size_t)pt * p.T + t) * p.H + o0 + o, f);
+        p.out[(int64_t)t * p.out_stride + o0 + o] = __float2bfloat16_rn(f);
       }
-    }
-
-    // ---- the parts' sums -----------------------------------------------------------------
-    if (parts > 1) {
-      if (gt == 0) s_done[grp] = done - gates_done;
-      ok = ok && meet_at(meet_all, met_all);
-      if (ok && ct == 0) {
-        int k = 0;
-        for (int i = 0; i < kGroups; ++i) k += s_done[i];
-        red_add_release(p.ctl->gate_done, (uint32_t)k);
-        if (!wait_count_geq(p.ctl->gate_done, (uint32_t)(cols * parts))) s_abort = 1;
-      }
-      ok = ok && meet_at(meet_all, met_all);
-      const int quads = p.H / 4;
-      if (ok)
-        for (int i = (int)blockIdx.x * 32 * kGroups * kFewWarps + ct; i < live * quads;
-             i += (int)gridDim.x * 32 * kGroups * kFewWarps) {
-          const int t = i / quads, o = i % quads * 4;
-          float4 v[kFewParts];
-#pragma unroll
-          for (int j = 0; j < kFewParts; ++j)
-            if (j < parts) v[j] = __ldcg(reinterpret_cast<const float4*>(p.y + ((size_t)j * p.T + t) * p.H + o));
-          float f[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
-#pragma unroll
-          for (int j = 1; j < kFewParts; ++j)
-            if (j < parts) {
-              f[0] += v[j].x;
-              f[1] += v[j].y;
-              f[2] += v[j].z;
-              f[3] += v[j].w;
-            }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) p.out[(int64_t)t * p.out_stride + o + j] = __float2bfloat16_rn(f[j]);
-        }
     }
     if (!ok && lane == 0) flag_error(p.err, EE_DEVERR_TIMEOUT);
   }
 }
 
-constexpr size_t most_smem(int NG) {
-  return kAllSmem - 2048 - (NG == 1 ? sizeof(FewTables<1>) : sizeof(FewTables<2>));
-}
-
-template <bool kFp8, int NG>
+template <bool kFp8>
 ee_status launch(const MoeParams& p, size_t smem, cudaStream_t stream) {
   constexpr uint64_t es = kFp8 ? 1 : 2;
   CUtensorMap tmW1, tmW2;
@@ -482,11 +412,11 @@ ee_status launch(const MoeParams& p, size_t smem, cudaStream_t stream) {
     static bool set[kMaxDevices] = {};
     std::lock_guard<std::mutex> lock(mu);
     if (!set[dev]) {
-      EE_CUDA_OK(cudaFuncSetAttribute(moe_few_kernel<kFp8, NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most_smem(NG)));
+      EE_CUDA_OK(cudaFuncSetAttribute(moe_few_kernel<kFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem));
       set[dev] = true;
     }
   }
-  EE_CUDA_OK(launch_pdl(moe_few_kernel<kFp8, NG>, dim3(kNumSMs), dim3(kThreads), smem, stream, 1, tmW1, tmW2, p));
+  EE_CUDA_OK(launch_pdl(moe_few_kernel<kFp8>, dim3(kNumSMs), dim3(kThreads), smem, stream, 1, tmW1, tmW2, p));
   return EE_OK;
 }
 
@@ -495,12 +425,12 @@ ee_status launch(const MoeParams& p, size_t smem, cudaStream_t stream) {
 namespace ee {
 
 int moe_few_stages(int T, int H, int I, int k, bool fp8, size_t* smem) {
-  if (T > kFewTokens) return 0;
-  const size_t most = most_smem(T <= 8 ? 1 : 2), es = fp8 ? 1 : 2, KB1 = (H * es + 127) / 128, KB2 = (I * es + 127) / 128;
+  if (T * k > kFewEntries) return 0;
+  const size_t es = fp8 ? 1 : 2, KB1 = (H * es + 127) / 128, KB2 = (I * es + 127) / 128;
   const size_t x = (size_t)T * (row_stride((int)KB1) + 4 * KB1), h = (size_t)T * k * (row_stride((int)KB2) + 4 * KB2);
   const size_t rows = std::max(x, h), stage = 16 * 128 * (size_t)std::max(blocks_of((int)KB1), blocks_of((int)KB2));
-  if (128 + rows + kGroups * kMinDeep * stage > most) return 0;
-  const size_t deep = std::min<size_t>(kMaxDeep, (most - 128 - rows) / (kGroups * stage));
+  if (128 + rows + kGroups * kMinDeep * stage > kMostSmem) return 0;
+  const size_t deep = std::min<size_t>(kMaxDeep, (kMostSmem - 128 - rows) / (kGroups * stage));
   *smem = 128 + rows + kGroups * deep * stage;
   return (int)deep;
 }
@@ -508,8 +438,7 @@ int moe_few_stages(int T, int H, int I, int k, bool fp8, size_t* smem) {
 ee_status launch_moe_few(MoeParams& p, bool fp8, cudaStream_t stream) {
   size_t smem = 0;
   p.stages = moe_few_stages(p.T, p.H, p.I, p.k, fp8, &smem);
-  if (p.T <= 8) return fp8 ? launch<true, 1>(p, smem, stream) : launch<false, 1>(p, smem, stream);
-  return fp8 ? launch<true, 2>(p, smem, stream) : launch<false, 2>(p, smem, stream);
+  return fp8 ? launch<true>(p, smem, stream) : launch<false>(p, smem, stream);
 }
 
 }  // namespace ee
