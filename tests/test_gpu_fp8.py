@@ -218,3 +218,24 @@ def test_linear_streams_and_graphs(ws):
         same_codes(q, want)
         check_linear(out, q, s, w, wsc, None)
     assert E.ee_read_errors(ws) == 0
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("n,c", [(2500, 1040), (700, 4624), (4100, 16)])
+def test_many_rows(n, c, gated):
+    """Sizes that fill the GPU, with rows and columns that end inside a CTA's."""
+    x = acts(n + c, n, 2 * c if gated else c, False)
+    q, s = torch.empty(n, c, dtype=F8, device=DEV), torch.empty(blocks(c), n, device=DEV)
+    E.ee_fp8_quantize(x, q, s, gated=gated)
+    if not gated:
+        wq, want = quant_rows(x.double())
+        same_codes(q, wq)
+        assert ((s.double() - want).abs() <= want * 2.0 ** -24).all()
+        return
+    g, u = x.double().chunk(2, 1)
+    h = g * torch.sigmoid(g) * u
+    _, want = quant_rows(h)
+    err = 40 * 2.0 ** -23                               # (as in test_gated: |g| <= 20 here as well)
+    assert ((s.double() - want).abs() <= want * (err + 2.0 ** -24)).all()
+    v, sc = rows_value(q, s), want.t().repeat_interleave(BLOCK, 1)[:, :c]
+    assert ((v - h).abs() <= torch.maximum(h.abs() * 2.0 ** -4, sc * 2.0 ** -10) * (1 + 1e-4) + h.abs() * err).all()
