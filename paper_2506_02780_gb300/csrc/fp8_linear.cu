@@ -23,7 +23,6 @@ constexpr int kThreads = 384;          // warp 0 TMA, 1 MMA, 2 TMEM, 3 none; 4..
 constexpr int kEpiWarps = 8;           // two per TMEM lane quarter, half of the columns each
 constexpr int kRegsAll = 168;          // a warp's at launch; the epilogue's take some of the others', kRegsEpi
 constexpr int BM = 128;
-constexpr int kFewRows = 8;            // tokens that a kernel of their own takes
 
 struct LinParams {
   int n, N, KB, MT, NT, ks, a_rows, stages;
@@ -377,51 +376,64 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
   }
 }
 
-// Up to 8 tokens: a CTA takes 16 weight rows, its warps every eighth block of them.
+// Up to 8 NG tokens: a CTA takes 16 weight rows, its warps every eighth block of them.
+template <int NG>
 __global__ void __launch_bounds__(kFewWarps * 32, 2) fp8_linear_few_kernel(const uint8_t* x, const uint8_t* w, int K, const LinParams p) {
-  constexpr int kFlight = 4;                      // blocks of a warp whose loads are under way together
-  __shared__ float s_part[kFewWarps][16][kFewRows];
+  constexpr int kFlight = NG == 1 ? 4 : 2;        // blocks of a warp whose loads are under way together
+  constexpr int NT = 8 * NG;
+  __shared__ float s_part[kFewWarps][16][NT];
   pdl_allow_next();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, tq = lane & 3;
   const int o0 = (int)blockIdx.x * 16;
   const int64_t r0 = o0 + g, r1 = r0 + 8;
   const float* ws = p.ws + (int64_t)(o0 / kBlk) * p.KB;
-  const int t0 = min(2 * tq, p.n - 1), t1 = min(2 * tq + 1, p.n - 1);
-  float acc[4] = {0.f, 0.f, 0.f, 0.f};
+  float acc[NG][4];
+#pragma unroll
+  for (int i = 0; i < NG; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
   if (threadIdx.x == 0) prefetch_l2(w + (int64_t)o0 * K, (uint32_t)(min(16, p.N - o0) * K));   // (K is at most 2^24)
   if (threadIdx.x >= 32 && (int)threadIdx.x - 32 < (p.KB + 31) / 32) prefetch_l2_line(ws + ((int)threadIdx.x - 32) * 32);
   pdl_wait();
   for (int k0 = warp; k0 < p.KB; k0 += kFewWarps * kFlight) {
-    FewFrag a[kFlight], b[kFlight], v[kFlight];
-    float s[kFlight][3];
+    FewFrag a[kFlight], b[kFlight], v[kFlight][NG];
+    float sw[kFlight], sx[kFlight][NG][2];
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
       const int kb = k0 + j * kFewWarps, left = K - kb * kBlk;
       const bool in = kb < p.KB;
       a[j] = few_load(w + r0 * K + (int64_t)kb * kBlk, left, tq, in && r0 < p.N);
       b[j] = few_load(w + r1 * K + (int64_t)kb * kBlk, left, tq, in && r1 < p.N);
-      v[j] = few_load(x + (int64_t)g * K + (int64_t)kb * kBlk, left, tq, in && g < p.n);
-      s[j][0] = in ? p.xs[(int64_t)kb * p.n + t0] : 0.f;
-      s[j][1] = in ? p.xs[(int64_t)kb * p.n + t1] : 0.f;
-      s[j][2] = in ? ws[kb] : 0.f;
+      sw[j] = in ? ws[kb] : 0.f;
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        const int t = 8 * i + g;
+        v[j][i] = few_load(x + (int64_t)t * K + (int64_t)kb * kBlk, left, tq, in && t < p.n);
+#pragma unroll
+        for (int d = 0; d < 2; ++d) sx[j][i][d] = in ? p.xs[(int64_t)kb * p.n + min(8 * i + 2 * tq + d, p.n - 1)] : 0.f;
+      }
     }
 #pragma unroll
     for (int j = 0; j < kFlight; ++j)
-      if (k0 + j * kFewWarps < p.KB) {
-        float c[4] = {0.f, 0.f, 0.f, 0.f};
-        few_block<true>(c, a[j], b[j], v[j]);
-        const float f0 = s[j][0] * s[j][2], f1 = s[j][1] * s[j][2];
-        acc[0] = __fmaf_rn(c[0], f0, acc[0]);
-        acc[1] = __fmaf_rn(c[1], f1, acc[1]);
-        acc[2] = __fmaf_rn(c[2], f0, acc[2]);
-        acc[3] = __fmaf_rn(c[3], f1, acc[3]);
-      }
+      if (k0 + j * kFewWarps < p.KB)
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+          float c[4] = {0.f, 0.f, 0.f, 0.f};
+          few_block<true>(c, a[j], b[j], v[j][i]);
+          const float f0 = sx[j][i][0] * sw[j], f1 = sx[j][i][1] * sw[j];
+          acc[i][0] = __fmaf_rn(c[0], f0, acc[i][0]);
+          acc[i][1] = __fmaf_rn(c[1], f1, acc[i][1]);
+          acc[i][2] = __fmaf_rn(c[2], f0, acc[i][2]);
+          acc[i][3] = __fmaf_rn(c[3], f1, acc[i][3]);
+        }
   }
-  *reinterpret_cast<float2*>(&s_part[warp][g][2 * tq]) = make_float2(acc[0], acc[1]);
-  *reinterpret_cast<float2*>(&s_part[warp][g + 8][2 * tq]) = make_float2(acc[2], acc[3]);
+#pragma unroll
+  for (int i = 0; i < NG; ++i) {
+    *reinterpret_cast<float2*>(&s_part[warp][g][8 * i + 2 * tq]) = make_float2(acc[i][0], acc[i][1]);
+    *reinterpret_cast<float2*>(&s_part[warp][g + 8][8 * i + 2 * tq]) = make_float2(acc[i][2], acc[i][3]);
+  }
   __syncthreads();
-  const int t = threadIdx.x >> 4, o = threadIdx.x & 15;
-  if (t < p.n && o0 + o < p.N) {
+  for (int e = threadIdx.x; e < 16 * NT; e += kFewWarps * 32) {
+    const int t = e >> 4, o = e & 15;
+    if (t >= p.n || o0 + o >= p.N) continue;
     float f = s_part[0][o][t];
 #pragma unroll
     for (int i = 1; i < kFewWarps; ++i) f += s_part[i][o][t];
@@ -488,9 +500,11 @@ extern "C" ee_status ee_fp8_linear(const uint8_t* x, const float* x_scale, const
   p.err = ee::err_word(ws);
   const int64_t t128 = (int64_t)p.MT * ((N + 127) / 128), t256 = (int64_t)p.MT * ((N + 255) / 256);
   if (t256 > (1 << 30)) return EE_ERR_UNSUPPORTED;
-  if (n <= kFewRows) {
-    EE_CUDA_OK(ee::launch_pdl(fp8_linear_few_kernel, dim3((unsigned)((N + 15) / 16)), dim3(kFewWarps * 32), 0,
-                              (cudaStream_t)stream, 1, x, w, K, p));
+  // Up to 8 tokens, and up to 16 where W is small, do without tiles (us, 3,584 x 3,584: 1 token 4.1, by tiles 6.6; 16
+  // tokens 6.0 and 7.2; 28,672 rows: 1 token 20.1 and 21.3, 8 tokens 22.4 and 21.4, 16 tokens 29 and 21).
+  if (n <= 8 || (n <= 16 && (int64_t)N * K <= (1 << 25))) {
+    const auto kernel = n <= 8 ? fp8_linear_few_kernel<1> : fp8_linear_few_kernel<2>;
+    EE_CUDA_OK(ee::launch_pdl(kernel, dim3((unsigned)((N + 15) / 16)), dim3(kFewWarps * 32), 0, (cudaStream_t)stream, 1, x, w, K, p));
     return EE_OK;
   }
   const cudaStream_t s = (cudaStream_t)stream;

@@ -132,7 +132,7 @@ def check_linear(out, x, xs, w, wsc, bias):
     assert not bad.any(), (int(bad.sum()), float((out.double() - y).abs().max()))
 
 
-LINEAR = [(1, 16, 1), (1, 128, 8), (1, 3584, 3584), (2, 112, 100), (7, 256, 128), (8, 144, 129), (9, 272, 257),
+LINEAR = [(10, 400, 37), (14, 3584, 1500), (12, 2064, 20000), (1, 16, 1), (1, 128, 8), (1, 3584, 3584), (2, 112, 100), (7, 256, 128), (8, 144, 129), (9, 272, 257),
           (16, 1040, 384), (33, 3584, 512), (63, 400, 1000), (64, 3584, 4608), (65, 384, 255), (127, 512, 131),
           (128, 896, 640), (129, 896, 640), (200, 2064, 20000), (300, 128, 40), (534, 1536, 3584), (700, 640, 9000),
           (1025, 272, 5121), (2048, 512, 4096)]
