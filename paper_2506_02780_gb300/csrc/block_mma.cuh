@@ -76,6 +76,24 @@ __device__ __forceinline__ void promote(uint64_t (&acc)[16 * G], uint32_t c, flo
   }
 }
 
+// acc += f0 * the 64 columns at c0 and f1 * the 64 at c1
+__device__ __forceinline__ void promote_2x64(uint64_t (&acc)[64], uint32_t c0, uint32_t c1, float f0, float f1) {
+  uint32_t a[32], b[32];
+  tc_ld32_nowait(c0, a);
+  tc_ld32_nowait(c0 + 32, b);
+  const uint64_t p0 = f2_pack(__float_as_uint(f0), __float_as_uint(f0)), p1 = f2_pack(__float_as_uint(f1), __float_as_uint(f1));
+  tc_wait_ld32(a);
+  tc_pin32(b);
+  add_scaled32<0>(acc, a, p0);
+  tc_ld32_nowait(c1, a);
+  add_scaled32<1>(acc, b, p0);
+  tc_ld32_nowait(c1 + 32, b);
+  tc_wait_ld32(a);
+  tc_pin32(b);
+  add_scaled32<2>(acc, a, p1);
+  add_scaled32<3>(acc, b, p1);
+}
+
 // The code of x in a block whose largest magnitude is a: the e4m3 number nearest to 448 x / a.
 // The quotient is x (hi + lo) with hi + lo = 448 / a to about 48 bits, rounded once to fp32: for a
 // bf16 x it is then never on the wrong side of a border between two codes (448 x / a is either a
@@ -113,6 +131,15 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t d;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
   return d;
+}
+
+__device__ __forceinline__ void st_shared_u4(uint32_t a, uint4 v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared_u4(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
 }
 
 }  // namespace ee

@@ -10,6 +10,10 @@
 // its 0.4 us with half the rows, too (the same layer with 64 rows 177 us, with 128 141; 8 experts of 2560 for 20
 // tokens 63 and 67).
 //
+// On 8-bit weights tiles of 128 tokens have tokens on the lanes all the same: a token's scale is then one
+// register, where the columns' scales come from shared memory, 128 of them a k-block and thread, whose reads
+// bound such tiles (2,048 tokens at 4 of 16 experts 281 us, so %TOK%).
+//
 // CTAs draw tasks from one queue, gate tasks first.  A down task waits for the gate tasks of its
 // token tile; those were drawn before it by CTAs that are running, so no wait depends on
 // a CTA that has not started.  Warp 0 draws, publishes the task to the other roles in a ring of
@@ -30,6 +34,7 @@ constexpr int kEpiWarps = 8;           // two per TMEM lane quarter, every other
 constexpr int kRegsAll = 128;          // a warp's at launch; the epilogue's take some of the others'
 constexpr int kGatherWarps = 4;
 constexpr int kTile = 128;             // rows of a weight tile
+constexpr uint32_t kOutBytes = 32 * 16 * 4;   // of an epilogue warp: 32 rows of 16 columns of y on their way out
 constexpr int kRing = 4;               // tasks published and not yet done with by every role
 constexpr int kScRing = 8;             // k-blocks' scales
 constexpr int kMaxStages = 6;
@@ -62,11 +67,12 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
   constexpr int kRegsEpi = NT == 128 ? 200 : 152, kRegsOther = 2 * kRegsAll - kRegsEpi;
   constexpr int kScBatch = NT == 128 ? 2 : 4;   // k-blocks whose scales' loads are in flight
   constexpr int kBufs = 512 / (2 * NT) < 8 ? 512 / (2 * NT) : 8;   // accumulators of two tiles
+  constexpr bool kTok = kFp8 && NT == 128;      // tokens on the MMA's M side
   constexpr int kChunks = NT / 32;              // groups of 16 tokens of an epilogue warp
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
-  __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 2 * 8 + 3 * kRing + 2 * kScRing + 2 + 1];
+  __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 2 * 8 + 3 * kRing + 2 * kScRing + 4 + 1];
   __shared__ uint32_t s_top[kFp8 ? 2 : 1][4][NT];
   __shared__ __align__(16) float s_scale[kFp8 ? kScRing : 1][2][NT];
   __shared__ Task s_task[kRing];
@@ -84,7 +90,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
   const uint32_t full0 = smem_u32(s_bars), empty0 = full0 + 8 * kMaxStages, tfull0 = empty0 + 8 * kMaxStages,
                  tempty0 = tfull0 + 8 * 8, qfull0 = tempty0 + 8 * 8, qempty0 = qfull0 + 8 * kRing,
                  edone0 = qempty0 + 8 * kRing, sfull0 = edone0 + 8 * kRing, sempty0 = sfull0 + 8 * kScRing,
-                 meet0 = sempty0 + 8 * kScRing, drain = meet0 + 8 * 2;
+                 meet0 = sempty0 + 8 * kScRing, drain = meet0 + 8 * 4;
   if (threadIdx.x == 0) {
     s_abort = 0;
     s_issued = 0;
@@ -106,8 +112,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
       mbar_init(sfull0 + 8 * a, 1);
       mbar_init(sempty0 + 8 * a, kEpiWarps);
     }
-    mbar_init(meet0, 4);
-    mbar_init(meet0 + 8, 4);
+    for (int a = 0; a < 4; ++a) mbar_init(meet0 + 8 * a, kTok ? 2 : 4);
     mbar_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
@@ -142,6 +147,100 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
       if (t.kind == kEnd) break;
       const bool gate = t.kind == kGate;
       const bool mine = half * 16 < t.rows;                   // the warp has something to keep
+      if constexpr (kTok) {
+        // this thread: token r; 64 columns of gate and of up, or 128 of down
+        const int KB = gate ? p.KB1 : p.KB2;
+        const bool some = 32 * q < t.rows;
+        const uint32_t c0 = gate ? half * 64 : half * 128, c1 = gate ? 128 + half * 64 : half * 128 + 64;
+        uint64_t acc[64];
+#pragma unroll
+        for (int i = 0; i < 64; ++i) acc[i] = 0;
+        bool ok = true;
+        for (int kb = 0; kb < KB; ++kb, ++it, ++sc) {
+          const uint32_t buf = it % kBufs, e = sc % kScRing;
+          if (!__all_sync(0xffffffffu, mbar_wait(sfull0 + 8 * e, (sc / kScRing) & 1, &s_abort)) ||
+              !__all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * buf, (it / kBufs) & 1, &s_abort))) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          promote_2x64(acc, tq + buf * (2 * NT) + c0, tq + buf * (2 * NT) + c1, s_scale[e][gate ? 0 : half][r],
+                       s_scale[e][gate ? 1 : half][r]);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(tempty0 + 8 * buf);
+            mbar_arrive(sempty0 + 8 * e);
+          }
+        }
+        if (!ok) break;
+        if (some && gate) {
+          const int i0 = t.blk * kTile + half * 64;
+          uint32_t top = 0;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            uint32_t g[2], u[2], h[2];
+            f2_unpack(acc[i], g[0], g[1]);
+            f2_unpack(acc[32 + i], u[0], u[1]);
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+              h[d] = __float_as_uint(silu_times(__uint_as_float(g[d]), __uint_as_float(u[d])));
+              if (i0 + 2 * i + d < p.I) top = max(top, h[d] & 0x7fffffffu);
+            }
+            acc[i] = f2_pack(h[0], h[1]);
+          }
+          // the block's other 64 columns are the neighbour warp's
+          s_top[meets & 1][half][r] = top;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(meet0 + 8 * q);
+          if (!__all_sync(0xffffffffu, mbar_wait(meet0 + 8 * q, meets & 1, &s_abort))) break;
+          const BlockScale s = block_scale(__uint_as_float(max(top, s_top[meets & 1][half ^ 1][r])));
+          ++meets;
+          if (r < t.rows) {
+            uint8_t* o = static_cast<uint8_t*>(p.h) + (size_t)(t.entry + r) * p.I + i0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t w[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                uint32_t h[4];
+                f2_unpack(acc[8 * i + 2 * j], h[0], h[1]);
+                f2_unpack(acc[8 * i + 2 * j + 1], h[2], h[3]);
+                w[j] = pack_e4m3(to_code(__uint_as_float(h[0]), s), to_code(__uint_as_float(h[1]), s),
+                                 to_code(__uint_as_float(h[2]), s), to_code(__uint_as_float(h[3]), s));
+              }
+              if (i0 + 16 * i < p.I) *reinterpret_cast<uint4*>(o + 16 * i) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            if (half == 0) p.hs[(size_t)t.blk * p.n + t.entry + r] = s.scale;
+          }
+        } else if (some) {
+          // 16 columns at a time through shared memory, so that a store is eight rows' 64 bytes
+          const int col = t.blk * 2 * kTile + half * 128 + 4 * (lane & 3);
+          const uint32_t out = ring + (uint32_t)S * stBytes + (uint32_t)(warp - 4) * kOutBytes;
+#pragma unroll
+          for (int h = 0; h < 8; ++h) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t v[4];
+              f2_unpack(acc[8 * h + 2 * i], v[0], v[1]);
+              f2_unpack(acc[8 * h + 2 * i + 1], v[2], v[3]);
+              st_shared_u4(out + (uint32_t)lane * 64 + (uint32_t)((i ^ (lane >> 1 & 3)) << 4), make_uint4(v[0], v[1], v[2], v[3]));
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int rr = 8 * i + (lane >> 2);
+              const uint4 v = ld_shared_u4(out + (uint32_t)rr * 64 + (uint32_t)(((lane & 3) ^ (rr >> 1 & 3)) << 4));
+              if (32 * q + rr < t.rows && col + 16 * h < p.H)
+                __stcg(reinterpret_cast<uint4*>(p.y + (size_t)(t.entry + 32 * q + rr) * p.H + col + 16 * h), v);
+            }
+            __syncwarp();
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(edone0 + 8 * slot);
+        continue;
+      }
       uint64_t acc0[kChunks][8], acc1[kChunks][8];            // tokens (2 j + half) 16 .. + 15 of the two tiles
 #pragma unroll
       for (int j = 0; j < kChunks; ++j)
@@ -397,7 +496,7 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
         const int KB = kind == kGate ? p.KB1 : p.KB2;
         constexpr uint64_t tile2 = kBoxBytes >> 4;
         const int N = (rows + 15) & ~15;
-        const uint32_t idesc = kFp8 ? idesc_e4m3(128, N) : idesc_bf16(128, N);
+        const uint32_t idesc = kTok ? idesc_e4m3(128, 2 * kTile) : kFp8 ? idesc_e4m3(128, N) : idesc_bf16(128, N);
         for (int kb = 0; kb < KB; ++kb) {
           const uint32_t buf = it % kBufs, ph = (it / kBufs) & 1;
           if (((kFp8 || kb == 0) && !__all_sync(0xffffffffu, mbar_wait(tempty0 + 8 * buf, ph ^ 1, &s_abort))) ||
@@ -413,7 +512,9 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
 #pragma unroll
             for (int k = 0; k < 4; ++k) {                     // 32 bytes along K each
               const uint32_t add = (kFp8 ? k : kb + k) != 0 ? 1u : 0u;
-              if constexpr (kFp8) {
+              if constexpr (kTok) {
+                tc_mma_f8(d, bd + (uint64_t)(2 * k), ad + (uint64_t)(2 * k), idesc, add);
+              } else if constexpr (kFp8) {
                 tc_mma_f8(d, ad + (uint64_t)(2 * k), bd + (uint64_t)(2 * k), idesc, add);
                 tc_mma_f8(d + NT, ad + tile2 + (uint64_t)(2 * k), bd + (uint64_t)(2 * k), idesc, add);
               } else {
@@ -669,9 +770,9 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
 template <bool kFp8, int NT>
 ee_status launch(MoeParams& p, cudaStream_t stream) {
   const uint64_t es = kFp8 ? 1 : 2;
-  const size_t stage = (size_t)p.b_rows * 128 + 2 * kTile * 128;
-  p.stages = (int)std::min<size_t>(kMaxStages, (size_t)(213 * 1024) / stage);
-  const size_t smem = 1024 + p.stages * stage;
+  const size_t stage = (size_t)p.b_rows * 128 + 2 * kTile * 128, outs = kFp8 && NT == 128 ? kEpiWarps * kOutBytes : 0;
+  p.stages = (int)std::min<size_t>(kMaxStages, ((size_t)(213 * 1024) - outs) / stage);
+  const size_t smem = 1024 + p.stages * stage + outs;
   CUtensorMap tmW1, tmH8, tmH32, tmW2;
   const auto encode = [](CUtensorMap* m, const void* base, uint64_t cols, uint64_t rows, uint64_t stride, uint32_t box) {
     if constexpr (kFp8) return encode_u8_tmap_2d(m, base, cols, rows, stride, 128, box);
