@@ -1,13 +1,13 @@
 // What the weight products of a pass share (ee_fp8_linear, ee_moe_layer):
-// 8-bit MMAs, gathering TMA loads, the promotion of one block's product into
-// fp32 registers, and the quantisation of a block.  Internal header.
+// 8-bit MMAs, the promotion of one block's product into fp32 registers, and the
+// quantisation of a block.  Internal header.
 //
 // A product with a scale for each block of 128 along K cannot stay in the
 // tensor cores' accumulator: y = sum_b s_b (x_b . w_b).  Each block's product
 // goes to tensor memory by itself (two accumulators in turn) and the epilogue
-// warps add it, scaled, to sums of their own in registers.  Tokens are the MMA's
-// M side (one tensor-memory lane, one thread), so a block's scale is one number a
-// thread and 128 columns; weight rows are the N side.
+// warps add it, scaled, to sums of their own in registers.  With tokens as the MMA's
+// M side (one tensor-memory lane, one thread) a block's scale is one number a
+// thread and 128 columns; tiles of few tokens have it the other way round (moe_experts.cu).
 #pragma once
 #include "ee_common.cuh"
 #include "ee_ptx.cuh"
@@ -37,16 +37,6 @@ __device__ __forceinline__ void tc_mma_f8(uint32_t d_tmem, uint64_t adesc, uint6
       "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// Four rows of a map whose box is one row high, to four consecutive rows of shared memory.
-__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int r0, int r1,
-                                            int r2, int r3) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, "
-      "%5, %6}], [%7];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar)
-      : "memory");
-}
-
 // acc[16 g .. 16 g + 15] (pairs) += s * 32 columns that a load left in r
 template <int G, int N>
 __device__ __forceinline__ void add_scaled32(uint64_t (&acc)[N], uint32_t (&r)[32], uint64_t s) {

@@ -12,7 +12,7 @@
 //
 // On 8-bit weights tiles of 128 tokens have tokens on the lanes all the same: a token's scale is then one
 // register, where the columns' scales come from shared memory, 128 of them a k-block and thread, whose reads
-// bound such tiles (2,048 tokens at 4 of 16 experts 281 us, so %TOK%).
+// bound such tiles (2,048 tokens at 4 of 16 experts 281 us, so 226).
 //
 // CTAs draw tasks from one queue, gate tasks first.  A down task waits for the gate tasks of its
 // token tile; those were drawn before it by CTAs that are running, so no wait depends on
@@ -21,6 +21,9 @@
 // tasks, so that the stream does not stop between them.  Warp 2 puts products of scales into shared memory,
 // warp 3 tells other CTAs what the epilogue warps 4..11 have stored (a release waits for the stores: it would hold them up
 // for 2 us a task).
+//
+// Measured with the routing, 64 experts of 1280 x 3584, 6 a token: 64 tokens on 8-bit weights 137 us (845 MB; the
+// experts' part 122 us, 6.9 TB/s), on bf16 ones 255 us; 534 tokens 173 and 298 us.
 #include <mutex>
 
 #include "moe.cuh"

@@ -11,6 +11,8 @@
 // each expert and token, so that an entry's place is a count of bits and does not depend on who comes first.
 // Up to 16 tokens are one cluster's: its first CTA then chooses and groups without a way through global memory.
 // CTAs of their own quantise x.
+// 8 us for one token, 12 for 64, 18 for 2,048 behind a layer whose weights went through L2 (5 on warm data): loads and
+// instructions come from HBM, and its CTAs can only start when one of the layer in front leaves its SM.
 #include <mutex>
 
 #include "moe.cuh"
@@ -50,7 +52,7 @@ __device__ __forceinline__ uint32_t logit_key(float f) {
 
 // NT: groups of 8 experts (E <= 8 NT)
 template <int NT>
-__global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const RouteParams p) {
+__global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const RouteParams p, const int keep) {
   constexpr int EP = 8 * NT, kWarps = warps_of(NT), kThreads = 32 * kWarps;
   extern __shared__ float s_red[];                 // [kWarps][kTok][EP], the first becomes the CTA's sums
   __shared__ int s_last;
@@ -230,21 +232,20 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
   }
 
   // ---- the last CTA groups the tokens by expert --------------------------------------
-  if (alone) {
-    if (rank != 0) return;
-    __syncthreads();
-  } else {
-    __syncthreads();
-    if (threadIdx.x == 0) s_last = atom_add_acq_rel(&p.ctl->route_ticket, 1u) == (uint32_t)routers - 1;
-    __syncthreads();
-    if (!s_last) return;
-  }
   const int words = (live + 31) >> 5, n = live * p.k;
   uint32_t* mask = alone ? s_bits : reinterpret_cast<uint32_t*>(s_red);   // [E][words]
   uint16_t* pre = reinterpret_cast<uint16_t*>(reinterpret_cast<uint32_t*>(s_red) + p.E * words);   // bits in an expert's earlier words
   int* s_off = reinterpret_cast<int*>(pre + ((p.E * words + 1) & ~1));
-  if (!alone)
+  uint8_t* s_e = reinterpret_cast<uint8_t*>(s_off + p.E);                 // [n] expert of a token's j-th place (where keep)
+  __syncthreads();
+  if (alone) {
+    if (rank != 0) return;
+  } else {
+    if (threadIdx.x == 0) s_last = atom_add_acq_rel(&p.ctl->route_ticket, 1u) == (uint32_t)routers - 1;
     for (int i = threadIdx.x; i < p.E * words; i += kThreads) mask[i] = 0;
+    __syncthreads();
+    if (!s_last) return;
+  }
   for (int i = threadIdx.x; i < p.max_tiles; i += kThreads) p.ctl->gate_done[i] = 0;
   if (threadIdx.x == 0) {
     p.ctl->route_ticket = 0;
@@ -252,7 +253,6 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
     p.ctl->down_done = 0;
   }
   constexpr int kAhead = 4;                        // entries of a thread whose loads are under way together
-  if (!alone) __syncthreads();
   for (int i0 = threadIdx.x; i0 < n && !alone; i0 += kThreads * kAhead) {
     int e[kAhead];
 #pragma unroll
@@ -263,7 +263,10 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const int i = i0 + j * kThreads, t = i / p.k;
-      if (i < n) atomicOr(&mask[e[j] * words + (t >> 5)], 1u << (t & 31));
+      if (i < n) {
+        atomicOr(&mask[e[j] * words + (t >> 5)], 1u << (t & 31));
+        if (keep) s_e[i] = (uint8_t)e[j];
+      }
     }
   }
   if (!alone) __syncthreads();
@@ -303,28 +306,13 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
     if ((int)threadIdx.x == p.E - 1) p.ctl->tiles = incl >> 20;
   }
   __syncthreads();
-  for (int i0 = threadIdx.x; i0 < n; i0 += kThreads * kAhead) {
-    int e[kAhead];
-    float pr[kAhead];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      const int i = i0 + j * kThreads;
-      if (i < n) {
-        e[j] = alone ? s_ids[i] : __ldcg(p.ids + i);
-        pr[j] = alone ? s_prob[i] : __ldcg(p.prob + i);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      const int i = i0 + j * kThreads;
-      if (i >= n) break;
-      const int t = i / p.k, at = e[j] * words + (t >> 5);
-      const int pos = s_off[e[j]] + pre[at] + __popc(mask[at] & ((1u << (t & 31)) - 1u));
-      p.list[pos] = t;
-      if (p.few) p.few[s_tile[e[j]] * kFewTokens + t] = FewEntry{pos, pr[j]};
-      p.inv[i] = pos;
-      if (alone) p.prob[i] = pr[j];
-    }
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const int t = i / p.k, e = alone ? s_ids[i] : keep ? s_e[i] : __ldcg(p.ids + i), at = e * words + (t >> 5);
+    const int pos = s_off[e] + pre[at] + __popc(mask[at] & ((1u << (t & 31)) - 1u));
+    p.list[pos] = t;
+    p.inv[i] = pos;
+    if (alone) p.prob[i] = s_prob[i];
+    if (p.few) p.few[s_tile[e] * kFewTokens + t] = FewEntry{pos, s_prob[i]};
   }
   if (alone && p.cl > 1 && live > 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -334,7 +322,9 @@ ee_status launch(const RouteParams& p, cudaStream_t stream) {
   constexpr int kWarps = warps_of(NT);
   const size_t sums = (size_t)kWarps * kTok * 8 * NT * 4;
   const size_t words = ((size_t)p.T + 31) / 32;
-  const size_t group = p.E * words * 6 + 4 + 4 * (size_t)p.E;
+  size_t group = p.E * words * 6 + 4 + 4 * (size_t)p.E;
+  const int keep = group + (size_t)p.T * p.k <= 220 * 1024;   // (4,096 tokens at 16 of 256 experts do not fit)
+  if (keep) group += (size_t)p.T * p.k;
   const size_t smem = std::max(sums, group);
   {
     int dev = 0;
@@ -351,7 +341,7 @@ ee_status launch(const RouteParams& p, cudaStream_t stream) {
   const int routers = (p.T + kTok - 1) / kTok * p.cl, per = kWarps * kQuantUnits;
   const int quants = p.xq ? (p.T * ((p.H + kBlk - 1) / kBlk) + per - 1) / per : 0;
   const unsigned grid = (unsigned)(routers + (quants + p.cl - 1) / p.cl * p.cl);
-  EE_CUDA_OK(launch_pdl(moe_route_kernel<NT>, dim3(grid), dim3(32 * kWarps), smem, stream, (unsigned)p.cl, p));
+  EE_CUDA_OK(launch_pdl(moe_route_kernel<NT>, dim3(grid), dim3(32 * kWarps), smem, stream, (unsigned)p.cl, p, keep));
   return EE_OK;
 }
 

@@ -142,7 +142,7 @@ SIZES = [(1, 16, 16, 1, 1), (8, 528, 208, 16, 3), (3, 400, 2064, 5, 2), (8, 272,
          (6, 640, 144, 200, 16), (65, 256, 128, 2, 2), (150, 272, 144, 5, 2), (180, 528, 400, 3, 1), (12, 400, 272, 30, 4), (9, 1040, 528, 256, 16), (15, 256, 2048, 6, 5), (16, 272, 16, 16, 16), (1, 528, 208, 8, 2), (1, 1024, 256, 64, 6), (2, 256, 128, 8, 8), (5, 272, 144, 9, 3),
          (16, 528, 208, 8, 2), (17, 640, 320, 60, 4), (33, 384, 112, 256, 16), (64, 1024, 384, 16, 4),
          (130, 512, 256, 4, 2), (200, 272, 80, 2, 1), (300, 400, 272, 1, 1), (576, 1536, 640, 64, 6),
-         (1000, 256, 128, 130, 8), (4096, 144, 48, 3, 2)]
+         (1000, 256, 128, 130, 8), (4096, 144, 48, 3, 2), (4096, 16, 16, 256, 16)]
 
 
 @pytest.mark.parametrize("fp8", [False, True])
