@@ -72,16 +72,31 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmW2)) : "memory");
   }
   pdl_wait();
-  const int na = (int)p.ctl->tiles;                            // an active expert has one tile
   int first = 0;
   if (warp < kGroups && lane == 0) first = (int)atomicAdd(&p.ctl->queue, 1u);
+  const int na = (int)p.ctl->tiles;                            // an active expert has one tile
+  const int live = p.live ? max(0, min(p.T, ld_pinned(p.live))) : p.T;
+  uint8_t* const s_rows = s_dyn + (size_t)kGroups * D * (16u * 128u * (uint32_t)max(blocks_of(p.KB1), blocks_of(p.KB2)));
+  const int h_bytes = p.H * es, i_bytes = p.I * es, xs = row_stride(p.KB1);
+  float* const s_xs = reinterpret_cast<float*>(s_rows + (size_t)p.T * xs);   // [T][KB1]
+  {
+    const int chunks = p.KB1 * 8;                              // 16 bytes; rows behind the live ones as zeros
+    for (int i = threadIdx.x; i < p.T * chunks; i += kThreads) {
+      const int t = i / chunks, c = i % chunks * 16;
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (t < live && c < h_bytes)
+        v = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.x) + (size_t)t * p.x_stride * es + c);
+      *reinterpret_cast<uint4*>(s_rows + (size_t)t * xs + c) = v;
+    }
+    if constexpr (kFp8)
+      for (int i = threadIdx.x; i < live * p.KB1; i += kThreads) s_xs[i] = p.xs[(size_t)(i % p.KB1) * p.T + i / p.KB1];
+  }
   for (int i = threadIdx.x; i < na; i += kThreads) s_exp[i] = p.tile[i].expert;
   for (int i = threadIdx.x; i < na * NT; i += kThreads) {
     const FewEntry e = p.few[i];
     s_map[i / NT][i % NT] = (int16_t)e.entry;
     s_p[i / NT][i % NT] = e.p;
   }
-  const int live = p.live ? max(0, min(p.T, ld_pinned(p.live))) : p.T;
   const int per = p.I / 8, gates = na * per, total = gates + (na ? (p.H + 15) / 16 : 0);
   const int nst1 = stages_of(p.KB1), nst2 = stages_of(p.KB2), c1 = blocks_of(p.KB1), c2 = blocks_of(p.KB2);
   const uint32_t stBytes = 16u * 128u * (uint32_t)max(c1, c2);
@@ -165,11 +180,8 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
     // ---- consumers --------------------------------------------------------------------
     const int w = (warp - kGroups) % kFewWarps, g = lane >> 2, tq = lane & 3;
     const int ct = (int)threadIdx.x - 32 * kGroups, gt = ct % (32 * kFewWarps);   // thread of all consumers, of the group
-    uint8_t* const s_rows = s_dyn + (size_t)kGroups * D * stBytes;
-    const int xs = row_stride(p.KB1), hs = row_stride(p.KB2);
-    float* const s_xs = reinterpret_cast<float*>(s_rows + (size_t)p.T * xs);   // [T][KB1]
+    const int hs = row_stride(p.KB2);
     float* const s_hs = reinterpret_cast<float*>(s_rows + (size_t)p.n * hs);   // [n][IB]
-    const int h_bytes = p.H * es, i_bytes = p.I * es;
     uint32_t met = 0, met_all = 0;
     // a meeting of the group's consumers (or all): false when it was given up
     const auto meet_at = [&](uint32_t bar, uint32_t& count) {
@@ -177,20 +189,7 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
       if (lane == 0) mbar_arrive(bar);
       return (bool)__all_sync(0xffffffffu, mbar_wait(bar, count++ & 1, &s_abort));
     };
-    {
-      const int chunks = p.KB1 * 8;                            // 16 bytes; rows behind the live ones as zeros
-      for (int i = ct; i < p.T * chunks; i += 32 * kGroups * kFewWarps) {
-        const int t = i / chunks, c = i % chunks * 16;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (t < live && c < h_bytes)
-          v = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.x) + (size_t)t * p.x_stride * es + c);
-        *reinterpret_cast<uint4*>(s_rows + (size_t)t * xs + c) = v;
-      }
-      if constexpr (kFp8)
-        for (int i = ct; i < live * p.KB1; i += 32 * kGroups * kFewWarps)
-          s_xs[i] = p.xs[(size_t)(i % p.KB1) * p.T + i / p.KB1];
-    }
-    bool ok = meet_at(meet_all, met_all);
+    bool ok = true;
     const int last = max(live, 1) - 1;
     const int t0 = min(2 * tq, last), t1 = min(2 * tq + 1, last);
     const uint32_t xrow = smem_u32(s_rows) + (uint32_t)(min(g, p.T - 1) * xs + tq * 16);
