@@ -732,6 +732,8 @@ ee_status ee_fp8_quantize_weights(const ee_bf16* w, int32_t batch, int32_t rows,
  *   out bf16, out_stride elements from one token to the next (at least N)
  * K a multiple of 16; x and w 16-byte aligned; n, N of any size (up to 2^24).  A
  * token's output depends on that token alone.
+ * out must not overlap inputs.  x_scale * w_scale is taken first: it has to fit in fp32.  Any call's workspace
+ * will do: only its error word is used.
  * Device errors: EE_DEVERR_TIMEOUT (outputs undefined).
  */
 size_t ee_linear_workspace_size(void);
@@ -758,7 +760,10 @@ ee_status ee_fp8_linear(const uint8_t* x, const float* x_scale, const uint8_t* w
  *   ids int32 [T][k], probs fp32 [T][k] or NULL: the choice and its weights
  * H and I multiples of 16, up to 65536; E up to 256, k up to 16; x, router, w1 and w2 16-byte aligned.
  * Always summed in the same order: repeated calls agree bit for bit.
- * ws: ee_moe_workspace_size(...) bytes for these sizes (a larger one serves too), zeroed once with ee_workspace_init().
+ * Outputs must not overlap inputs.
+ * ws: ee_moe_workspace_size(...) bytes for these sizes (a larger one serves too; 0: sizes out of range), zeroed once
+ *   with ee_workspace_init().  A workspace of its own: its arrays lie where the attention and the LM head keep counts
+ *   from call to call, so of the other entry points only ee_fp8_linear may share it.
  * Device errors: EE_DEVERR_TIMEOUT (outputs undefined).
  */
 size_t ee_moe_workspace_size(int32_t T, int32_t H, int32_t I, int32_t E, int32_t k);

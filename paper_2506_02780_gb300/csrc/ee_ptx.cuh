@@ -255,6 +255,16 @@ __device__ __forceinline__ int32_t ld_pinned(const int32_t* a) {
   asm volatile("ld.global.s32 %0, [%1];" : "=r"(v) : "l"(a));
   return v;
 }
+__device__ __forceinline__ uint4 ld_pinned16(const void* a) {
+  uint4 v;
+  asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(a));
+  return v;
+}
+__device__ __forceinline__ float ld_pinned_f(const float* a) {
+  float v;
+  asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(a));
+  return v;
+}
 // gpu-scope acquire load of a global counter
 __device__ __forceinline__ uint32_t ld_acquire(const uint32_t* a) {
   uint32_t v;

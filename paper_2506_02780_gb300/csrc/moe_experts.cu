@@ -685,13 +685,6 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
   __syncthreads();
 
   // ---- the sum over a token's experts, all warps ------------------------------------
-  // one code for all warps from here: as many registers as it was compiled for (a warpgroup has to
-  // meet between two changes of its registers)
-  __syncthreads();
-  if (warp >= 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsAll));
-  else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsAll));
-  tc_fence_before();
-  __syncthreads();
   if (!s_abort) {
     if (threadIdx.x == 0 && !wait_count_geq(&p.ctl->down_done, p.ctl->tiles * (uint32_t)p.HT)) s_abort = 1;
     __syncthreads();
@@ -772,7 +765,6 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
 
 template <bool kFp8, int NT>
 ee_status launch(MoeParams& p, cudaStream_t stream) {
-  const uint64_t es = kFp8 ? 1 : 2;
   const size_t stage = (size_t)p.b_rows * 128 + 2 * kTile * 128, outs = kFp8 && NT == 128 ? kEpiWarps * kOutBytes : 0;
   p.stages = (int)std::min<size_t>(kMaxStages, ((size_t)(213 * 1024) - outs) / stage);
   const size_t smem = 1024 + p.stages * stage + outs;
@@ -805,7 +797,9 @@ ee_status launch(MoeParams& p, cudaStream_t stream) {
 }  // namespace
 
 extern "C" size_t ee_moe_workspace_size(int32_t T, int32_t H, int32_t I, int32_t E, int32_t k) {
-  if (T < 0 || H < 1 || I < 1 || E < 1 || k < 1) return 0;
+  if (T < 0 || H < 1 || I < 1 || E < 1 || k < 1 || T > kMoeMaxTokens || H > (1 << 16) || I > (1 << 16) ||
+      E > kMoeMaxExperts || k > kMoeMaxTopK)
+    return 0;
   return ee::moe_layout(T, H, I, E, k).total;
 }
 

@@ -72,31 +72,55 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmW2)) : "memory");
   }
   pdl_wait();
+  // All of a thread's loads are under way before the first is waited for (one after another they took 2.5 us): of the
+  // tables what could be there, behind the active experts something that nobody looks at.
   int first = 0;
   if (warp < kGroups && lane == 0) first = (int)atomicAdd(&p.ctl->queue, 1u);
-  const int na = (int)p.ctl->tiles;                            // an active expert has one tile
-  const int live = p.live ? max(0, min(p.T, ld_pinned(p.live))) : p.T;
+  const int na = (int)ld_pinned(reinterpret_cast<const int32_t*>(&p.ctl->tiles));   // an active expert has one tile
+  const int most = min(p.n, p.E);                              // of them
+  const int live_word = p.live ? ld_pinned(p.live) : p.T;
+  int expert = 0;
+  FewEntry entry{-1, 0.f};
+  if ((int)threadIdx.x < most) expert = ld_pinned(&p.tile[threadIdx.x].expert);
+  if ((int)threadIdx.x < most * NT) {
+    entry.entry = ld_pinned(&p.few[threadIdx.x].entry);
+    entry.p = ld_pinned_f(&p.few[threadIdx.x].p);
+  }
   uint8_t* const s_rows = s_dyn + (size_t)kGroups * D * (16u * 128u * (uint32_t)max(blocks_of(p.KB1), blocks_of(p.KB2)));
   const int h_bytes = p.H * es, i_bytes = p.I * es, xs = row_stride(p.KB1);
   float* const s_xs = reinterpret_cast<float*>(s_rows + (size_t)p.T * xs);   // [T][KB1]
-  {
-    const int chunks = p.KB1 * 8;                              // 16 bytes; rows behind the live ones as zeros
-    for (int i = threadIdx.x; i < p.T * chunks; i += kThreads) {
-      const int t = i / chunks, c = i % chunks * 16;
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (t < live && c < h_bytes)
-        v = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.x) + (size_t)t * p.x_stride * es + c);
-      *reinterpret_cast<uint4*>(s_rows + (size_t)t * xs + c) = v;
-    }
-    if constexpr (kFp8)
-      for (int i = threadIdx.x; i < live * p.KB1; i += kThreads) s_xs[i] = p.xs[(size_t)(i % p.KB1) * p.T + i / p.KB1];
+  const int chunks = p.KB1 * 8;                                // 16 bytes; rows behind the live ones (whatever they hold) are
+  constexpr int kFirst = 2;                                    // not looked at
+  uint4 v[kFirst];
+  float sv = 0.f;
+#pragma unroll
+  for (int j = 0; j < kFirst; ++j) {
+    const int i = (int)threadIdx.x + j * kThreads, t = i / chunks, c = i % chunks * 16;
+    v[j] = make_uint4(0, 0, 0, 0);
+    if (t < p.T && c < h_bytes) v[j] = ld_pinned16(static_cast<const uint8_t*>(p.x) + (size_t)t * p.x_stride * es + c);
   }
-  for (int i = threadIdx.x; i < na; i += kThreads) s_exp[i] = p.tile[i].expert;
-  for (int i = threadIdx.x; i < na * NT; i += kThreads) {
-    const FewEntry e = p.few[i];
-    s_map[i / NT][i % NT] = (int16_t)e.entry;
-    s_p[i / NT][i % NT] = e.p;
+  if (kFp8 && (int)threadIdx.x < p.T * p.KB1)
+    sv = ld_pinned_f(p.xs + (size_t)(threadIdx.x % p.KB1) * p.T + threadIdx.x / p.KB1);
+  const int live = max(0, min(p.T, live_word));
+  if ((int)threadIdx.x < na) s_exp[threadIdx.x] = expert;
+  if ((int)threadIdx.x < na * NT) {
+    s_map[threadIdx.x / NT][threadIdx.x % NT] = (int16_t)entry.entry;
+    s_p[threadIdx.x / NT][threadIdx.x % NT] = entry.p;
   }
+#pragma unroll
+  for (int j = 0; j < kFirst; ++j) {
+    const int i = (int)threadIdx.x + j * kThreads;
+    if (i < p.T * chunks) *reinterpret_cast<uint4*>(s_rows + (size_t)(i / chunks) * xs + i % chunks * 16) = v[j];
+  }
+  for (int i = (int)threadIdx.x + kFirst * kThreads; i < p.T * chunks; i += kThreads) {
+    const int t = i / chunks, c = i % chunks * 16;
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (c < h_bytes) w = ld_pinned16(static_cast<const uint8_t*>(p.x) + (size_t)t * p.x_stride * es + c);
+    *reinterpret_cast<uint4*>(s_rows + (size_t)t * xs + c) = w;
+  }
+  if constexpr (kFp8)
+    for (int i = threadIdx.x; i < p.T * p.KB1; i += kThreads)
+      s_xs[i] = i < kThreads ? sv : p.xs[(size_t)(i % p.KB1) * p.T + i / p.KB1];
   const int per = p.I / 8, gates = na * per, total = gates + (na ? (p.H + 15) / 16 : 0);
   const int nst1 = stages_of(p.KB1), nst2 = stages_of(p.KB2), c1 = blocks_of(p.KB1), c2 = blocks_of(p.KB2);
   const uint32_t stBytes = 16u * 128u * (uint32_t)max(c1, c2);

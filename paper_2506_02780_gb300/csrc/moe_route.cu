@@ -38,12 +38,6 @@ __device__ __forceinline__ float ld_cluster_f(uint32_t a) {
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
   return v;
 }
-// (in the order in which they are written, so that all of a warp's loads are under way together)
-__device__ __forceinline__ uint4 ld_pinned16(const __nv_bfloat16* a) {
-  uint4 v;
-  asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(a));
-  return v;
-}
 // larger key, better logit; at least 1: a NaN is the worst
 __device__ __forceinline__ uint32_t logit_key(float f) {
   const uint32_t u = __float_as_uint(f);

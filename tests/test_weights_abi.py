@@ -104,6 +104,13 @@ def test_workspace_sizes(L):
     assert L.ee_moe_workspace_size(4096, 1 << 16, 1 << 16, 256, 16) > 4 * 4096 * 16 * (1 << 16)
 
 
+@pytest.mark.parametrize("sizes", [(4097, 512, 256, 16, 4), (64, (1 << 16) + 16, 256, 16, 4), (64, 512, (1 << 16) + 16, 16, 4),
+                                   (64, 512, 256, 257, 4), (64, 512, 256, 32, 17), (2**31 - 1,) * 5])
+def test_no_workspace_for_sizes_out_of_range(L, sizes):
+    """... whose layer is refused, too: nobody finds out at the first call."""
+    assert L.ee_moe_workspace_size(*sizes) == 0
+
+
 # ---------------------------------------------------------------- the binding
 
 def t(*shape, dtype=torch.bfloat16):
