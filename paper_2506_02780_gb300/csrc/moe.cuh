@@ -30,13 +30,10 @@ struct __align__(32) MoeTile {   // a token tile's expert
   int pad[3];
 };
 constexpr int kFewEntries = 8, kFewTokens = 8;   // what moe_few.cu takes
-struct FewEntry {            // of so few: an active expert's entry of a token, or -1, and its weight
-  int entry;
-  float p;
-};
+constexpr int kRouteParts = 8;   // CTAs that share the hidden dimension, at most
 
 struct MoeLayout {
-  size_t ctl, tile, few, ids, prob, list, inv, xq, xs, h, hf, hs, y, total;
+  size_t ctl, tile, part, ids, prob, list, inv, xq, xs, h, hf, hs, y, total;
   int max_tiles;             // token tiles of all experts, at most
 };
 inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t k) {
@@ -51,7 +48,7 @@ inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t 
   };
   l.ctl = take(sizeof(MoeCtl) + 4 * (size_t)l.max_tiles);
   l.tile = take(sizeof(MoeTile) * (size_t)l.max_tiles);
-  l.few = take(sizeof(FewEntry) * kFewEntries * kFewTokens);
+  l.part = take(4 * (size_t)(kRouteParts * kFewTokens * E));
   l.ids = take(4 * (size_t)n);
   l.prob = take(4 * (size_t)n);
   l.list = take(4 * (size_t)n);
@@ -74,7 +71,7 @@ struct RouteParams {
   int T, H, E, k, renorm, cl, max_tiles, tile_rows;
   MoeCtl* ctl;
   MoeTile* tile;
-  FewEntry* few;             // or NULL (more than 8 entries): [active expert][8]
+  float* part;               // [cl][T][E] sums over a CTA's columns for moe_few.cu, which chooses itself; or NULL
   int32_t* ids;              // [T][k] experts of a token, ascending
   float* prob;               // [T][k]
   int32_t* list;             // [T k] token of an entry
@@ -85,6 +82,66 @@ struct RouteParams {
   float* prob_out;
 };
 ee_status launch_moe_route(const RouteParams& p, cudaStream_t stream);
+
+// larger key, better logit; at least 1: a NaN is the worst
+__device__ __forceinline__ uint32_t logit_key(float f) {
+  const uint32_t u = __float_as_uint(f);
+  return f != f ? 1u : (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+// A warp chooses one token's k experts; lane + 32 i holds expert lane + 32 i's logit.  Lane j < k: an expert, its weight
+// and its place among the chosen ones in ascending order.
+struct MoeChoice {
+  int expert, place;
+  float p;
+};
+template <int kPer>
+__device__ __forceinline__ MoeChoice choose_experts(const float (&l)[kPer], int E, int k, bool renorm, int lane) {
+  uint32_t key[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) key[i] = lane + 32 * i < E ? logit_key(l[i]) : 0u;
+  MoeChoice c;
+  c.expert = 0x7fffffff;
+  float my_l = 0.f, top = 0.f;
+  for (int j = 0; j < k; ++j) {
+    uint32_t best = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) best = max(best, key[i]);
+    const uint32_t all = __reduce_max_sync(0xffffffffu, best);
+    uint32_t e = 0xffffffffu;
+#pragma unroll
+    for (int i = kPer - 1; i >= 0; --i)
+      if (key[i] == all) e = lane + 32 * i;
+    e = __reduce_min_sync(0xffffffffu, e);         // of equal logits the lowest expert
+    float le = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (e == (uint32_t)(lane + 32 * i)) {
+        le = l[i];
+        key[i] = 0;
+      }
+    le = __shfl_sync(0xffffffffu, le, e & 31);
+    if (j == 0) top = le;
+    if (lane == j) {
+      c.expert = (int)e;
+      my_l = le;
+    }
+  }
+  float sum = 0.f;
+  const float pe = lane < k ? expf(my_l - top) : 0.f;
+  if (renorm) {
+    sum = pe;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (lane + 32 * i < E) sum += expf(l[i] - top);
+  }
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  c.place = 0;
+  for (int j = 0; j < k; ++j) c.place += __shfl_sync(0xffffffffu, c.expert, j) < c.expert;
+  c.p = __fdiv_rn(pe, sum);
+  return c;
+}
 
 struct MoeParams {
   int T, H, I, E, k, n;                // n = T k
@@ -98,7 +155,10 @@ struct MoeParams {
   int64_t x_stride;
   MoeCtl* ctl;
   const MoeTile* tile;
-  const FewEntry* few;
+  const float* part;                   // few entries: [cl][T][E] parts of the logits
+  int cl, renorm;
+  int32_t* ids_out;
+  float* prob_out;
   const int32_t* list;
   const int32_t* inv;
   const float* prob;

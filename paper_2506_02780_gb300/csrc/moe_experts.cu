@@ -838,7 +838,9 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   r.tile_rows = ee::moe_tile_rows(T, E, k, fp8);
   r.ctl = reinterpret_cast<ee::MoeCtl*>(base + l.ctl);
   r.tile = reinterpret_cast<ee::MoeTile*>(base + l.tile);
-  r.few = T * k <= ee::kFewEntries ? reinterpret_cast<ee::FewEntry*>(base + l.few) : nullptr;
+  size_t few_smem = 0;
+  const bool few = ee::moe_few_stages(T, H, I, k, fp8, &few_smem) > 0;
+  r.part = few ? reinterpret_cast<float*>(base + l.part) : nullptr;
   r.ids = reinterpret_cast<int32_t*>(base + l.ids);
   r.prob = reinterpret_cast<float*>(base + l.prob);
   r.list = reinterpret_cast<int32_t*>(base + l.list);
@@ -849,7 +851,7 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   r.prob_out = probs_or_null;
   // the widest share of the hidden dimension that the SMs hold at once
   const int groups = (T + 15) / 16, blocks = (H + kBlk - 1) / kBlk;
-  r.cl = 8;
+  r.cl = ee::kRouteParts;
   while (r.cl > 1 && (groups * r.cl > ee::kNumSMs || r.cl > blocks)) r.cl /= 2;
   MoeParams p;
   p.T = T;
@@ -871,7 +873,11 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   p.x_stride = fp8 ? H : x_stride;
   p.ctl = r.ctl;
   p.tile = r.tile;
-  p.few = r.few;
+  p.part = r.part;
+  p.cl = r.cl;
+  p.renorm = r.renorm;
+  p.ids_out = ids_or_null;
+  p.prob_out = probs_or_null;
   p.list = r.list;
   p.inv = r.inv;
   p.prob = r.prob;
@@ -890,8 +896,7 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   const ee_status st = ee::launch_moe_route(r, (cudaStream_t)stream);
   if (st != EE_OK) return st;
   const cudaStream_t s = (cudaStream_t)stream;
-  size_t few = 0;
-  if (ee::moe_few_stages(T, H, I, k, fp8, &few)) return ee::launch_moe_few(p, fp8, s);
+  if (few) return ee::launch_moe_few(p, fp8, s);
   if (fp8) return nt == 32 ? launch<true, 32>(p, s) : nt == 64 ? launch<true, 64>(p, s) : launch<true, 128>(p, s);
   return nt == 32 ? launch<false, 32>(p, s) : nt == 64 ? launch<false, 64>(p, s) : launch<false, 128>(p, s);
 }

@@ -1,5 +1,6 @@
-// ee_moe_layer for up to 8 entries (tokens times chosen experts), after the router (moe_route.cu): one persistent
-// kernel, a CTA an SM.  So few experts make few tiles for the tensor cores (6 experts of 1280 x 3584 60 gate
+// ee_moe_layer for up to 8 entries (tokens times chosen experts), after the router's product (moe_route.cu): one
+// persistent kernel, a CTA an SM.  Every CTA adds up the product's parts and chooses the experts itself, which costs less than a way of the
+// choice through memory.  So few experts make few tiles for the tensor cores (6 experts of 1280 x 3584 60 gate
 // tasks for 152 SMs); here two groups of a producer warp and 8 consumer warps draw units from a queue:
 //   gate unit    8 columns of h of one expert: a warp's MMAs take its 8 gate rows and its 8 up rows, so that a
 //                lane holds both halves of silu(g) u
@@ -50,6 +51,8 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
   __shared__ float s_p[kFewEntries][kFewTokens];               // an active expert's weight for a token
   __shared__ int16_t s_map[kFewEntries][kFewTokens];           // ... and the entry, or -1
   __shared__ int s_exp[kFewEntries];
+  __shared__ int s_ids[kFewEntries], s_active;                 // experts of a token's j-th place; how many different ones
+  __shared__ float s_prob[kFewEntries];
   __shared__ int s_done[kGroups];                              // gate units of the group
   __shared__ volatile int s_abort;
   pdl_allow_next();
@@ -72,55 +75,94 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmW2)) : "memory");
   }
   pdl_wait();
-  // All of a thread's loads are under way before the first is waited for (one after another they took 2.5 us): of the
-  // tables what could be there, behind the active experts something that nobody looks at.
+  // All of a thread's loads are under way before the first is waited for.
   int first = 0;
   if (warp < kGroups && lane == 0) first = (int)atomicAdd(&p.ctl->queue, 1u);
-  const int na = (int)ld_pinned(reinterpret_cast<const int32_t*>(&p.ctl->tiles));   // an active expert has one tile
-  const int most = min(p.n, p.E);                              // of them
-  const int live_word = p.live ? ld_pinned(p.live) : p.T;
-  int expert = 0;
-  FewEntry entry{-1, 0.f};
-  if ((int)threadIdx.x < most) expert = ld_pinned(&p.tile[threadIdx.x].expert);
-  if ((int)threadIdx.x < most * NT) {
-    entry.entry = ld_pinned(&p.few[threadIdx.x].entry);
-    entry.p = ld_pinned_f(&p.few[threadIdx.x].p);
-  }
+  const int live = p.live ? max(0, min(p.T, ld_pinned(p.live))) : p.T;
   uint8_t* const s_rows = s_dyn + (size_t)kGroups * D * (16u * 128u * (uint32_t)max(blocks_of(p.KB1), blocks_of(p.KB2)));
   const int h_bytes = p.H * es, i_bytes = p.I * es, xs = row_stride(p.KB1);
   float* const s_xs = reinterpret_cast<float*>(s_rows + (size_t)p.T * xs);   // [T][KB1]
-  const int chunks = p.KB1 * 8;                                // 16 bytes; rows behind the live ones (whatever they hold) are
-  constexpr int kFirst = 2;                                    // not looked at
-  uint4 v[kFirst];
+  const int chunks = p.KB1 * 8, logits = p.T * p.E;            // of 16 bytes; of tokens behind the live ones nobody looks at
+  float part[kRouteParts];                                     // either
+  uint4 v = make_uint4(0, 0, 0, 0);
   float sv = 0.f;
 #pragma unroll
-  for (int j = 0; j < kFirst; ++j) {
-    const int i = (int)threadIdx.x + j * kThreads, t = i / chunks, c = i % chunks * 16;
-    v[j] = make_uint4(0, 0, 0, 0);
-    if (t < p.T && c < h_bytes) v[j] = ld_pinned16(static_cast<const uint8_t*>(p.x) + (size_t)t * p.x_stride * es + c);
-  }
-  if (kFp8 && (int)threadIdx.x < p.T * p.KB1)
-    sv = ld_pinned_f(p.xs + (size_t)(threadIdx.x % p.KB1) * p.T + threadIdx.x / p.KB1);
-  const int live = max(0, min(p.T, live_word));
-  if ((int)threadIdx.x < na) s_exp[threadIdx.x] = expert;
-  if ((int)threadIdx.x < na * NT) {
-    s_map[threadIdx.x / NT][threadIdx.x % NT] = (int16_t)entry.entry;
-    s_p[threadIdx.x / NT][threadIdx.x % NT] = entry.p;
-  }
-#pragma unroll
-  for (int j = 0; j < kFirst; ++j) {
-    const int i = (int)threadIdx.x + j * kThreads;
-    if (i < p.T * chunks) *reinterpret_cast<uint4*>(s_rows + (size_t)(i / chunks) * xs + i % chunks * 16) = v[j];
-  }
-  for (int i = (int)threadIdx.x + kFirst * kThreads; i < p.T * chunks; i += kThreads) {
+  for (int r = 0; r < kRouteParts; ++r)
+    if (r < p.cl && (int)threadIdx.x < logits) part[r] = ld_pinned_f(p.part + (size_t)r * logits + threadIdx.x);
+  const auto x_at = [&](int i) {                               // NULL: zeros
     const int t = i / chunks, c = i % chunks * 16;
-    uint4 w = make_uint4(0, 0, 0, 0);
-    if (c < h_bytes) w = ld_pinned16(static_cast<const uint8_t*>(p.x) + (size_t)t * p.x_stride * es + c);
-    *reinterpret_cast<uint4*>(s_rows + (size_t)t * xs + c) = w;
+    return t < p.T && c < h_bytes ? static_cast<const uint8_t*>(p.x) + (size_t)t * p.x_stride * es + c : nullptr;
+  };
+  if (const uint8_t* at = x_at((int)threadIdx.x)) v = ld_pinned16(at);
+  const auto xs_at = [&](int i) { return p.xs + (size_t)(i % p.KB1) * p.T + i / p.KB1; };
+  if (kFp8 && (int)threadIdx.x < p.T * p.KB1) sv = ld_pinned_f(xs_at((int)threadIdx.x));
+  // the routing's parts of the logits in a fixed order
+  float* const s_logit = &s_part[0][0][0][0][0];               // [T][E], in front of the units' sums
+  static_assert(sizeof(s_part) >= kFewTokens * kMoeMaxExperts * sizeof(float));
+  for (int i = threadIdx.x; i < logits; i += kThreads) {
+    if (i >= kThreads)
+#pragma unroll
+      for (int r = 0; r < kRouteParts; ++r)
+        if (r < p.cl) part[r] = ld_pinned_f(p.part + (size_t)r * logits + i);
+    float f = part[0];
+#pragma unroll
+    for (int r = 1; r < kRouteParts; ++r)
+      if (r < p.cl) f += part[r];
+    s_logit[i] = f;
+  }
+  if (threadIdx.x < kFewEntries * NT) s_map[threadIdx.x / NT][threadIdx.x % NT] = -1;
+  __syncthreads();
+  if (warp < live) {                                           // a warp a token (live is at most 8)
+    MoeChoice c;
+    if (p.E <= 64) {
+      const float l[2] = {s_logit[min(warp * p.E + lane, logits - 1)], s_logit[min(warp * p.E + lane + 32, logits - 1)]};
+      c = choose_experts(l, p.E, p.k, p.renorm, lane);
+    } else {
+      float l[kMoeMaxExperts / 32];
+#pragma unroll
+      for (int i = 0; i < kMoeMaxExperts / 32; ++i) l[i] = s_logit[min(warp * p.E + lane + 32 * i, logits - 1)];
+      c = choose_experts(l, p.E, p.k, p.renorm, lane);
+    }
+    if (lane < p.k) {
+      s_ids[warp * p.k + c.place] = c.expert;
+      s_prob[warp * p.k + c.place] = c.p;
+      const size_t at = (size_t)warp * p.k + c.place;
+      if (blockIdx.x == 0 && p.ids_out) p.ids_out[at] = c.expert;
+      if (blockIdx.x == 0 && p.prob_out) p.prob_out[at] = c.p;
+    }
+  }
+  // x, and behind it the next barrier: a thread's first pieces are here by now
+  for (int i = threadIdx.x; i < p.T * chunks; i += kThreads) {
+    if (i >= kThreads) {
+      const uint8_t* at = x_at(i);
+      v = at ? ld_pinned16(at) : make_uint4(0, 0, 0, 0);
+    }
+    *reinterpret_cast<uint4*>(s_rows + (size_t)(i / chunks) * xs + i % chunks * 16) = v;
   }
   if constexpr (kFp8)
-    for (int i = threadIdx.x; i < p.T * p.KB1; i += kThreads)
-      s_xs[i] = i < kThreads ? sv : p.xs[(size_t)(i % p.KB1) * p.T + i / p.KB1];
+    for (int i = threadIdx.x; i < p.T * p.KB1; i += kThreads) s_xs[i] = i < kThreads ? sv : *xs_at(i);
+  __syncthreads();
+  if (warp == 0) {                                             // entries by expert, then by token; lane: an entry
+    const int n = live * p.k;
+    const int e = lane < n ? s_ids[lane] : 0x7fffffff, t = lane < n ? lane / p.k : 0;
+    int pos = 0, active = 0;
+    bool one = lane < n;                                       // the first of its expert
+    for (int j = 0; j < n; ++j) {
+      const int ej = __shfl_sync(0xffffffffu, e, j);
+      pos += ej < e || (ej == e && j < lane);                  // (lanes are in the order of their tokens)
+      if (ej == e && j < lane) one = false;
+    }
+    const uint32_t ones = __ballot_sync(0xffffffffu, one);
+    for (int j = 0; j < n; ++j) active += (ones >> j & 1u) && __shfl_sync(0xffffffffu, e, j) < e;
+    if (lane < n) {
+      s_exp[active] = e;                                       // (the same from all of its entries)
+      s_map[active][t] = (int16_t)pos;
+      s_p[active][t] = s_prob[lane];
+    }
+    if (lane == 0) s_active = __popc(ones);
+  }
+  __syncthreads();
+  const int na = s_active;
   const int per = p.I / 8, gates = na * per, total = gates + (na ? (p.H + 15) / 16 : 0);
   const int nst1 = stages_of(p.KB1), nst2 = stages_of(p.KB2), c1 = blocks_of(p.KB1), c2 = blocks_of(p.KB2);
   const uint32_t stBytes = 16u * 128u * (uint32_t)max(c1, c2);
@@ -136,7 +178,6 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
       phase ^= 1;
     }
   };
-  __syncthreads();
 
   if (warp < kGroups) {
     // ---- producer ---------------------------------------------------------------------

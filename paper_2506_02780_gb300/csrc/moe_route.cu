@@ -10,6 +10,7 @@
 // distributed shared memory, in a fixed order.  The last CTA to finish groups the tokens: a bit for
 // each expert and token, so that an entry's place is a count of bits and does not depend on who comes first.
 // Up to 16 tokens are one cluster's: its first CTA then chooses and groups without a way through global memory.
+// Of up to 8 entries (moe_few.cu) only the CTAs' sums are made here.
 // CTAs of their own quantise x.
 // 8 us for one token, 12 for 64, 18 for 2,048 behind a layer whose weights went through L2 (5 on warm data): loads and
 // instructions come from HBM, and its CTAs can only start when one of the layer in front leaves its SM.
@@ -38,12 +39,6 @@ __device__ __forceinline__ float ld_cluster_f(uint32_t a) {
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
   return v;
 }
-// larger key, better logit; at least 1: a NaN is the worst
-__device__ __forceinline__ uint32_t logit_key(float f) {
-  const uint32_t u = __float_as_uint(f);
-  return f != f ? 1u : (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-
 // NT: groups of 8 experts (E <= 8 NT)
 template <int NT>
 __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const RouteParams p, const int keep) {
@@ -53,7 +48,6 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
   __shared__ int s_ids[kTok * kMoeMaxTopK];        // of a single cluster's tokens
   __shared__ float s_prob[kTok * kMoeMaxTopK];
   __shared__ uint32_t s_bits[kMoeMaxExperts];      // ... a bit for each expert and token
-  __shared__ int s_tile[kMoeMaxExperts];           // an expert's first tile
   __shared__ uint32_t s_scan[kWarps];
   pdl_allow_next();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -137,6 +131,14 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
 #pragma unroll
       for (int w = 1; w < kWarps; ++w) s += s_red[w * kTok * EP + i];
       s_red[i] = s;
+      if (p.part && i / EP < live && i % EP < p.E) p.part[((size_t)rank * p.T + i / EP) * p.E + i % EP] = s;
+    }
+    if (p.part) {                                  // moe_few.cu's CTAs choose themselves
+      if (blockIdx.x == 0 && threadIdx.x == 0) {
+        p.ctl->queue = 0;
+        p.ctl->down_done = 0;
+      }
+      return;
     }
     if (p.cl > 1) cluster_sync();
     else __syncthreads();
@@ -145,12 +147,10 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
     for (int row = alone ? (rank == 0 ? warp : kTok) : rank + p.cl * warp; row < kTok && t0 + row < live; row += step) {
       constexpr int kPer = (EP + 31) / 32;
       float l[kPer];
-      uint32_t key[kPer];
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const int e = lane + 32 * i;
         l[i] = 0.f;
-        key[i] = 0;
         if (e < p.E) {
           const uint32_t at = smem_u32(s_red + row * EP + e);
           float part[8];
@@ -161,61 +161,21 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
 #pragma unroll
           for (int r = 1; r < 8; ++r)
             if (r < p.cl) l[i] += part[r];
-          key[i] = logit_key(l[i]);
         }
       }
-      int my_e = 0x7fffffff;                       // lane j: the j-th choice and its logit
-      float my_l = 0.f, top = 0.f;
-      for (int j = 0; j < p.k; ++j) {
-        uint32_t best = 0;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) best = max(best, key[i]);
-        const uint32_t all = __reduce_max_sync(0xffffffffu, best);
-        uint32_t e = 0xffffffffu;
-#pragma unroll
-        for (int i = kPer - 1; i >= 0; --i)
-          if (key[i] == all) e = lane + 32 * i;
-        e = __reduce_min_sync(0xffffffffu, e);     // of equal logits the lowest expert
-        float le = 0.f;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-          if (e == (uint32_t)(lane + 32 * i)) {
-            le = l[i];
-            key[i] = 0;
-          }
-        le = __shfl_sync(0xffffffffu, le, e & 31);
-        if (j == 0) top = le;
-        if (lane == j) {
-          my_e = (int)e;
-          my_l = le;
-        }
-      }
-      float sum = 0.f;
-      const float pe = lane < p.k ? expf(my_l - top) : 0.f;
-      if (p.renorm) {
-        sum = pe;
-      } else {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-          if (lane + 32 * i < p.E) sum += expf(l[i] - top);
-      }
-#pragma unroll
-      for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-      int before = 0;
-      for (int j = 0; j < p.k; ++j) before += __shfl_sync(0xffffffffu, my_e, j) < my_e;
+      const MoeChoice ch = choose_experts(l, p.E, p.k, p.renorm, lane);
       if (lane < p.k) {
-        const size_t at = (size_t)(t0 + row) * p.k + before;
-        const float pr = __fdiv_rn(pe, sum);
+        const size_t at = (size_t)(t0 + row) * p.k + ch.place;
         if (alone) {
-          atomicOr(&s_bits[my_e], 1u << row);
-          s_ids[at] = my_e;
-          s_prob[at] = pr;
+          atomicOr(&s_bits[ch.expert], 1u << row);
+          s_ids[at] = ch.expert;
+          s_prob[at] = ch.p;
         } else {
-          p.ids[at] = my_e;
-          p.prob[at] = pr;
+          p.ids[at] = ch.expert;
+          p.prob[at] = ch.p;
         }
-        if (p.ids_out) p.ids_out[at] = my_e;
-        if (p.prob_out) p.prob_out[at] = pr;
+        if (p.ids_out) p.ids_out[at] = ch.expert;
+        if (p.prob_out) p.prob_out[at] = ch.p;
       }
     }
     // nobody leaves while a peer reads its sums; who groups a single cluster's tokens waits at its end
@@ -292,10 +252,6 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
     m.tiles = tiles;
     m.pad[0] = m.pad[1] = m.pad[2] = 0;
     s_off[threadIdx.x] = m.entry0;
-    s_tile[threadIdx.x] = m.first;
-    if (p.few && tiles)                            // (the entries' own are written behind the next barrier)
-      for (int t = 0; t < kFewTokens; ++t)
-        if (!(mask[threadIdx.x] >> t & 1u)) p.few[m.first * kFewTokens + t] = FewEntry{-1, 0.f};
     for (int i = 0; i < tiles; ++i) p.tile[m.first + i] = m;
     if ((int)threadIdx.x == p.E - 1) p.ctl->tiles = incl >> 20;
   }
@@ -306,7 +262,6 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
     p.list[pos] = t;
     p.inv[i] = pos;
     if (alone) p.prob[i] = s_prob[i];
-    if (p.few) p.few[s_tile[e] * kFewTokens + t] = FewEntry{pos, s_prob[i]};
   }
   if (alone && p.cl > 1 && live > 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -335,7 +290,7 @@ ee_status launch(const RouteParams& p, cudaStream_t stream) {
   const int routers = (p.T + kTok - 1) / kTok * p.cl, per = kWarps * kQuantUnits;
   const int quants = p.xq ? (p.T * ((p.H + kBlk - 1) / kBlk) + per - 1) / per : 0;
   const unsigned grid = (unsigned)(routers + (quants + p.cl - 1) / p.cl * p.cl);
-  EE_CUDA_OK(launch_pdl(moe_route_kernel<NT>, dim3(grid), dim3(32 * kWarps), smem, stream, (unsigned)p.cl, p, keep));
+  EE_CUDA_OK(launch_pdl(moe_route_kernel<NT>, dim3(grid), dim3(32 * kWarps), smem, stream, p.part ? 1u : (unsigned)p.cl, p, keep));
   return EE_OK;
 }
 
