@@ -10,7 +10,7 @@
 // distributed shared memory, in a fixed order.  The last CTA to finish groups the tokens: a bit for
 // each expert and token, so that an entry's place is a count of bits and does not depend on who comes first.
 // Up to 16 tokens are one cluster's: its first CTA then chooses and groups without a way through global memory.
-// Of up to 8 entries (moe_few.cu) only the CTAs' sums are made here.
+// Of up to 8 entries (moe_few.cu) only the CTAs' sums are made here, of 8 experts each.
 // CTAs of their own quantise x.
 // 8 us for one token, 12 for 64, 18 for 2,048 behind a layer whose weights went through L2 (5 on warm data): loads and
 // instructions come from HBM, and its CTAs can only start when one of the layer in front leaves its SM.
@@ -39,7 +39,7 @@ __device__ __forceinline__ float ld_cluster_f(uint32_t a) {
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
   return v;
 }
-// NT: groups of 8 experts (E <= 8 NT)
+// NT: groups of 8 experts (E <= 8 NT; where only the sums are made, a CTA takes 8 of any number)
 template <int NT>
 __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const RouteParams p, const int keep) {
   constexpr int EP = 8 * NT, kWarps = warps_of(NT), kThreads = 32 * kWarps;
@@ -51,15 +51,16 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
   __shared__ uint32_t s_scan[kWarps];
   pdl_allow_next();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = (int)blockIdx.x % p.cl, t0 = (int)blockIdx.x / p.cl * kTok;
-  const int groups = (p.T + kTok - 1) / kTok, routers = groups * p.cl;
+  const int rank = (int)blockIdx.x % p.cl, t0 = p.part ? 0 : (int)blockIdx.x / p.cl * kTok;
+  const int e0 = p.part ? (int)blockIdx.x / p.cl * EP : 0;     // the CTA's first expert
+  const int groups = (p.T + kTok - 1) / kTok, routers = (p.part ? (p.E + EP - 1) / EP : groups) * p.cl;
   const bool alone = groups == 1;
   if (alone)
     for (int i = threadIdx.x; i < kMoeMaxExperts; i += kThreads) s_bits[i] = 0;
   if ((int)blockIdx.x < routers && t0 == 0) {      // this CTA's columns of the router, while the kernel in front still runs
     const int blocks = (p.H + kBlk - 1) / kBlk, c0 = blocks * rank / p.cl * kBlk, c1 = min(p.H, blocks * (rank + 1) / p.cl * kBlk);
     if (c0 < c1)
-      for (int e = threadIdx.x; e < p.E; e += kThreads) prefetch_l2(p.router + (size_t)e * p.H + c0, (uint32_t)(c1 - c0) * 2);
+      for (int e = e0 + (int)threadIdx.x; e < min(p.E, e0 + EP); e += kThreads) prefetch_l2(p.router + (size_t)e * p.H + c0, (uint32_t)(c1 - c0) * 2);
   }
   pdl_wait();
   const int live = p.live ? max(0, min(p.T, ld_pinned(p.live))) : p.T;
@@ -108,7 +109,7 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
         uint4 w[kStep];
 #pragma unroll
         for (int n = 0; n < kStep; ++n) {
-          const int e = (n0 + n) * 8 + g;
+          const int e = e0 + (n0 + n) * 8 + g;
           w[n] = zero;
           if (in && e < p.E) w[n] = ld_pinned16(p.router + (size_t)e * p.H + col);
         }
@@ -131,7 +132,7 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
 #pragma unroll
       for (int w = 1; w < kWarps; ++w) s += s_red[w * kTok * EP + i];
       s_red[i] = s;
-      if (p.part && i / EP < live && i % EP < p.E) p.part[((size_t)rank * p.T + i / EP) * p.E + i % EP] = s;
+      if (p.part && i / EP < live && e0 + i % EP < p.E) p.part[((size_t)rank * p.T + i / EP) * p.E + e0 + i % EP] = s;
     }
     if (p.part) {                                  // moe_few.cu's CTAs choose themselves
       if (blockIdx.x == 0 && threadIdx.x == 0) {
@@ -287,7 +288,7 @@ ee_status launch(const RouteParams& p, cudaStream_t stream) {
       have[dev] = smem;
     }
   }
-  const int routers = (p.T + kTok - 1) / kTok * p.cl, per = kWarps * kQuantUnits;
+  const int routers = (p.part ? (p.E + 8 * NT - 1) / (8 * NT) : (p.T + kTok - 1) / kTok) * p.cl, per = kWarps * kQuantUnits;
   const int quants = p.xq ? (p.T * ((p.H + kBlk - 1) / kBlk) + per - 1) / per : 0;
   const unsigned grid = (unsigned)(routers + (quants + p.cl - 1) / p.cl * p.cl);
   EE_CUDA_OK(launch_pdl(moe_route_kernel<NT>, dim3(grid), dim3(32 * kWarps), smem, stream, p.part ? 1u : (unsigned)p.cl, p, keep));
@@ -298,7 +299,8 @@ ee_status launch(const RouteParams& p, cudaStream_t stream) {
 
 namespace ee {
 ee_status launch_moe_route(const RouteParams& p, cudaStream_t stream) {
-  if (p.E <= 8) return launch<1>(p, stream);
+  // (little code: with all of 64 experts in a CTA the first instructions' way from memory takes 3 of 4 us)
+  if (p.E <= 8 || p.part) return launch<1>(p, stream);
   if (p.E <= 64) return launch<8>(p, stream);
   if (p.E <= 128) return launch<16>(p, stream);
   return launch<32>(p, stream);
