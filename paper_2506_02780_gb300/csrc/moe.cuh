@@ -22,6 +22,7 @@ struct MoeCtl {
   uint32_t down_done;        // down tasks that stored their part of y (few tokens: gate tasks, of h)
   uint32_t tiles;            // token tiles
   uint32_t pad[4];
+  uint32_t group_ticket[kMoeMaxTokens / 16];   // per 16 tokens; zero between calls
   uint32_t gate_done[1];     // per token tile: gate tasks that stored their part of h
 };
 struct __align__(32) MoeTile {   // a token tile's expert
@@ -30,7 +31,7 @@ struct __align__(32) MoeTile {   // a token tile's expert
   int pad[3];
 };
 constexpr int kFewEntries = 8, kFewTokens = 8;   // what moe_few.cu takes
-constexpr int kRouteParts = 8;   // CTAs that share the hidden dimension, at most
+constexpr int kRouteParts = 8, kRouteCtas = 2 * kNumSMs;   // CTAs that share the hidden dimension, at most; so many in all
 
 struct MoeLayout {
   size_t ctl, tile, part, ids, prob, list, inv, xq, xs, h, hf, hs, y, total;
@@ -48,7 +49,7 @@ inline MoeLayout moe_layout(int64_t T, int64_t H, int64_t I, int64_t E, int64_t 
   };
   l.ctl = take(sizeof(MoeCtl) + 4 * (size_t)l.max_tiles);
   l.tile = take(sizeof(MoeTile) * (size_t)l.max_tiles);
-  l.part = take(4 * (size_t)(kRouteParts * kFewTokens * E));
+  l.part = take(4 * (size_t)(std::min<int64_t>(kRouteParts * T, 16 * kRouteCtas) * E));
   l.ids = take(4 * (size_t)n);
   l.prob = take(4 * (size_t)n);
   l.list = take(4 * (size_t)n);
@@ -71,7 +72,8 @@ struct RouteParams {
   int T, H, E, k, renorm, cl, max_tiles, tile_rows;
   MoeCtl* ctl;
   MoeTile* tile;
-  float* part;               // [cl][T][E] sums over a CTA's columns for moe_few.cu, which chooses itself; or NULL
+  float* part;               // [cl][T][E] sums over a CTA's columns
+  int few;                   // moe_few.cu chooses itself
   int32_t* ids;              // [T][k] experts of a token, ascending
   float* prob;               // [T][k]
   int32_t* list;             // [T k] token of an entry
@@ -81,21 +83,24 @@ struct RouteParams {
   int32_t* ids_out;          // the caller's copies, or NULL
   float* prob_out;
 };
-ee_status launch_moe_route(const RouteParams& p, cudaStream_t stream);
+ee_status launch_moe_route(RouteParams& p, cudaStream_t stream);   // sets cl
 
 // larger key, better logit; at least 1: a NaN is the worst
 __device__ __forceinline__ uint32_t logit_key(float f) {
   const uint32_t u = __float_as_uint(f);
   return f != f ? 1u : (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
-// A warp chooses one token's k experts; lane + 32 i holds expert lane + 32 i's logit.  Lane j < k: an expert, its weight
+// A warp chooses one token's k experts; lane holds those of number lane + 32 i.  Lane j < k: an expert, its weight
 // and its place among the chosen ones in ascending order.
 struct MoeChoice {
   int expert, place;
   float p;
 };
-template <int kPer>
-__device__ __forceinline__ MoeChoice choose_experts(const float (&l)[kPer], int E, int k, bool renorm, int lane) {
+template <int kPer, class Logit>
+__device__ __forceinline__ MoeChoice choose_of(const Logit& logit, int E, int k, bool renorm, int lane) {
+  float l[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) l[i] = lane + 32 * i < E ? logit(lane + 32 * i) : 0.f;
   uint32_t key[kPer];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) key[i] = lane + 32 * i < E ? logit_key(l[i]) : 0u;
@@ -142,6 +147,10 @@ __device__ __forceinline__ MoeChoice choose_experts(const float (&l)[kPer], int 
   c.p = __fdiv_rn(pe, sum);
   return c;
 }
+__device__ __forceinline__ MoeChoice choose_experts(const float* logits, int E, int k, bool renorm, int lane) {
+  const auto logit = [logits](int e) { return logits[e]; };
+  return E <= 64 ? choose_of<2>(logit, E, k, renorm, lane) : choose_of<kMoeMaxExperts / 32>(logit, E, k, renorm, lane);
+}
 
 struct MoeParams {
   int T, H, I, E, k, n;                // n = T k
@@ -155,7 +164,7 @@ struct MoeParams {
   int64_t x_stride;
   MoeCtl* ctl;
   const MoeTile* tile;
-  const float* part;                   // few entries: [cl][T][E] parts of the logits
+  const float* part;                   // [cl][T][E] parts of the logits
   int cl, renorm;
   int32_t* ids_out;
   float* prob_out;

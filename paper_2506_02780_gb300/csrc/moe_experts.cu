@@ -840,7 +840,8 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   r.tile = reinterpret_cast<ee::MoeTile*>(base + l.tile);
   size_t few_smem = 0;
   const bool few = ee::moe_few_stages(T, H, I, k, fp8, &few_smem) > 0;
-  r.part = few ? reinterpret_cast<float*>(base + l.part) : nullptr;
+  r.part = reinterpret_cast<float*>(base + l.part);
+  r.few = few;
   r.ids = reinterpret_cast<int32_t*>(base + l.ids);
   r.prob = reinterpret_cast<float*>(base + l.prob);
   r.list = reinterpret_cast<int32_t*>(base + l.list);
@@ -849,10 +850,6 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   r.xs = reinterpret_cast<float*>(base + l.xs);
   r.ids_out = ids_or_null;
   r.prob_out = probs_or_null;
-  // the widest share of the hidden dimension that the SMs hold at once
-  const int groups = (T + 15) / 16, blocks = (H + kBlk - 1) / kBlk;
-  r.cl = ee::kRouteParts;
-  while (r.cl > 1 && (groups * r.cl > ee::kNumSMs || r.cl > blocks)) r.cl /= 2;
   MoeParams p;
   p.T = T;
   p.H = H;
@@ -864,7 +861,7 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   p.KB2 = (I * (fp8 ? 1 : 2) + 127) / 128;
   p.IB = (I + kBlk - 1) / kBlk;
   p.HT = (H + 2 * kTile - 1) / (2 * kTile);
-  p.HB = blocks;
+  p.HB = (H + kBlk - 1) / kBlk;
   const int nt = ee::moe_tile_rows(T, E, k, fp8);
   p.b_rows = std::min(nt, (T + 15) / 16 * 16);
   p.w1 = w1;
@@ -874,7 +871,6 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   p.ctl = r.ctl;
   p.tile = r.tile;
   p.part = r.part;
-  p.cl = r.cl;
   p.renorm = r.renorm;
   p.ids_out = ids_or_null;
   p.prob_out = probs_or_null;
@@ -895,6 +891,7 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
   p.err = ee::err_word(ws);
   const ee_status st = ee::launch_moe_route(r, (cudaStream_t)stream);
   if (st != EE_OK) return st;
+  p.cl = r.cl;
   const cudaStream_t s = (cudaStream_t)stream;
   if (few) return ee::launch_moe_few(p, fp8, s);
   if (fp8) return nt == 32 ? launch<true, 32>(p, s) : nt == 64 ? launch<true, 64>(p, s) : launch<true, 128>(p, s);

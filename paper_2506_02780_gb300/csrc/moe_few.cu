@@ -113,16 +113,7 @@ moe_few_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_constant__
   if (threadIdx.x < kFewEntries * NT) s_map[threadIdx.x / NT][threadIdx.x % NT] = -1;
   __syncthreads();
   if (warp < live) {                                           // a warp a token (live is at most 8)
-    MoeChoice c;
-    if (p.E <= 64) {
-      const float l[2] = {s_logit[min(warp * p.E + lane, logits - 1)], s_logit[min(warp * p.E + lane + 32, logits - 1)]};
-      c = choose_experts(l, p.E, p.k, p.renorm, lane);
-    } else {
-      float l[kMoeMaxExperts / 32];
-#pragma unroll
-      for (int i = 0; i < kMoeMaxExperts / 32; ++i) l[i] = s_logit[min(warp * p.E + lane + 32 * i, logits - 1)];
-      c = choose_experts(l, p.E, p.k, p.renorm, lane);
-    }
+    const MoeChoice c = choose_experts(s_logit + warp * p.E, p.E, p.k, p.renorm, lane);
     if (lane < p.k) {
       s_ids[warp * p.k + c.place] = c.expert;
       s_prob[warp * p.k + c.place] = c.p;

@@ -1,19 +1,16 @@
 // First kernel of ee_moe_layer: the router's product, each token's experts and their
 // probabilities, x as e4m3 codes (for 8-bit weights), and the tokens grouped by expert.
 //
-// A cluster of up to 8 CTAs takes 16 tokens and shares the hidden dimension: an m16n8k16 MMA
+// A CTA takes 16 tokens, 8 or 64 experts and up to an eighth of the hidden dimension: an m16n8k16 MMA
 // of bf16 a warp and 16 columns, operands straight from global memory (a lane takes 8
 // neighbouring columns of its row of x and of the router; the order of the columns within
 // a sum is free, so x's and the router's fragments need only agree).  2 T E H operations are too few for
-// the tensor memory's set-up; what bounds the kernel is the chain of waits for memory, so every warp's loads are
-// under way at once and the router's rows are read by many SMs.  Warps' sums are added in shared memory, CTAs' in
-// distributed shared memory, in a fixed order.  The last CTA to finish groups the tokens: a bit for
-// each expert and token, so that an entry's place is a count of bits and does not depend on who comes first.
-// Up to 16 tokens are one cluster's: its first CTA then chooses and groups without a way through global memory.
-// Of up to 8 entries (moe_few.cu) only the CTAs' sums are made here, of 8 experts each.
-// CTAs of their own quantise x.
-// 8 us for one token, 12 for 64, 18 for 2,048 behind a layer whose weights went through L2 (5 on warm data): loads and
-// instructions come from HBM, and its CTAs can only start when one of the layer in front leaves its SM.
+// the tensor memory's set-up; what bounds the kernel is the chain of waits for memory, of its instructions, too, which
+// weights of the layer in front have driven out: the loop over 64 experts alone takes 3 to 4 us then, over 8 1, so there are
+// CTAs for every 8 experts as long as the SMs hold them at once.  Warps' sums are added in shared memory, CTAs' through a
+// cluster's, or by the last of a token group's CTAs through global memory, always in the same order; then the experts are chosen.  The last
+// CTA to finish groups the tokens: a bit for each expert and token, so that an entry's place is a count of bits and does not depend on who comes first.
+// Of up to 8 entries only the CTAs' sums are made here (moe_few.cu).  CTAs of their own quantise x.
 #include <mutex>
 
 #include "moe.cuh"
@@ -22,10 +19,13 @@ namespace {
 
 using namespace ee;
 
-constexpr int kTok = 16, kQuantUnits = 4;
-// more warps where their sums fit in shared memory
-__host__ __device__ constexpr int warps_of(int NT) { return NT <= 16 ? 16 : 8; }
+constexpr int kTok = 16, kQuantUnits = 4, kWarps = 16, kThreads = 32 * kWarps;
 
+__device__ __forceinline__ float ld_cluster_f(uint32_t a) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                           uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -34,39 +34,40 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float ld_cluster_f(uint32_t a) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
-  return v;
-}
-// NT: groups of 8 experts (E <= 8 NT; where only the sums are made, a CTA takes 8 of any number)
-template <int NT>
-__global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const RouteParams p, const int keep) {
-  constexpr int EP = 8 * NT, kWarps = warps_of(NT), kThreads = 32 * kWarps;
-  extern __shared__ float s_red[];                 // [kWarps][kTok][EP], the first becomes the CTA's sums
+// NT: groups of 8 experts of a CTA; kCluster: a token group's CTAs are a cluster
+template <int NT, bool kCluster>
+__global__ void __launch_bounds__(kThreads) moe_route_kernel(const RouteParams p, const int keep) {
+  constexpr int EP = 8 * NT;
+  extern __shared__ float s_red[];                 // [kWarps][kTok][EP]; the logits [kTok][E]
   __shared__ int s_last;
-  __shared__ int s_ids[kTok * kMoeMaxTopK];        // of a single cluster's tokens
+  __shared__ int s_ids[kTok * kMoeMaxTopK];        // of a single group's tokens
   __shared__ float s_prob[kTok * kMoeMaxTopK];
   __shared__ uint32_t s_bits[kMoeMaxExperts];      // ... a bit for each expert and token
   __shared__ uint32_t s_scan[kWarps];
   pdl_allow_next();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = (int)blockIdx.x % p.cl, t0 = p.part ? 0 : (int)blockIdx.x / p.cl * kTok;
-  const int e0 = p.part ? (int)blockIdx.x / p.cl * EP : 0;     // the CTA's first expert
-  const int groups = (p.T + kTok - 1) / kTok, routers = (p.part ? (p.E + EP - 1) / EP : groups) * p.cl;
+  // the grid is CTAs that share the columns x those that share the experts x token groups, then those that quantise
+  // (a division costs more than it looks where its instructions come from memory)
+  const int groups = (p.T + kTok - 1) / kTok, parts = (int)(gridDim.x * gridDim.y);
+  const int rank = (int)blockIdx.x, e0 = (int)blockIdx.y * EP, group = (int)blockIdx.z, t0 = group * kTok;
+  const bool first = rank == 0 && e0 == 0;
   const bool alone = groups == 1;
   if (alone)
     for (int i = threadIdx.x; i < kMoeMaxExperts; i += kThreads) s_bits[i] = 0;
-  if ((int)blockIdx.x < routers && t0 == 0) {      // this CTA's columns of the router, while the kernel in front still runs
+  if (t0 == 0) {      // this CTA's columns of the router, while the kernel in front still runs
     const int blocks = (p.H + kBlk - 1) / kBlk, c0 = blocks * rank / p.cl * kBlk, c1 = min(p.H, blocks * (rank + 1) / p.cl * kBlk);
     if (c0 < c1)
       for (int e = e0 + (int)threadIdx.x; e < min(p.E, e0 + EP); e += kThreads) prefetch_l2(p.router + (size_t)e * p.H + c0, (uint32_t)(c1 - c0) * 2);
   }
   pdl_wait();
   const int live = p.live ? max(0, min(p.T, ld_pinned(p.live))) : p.T;
-  if ((int)blockIdx.x >= routers) {                // x as codes: a warp and a block of one token, four at once
+  if (first && group == 0 && threadIdx.x == 0) {
+    p.ctl->queue = 0;
+    p.ctl->down_done = 0;
+  }
+  if (group >= groups) {                // x as codes: a warp and a block of one token, four at once
     const int blocks = (p.H + kBlk - 1) / kBlk, units = live * blocks;
-    const int u0 = (((int)blockIdx.x - routers) * kWarps + warp) * kQuantUnits;
+    const int u0 = ((((group - groups) * (int)gridDim.y + (int)blockIdx.y) * p.cl + rank) * kWarps + warp) * kQuantUnits;
     uint2 v[kQuantUnits];
 #pragma unroll
     for (int j = 0; j < kQuantUnits; ++j) {
@@ -87,9 +88,9 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
                       to_code(bf16_hi(v[j].y), s));
       if (lane == 0) p.xs[(size_t)b * p.T + t] = s.scale;
     }
-    return;                                        // (all CTAs of a cluster)
+    return;
   }
-  if (t0 < live) {                                 // (the same in the whole cluster)
+  if (t0 < live) {
     const int nb = (p.H + kBlk - 1) / kBlk;
     const int b0 = nb * rank / p.cl, b1 = nb * (rank + 1) / p.cl;
     const int g = lane >> 2, tq = lane & 3;
@@ -131,40 +132,53 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
       float s = s_red[i];
 #pragma unroll
       for (int w = 1; w < kWarps; ++w) s += s_red[w * kTok * EP + i];
-      s_red[i] = s;
-      if (p.part && i / EP < live && e0 + i % EP < p.E) p.part[((size_t)rank * p.T + i / EP) * p.E + e0 + i % EP] = s;
+      const int row = i / EP, e = e0 + i % EP;
+      if (kCluster) s_red[i] = s;
+      else if (t0 + row < live && e < p.E) p.part[((size_t)rank * p.T + t0 + row) * p.E + e] = s;
     }
-    if (p.part) {                                  // moe_few.cu's CTAs choose themselves
-      if (blockIdx.x == 0 && threadIdx.x == 0) {
-        p.ctl->queue = 0;
-        p.ctl->down_done = 0;
+    if (!kCluster && p.few) return;
+    const int rows = min(kTok, live - t0);
+    int row = warp;                                // a warp chooses a token's experts
+    if constexpr (kCluster) {
+      if (p.cl > 1) cluster_sync();
+      else __syncthreads();
+      // the cluster's CTAs take the tokens in turn, a single group's first CTA all of them
+      row = !alone ? rank + p.cl * warp : rank == 0 ? warp : kTok;
+    } else {                                       // the last of the group's CTAs all of them
+      __syncthreads();
+      if (threadIdx.x == 0) s_last = atom_add_acq_rel(&p.ctl->group_ticket[group], 1u) == (uint32_t)parts - 1;
+      __syncthreads();
+      if (!s_last) return;
+      if (threadIdx.x == 0) p.ctl->group_ticket[group] = 0;
+      for (int i = threadIdx.x; i < rows * p.E; i += kThreads) {
+        float part[kRouteParts];
+#pragma unroll
+        for (int r = 0; r < kRouteParts; ++r)
+          if (r < p.cl) part[r] = __ldcg(p.part + ((size_t)r * p.T + t0) * p.E + i);
+        float f = part[0];
+#pragma unroll
+        for (int r = 1; r < kRouteParts; ++r)
+          if (r < p.cl) f += part[r];
+        s_red[i] = f;
       }
-      return;
+      __syncthreads();
     }
-    if (p.cl > 1) cluster_sync();
-    else __syncthreads();
-    // the CTAs of the cluster take the tokens in turn, a warp each (a single cluster's first CTA all of them)
-    const int step = alone ? kWarps : p.cl * kWarps;
-    for (int row = alone ? (rank == 0 ? warp : kTok) : rank + p.cl * warp; row < kTok && t0 + row < live; row += step) {
-      constexpr int kPer = (EP + 31) / 32;
-      float l[kPer];
+    if (row < rows) {
+      const auto sum_of = [&](int e) {
+        const uint32_t at = smem_u32(s_red + row * EP + e);
+        float part[kRouteParts];
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int e = lane + 32 * i;
-        l[i] = 0.f;
-        if (e < p.E) {
-          const uint32_t at = smem_u32(s_red + row * EP + e);
-          float part[8];
+        for (int r = 0; r < kRouteParts; ++r)
+          if (r < p.cl) part[r] = p.cl > 1 ? ld_cluster_f(map_cluster(at, r)) : s_red[row * EP + e];
+        float f = part[0];
 #pragma unroll
-          for (int r = 0; r < 8; ++r)
-            if (r < p.cl) part[r] = p.cl > 1 ? ld_cluster_f(map_cluster(at, r)) : s_red[row * EP + e];
-          l[i] = part[0];
-#pragma unroll
-          for (int r = 1; r < 8; ++r)
-            if (r < p.cl) l[i] += part[r];
-        }
-      }
-      const MoeChoice ch = choose_experts(l, p.E, p.k, p.renorm, lane);
+        for (int r = 1; r < kRouteParts; ++r)
+          if (r < p.cl) f += part[r];
+        return f;
+      };
+      MoeChoice ch;
+      if constexpr (kCluster) ch = choose_of<(EP + 31) / 32>(sum_of, p.E, p.k, p.renorm, lane);
+      else ch = choose_experts(s_red + row * p.E, p.E, p.k, p.renorm, lane);
       if (lane < p.k) {
         const size_t at = (size_t)(t0 + row) * p.k + ch.place;
         if (alone) {
@@ -180,10 +194,12 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
       }
     }
     // nobody leaves while a peer reads its sums; who groups a single cluster's tokens waits at its end
-    if (p.cl > 1) {
+    if (kCluster && p.cl > 1) {
       asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
       if (!alone || rank != 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
+  } else if (!kCluster && (p.few || !first)) {
+    return;
   }
 
   // ---- the last CTA groups the tokens by expert --------------------------------------
@@ -194,19 +210,16 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
   uint8_t* s_e = reinterpret_cast<uint8_t*>(s_off + p.E);                 // [n] expert of a token's j-th place (where keep)
   __syncthreads();
   if (alone) {
-    if (rank != 0) return;
+    if (kCluster && rank != 0) return;
   } else {
-    if (threadIdx.x == 0) s_last = atom_add_acq_rel(&p.ctl->route_ticket, 1u) == (uint32_t)routers - 1;
+    if (threadIdx.x == 0)
+      s_last = atom_add_acq_rel(&p.ctl->route_ticket, 1u) == (uint32_t)(kCluster ? groups * p.cl : groups) - 1;
     for (int i = threadIdx.x; i < p.E * words; i += kThreads) mask[i] = 0;
     __syncthreads();
     if (!s_last) return;
   }
   for (int i = threadIdx.x; i < p.max_tiles; i += kThreads) p.ctl->gate_done[i] = 0;
-  if (threadIdx.x == 0) {
-    p.ctl->route_ticket = 0;
-    p.ctl->queue = 0;
-    p.ctl->down_done = 0;
-  }
+  if (threadIdx.x == 0) p.ctl->route_ticket = 0;
   constexpr int kAhead = 4;                        // entries of a thread whose loads are under way together
   for (int i0 = threadIdx.x; i0 < n && !alone; i0 += kThreads * kAhead) {
     int e[kAhead];
@@ -264,13 +277,12 @@ __global__ void __launch_bounds__(32 * warps_of(NT)) moe_route_kernel(const Rout
     p.inv[i] = pos;
     if (alone) p.prob[i] = s_prob[i];
   }
-  if (alone && p.cl > 1 && live > 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (kCluster && alone && p.cl > 1 && live > 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-template <int NT>
+template <int NT, bool kCluster>
 ee_status launch(const RouteParams& p, cudaStream_t stream) {
-  constexpr int kWarps = warps_of(NT);
-  const size_t sums = (size_t)kWarps * kTok * 8 * NT * 4;
+  const size_t sums = std::max((size_t)kWarps * kTok * 8 * NT * 4, (size_t)kTok * p.E * 4);
   const size_t words = ((size_t)p.T + 31) / 32;
   size_t group = p.E * words * 6 + 4 + 4 * (size_t)p.E;
   const int keep = group + (size_t)p.T * p.k <= 220 * 1024;   // (4,096 tokens at 16 of 256 experts do not fit)
@@ -284,25 +296,32 @@ ee_status launch(const RouteParams& p, cudaStream_t stream) {
     static size_t have[kMaxDevices] = {};
     std::lock_guard<std::mutex> lock(mu);
     if (have[dev] < smem) {
-      EE_CUDA_OK(cudaFuncSetAttribute(moe_route_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+      EE_CUDA_OK(cudaFuncSetAttribute(moe_route_kernel<NT, kCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
       have[dev] = smem;
     }
   }
-  const int routers = (p.part ? (p.E + 8 * NT - 1) / (8 * NT) : (p.T + kTok - 1) / kTok) * p.cl, per = kWarps * kQuantUnits;
-  const int quants = p.xq ? (p.T * ((p.H + kBlk - 1) / kBlk) + per - 1) / per : 0;
-  const unsigned grid = (unsigned)(routers + (quants + p.cl - 1) / p.cl * p.cl);
-  EE_CUDA_OK(launch_pdl(moe_route_kernel<NT>, dim3(grid), dim3(32 * kWarps), smem, stream, p.part ? 1u : (unsigned)p.cl, p, keep));
+  const int sets = (p.E + 8 * NT - 1) / (8 * NT), units = p.xq ? p.T * ((p.H + kBlk - 1) / kBlk) : 0;
+  const int per = p.cl * sets * kWarps * kQuantUnits;
+  const dim3 grid(p.cl, sets, (p.T + kTok - 1) / kTok + (units + per - 1) / per);
+  EE_CUDA_OK(launch_pdl(moe_route_kernel<NT, kCluster>, grid, dim3(kThreads), smem, stream, kCluster ? (unsigned)p.cl : 1u, p, keep));
   return EE_OK;
 }
 
 }  // namespace
 
 namespace ee {
-ee_status launch_moe_route(const RouteParams& p, cudaStream_t stream) {
-  // (little code: with all of 64 experts in a CTA the first instructions' way from memory takes 3 of 4 us)
-  if (p.E <= 8 || p.part) return launch<1>(p, stream);
-  if (p.E <= 64) return launch<8>(p, stream);
-  if (p.E <= 128) return launch<16>(p, stream);
-  return launch<32>(p, stream);
+ee_status launch_moe_route(RouteParams& p, cudaStream_t stream) {
+  const int groups = (p.T + kTok - 1) / kTok, blocks = (p.H + kBlk - 1) / kBlk;
+  // Few experts a CTA where that leaves the hidden dimension to four of them or more (4 tokens, 60 experts, whole layer 24.8 us and 26.2;
+  // 576 tokens, 64 experts 299 and 295).  One CTA for all experts: sums through the cluster (16 tokens, 8 experts 17.4 us, through global
+  // memory 18.7); more: through global memory (1,500 tokens, 160 experts 179 us; one CTA for all of them 236).
+  const bool narrow = groups * ((p.E + 7) / 8) * 4 <= kRouteCtas || p.E <= 8 || p.few;
+  const int sets = narrow ? (p.E + 7) / 8 : (p.E + 63) / 64, each = groups * sets;
+  const bool clustered = sets == 1 && !p.few;
+  // the widest share of the hidden dimension that the SMs hold at once (clusters: one CTA an SM, of two the layer took 310 us)
+  p.cl = kRouteParts;
+  while (p.cl > 1 && (each * p.cl > (clustered ? kNumSMs : kRouteCtas) || p.cl > blocks)) p.cl /= 2;
+  if (clustered) return narrow ? launch<1, true>(p, stream) : launch<8, true>(p, stream);
+  return narrow ? launch<1, false>(p, stream) : launch<8, false>(p, stream);
 }
 }  // namespace ee
