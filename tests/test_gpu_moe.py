@@ -172,6 +172,47 @@ def test_live_tokens(T, live, fp8):
     m.check(True, n)
 
 
+@pytest.mark.parametrize("T,n_exp,k,live", [(4, 24, 2, 0), (4, 24, 2, 1), (4, 24, 2, 3), (2, 130, 4, 1), (40, 24, 2, 0),
+                                            (40, 24, 2, 17), (40, 130, 3, 16), (200, 130, 2, 0), (200, 130, 2, 37),
+                                            (700, 130, 2, 513), (700, 24, 2, 1), (2500, 8, 2, 900)])
+def test_live_tokens_by_experts(T, n_exp, k, live):
+    """The same where several CTAs share a token's experts, and for few entries."""
+    m = Layer(T, 272, 80, n_exp, k, True, seed=live + 20)
+    m.x[live:] = float("nan")
+    m.run(True, torch.tensor([live], dtype=torch.int32, device=DEV))
+    assert E.ee_read_errors(m.ws) == 0
+    m.check(True, live)
+
+
+def test_one_workspace_for_all_sizes():
+    """Calls of any sizes after one another on one workspace: counts are left as the next call needs them."""
+    sizes = [(2500, 8, 2), (3, 24, 2), (64, 24, 4), (700, 24, 2), (1, 8, 8), (300, 130, 2), (16, 8, 2), (700, 130, 3)]
+    layers = [Layer(T, 272, 80, n, k, i % 2 == 0, seed=30 + i) for i, (T, n, k) in enumerate(sizes)]
+    ws = E.new_moe_workspace(2500, 272, 80, 130, 8)
+    for turn in range(3):
+        for m in layers:
+            m.ws = ws
+            m.clear()
+            m.run(True, torch.tensor([m.T if turn != 1 else m.T // 2], dtype=torch.int32, device=DEV))
+            m.check(True, m.T if turn != 1 else m.T // 2)
+    assert E.ee_read_errors(ws) == 0
+
+
+@pytest.mark.parametrize("T,n_exp", [(2, 12), (40, 12), (40, 200), (1000, 200)])
+def test_equal_logits_in_any_share(T, n_exp):
+    """Equal logits go to the lowest experts, a NaN logit is the last choice, wherever an expert's logit was summed."""
+    m = Layer(T, 256, 32, n_exp, 3, False, seed=40)
+    m.x.abs_()
+    best = [1, 6, n_exp - 5, n_exp - 2]
+    m.router[best] = m.router[1].abs() + 1.0
+    m.run(True)
+    assert (m.ids == torch.tensor(best[:3], dtype=torch.int32, device=DEV)).all()
+    m.router[6] = float("nan")
+    m.run(True)
+    assert (m.ids == torch.tensor([1, n_exp - 5, n_exp - 2], dtype=torch.int32, device=DEV)).all()
+    assert ((m.p - 1.0 / 3).abs() <= 2.0 ** -22).all()
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 def test_rows_of_wider_arrays(fp8):
     m = Layer(37, 400, 144, 8, 3, fp8, seed=3, wide=48)
