@@ -22,8 +22,8 @@
 // warp 3 tells other CTAs what the epilogue warps 4..11 have stored (a release waits for the stores: it would hold them up
 // for 2 us a task).
 //
-// Measured with the routing, 64 experts of 1280 x 3584, 6 a token: 64 tokens on 8-bit weights 137 us (845 MB; the
-// experts' part 122 us, 6.9 TB/s), on bf16 ones 255 us; 534 tokens 173 and 298 us.
+// Measured with the routing, 64 experts of 1280 x 3584, 6 a token: 64 tokens on 8-bit weights 133 to 137 us (845 MB; the
+// experts' part 122 us, 6.9 TB/s), on bf16 ones 247 to 255 us; 534 tokens 171 to 175 and 292 to 300 us.
 #include <mutex>
 
 #include "moe.cuh"
