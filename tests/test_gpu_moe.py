@@ -184,6 +184,16 @@ def test_live_tokens_by_experts(T, n_exp, k, live):
     m.check(True, live)
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T,H,I,n_exp,k", [(1, 64, 16384, 8, 8), (8, 16384, 64, 3, 1), (8, 32768, 64, 3, 1), (1, 64, 32768, 9, 8)])
+def test_few_entries_of_long_rows(T, H, I, n_exp, k, fp8):
+    """Few entries whose rows do, or do not, fit in shared memory beside the weights' rings."""
+    m = Layer(T, H, I, n_exp, k, fp8, seed=50)
+    m.run()
+    assert E.ee_read_errors(m.ws) == 0
+    m.check()
+
+
 def test_one_workspace_for_all_sizes():
     """Calls of any sizes after one another on one workspace: counts are left as the next call needs them."""
     sizes = [(2500, 8, 2), (3, 24, 2), (64, 24, 4), (700, 24, 2), (1, 8, 8), (300, 130, 2), (16, 8, 2), (700, 130, 3)]
