@@ -706,7 +706,8 @@ ee_status ee_chunk_attn(const ee_bf16* q, int64_t q_stride, const ee_bf16* k_cac
  *   x      bf16 [rows] of cols elements, x_stride elements apart (a multiple of 8,
  *          at least the row's elements); 16-byte aligned
  *   gated  0: x as it is; else a row holds 2 cols elements, gate then up, and what
- *          is quantised is silu(gate) * up in fp32, silu(g) = g / (1 + e^-g)
+ *          is quantised is silu(gate) * up in fp32, silu(g) = g / (1 + e^-g), to 2^-19 of
+ *          its value for any gate, also where e^-g has no fp32 number (0 below -174)
  *   q      uint8 [rows][cols], 16-byte aligned; scale fp32 [ceil(cols/128)][rows]
  * cols a multiple of 16.  No workspace; outputs must not overlap x.
  */
@@ -747,7 +748,7 @@ ee_status ee_fp8_linear(const uint8_t* x, const float* x_scale, const uint8_t* w
  *   choice   the k experts with the largest logits (of equal ones the lowest; a NaN
  *            counts as less than any number), in ascending order of their number
  *   weights  p = e^l / sum e^l, the sum over all experts, or with renorm != 0 over the k chosen ones
- *   expert e h = silu(x Wg[e]^T) * (x Wu[e]^T),  y_e = h Wd[e]^T
+ *   expert e h = silu(x Wg[e]^T) * (x Wu[e]^T), silu as in ee_fp8_quantize,  y_e = h Wd[e]^T
  *   out[t]   = bf16( sum_j p[t][j] y_{ids[t][j]} ), experts in ascending order, fp32
  * w1 [E][2 I][H] holds an expert's gate rows, then its up rows; w2 [E][H][I] is Wd.  Both are
  *   bf16 (scales NULL): h is rounded to bf16 between the products; or

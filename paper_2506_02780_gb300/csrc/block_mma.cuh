@@ -111,9 +111,52 @@ __device__ __forceinline__ uint32_t pack_e4m3(float x0, float x1, float x2, floa
       : "f"(x0), "f"(x1), "f"(x2), "f"(x3));
   return d;
 }
-// silu(g) u; the fast division's error is 2 units in the last place (its result for a divisor
-// above 2^126, g < -87.3, is 0, off by less than 1e-36 u)
-__device__ __forceinline__ float silu_times(float g, float u) { return __fdividef(g, 1.f + __expf(-g)) * u; }
+// silu(g) u = g u / (1 + e^-g) for two pairs.  An exponent y = x / ln 2 is rounded, which puts 2^y off by more the larger x is; what it
+// is off by is put back: e^x = 2^y (1 + c), c = x - y ln 2 with ln 2 in two parts.  Errors are counted in 2^-24; ex2.approx's is 4 (2
+// units in the last place), rcp.approx's 2.
+__device__ __forceinline__ uint64_t f2_both(float f) { return f2_pack(__float_as_uint(f), __float_as_uint(f)); }
+__device__ __forceinline__ uint64_t f2_rcp(uint64_t v) {
+  uint32_t a, b;
+  f2_unpack(v, a, b);
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+r"(a));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+r"(b));
+  return f2_pack(a, b);
+}
+// e^x where y is x / ln 2, rounded
+__device__ __forceinline__ uint64_t f2_exp(uint64_t x, uint64_t y) {
+  uint32_t a, b;
+  f2_unpack(y, a, b);
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+r"(a));
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+r"(b));
+  const uint64_t e = f2_pack(a, b), c = f2_fma(y, f2_both(1.90465421e-9f), f2_fma(y, f2_both(-0.693147182f), x));
+  return f2_fma(e, c, e);
+}
+// For |g| <= 80, from -g and -u: errors e^-g 5, 1 + e^-g at most 6, its reciprocal 2, products 2; together 10.
+constexpr float kSiluNear = 80.f;
+__device__ __forceinline__ uint64_t silu_near2(uint64_t ng, uint64_t nu) {
+  const uint64_t e = f2_exp(ng, f2_mul(ng, f2_both(1.44269502f)));
+  return f2_mul(f2_mul(ng, f2_rcp(f2_add(e, f2_both(1.f)))), nu);
+}
+// For every g, with m = e^(-|g| / 2):   g < 0:  (g m) (u m) / (1 + m^2),   else  g u / (1 + m^2),   in which neither e^-g nor a divisor
+// above 2 occurs, so that a far gate of a large u keeps its digits.  Errors: m 5, twice in the result, 1 + m^2 at most 6, its reciprocal 2,
+// products 4; together 22.  Below g = -174 m is 0, off by less than 1e-35.
+__device__ __forceinline__ uint64_t silu_times2(uint64_t g, uint64_t u) {
+  uint32_t g0, g1, m0, m1;
+  f2_unpack(g, g0, g1);
+  // (no further than 2^8: an infinite g would make c a NaN)
+  const uint64_t a = f2_pack(__float_as_uint(fminf(fabsf(__uint_as_float(g0)), 256.f)),
+                             __float_as_uint(fminf(fabsf(__uint_as_float(g1)), 256.f)));
+  uint64_t m = f2_exp(f2_mul(a, f2_both(-0.5f)), f2_mul(a, f2_both(-0.72134751f)));
+  const uint64_t r = f2_rcp(f2_fma(m, m, f2_both(1.f)));
+  f2_unpack(m, m0, m1);
+  m = f2_pack((int)g0 < 0 ? m0 : 0x3f800000u, (int)g1 < 0 ? m1 : 0x3f800000u);
+  return f2_mul(f2_mul(f2_mul(g, m), r), f2_mul(u, m));
+}
+__device__ __forceinline__ float silu_times(float g, float u) {
+  uint32_t lo, hi;
+  f2_unpack(silu_times2(f2_pack(__float_as_uint(g), __float_as_uint(g)), f2_pack(__float_as_uint(u), __float_as_uint(u))), lo, hi);
+  return __uint_as_float(lo);
+}
 
 __device__ __forceinline__ float bf16_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }

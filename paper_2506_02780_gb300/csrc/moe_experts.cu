@@ -182,15 +182,12 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
           uint32_t top = 0;
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
-            uint32_t g[2], u[2], h[2];
-            f2_unpack(acc[i], g[0], g[1]);
-            f2_unpack(acc[32 + i], u[0], u[1]);
+            uint32_t h[2];
+            acc[i] = silu_times2(acc[i], acc[32 + i]);
+            f2_unpack(acc[i], h[0], h[1]);
 #pragma unroll
-            for (int d = 0; d < 2; ++d) {
-              h[d] = __float_as_uint(silu_times(__uint_as_float(g[d]), __uint_as_float(u[d])));
+            for (int d = 0; d < 2; ++d)
               if (i0 + 2 * i + d < p.I) top = max(top, h[d] & 0x7fffffffu);
-            }
-            acc[i] = f2_pack(h[0], h[1]);
           }
           // the block's other 64 columns are the neighbour warp's
           s_top[meets & 1][half][r] = top;
@@ -304,16 +301,14 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
           __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.h) + (size_t)(t.entry + c) * p.I + col;
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            uint32_t g[2], u[2];
-            f2_unpack(acc0[j][i / 2], g[0], g[1]);
-            f2_unpack(acc1[j][i / 2], u[0], u[1]);
-            const float h = silu_times(__uint_as_float(g[i & 1]), __uint_as_float(u[i & 1]));
+            if (i % 2 == 0) acc0[j][i / 2] = silu_times2(acc0[j][i / 2], acc1[j][i / 2]);
+            uint32_t h[2];
+            f2_unpack(acc0[j][i / 2], h[0], h[1]);
             if constexpr (kFp8) {
-              const uint32_t m = __reduce_max_sync(0xffffffffu, in ? __float_as_uint(h) & 0x7fffffffu : 0u);
+              const uint32_t m = __reduce_max_sync(0xffffffffu, in ? h[i & 1] & 0x7fffffffu : 0u);
               if (lane == i) top[j] = m;
-              acc0[j][i / 2] = i & 1 ? f2_pack(g[0], __float_as_uint(h)) : f2_pack(__float_as_uint(h), g[1]);
             } else if (in && c + i < t.rows) {
-              o[(size_t)i * p.I] = __float2bfloat16_rn(h);
+              o[(size_t)i * p.I] = __float2bfloat16_rn(__uint_as_float(h[i & 1]));
             }
           }
           if (kFp8 && lane < 16) s_top[meets & 1][q][c + lane] = top[j];
