@@ -762,7 +762,7 @@ ee_status ee_fp8_linear(const uint8_t* x, const float* x_scale, const uint8_t* w
  * H and I multiples of 16, up to 65536; E up to 256, k up to 16; x, router, w1 and w2 16-byte aligned.
  * Always summed in the same order: repeated calls agree bit for bit.
  * Outputs must not overlap inputs.
- * ws: ee_moe_workspace_size(...) bytes for these sizes (a larger one serves too; 0: sizes out of range), zeroed once
+ * ws: ee_moe_workspace_size(...) bytes for these sizes (a larger one serves too; 0: sizes that the layer refuses), zeroed once
  *   with ee_workspace_init().  A workspace of its own: its arrays lie where the attention and the LM head keep counts
  *   from call to call, so of the other entry points only ee_fp8_linear may share it.
  * Device errors: EE_DEVERR_TIMEOUT (outputs undefined).

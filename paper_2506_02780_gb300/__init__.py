@@ -621,7 +621,10 @@ def ee_moe_workspace_size(T, H, I, E, k) -> int:
 def new_moe_workspace(T, H, I, E, k, device="cuda", stream=None):
     """Allocate (through torch) and zero a workspace for ee_moe_layer calls of up to these sizes; of the other
     entry points only ee_fp8_linear may share it."""
-    ws = torch.empty(ee_moe_workspace_size(T, H, I, E, k), dtype=torch.uint8, device=device)
+    size = ee_moe_workspace_size(T, H, I, E, k)
+    if not size:
+        raise ValueError(f"ee_moe_layer: unsupported sizes T {T}, H {H}, I {I}, E {E}, k {k}")
+    ws = torch.empty(size, dtype=torch.uint8, device=device)
     ee_workspace_init(ws, stream)
     return ws
 

@@ -791,11 +791,17 @@ ee_status launch(MoeParams& p, cudaStream_t stream) {
 
 }  // namespace
 
+// what both entry points take
+static ee_status moe_sizes(int32_t T, int32_t H, int32_t I, int32_t E, int32_t k) {
+  if (T < 0 || H < 1 || I < 1 || E < 1 || k < 1 || k > E) return EE_ERR_INVALID_ARG;
+  if (H % 16 != 0 || I % 16 != 0 || H > (1 << 16) || I > (1 << 16) || E > kMoeMaxExperts || k > kMoeMaxTopK ||
+      T > kMoeMaxTokens)
+    return EE_ERR_UNSUPPORTED;
+  return EE_OK;
+}
+
 extern "C" size_t ee_moe_workspace_size(int32_t T, int32_t H, int32_t I, int32_t E, int32_t k) {
-  if (T < 0 || H < 1 || I < 1 || E < 1 || k < 1 || T > kMoeMaxTokens || H > (1 << 16) || I > (1 << 16) ||
-      E > kMoeMaxExperts || k > kMoeMaxTopK)
-    return 0;
-  return ee::moe_layout(T, H, I, E, k).total;
+  return moe_sizes(T, H, I, E, k) == EE_OK ? ee::moe_layout(T, H, I, E, k).total : 0;
 }
 
 extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_bf16* router, const void* w1,
@@ -803,10 +809,8 @@ extern "C" ee_status ee_moe_layer(const ee_bf16* x, int64_t x_stride, const ee_b
                                   int32_t H, int32_t I, int32_t E, int32_t k, int32_t renorm, const int32_t* live_or_null,
                                   ee_bf16* out, int64_t out_stride, int32_t* ids_or_null, float* probs_or_null, void* ws,
                                   size_t ws_bytes, ee_stream_t stream) {
-  if (T < 0 || H < 1 || I < 1 || E < 1 || k < 1 || k > E) return EE_ERR_INVALID_ARG;
-  if (H % 16 != 0 || I % 16 != 0 || H > (1 << 16) || I > (1 << 16) || E > kMoeMaxExperts || k > kMoeMaxTopK ||
-      T > kMoeMaxTokens)
-    return EE_ERR_UNSUPPORTED;
+  const ee_status sizes = moe_sizes(T, H, I, E, k);
+  if (sizes != EE_OK) return sizes;
   if (T == 0) return EE_OK;
   if (!x || !router || !w1 || !w2 || !out || !ws || !w1_scale_or_null != !w2_scale_or_null) return EE_ERR_INVALID_ARG;
   if (!ee::aligned(ws, 256) || !ee::aligned(x, 16) || !ee::aligned(router, 16) || !ee::aligned(w1, 16) ||

@@ -81,6 +81,10 @@ class Experts:
             raise ValueError("w1 must be [E, 2 I, H] and w2 [E, H, I]")
         self.E, self.H, self.I = w2.shape
         self.k, self.renorm = int(k), bool(renorm)
+        if router.shape != (self.E, self.H):
+            raise ValueError("router must be [E, H]")
+        n, dev = int(max_tokens), w1.device
+        self.ws = new_moe_workspace(n, self.H, self.I, self.E, self.k, device=dev)   # (refuses sizes that a call would)
         if quantize:
             if w1_scale is not None or w2_scale is not None:
                 raise ValueError("quantize takes bf16 weights without scales")
@@ -88,11 +92,9 @@ class Experts:
             w1 = w1.view(self.E, 2 * self.I, self.H)
             w2, w2_scale = quantize_weights(w2)
         self.router, self.w1, self.w2, self.w1_scale, self.w2_scale = router, w1, w2, w1_scale, w2_scale
-        n, dev = int(max_tokens), w1.device
         self._out = torch.empty((n, self.H), dtype=torch.bfloat16, device=dev)
         self._ids = torch.empty(n * self.k, dtype=torch.int32, device=dev)
         self._probs = torch.empty(n * self.k, dtype=torch.float32, device=dev)
-        self.ws = new_moe_workspace(n, self.H, self.I, self.E, self.k, device=dev)
 
     def __call__(self, x, live=None, out=None, stream=None):
         """x bf16 [n, H]; live (device int32 [1]): only its first tokens are computed, what is behind them
