@@ -1,4 +1,4 @@
-// Weight products for a few tokens (up to 8): a warp takes 16 weight rows
+// Weight products for a few tokens (up to 8 an MMA, 16 in ee_fp8_linear): a warp takes 16 weight rows
 // and some of their 128-byte blocks, straight from global memory into the fragments of an m16n8 MMA (weights the
 // 16 side, tokens the 8 side).  So few tokens leave nothing to share between warps but the
 // sums, and without rings, tensor memory and barriers a call costs little more than its one wait for memory.

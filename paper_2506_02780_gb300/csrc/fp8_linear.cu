@@ -495,9 +495,11 @@ extern "C" ee_status ee_fp8_linear(const uint8_t* x, const float* x_scale, const
   p.err = ee::err_word(ws);
   const int64_t t128 = (int64_t)p.MT * ((N + 127) / 128), t256 = (int64_t)p.MT * ((N + 255) / 256);
   if (t256 > (1 << 30)) return EE_ERR_UNSUPPORTED;
-  // Up to 8 tokens, and up to 16 where W is small, do without tiles (us, 3,584 x 3,584: 1 token 4.1, by tiles 6.6; 16
-  // tokens 6.0 and 7.2; 28,672 rows: 1 token 20.1 and 21.3, 8 tokens 22.4 and 21.4, 16 tokens 29 and 21).
-  if (n <= 8 || (n <= 16 && (int64_t)N * K <= (1 << 25))) {
+  // Few tokens do without tiles where W is small: its call is over sooner, but its stream is slower.  (us without tiles and by
+  // tiles, captured, weights from HBM, for 1, 8 and 16 tokens: 3,584 x 3,584 4.6 and 7.4, 5.1 and 8.3, 6.1 and 8.6; 14,336 x 3,584 11.7 and
+  // 13.5, 12.8 and 14.1, 15.8 and 14.4; 18,944 x 3,584 14.5 and 14.7, 15.8 and 15.4; 28,672 x 3,584 20.2 and 20.3, 22.1 and 21.0, 28.3 and
+  // 21.9; 76,032 x 3,584 47.6 and 42.3, 51.3 and 42.9.)
+  if (n <= 16 && (int64_t)N * K < (n <= 8 ? 1 << 26 : (1 << 25) + 1)) {
     const auto kernel = n <= 8 ? fp8_linear_few_kernel<1> : fp8_linear_few_kernel<2>;
     EE_CUDA_OK(ee::launch_pdl(kernel, dim3((unsigned)((N + 15) / 16)), dim3(kFewWarps * 32), 0, (cudaStream_t)stream, 1, x, w, K, p));
     return EE_OK;
