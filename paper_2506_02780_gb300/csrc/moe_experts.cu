@@ -237,131 +237,129 @@ moe_experts_kernel(const __grid_constant__ CUtensorMap tmW1, const __grid_consta
             __syncwarp();
           }
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(edone0 + 8 * slot);
-        continue;
-      }
-      uint64_t acc0[kChunks][8], acc1[kChunks][8];            // tokens (2 j + half) 16 .. + 15 of the two tiles
+      } else {
+        uint64_t acc0[kChunks][8], acc1[kChunks][8];            // tokens (2 j + half) 16 .. + 15 of the two tiles
 #pragma unroll
-      for (int j = 0; j < kChunks; ++j)
+        for (int j = 0; j < kChunks; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc0[j][i] = acc1[j][i] = 0;
-      const int KB = kFp8 ? (gate ? p.KB1 : p.KB2) : 1;
-      bool ok = true;
-      for (int kb = 0; kb < KB; ++kb, ++it) {
-        const uint32_t buf = it % kBufs, ph = (it / kBufs) & 1;
-        if constexpr (kFp8)
-          ok = __all_sync(0xffffffffu, mbar_wait(sfull0 + 8 * (sc % kScRing), (sc / kScRing) & 1, &s_abort));
-        if (!ok || !__all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * buf, ph, &s_abort))) {
-          ok = false;
-          break;
-        }
-        tc_fence_after();
-        if (mine) {
-          const uint32_t sa = smem_u32(&s_scale[kFp8 ? sc % kScRing : 0][0][0]);
+          for (int i = 0; i < 8; ++i) acc0[j][i] = acc1[j][i] = 0;
+        const int KB = kFp8 ? (gate ? p.KB1 : p.KB2) : 1;
+        bool ok = true;
+        for (int kb = 0; kb < KB; ++kb, ++it) {
+          const uint32_t buf = it % kBufs, ph = (it / kBufs) & 1;
+          if constexpr (kFp8)
+            ok = __all_sync(0xffffffffu, mbar_wait(sfull0 + 8 * (sc % kScRing), (sc / kScRing) & 1, &s_abort));
+          if (!ok || !__all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * buf, ph, &s_abort))) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          if (mine) {
+            const uint32_t sa = smem_u32(&s_scale[kFp8 ? sc % kScRing : 0][0][0]);
 #pragma unroll
-          for (int j = 0; j < kChunks; ++j) {
-            const int c = (2 * j + half) * 16;
-            if (c < t.rows) {
-              uint32_t a[16], b[16];
-              tc_ld16_nowait(tq + buf * (2 * NT) + c, a);
-              tc_ld16_nowait(tq + buf * (2 * NT) + NT + c, b);
-              tc_wait_ld16x2(a, b);
-              if constexpr (kFp8) {
-                add_scaled16(acc0[j], a, sa + 4 * c);
-                add_scaled16(acc1[j], b, sa + 4 * (NT + c));
-              } else {
+            for (int j = 0; j < kChunks; ++j) {
+              const int c = (2 * j + half) * 16;
+              if (c < t.rows) {
+                uint32_t a[16], b[16];
+                tc_ld16_nowait(tq + buf * (2 * NT) + c, a);
+                tc_ld16_nowait(tq + buf * (2 * NT) + NT + c, b);
+                tc_wait_ld16x2(a, b);
+                if constexpr (kFp8) {
+                  add_scaled16(acc0[j], a, sa + 4 * c);
+                  add_scaled16(acc1[j], b, sa + 4 * (NT + c));
+                } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                  acc0[j][i] = f2_pack(a[2 * i], a[2 * i + 1]);
-                  acc1[j][i] = f2_pack(b[2 * i], b[2 * i + 1]);
+                  for (int i = 0; i < 8; ++i) {
+                    acc0[j][i] = f2_pack(a[2 * i], a[2 * i + 1]);
+                    acc1[j][i] = f2_pack(b[2 * i], b[2 * i + 1]);
+                  }
                 }
               }
             }
           }
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(tempty0 + 8 * buf);
-          if constexpr (kFp8) mbar_arrive(sempty0 + 8 * (sc % kScRing));
-        }
-        ++sc;
-      }
-      if (!ok) break;
-      if (mine && gate) {
-        const int col = t.blk * kTile + r;
-        const bool in = col < p.I;
-        uint32_t top[kChunks];                                // lane i: the largest |h| of token i in these 32 columns
-#pragma unroll
-        for (int j = 0; j < kChunks; ++j) {
-          const int c = (2 * j + half) * 16;
-          top[j] = 0;
-          if (c >= t.rows) break;
-          __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.h) + (size_t)(t.entry + c) * p.I + col;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            if (i % 2 == 0) acc0[j][i / 2] = silu_times2(acc0[j][i / 2], acc1[j][i / 2]);
-            uint32_t h[2];
-            f2_unpack(acc0[j][i / 2], h[0], h[1]);
-            if constexpr (kFp8) {
-              const uint32_t m = __reduce_max_sync(0xffffffffu, in ? h[i & 1] & 0x7fffffffu : 0u);
-              if (lane == i) top[j] = m;
-            } else if (in && c + i < t.rows) {
-              o[(size_t)i * p.I] = __float2bfloat16_rn(__uint_as_float(h[i & 1]));
-            }
-          }
-          if (kFp8 && lane < 16) s_top[meets & 1][q][c + lane] = top[j];
-        }
-        if constexpr (kFp8) {
-          // the block's other columns are the three warps' of the same tokens
+          tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(meet0 + 8 * half);
-          if (!__all_sync(0xffffffffu, mbar_wait(meet0 + 8 * half, meets & 1, &s_abort))) break;
+          if (lane == 0) {
+            mbar_arrive(tempty0 + 8 * buf);
+            if constexpr (kFp8) mbar_arrive(sempty0 + 8 * (sc % kScRing));
+          }
+          ++sc;
+        }
+        if (!ok) break;
+        if (mine && gate) {
+          const int col = t.blk * kTile + r;
+          const bool in = col < p.I;
+          uint32_t top[kChunks];                                // lane i: the largest |h| of token i in these 32 columns
+#pragma unroll
+          for (int j = 0; j < kChunks; ++j) {
+            const int c = (2 * j + half) * 16;
+            top[j] = 0;
+            if (c >= t.rows) break;
+            __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.h) + (size_t)(t.entry + c) * p.I + col;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              if (i % 2 == 0) acc0[j][i / 2] = silu_times2(acc0[j][i / 2], acc1[j][i / 2]);
+              uint32_t h[2];
+              f2_unpack(acc0[j][i / 2], h[0], h[1]);
+              if constexpr (kFp8) {
+                const uint32_t m = __reduce_max_sync(0xffffffffu, in ? h[i & 1] & 0x7fffffffu : 0u);
+                if (lane == i) top[j] = m;
+              } else if (in && c + i < t.rows) {
+                o[(size_t)i * p.I] = __float2bfloat16_rn(__uint_as_float(h[i & 1]));
+              }
+            }
+            if (kFp8 && lane < 16) s_top[meets & 1][q][c + lane] = top[j];
+          }
+          if constexpr (kFp8) {
+            // the block's other columns are the three warps' of the same tokens
+            __syncwarp();
+            if (lane == 0) mbar_arrive(meet0 + 8 * half);
+            if (!__all_sync(0xffffffffu, mbar_wait(meet0 + 8 * half, meets & 1, &s_abort))) break;
+#pragma unroll
+            for (int j = 0; j < kChunks; ++j) {
+              const int c = (2 * j + half) * 16;
+              if (c >= t.rows) break;
+              uint32_t m = 0;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) m = max(m, s_top[meets & 1][i][c + (lane & 15)]);
+              const BlockScale mine_s = block_scale(__uint_as_float(m));
+              if (q == 0 && lane < 16 && c + lane < t.rows) p.hs[(size_t)t.blk * p.n + t.entry + c + lane] = mine_s.scale;
+              uint8_t* o = static_cast<uint8_t*>(p.h) + (size_t)(t.entry + c) * p.I + col;
+#pragma unroll
+              for (int i = 0; i < 16; i += 2) {
+                uint32_t h[2];
+                f2_unpack(acc0[j][i / 2], h[0], h[1]);
+                float v[2];
+#pragma unroll
+                for (int d = 0; d < 2; ++d) {
+                  BlockScale s;
+                  s.hi = __shfl_sync(0xffffffffu, mine_s.hi, i + d);
+                  s.lo = __shfl_sync(0xffffffffu, mine_s.lo, i + d);
+                  v[d] = to_code(__uint_as_float(h[d]), s);
+                }
+                const uint32_t code = pack_e4m3(v[0], v[1], 0.f, 0.f);
+                if (in && c + i < t.rows) o[(size_t)i * p.I] = (uint8_t)code;
+                if (in && c + i + 1 < t.rows) o[(size_t)(i + 1) * p.I] = (uint8_t)(code >> 8);
+              }
+            }
+            ++meets;
+          }
+        } else if (mine) {
+          const int col = t.blk * 2 * kTile + r;
+          const bool in0 = col < p.H, in1 = col + kTile < p.H;
 #pragma unroll
           for (int j = 0; j < kChunks; ++j) {
             const int c = (2 * j + half) * 16;
             if (c >= t.rows) break;
-            uint32_t m = 0;
+            float* o = p.y + (size_t)(t.entry + c) * p.H + col;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) m = max(m, s_top[meets & 1][i][c + (lane & 15)]);
-            const BlockScale mine_s = block_scale(__uint_as_float(m));
-            if (q == 0 && lane < 16 && c + lane < t.rows) p.hs[(size_t)t.blk * p.n + t.entry + c + lane] = mine_s.scale;
-            uint8_t* o = static_cast<uint8_t*>(p.h) + (size_t)(t.entry + c) * p.I + col;
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-              uint32_t h[2];
-              f2_unpack(acc0[j][i / 2], h[0], h[1]);
-              float v[2];
-#pragma unroll
-              for (int d = 0; d < 2; ++d) {
-                BlockScale s;
-                s.hi = __shfl_sync(0xffffffffu, mine_s.hi, i + d);
-                s.lo = __shfl_sync(0xffffffffu, mine_s.lo, i + d);
-                v[d] = to_code(__uint_as_float(h[d]), s);
-              }
-              const uint32_t code = pack_e4m3(v[0], v[1], 0.f, 0.f);
-              if (in && c + i < t.rows) o[(size_t)i * p.I] = (uint8_t)code;
-              if (in && c + i + 1 < t.rows) o[(size_t)(i + 1) * p.I] = (uint8_t)(code >> 8);
+            for (int i = 0; i < 16; ++i, o += p.H) {
+              uint32_t a[2], b[2];
+              f2_unpack(acc0[j][i / 2], a[0], a[1]);
+              f2_unpack(acc1[j][i / 2], b[0], b[1]);
+              if (in0 && c + i < t.rows) __stcg(o, __uint_as_float(a[i & 1]));
+              if (in1 && c + i < t.rows) __stcg(o + kTile, __uint_as_float(b[i & 1]));
             }
-          }
-          ++meets;
-        }
-      } else if (mine) {
-        const int col = t.blk * 2 * kTile + r;
-        const bool in0 = col < p.H, in1 = col + kTile < p.H;
-#pragma unroll
-        for (int j = 0; j < kChunks; ++j) {
-          const int c = (2 * j + half) * 16;
-          if (c >= t.rows) break;
-          float* o = p.y + (size_t)(t.entry + c) * p.H + col;
-#pragma unroll
-          for (int i = 0; i < 16; ++i, o += p.H) {
-            uint32_t a[2], b[2];
-            f2_unpack(acc0[j][i / 2], a[0], a[1]);
-            f2_unpack(acc1[j][i / 2], b[0], b[1]);
-            if (in0 && c + i < t.rows) __stcg(o, __uint_as_float(a[i & 1]));
-            if (in1 && c + i < t.rows) __stcg(o + kTile, __uint_as_float(b[i & 1]));
           }
         }
       }
