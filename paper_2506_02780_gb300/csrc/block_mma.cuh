@@ -4,7 +4,7 @@
 //
 // A product with a scale for each block of 128 along K cannot stay in the
 // tensor cores' accumulator: y = sum_b s_b (x_b . w_b).  Each block's product
-// goes to tensor memory by itself (two accumulators in turn) and the epilogue
+// goes to tensor memory by itself (two to eight accumulators in turn) and the epilogue
 // warps add it, scaled, to sums of their own in registers.  With tokens as the MMA's
 // M side (one tensor-memory lane, one thread) a block's scale is one number a
 // thread and 128 columns; tiles of few tokens have it the other way round (moe_experts.cu).
@@ -112,7 +112,7 @@ __device__ __forceinline__ uint32_t pack_e4m3(float x0, float x1, float x2, floa
   return d;
 }
 // silu(g) u = g u / (1 + e^-g) for two pairs.  An exponent y = x / ln 2 is rounded, which puts 2^y off by more the larger x is; what it
-// is off by is put back: e^x = 2^y (1 + c), c = x - y ln 2 with ln 2 in two parts.  Errors are counted in 2^-24; ex2.approx's is 4 (2
+// is off by is put back: e^x = 2^y (1 + c), c = x - y ln 2 with ln 2 in two parts (Cody and Waite).  Errors are counted in 2^-24; ex2.approx's is 4 (2
 // units in the last place), rcp.approx's 2.
 __device__ __forceinline__ uint64_t f2_both(float f) { return f2_pack(__float_as_uint(f), __float_as_uint(f)); }
 __device__ __forceinline__ uint64_t f2_rcp(uint64_t v) {

@@ -12,8 +12,12 @@
 // are fewer tiles than SMs, a cluster of up to 8 CTAs shares a tile's k-blocks and adds its
 // partial sums through distributed shared memory, always in the same order.
 // Many tokens: a k-block is 48 KB a CTA and 0.33 us of MMAs; loads alone run at 0.41 us (L2 to an SM about 118 GB/s),
-// the whole at 0.48: 8,191 tokens x 3,584 x 28,672 650 to 720 us, at the power cap 2.2 PFLOP/s.  (CTA pairs that share
-// their MMAs load 32 KB, but hand every k-block's accumulator over between two CTAs and back: twice the time.)
+// the whole at 0.48: 8,191 tokens x 3,584 x 28,672 646 to 690 us in a graph, 694 to 780 one call after another at the power cap
+// (2.2 to 2.4 PFLOP/s).  (CTA pairs that share their MMAs load 32 KB, but hand every k-block's accumulator over between two CTAs and
+// back: twice the time.)
+// Rows of out that are not 16-byte aligned (N or the stride no multiple of 8) are stored by 2 bytes, which the epilogue warps pay for: 4,000
+// tokens x 3,584 x 3,584 44 us, with a row of out one element longer 97.  K no multiple of 128 costs loads, for a box's rows then begin inside
+// of 128-byte lines: K = 3,600 58 us.
 #include <mutex>
 
 #include "few.cuh"
@@ -120,7 +124,6 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
   tc_fence_after();
   const uint32_t tmem = s_tmem;
   pdl_wait();
-
 
   if (warp >= 4) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpi));

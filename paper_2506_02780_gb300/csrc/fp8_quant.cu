@@ -194,8 +194,8 @@ extern "C" ee_status ee_fp8_quantize(const ee_bf16* x, int64_t x_stride, int32_t
   p.scale = scale;
   p.rows = rows;
   p.cols = cols;
-  // four steps a warp where that leaves work for every SM, two where it does not (8,191 gated rows of 14,336 93 us, by
-  // two steps 102; 16,384 rows of 7,168 54 and 64; 64 rows of 3,584 2.0 and 1.7)
+  // four steps a warp where that leaves work for every SM, two where it does not (8,191 gated rows of 14,336 94 us, by
+  // two steps 116; 16,384 rows of 7,168 56 and 66; 64 rows of 3,584 2.1 and 1.7)
   const int64_t row_ctas = ((int64_t)rows + kWarps - 1) / kWarps;
   const bool many = row_ctas * ((cols + 1023) / 1024) >= 2 * ee::kNumSMs;
   p.chunks = many ? (cols + 1023) / 1024 : (cols + 511) / 512;

@@ -5,10 +5,9 @@
 //   the sum      out[t] = sum_j p[t][j] y[entry of t's j-th expert]
 // The experts' weights are read once and bound the call.  Weight rows are the MMA's M side (two tiles of
 // 128: gate and up, or two of down), tokens its N side: a few tokens then cost the epilogue a few
-// columns of every lane, where with tokens on the lanes two warps of eight would do all of its work (a draft
-// tree's layer of 64 experts of 1280 x 3584 took 194 us so).  Narrower tiles make more tasks, but a k-block takes
-// its 0.4 us with half the rows, too (the same layer with 64 rows 177 us, with 128 141; 8 experts of 2560 for 20
-// tokens 63 and 67).
+// columns of every lane, where with tokens on the lanes two warps of eight would do all of its work (when it was turned, a draft
+// tree's layer of 64 experts of 1280 x 3584 went from 194 us to 155).  A k-block of narrower weight tiles takes
+// the same 0.4 us, so there are only those of 128 rows.
 //
 // On 8-bit weights tiles of 128 tokens have tokens on the lanes all the same: a token's scale is then one
 // register, where the columns' scales come from shared memory, 128 of them a k-block and thread, whose reads

@@ -12,7 +12,8 @@
 // (all drawn before, by CTAs that are running), during which the first down units' weights are under way; then
 // every CTA brings h into its own shared memory, as e4m3 codes for 8-bit weights.
 // One token at 6 of 64 experts of 1280 x 3584, 8-bit: 29 us, by the tiles of moe_experts.cu 33; at 2 of 8 of 2560: 25 and 34; at
-// 4 of 60 of 512 x 1024, bf16: 14 and 22.  More entries are those tiles' (8 tokens at 6 of 64: 76 us, here 98).
+// 4 of 60 of 512 x 1024, bf16: 14 and 22; 8 tokens at 1 of 8 of 2560, 8-bit: 40 and 39.  8 entries are what an MMA's columns and the tables
+// hold; more are those tiles'.
 #include <mutex>
 
 #include "moe.cuh"
