@@ -28,3 +28,15 @@ def test_few_tokens_on_large_weights(n, K, N):
     again = torch.empty(n, N, dtype=torch.bfloat16, device=DEV)
     E.ee_fp8_linear(x, xs, w, wsc, again, ws, bias=bias)
     assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("n,K,N", [(20, 16, 300), (64, 48, 5000), (200, 16, 257), (3, 16, 1 << 22), (8, 112, 600007)])
+def test_rows_shorter_than_a_block_by_tiles(n, K, N):
+    g = gen(n + K + N)
+    x, xs = make_rows(g, n, K)
+    w, wsc = make_weights(g, N, K)
+    ws = E.new_linear_workspace()
+    out = torch.empty(n, N, dtype=torch.bfloat16, device=DEV)
+    E.ee_fp8_linear(x, xs, w, wsc, out, ws)
+    assert E.ee_read_errors(ws) == 0
+    check_linear(out, x, xs, w, wsc, None)
